@@ -293,6 +293,74 @@ BC_API bc_status bc_rope_split(bc_cache* cache, const void* qkv, const int32_t* 
 BC_API bc_status bc_rope_decode_step(bc_cache* cache, int32_t layer, const int32_t* slots, int32_t n, const void* qkv,
                                      const int32_t* positions, float theta, void* out, float sm_scale, void* stream);
 
+/* ---- norms of the query and key heads, with the rotation ------------------------------------------
+ * For models that normalise every query and key head between the QKV projection and the rotation:
+ * what bc_rope_split does, with y = x / sqrt(mean(x^2) + eps) * weight on every q and k head (the mean
+ * over the head's coordinates) ahead of the rotation, in one pass, in fp32 with one rounding to bf16 at
+ * the end; v is copied.  Stateless like the layer operators below (no cache handle, nothing latched), so
+ * that the teacher-forced form can use it as well; one kernel launch, ordinary stream order.
+ * qkv: device bf16, n rows of (q_heads + 2 kv_heads) * head_dim values, row i at qkv + i * row_stride
+ * (elements; a multiple of 8, at least a row's length: rows of a wider fused projection need no copy);
+ * positions: device int32 [n]; theta > 1; q_weight, k_weight: bf16 [head_dim], NULL = ones; eps >= 0;
+ * q_out [n, q_heads, head_dim], k_out, v_out [n, kv_heads, head_dim] bf16, contiguous, not overlapping
+ * qkv.  All 16-byte aligned.  head_dim 64 or 128 (else BC_ERR_UNSUPPORTED); other violations:
+ * BC_ERR_INVALID_ARG. */
+BC_API bc_status bc_norm_rope_split(int32_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* qkv,
+                                    int64_t row_stride, const int32_t* positions, float theta, const void* q_weight,
+                                    const void* k_weight, float eps, void* q_out, void* k_out, void* v_out, void* stream);
+
+/* Its gradient: from dq, dk, dv (bf16, laid out like q_out, k_out, v_out) and the forward call's inputs to
+ * dqkv (bf16 [n, (q_heads + 2 kv_heads) * head_dim], contiguous; the v heads are dv) and the weights'
+ * gradients dq_weight, dk_weight (fp32 [head_dim], summed over rows and heads; NULL: not written).
+ * fp32 arithmetic, additions in a fixed order (results are reproducible).  workspace: device memory of
+ * at least bc_norm_rope_query_bytes bytes, 16-byte aligned, one call at a time.  Two launches (one
+ * without weight gradients).  Outputs must not overlap inputs. */
+BC_API bc_status bc_norm_rope_query_bytes(int32_t head_dim, size_t* workspace_bytes);
+BC_API bc_status bc_norm_rope_split_backward(int32_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* qkv,
+                                             int64_t row_stride, const int32_t* positions, float theta, const void* q_weight,
+                                             const void* k_weight, float eps, const void* dq, const void* dk, const void* dv,
+                                             void* dqkv, float* dq_weight, float* dk_weight, void* workspace,
+                                             size_t workspace_bytes, void* stream);
+
+/* bc_norm_rope_split (rows contiguous, head counts of the cache) followed by bc_decode_step on its results,
+ * as bc_rope_decode_step: same staging buffer, limits and errors. */
+BC_API bc_status bc_norm_rope_decode_step(bc_cache* cache, int32_t layer, const int32_t* slots, int32_t n, const void* qkv,
+                                          const int32_t* positions, float theta, const void* q_weight, const void* k_weight,
+                                          float eps, void* out, float sm_scale, void* stream);
+
+/* ---- attention of a chunk of new tokens over the cache --------------------------------------------
+ * Several queries per sequence in one call: item i of the batch has m_i = cu_q[i + 1] - cu_q[i] query rows
+ * (any number, 0 included; ragged), packed in q, and its row r sees the first first[i] + r + 1 live entries of
+ * sequence slots[i] in logical order (prompt, beacons, window), all of them where there are fewer:
+ *   out[cu_q[i] + r, h] = softmax_j(sm_scale * <q, K_j>) V_j over those entries; zeros where there is none (a
+ *   slot that is not open included, as in bc_decode_attn).
+ * first == NULL: the queries belong to the sequence's last m_i entries (first[i] = live entries - m_i), e.g.
+ * m_i tokens that bc_append has put into the window and that are checked at once.  With
+ * first[i] = 0 and m_i = the prompt's length it is the causal attention of a stored prompt.
+ * slots, first: device int32 [n]; cu_q: device int32 [n + 1], prefix sums, cu_q[0] = 0 and cu_q[n] ==
+ * total_q (host; rows at or past total_q are neither read nor written); q [total_q, q_heads, head_dim]
+ * bf16; out: same shape, bf16 (fp32 with BC_FLAG_OUT_F32), not overlapping q.  n <= 512, total_q <= 2^28 (else
+ * BC_ERR_UNSUPPORTED), sm_scale > 0.  total_q == 0 does nothing.  Accumulation in fp32, softmax
+ * weights rounded to bf16 before the second product.  Entries that no row of the chunk sees are never
+ * used; an entry that only later rows of the same chunk see must be finite (its weight in the earlier
+ * rows is exactly 0).
+ * The call changes no bookkeeping and may be issued at any point of the layer order; it uses scratch in the
+ * cache's workspace (one call at a time per cache, like every call).  One launch; it completes before
+ * any later kernel of the stream starts.  bc_set_attn_ctas sets its number of thread blocks too (0 = two per SM),
+ * bc_set_wait_limit its waits' limit, and a wait that runs out is reported as there. */
+BC_API bc_status bc_chunk_attn(bc_cache* cache, int32_t layer, const int32_t* slots, const int32_t* first,
+                               const int32_t* cu_q, int32_t n, int32_t total_q, const void* q, void* out, float sm_scale,
+                               void* stream);
+
+/* A chunk of every prompt: stores the K/V rows of item i at prompt positions first[i] .. first[i] + m_i - 1
+ * (bc_prefill for part of a prompt; positions at or past the length the sequence was opened with, and items
+ * whose slot is not open, are not stored), then bc_chunk_attn with the same `first`.  A prompt of any
+ * length is processed by successive calls, per layer, chunks in ascending order.  k, v [total, kv_heads,
+ * head_dim] bf16 packed like q; first must not be NULL.  Two launches. */
+BC_API bc_status bc_prefill_chunk(bc_cache* cache, int32_t layer, const int32_t* slots, const int32_t* first,
+                                  const int32_t* cu_chunk, int32_t n, int32_t total, const void* q, const void* k,
+                                  const void* v, void* out, float sm_scale, void* stream);
+
 /* The step whose token fills the window, in one call: bc_append(k, v), bc_decode_attn_pair(q, beacon_q;
  * extra = beacon_k, beacon_v) and bc_compress(beacon_k, beacon_v) (Algorithm 1: the token's forward
  * pass, the beacon's forward pass, the eviction).  Results, bookkeeping, layer-order rule (the layer
@@ -328,6 +396,27 @@ BC_API bc_status bc_add_rmsnorm(const void* h, const void* delta, const void* we
                                 float eps, void* h_out, void* normed_out, void* stream);
 BC_API bc_status bc_swiglu(const void* gate_up, int32_t n, int32_t m, void* out, void* stream);
 BC_API bc_status bc_argmax(const void* logits, int32_t n, int32_t vocab, int64_t* out, void* stream);
+
+/* Sampling of the next token (Algorithm 1 samples from the model's distribution), one token per row from a
+ * given uniform random number per row.  For a row x of logits with maximum m, temperature T > 0 and
+ * e_j = exp((x_j - m) / T):
+ *   K = the top_k largest elements (of equal ones the lowest indices; all if top_k <= 0 or >= vocab),
+ *   N = the shortest prefix of K, largest first (equal ones by index), whose mass (sum of e) reaches
+ *       top_p * mass(K) -- at least one element; all of K if top_p >= 1 --,
+ *   S = the elements of N with e_j >= min_p (min_p <= 0: all; values above 1 count as 1),
+ *   out = the first j of S in index order with the sum of e over S up to j ABOVE uniform * mass(S).
+ * T <= 0 (or NaN): the greedy choice, as bc_argmax.  A row whose maximum is -inf: its lowest index of a
+ * maximum, as bc_argmax.  NaN logits count as -inf; -inf logits are never chosen beside finite ones; +inf
+ * logits share the whole mass.  top_p, min_p NaN: off.  uniform below 0 or NaN counts as 0, 1 and above as the
+ * largest number below 1.  Weights are evaluated in double precision and added up exactly as multiples of
+ * 2^-45 (an element below that is never chosen), so the result does not depend on the order of additions.
+ * logits: device, n rows of vocab elements, bf16 (logits_f32 == 0) or fp32, row i at logits + i * row_stride
+ * elements (row_stride >= vocab; any value, any vocab up to 262144, else BC_ERR_UNSUPPORTED), aligned to the
+ * element; temperature, top_p, min_p fp32 [n], top_k int32 [n]: device, each NULL = 1, off, off, off for all
+ * rows; uniform fp32 [n]; out int64 [n].  One launch. */
+BC_API bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t row_stride, int32_t n, int32_t vocab,
+                           const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                           const float* uniform, int64_t* out, void* stream);
 
 /* Limits of bc_decode_attn_static. */
 #define BC_STATIC_MAX_BATCH 128   /* sequences per call */

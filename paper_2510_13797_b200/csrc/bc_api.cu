@@ -41,7 +41,7 @@ constexpr int kHostRing = 8;
 
 struct WorkLayout {
   size_t append_row[2], append_pos[2], plan[2], compress_row, compress_pos, restore_ok, restore_bea, tickets, book_flag, part_ml, part_o, part_ml2, part_o2, stage_in[kHostRing],
-      stage_out[kHostRing], stage_out2[kHostRing], rope_stage, host_words,
+      stage_out[kHostRing], stage_out2[kHostRing], rope_stage, host_words, chunk_tickets, chunk_ml, chunk_o,
       total;
 };
 WorkLayout work_layout(const bc_config& c) {
@@ -75,6 +75,9 @@ WorkLayout work_layout(const bc_config& c) {
     l.stage_out2[b] = take(max_n * c.q_heads * c.head_dim * 4);
   }
   l.rope_stage = take(max_n * (c.q_heads + 2 * c.kv_heads) * c.head_dim * 2);   // bc_rope_decode_step: q | k | v
+  l.chunk_tickets = take(BC_MAX_CHUNK_CTAS * 4);
+  l.chunk_ml = take(bc_chunk_part_ml_bytes());
+  l.chunk_o = take(bc_chunk_part_o_bytes(c.head_dim));
   l.total = o;
   return l;
 }
@@ -125,6 +128,8 @@ struct bc_cache {
   // has not been followed by an ordinarily launched kernel or an attention launch of this handle: an
   // attention kernel enqueued now could begin before that writer has ended and must not read early
   bool meta_unsettled = true;
+  bool chunk_map_ok = false;    // bc_chunk_attn: the pool's tensor map, made by the first call
+  CUtensorMap chunk_map;
   uint32_t wait_limit = 0;      // bc_set_wait_limit: polls of the attention kernel's bounded waits (0: default)
   void* timeline = nullptr;     // bc_attn_timeline: device buffer the attention kernel stamps, or NULL
   int device = -1;              // the CUDA device that was current at bc_cache_create
@@ -355,7 +360,7 @@ namespace {
 bc_status flush_pending(bc_cache* c);   // defined with the host-buffer entry points below
 }
 
-int32_t bc_version(void) { return 231; }
+int32_t bc_version(void) { return 240; }
 
 const char* bc_status_string(bc_status s) {
   switch (s) {
@@ -420,6 +425,7 @@ bc_status bc_cache_create(const bc_config* cfg, void* pool, void* meta, void* wo
   if (e == cudaSuccess) e = bc_launch_init(c->meta, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.tickets, 0, (size_t)BC_MAX_ATTN_BATCH * 4 * c->cfg.layers, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.book_flag, 0, 4, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream);
   if (e != cudaSuccess) { delete c; return BC_ERR_CUDA; }
   c->launches += 1;
   *out = c;
@@ -684,6 +690,83 @@ bc_status bc_rope_decode_step(bc_cache* c, int32_t layer, const int32_t* slots, 
   uint8_t* v = k + (size_t)n * c->cfg.kv_heads * c->cfg.head_dim * 2;
   st = bc_rope_split(c, qkv, positions, n, theta, q, k, v, stream);
   if (st) return st;
+  return bc_decode_step(c, layer, slots, n, q, k, v, out, sm_scale, stream);
+}
+
+namespace {
+// Checks and launch shared by bc_chunk_attn and bc_prefill_chunk.
+bc_status check_chunk(bc_cache* c, int layer, const int32_t* slots, const int32_t* cu_q, int n, int total_q, const void* q,
+                      void* out, float sm_scale) {
+  const bc_status st = check_batch(c, layer, slots, n);
+  if (st) return st;
+  if (n > BC_MAX_ATTN_BATCH || !cu_q || total_q < 0 || !(sm_scale > 0.f)) return BC_ERR_INVALID_ARG;
+  if (total_q > 0 && (!q || !out || !aligned16(q) || !aligned16(out))) return BC_ERR_INVALID_ARG;
+  if (total_q > 1 << 28) return BC_ERR_UNSUPPORTED;
+  return BC_OK;
+}
+
+bc_status chunk_impl(bc_cache* c, int layer, const int32_t* slots, const int32_t* first, const int32_t* cu_q, int n, int total_q,
+                     const void* q, void* out, float sm_scale, cudaStream_t s) {
+  BcChunkArgs a;
+  a.pool_layer = layer_base(c, layer); a.layer = layer;
+  a.slots = slots; a.first = first; a.cu_q = cu_q; a.n = n; a.total_q = total_q;
+  a.q = q; a.out = out; a.out_f32 = (c->cfg.flags & BC_FLAG_OUT_F32) ? 1 : 0; a.sm_scale = sm_scale;
+  a.part_o = work_ptr<float>(c, c->wl.chunk_o); a.part_ml = work_ptr<float>(c, c->wl.chunk_ml);
+  a.tickets = work_ptr<int32_t>(c, c->wl.chunk_tickets);
+  a.ctas = c->attn_ctas; a.wait_limit = c->wait_limit;
+  if (c->cfg.flags & BC_FLAG_ATTN_REFERENCE) {
+    BC_CUDA(c, bc_launch_chunk_reference(c->meta, c->geom, a, s));
+  } else {
+    if (!c->chunk_map_ok) {
+      if (!bc_chunk_pool_map(c->geom, c->cfg.layers, (int64_t)c->cfg.num_pages * c->cfg.page_size, c->pool, &c->chunk_map))
+        return cuda_fail(c, cudaErrorInvalidValue);
+      c->chunk_map_ok = true;
+    }
+    BC_CUDA(c, bc_launch_chunk(c->meta, c->geom, a, c->chunk_map, c->sm_count, s));
+  }
+  c->launches += 1;
+  c->meta_unsettled = false;   // an ordinarily launched kernel: it starts after everything before it has ended
+  return BC_OK;
+}
+}  // namespace
+
+bc_status bc_chunk_attn(bc_cache* c, int32_t layer, const int32_t* slots, const int32_t* first, const int32_t* cu_q, int32_t n,
+                        int32_t total_q, const void* q, void* out, float sm_scale, void* stream) {
+  const bc_status st = check_chunk(c, layer, slots, cu_q, n, total_q, q, out, sm_scale);
+  if (st || total_q == 0) return st;
+  return chunk_impl(c, layer, slots, first, cu_q, n, total_q, q, out, sm_scale, (cudaStream_t)stream);
+}
+
+bc_status bc_prefill_chunk(bc_cache* c, int32_t layer, const int32_t* slots, const int32_t* first, const int32_t* cu_chunk, int32_t n,
+                           int32_t total, const void* q, const void* k, const void* v, void* out, float sm_scale, void* stream) {
+  const bc_status st = check_chunk(c, layer, slots, cu_chunk, n, total, q, out, sm_scale);
+  if (st) return st;
+  if (!first) return BC_ERR_INVALID_ARG;
+  if (total == 0) return BC_OK;
+  if (!k || !v || !aligned16(k) || !aligned16(v)) return BC_ERR_INVALID_ARG;
+  cudaStream_t s = (cudaStream_t)stream;
+  BC_CUDA(c, bc_launch_prefill(c->meta, c->geom, layer_base(c, layer), slots, cu_chunk, n, total, k, v, s, first));
+  c->launches += 1;
+  c->meta_unsettled = false;
+  return chunk_impl(c, layer, slots, first, cu_chunk, n, total, q, out, sm_scale, s);
+}
+
+bc_status bc_norm_rope_decode_step(bc_cache* c, int32_t layer, const int32_t* slots, int32_t n, const void* qkv,
+                                   const int32_t* positions, float theta, const void* q_weight, const void* k_weight, float eps,
+                                   void* out, float sm_scale, void* stream) {
+  bc_status st = check_batch(c, layer, slots, n);
+  if (st) return st;
+  if (n > BC_MAX_ATTN_BATCH || !out || !aligned16(out)) return BC_ERR_INVALID_ARG;
+  if (layer != c->append_next_layer) return BC_ERR_ORDER;
+  uint8_t* q = work_ptr<uint8_t>(c, c->wl.rope_stage);
+  uint8_t* k = q + (size_t)n * c->cfg.q_heads * c->cfg.head_dim * 2;
+  uint8_t* v = k + (size_t)n * c->cfg.kv_heads * c->cfg.head_dim * 2;
+  st = bc_norm_rope_split(n, c->cfg.q_heads, c->cfg.kv_heads, c->cfg.head_dim, qkv,
+                          (int64_t)(c->cfg.q_heads + 2 * c->cfg.kv_heads) * c->cfg.head_dim, positions, theta, q_weight, k_weight, eps,
+                          q, k, v, stream);
+  if (st) return st;
+  c->launches += 1;
+  c->meta_unsettled = false;
   return bc_decode_step(c, layer, slots, n, q, k, v, out, sm_scale, stream);
 }
 
@@ -1193,6 +1276,7 @@ bc_status bc_clear_error(bc_cache* c, void* stream) {
   BC_CUDA(c, cudaMemsetAsync(c->meta.status, 0, 16, (cudaStream_t)stream));
   // an attention launch that gave up (BC_ERR_TIMEOUT) may have left ticket counters non-zero
   BC_CUDA(c, cudaMemsetAsync(c->work + c->wl.tickets, 0, (size_t)BC_MAX_ATTN_BATCH * 4 * c->cfg.layers, (cudaStream_t)stream));
+  BC_CUDA(c, cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream));
   // The counters of the built-in array are shared by every cache of the process: they are touched
   // only when THIS cache has used the static entry point since its last clear (a launch of its own
   // may have left them non-zero), never on behalf of a cache that did not.

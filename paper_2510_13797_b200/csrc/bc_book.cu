@@ -334,13 +334,18 @@ __global__ void k_write_rows(BcMeta m, BcGeom g, uint8_t* __restrict__ pool_laye
 // One block per prompt token of the packed [total, kv_heads, head_dim] input.
 __global__ void k_prefill(BcMeta m, BcGeom g, uint8_t* __restrict__ pool_layer, const int32_t* __restrict__ slots,
                           const int32_t* __restrict__ cu, int n, const uint8_t* __restrict__ k,
-                          const uint8_t* __restrict__ v) {
+                          const uint8_t* __restrict__ v, const int32_t* __restrict__ first) {
   const int tok = blockIdx.x;
   __shared__ int sh_row, sh_pos;
   if (threadIdx.x == 0) {
     int lo = 0, hi = n;  // largest s with cu[s] <= tok
     while (hi - lo > 1) { int mid = (lo + hi) >> 1; if (cu[mid] <= tok) lo = mid; else hi = mid; }
-    const int slot = slots[lo], pos = tok - cu[lo];
+    const int slot = slots[lo];
+    int pos = tok - cu[lo];
+    if (first != nullptr) {   // a chunk of a prompt: item lo's rows go to positions first[lo], first[lo] + 1, ...
+      const long long at = (long long)first[lo] + pos;
+      pos = cu[lo] <= tok && tok < cu[lo + 1] && at >= 0 && at < 0x7fffffff ? (int)at : 0x7fffffff;
+    }
     int row = -1;
     if (slot >= 0 && slot < m.max_seqs && m.open[slot] && pos < m.prompt_len[slot]) {
       const int col = pos / g.page_size;
@@ -599,9 +604,10 @@ cudaError_t bc_launch_write_rows(const BcMeta& m, const BcGeom& g, uint8_t* pool
   return cudaGetLastError();
 }
 cudaError_t bc_launch_prefill(const BcMeta& m, const BcGeom& g, uint8_t* pool_layer, const int32_t* slots,
-                              const int32_t* cu, int n, int total, const void* k, const void* v, cudaStream_t s) {
+                              const int32_t* cu, int n, int total, const void* k, const void* v, cudaStream_t s,
+                              const int32_t* first) {
   if (total == 0) return cudaSuccess;
-  k_prefill<<<total, copy_threads(g), 0, s>>>(m, g, pool_layer, slots, cu, n, (const uint8_t*)k, (const uint8_t*)v);
+  k_prefill<<<total, copy_threads(g), 0, s>>>(m, g, pool_layer, slots, cu, n, (const uint8_t*)k, (const uint8_t*)v, first);
   return cudaGetLastError();
 }
 cudaError_t bc_launch_restore_book(const BcMeta& m, const int32_t* slots, const int32_t* cu, int n, int64_t call, int32_t* ok,

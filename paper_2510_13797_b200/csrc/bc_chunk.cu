@@ -1,0 +1,801 @@
+// Attention of a chunk of new tokens of every sequence over the paged, segmented (prompt | beacons | window) store.
+//
+// Item i of the batch brings m_i = cu_q[i + 1] - cu_q[i] query rows; row r sees the first first_i + r + 1 live entries
+// of its sequence in logical order (all of them where there are fewer):
+//     out[r, h] = softmax_j(sm_scale <q[r, h], K_j>) V_j,   j < min(first_i + r + 1, live_i),
+// zeros where that is nothing.  That is the attention of a prompt chunk behind the entries stored before it, and of
+// the last m_i entries of a window (several guessed tokens checked at once).
+//
+// k_chunk_attn runs on the tcgen05 tensor cores, with the structure of the mask-form kernel (bc_mask_attn.cu): 128
+// query rows = floor(128 / G) tokens times the G query heads of a KV head against tiles of 128 keys, S = Q K^T into
+// tensor memory, softmax by one thread per row, P as bf16 back into tensor memory, O += P V.  What differs:
+//   * Keys come from pages.  The live entries lie in a virtual row space, prompt from 0, beacons and window each from
+//     the next multiple of the copy height, so that (row & 7) equals the entry's position in its segment modulo 8:
+//     the store's chunk permutation IS the 128-byte swizzle of the product's operand layout, and unswizzled tensor
+//     copies of up to 16 entries of one page (64 of the head's coordinates each) put a tile together, K and V alike.
+//     The copy height R is the largest power of two up to 16 that divides the page size, so no copy crosses a page.
+//   * The key tiles of all (sequence, KV head, query tile) units form one line that is cut into equal spans, one per
+//     thread block: a unit that is cut leaves unnormalised partial results (m, l, O) per row in the workspace,
+//     and the block that takes the unit's last ticket joins them in the order of the keys, so results do not depend
+//     on which block that is.  Few rows over a long cache are spread over all SMs this way, and a large
+//     prompt chunk ends everywhere at the same time.
+//   * Every block works the line out from the lengths on the device by itself: no host copy of a length, no plan
+//     kernel, and the call can be captured.
+// Bounds: at many rows per key the tensor pipe and the exponentials (as the mask form), at few rows the reads of the
+// cache; one tile of a block's work is 64 KB of K and V and 8.4 MFLOP.
+//
+// Entries that no row of a query tile can see are not read into a product: their scores are overwritten with -inf, and
+// V rows that are past the last visible entry of the tile are cleared in shared memory, so that whatever the
+// pool holds there (it is never initialised) cannot reach a result.  Every wait is bounded; on expiry the block
+// records BC_ERR_TIMEOUT, waits for what it has in flight, releases its tensor memory and returns.
+//
+// k_chunk_reference is the simple form behind BC_FLAG_ATTN_REFERENCE: one warp per query row and head.
+#include <cuda.h>
+
+#include "bc_common.cuh"
+
+namespace {
+
+#include "bc_tc.cuh"
+#include "bc_book_device.cuh"
+
+constexpr int kRowThreads = 128;               // one per query row
+constexpr int kThreads = kRowThreads + 32;     // plus the control warp
+constexpr int kMaxItems = BC_MAX_ATTN_BATCH;
+
+// ---- the simple form -----------------------------------------------------------------------------------------------
+// item of packed row `row`: the largest i with cu[i] <= row; false if the row belongs to none
+__device__ __forceinline__ bool find_item(const int32_t* cu, int n, int row, int* item) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (cu[mid] <= row) lo = mid; else hi = mid; }
+  *item = lo;
+  return cu[lo] <= row && row < cu[lo + 1];
+}
+
+__global__ void k_chunk_reference(BcMeta m, BcGeom g, BcChunkArgs a) {
+  const int row = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+  const int D = g.head_dim, per = D / 32, kvh = h / (g.q_heads / g.kv_heads);
+  int i;
+  if (!find_item(a.cu_q, a.n, row, &i)) return;
+  const int slot = a.slots[i], len = a.cu_q[i + 1] - a.cu_q[i];
+  int P = 0, nb = 0, w = 0;
+  if (slot >= 0 && slot < m.max_seqs && m.open[slot]) { P = m.prompt_len[slot]; nb = m.n_beacons[slot]; w = m.window_len[slot]; }
+  const int live = P + nb + w;
+  const long long first = a.first != nullptr ? a.first[i] : live - len;
+  const long long vis = min((long long)live, max(0ll, first + (row - a.cu_q[i]) + 1));
+  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q) + ((int64_t)row * g.q_heads + h) * D;
+  float qv[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int e = 0; e < per; ++e) qv[e] = __bfloat162float(q[lane * per + e]);
+  float mrun = -INFINITY, lrun = 0.f;
+  for (int e = 0; e < (int)vis; ++e) {
+    int pos, col;
+    if (e < P) { pos = e; col = 0; }
+    else if (e < P + nb) { pos = e - P; col = m.beacon_off[slot]; }
+    else { pos = e - P - nb; col = m.window_off[slot]; }
+    col += pos / g.page_size;
+    int page = 0;
+    if (!m.debug || (unsigned)col < (unsigned)m.max_pages_per_seq) page = m.page_table[(int64_t)slot * m.max_pages_per_seq + col];
+    if (m.debug && (unsigned)page >= (unsigned)m.num_pages) page = 0;
+    const uint8_t* at = a.pool_layer + ((int64_t)page * g.page_size + pos % g.page_size) * g.entry_bytes;
+    const __nv_bfloat16* kp = reinterpret_cast<const __nv_bfloat16*>(at + kvh * g.head_row_bytes);
+    const __nv_bfloat16* vp = reinterpret_cast<const __nv_bfloat16*>(at + (g.kv_heads + kvh) * g.head_row_bytes);
+    float dot = 0.f, vv[4];
+    for (int x = 0; x < per; ++x) {
+      const int d = lane * per + x, idx = (((d >> 3) ^ (pos & 7)) << 3) + (d & 7);
+      dot += qv[x] * __bfloat162float(kp[idx]);
+      vv[x] = __bfloat162float(vp[idx]);
+    }
+    for (int s = 16; s; s >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, s);
+    const float sc = dot * a.sm_scale;
+    const float mn = fmaxf(mrun, sc);
+    const float al = expf(mrun - mn), pe = expf(sc - mn);
+    lrun = lrun * al + pe;
+    for (int x = 0; x < per; ++x) acc[x] = acc[x] * al + pe * vv[x];
+    mrun = mn;
+  }
+  for (int x = 0; x < per; ++x) {
+    const float val = lrun > 0.f ? acc[x] / lrun : 0.f;
+    const int64_t o = ((int64_t)row * g.q_heads + h) * D + lane * per + x;
+    if (a.out_f32) reinterpret_cast<float*>(a.out)[o] = val;
+    else reinterpret_cast<__nv_bfloat16*>(a.out)[o] = __float2bfloat16_rn(val);
+  }
+}
+
+// ---- the tensor-core form ------------------------------------------------------------------------------------------
+struct ChunkParams {
+  BcMeta m;
+  const int32_t *slots, *first, *cu_q;
+  int32_t n, total_q;
+  void* out;
+  int32_t out_f32, layer;
+  float* part_o;      // [2 grid][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
+  float* part_ml;     // [2 grid][2][128]
+  int32_t* tickets;   // [grid], by the block that begins the unit; zero between launches
+  int32_t Hq, Hkv, G, page_size;
+  int32_t tokens;     // per query tile: 128 / G
+  int32_t R;          // entries per copy, 2^k <= 16
+  int32_t align;      // segment starts in the virtual row space: max(8, R)
+  int32_t min_span;   // key tiles a block works on at least
+  uint32_t wait_limit;
+  float scale_log2;
+};
+
+// Lengths of the items, in shared memory (structure of arrays).
+struct Items {
+  int m[kMaxItems], first[kMaxItems], P[kMaxItems], nb[kMaxItems], w[kMaxItems];
+  long long before[kMaxItems + 1];   // key tiles of one KV head in the items before
+  int large[64], n_large;            // items whose tiles all threads count together
+  long long total, span;
+  int item0, head0, tile0;           // where this block's span begins
+  int n0;
+};
+
+// One unit: the query tile `t` of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
+struct Unit {
+  int i, h, t;
+  int count, vis_last;     // tokens in the tile; entries its last token sees
+  int P, nb, w, base;      // lengths of the sequence; base: entries the tile's first token sees, minus 1
+  int n0, n1, N;
+};
+// Entries `vis` of a sequence as intervals of the virtual row space: [0, p), [b0, b0 + b), [w0, w0 + w).
+struct Seen {
+  int p, b0, b, w0, w;
+};
+__device__ __forceinline__ Seen seen_of(int vis, int P, int nb, int w, int align) {
+  Seen s;
+  s.b0 = (P + align - 1) & -align;
+  s.w0 = s.b0 + ((nb + align - 1) & -align);
+  s.p = min(vis, P);
+  s.b = min(max(vis - P, 0), nb);
+  s.w = min(max(vis - P - nb, 0), w);
+  return s;
+}
+__device__ __forceinline__ int virtual_end(const Seen& s) { return s.w > 0 ? s.w0 + s.w : (s.b > 0 ? s.b0 + s.b : s.p); }
+__device__ __forceinline__ int clamp_vis(int first, int r, int live) {   // entries that row r of an item sees
+  return (int)min((long long)live, max(0ll, (long long)first + r + 1));
+}
+__device__ __forceinline__ int key_tiles(const Items& it, int i, int t, int tokens, int align) {
+  const int last = min((t + 1) * tokens, it.m[i]) - 1;
+  const int vis = clamp_vis(it.first[i], last, it.P[i] + it.nb[i] + it.w[i]);
+  return max(1, (virtual_end(seen_of(vis, it.P[i], it.nb[i], it.w[i], align)) + kTile - 1) / kTile);
+}
+__device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, int n0, long long left, int tokens, int align) {
+  Unit u;
+  u.i = i; u.h = h; u.t = t; u.n0 = n0;
+  u.P = it.P[i]; u.nb = it.nb[i]; u.w = it.w[i];
+  u.count = min(tokens, it.m[i] - t * tokens);
+  const int live = u.P + u.nb + u.w;
+  u.vis_last = clamp_vis(it.first[i], t * tokens + u.count - 1, live);
+  u.base = it.first[i] + t * tokens;
+  u.N = key_tiles(it, i, t, tokens, align);
+  u.n1 = (int)min((long long)u.N, n0 + left);
+  return u;
+}
+// The unit behind u on the line (there is one: the caller knows how many key tiles are left).
+__device__ __forceinline__ Unit next_unit(const Items& it, const Unit& u, long long left, int Hkv, int tokens, int align) {
+  int i = u.i, h = u.h, t = u.t + 1;
+  if (t * tokens >= it.m[i]) {
+    t = 0;
+    if (++h == Hkv) {
+      h = 0;
+      do ++i; while (it.m[i] == 0);
+    }
+  }
+  return make_unit(it, i, h, t, 0, left, tokens, align);
+}
+
+// 128-bit mask (bit j of word j / 32: column j of the tile) of the tile's columns inside [lo, hi) of the virtual space
+__device__ __forceinline__ void add_range(uint32_t (&mask)[4], int lo, int hi) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int l = min(max(lo - 32 * q, 0), 32), e = min(max(hi - 32 * q, 0), 32);
+    if (e > l) mask[q] |= (e - l == 32 ? 0xffffffffu : ((1u << (e - l)) - 1u)) << l;
+  }
+}
+__device__ __forceinline__ void tile_mask(uint32_t (&mask)[4], const Seen& s, int k0) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) mask[q] = 0;
+  add_range(mask, -k0, s.p - k0);
+  add_range(mask, s.b0 - k0, s.b0 + s.b - k0);
+  add_range(mask, s.w0 - k0, s.w0 + s.w - k0);
+}
+
+// What the control warp needs to issue a tile's copies.  Lane l holds the copies l, l + 32, ... of the tile's 128 / R.
+template <int KP>
+struct TileIssue {
+  int page[KP], rem[KP];     // page id and first entry inside the page
+  uint32_t valid[KP];        // ballots: which copies there are
+  int h, qrow;               // KV head; packed row of the unit's first token, -1: same unit as the tile before
+};
+
+__device__ __forceinline__ void tma_pool(uint32_t dst, const CUtensorMap* map, int head_half, int row, int layer, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(head_half), "r"(row), "r"(layer), "r"(bar)
+      : "memory");
+}
+
+// D: head_dim.  KP: copies per lane, tensor and tile (1 for pages that are a multiple of 4 entries, else 4).
+// Barriers and the order of products are those of bc_mask_attn.cu.
+template <int D, int KP, bool SHORTW>
+__global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
+                                                           const __grid_constant__ CUtensorMap pool_map) {
+  constexpr int kHalves = D / 64;
+  constexpr int kHalfBytes = kTile * 128;                  // 128 rows of 64 coordinates
+  constexpr int kOperandBytes = kHalves * kHalfBytes;
+  constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sQ = smem_addr(smem), sK = sQ + kOperandBytes, sV = sK + kOperandBytes;
+  Items& it = *reinterpret_cast<Items*>(smem + 3 * kOperandBytes);
+  __shared__ __align__(8) uint64_t s_bars[9];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail_word, s_ticket;
+  volatile int* s_fail = &s_fail_word;
+  const uint32_t bar_k = smem_addr(&s_bars[0]), bar_in = bar_k + 8, bar_s = bar_k + 16, bar_p = bar_k + 24, bar_o = bar_k + 32,
+                 bar_f = bar_k + 40, bar_e = bar_k + 48, bar_d = bar_k + 56,
+                 bar_r = bar_k + 64;   // bar_r: the row threads among themselves (bounded, unlike a block barrier)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.G, Hq = a.Hq, Hkv = a.Hkv, tokens = a.tokens, align = a.align;
+
+  if (tid == 0) {
+    const uint32_t counts[9] = {1, 2, 1, (uint32_t)kRowThreads, 1, 1, (uint32_t)kRowThreads, 1, (uint32_t)kRowThreads};
+    for (int i = 0; i < 9; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar_k + i * 8), "r"(counts[i]) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    *s_fail = 0;
+    it.n_large = 0;
+  }
+  __syncthreads();
+
+  // ---- the line: every item's lengths, its key tiles per KV head, and where this block's span begins ------------------
+  for (int i = tid; i < a.n; i += kThreads) {
+    const int slot = a.slots[i], c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
+    int P = 0, nb = 0, w = 0;
+    if (slot >= 0 && slot < a.m.max_seqs && a.m.open[slot]) { P = a.m.prompt_len[slot]; nb = a.m.n_beacons[slot]; w = a.m.window_len[slot]; }
+    const int m = c0 < 0 || c0 > a.total_q ? 0 : max(0, min(c1, a.total_q) - c0);
+    const int first = a.first != nullptr ? a.first[i] : P + nb + w - m;
+    it.m[i] = m; it.first[i] = min(max(first, -(1 << 30)), 1 << 30); it.P[i] = P; it.nb[i] = nb; it.w[i] = w;
+    const int tiles = (m + tokens - 1) / tokens;
+    long long cost = 0;
+    bool mine = true;
+    if (tiles > 8) {                                        // a long chunk: counted by all threads below
+      const int at = atomicAdd(&it.n_large, 1);
+      if (at < 64) { it.large[at] = i; mine = false; }
+    }
+    if (mine)
+      for (int t = 0; t < tiles; ++t) cost += key_tiles(it, i, t, tokens, align);
+    it.before[i + 1] = cost;
+  }
+  __syncthreads();
+  const int n_large = min(it.n_large, 64);
+  for (int x = 0; x < n_large; ++x) {
+    const int i = it.large[x], tiles = (it.m[i] + tokens - 1) / tokens;
+    long long cost = 0;
+    for (int t = tid; t < tiles; t += kThreads) cost += key_tiles(it, i, t, tokens, align);
+    atomicAdd(reinterpret_cast<unsigned long long*>(&it.before[i + 1]), (unsigned long long)cost);
+  }
+  __syncthreads();
+  if (warp == 0) {
+    long long carry = 0;
+    for (int i0 = 0; i0 < a.n; i0 += 32) {
+      const int i = i0 + lane;
+      long long x = i < a.n ? it.before[i + 1] : 0;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (i < a.n) it.before[i + 1] = carry + x;
+      carry += __shfl_sync(0xffffffffu, x, 31);
+    }
+    const long long total = carry * Hkv;
+    long long span = (total + gridDim.x - 1) / gridDim.x;
+    if (span < a.min_span) span = a.min_span;
+    if (lane == 0) { it.before[0] = 0; it.total = total; it.span = span; }
+    __syncwarp();
+    const long long x0 = (long long)blockIdx.x * span;
+    if (x0 < total) {
+      int lo = 0, hi = a.n;                                 // the item: largest i with before[i] * Hkv <= x0 (a non-empty one)
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (it.before[mid] * Hkv <= x0) lo = mid; else hi = mid; }
+      const long long cost = it.before[lo + 1] - it.before[lo], rest = x0 - it.before[lo] * Hkv;
+      const int head = (int)(rest / cost);
+      long long in_head = rest - head * cost;
+      int t = 0;                                            // the query tile: 32 at a time
+      for (;; t += 32) {
+        const int tt = t + lane;
+        int x = tt * tokens < it.m[lo] ? key_tiles(it, lo, tt, tokens, align) : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, d);
+          if (lane >= d) x += y;
+        }
+        const uint32_t over = __ballot_sync(0xffffffffu, x > in_head);
+        if (over) {
+          const int l = __ffs(over) - 1;
+          const int before = __shfl_sync(0xffffffffu, x, l > 0 ? l - 1 : 0);
+          t += l;
+          if (l > 0) in_head -= before;
+          break;
+        }
+        in_head -= __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) { it.item0 = lo; it.head0 = head; it.tile0 = t; it.n0 = (int)in_head; }
+    }
+  }
+  __syncthreads();
+  const long long x_begin = (long long)blockIdx.x * it.span;
+  const long long x_end = min(it.total, x_begin + it.span);
+  if (x_begin >= x_end) return;                             // nothing to do: no tensor memory has been taken yet
+
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(256) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // Rows of the Q buffer that no tensor copy writes (only when G does not divide 128) stay zero.
+  const int box_rows = tokens * G;
+  for (int idx = tid; idx < (kTile - box_rows) * (D / 8); idx += kThreads) st_zero16(sQ + swz(box_rows + idx / (D / 8), idx % (D / 8)));
+  proxy_fence();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const uint32_t tS = tmem, tO = tmem + kTile, tP = tS;     // columns [0, 128): S, then P in its first 64; [128, 128 + D): O
+  const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align);
+
+  if (warp == kRowThreads / 32) {
+    // ======================================= control warp ===========================================
+    const int R = a.R, copies = kTile / R;
+    // cursor of the look-ahead: the tile whose copies are worked out next
+    Unit lu = u0;
+    int ln = u0.n0;
+    long long lx = x_begin;                                 // position of (lu, ln) on the line
+    bool fresh = true;                                      // the first tile of lu has not been handed out yet
+    const int32_t* table = nullptr;
+    int boff = 0, woff = 0;
+    Seen lseen = {};
+    auto look = [&]() {                                     // the tile at the cursor; the page ids' loads are left in flight
+      TileIssue<KP> ti;
+      if (fresh) {
+        const int slot = a.slots[lu.i];
+        // a slot that is not open has no live entry: no copy is valid and nothing below is read
+        if (lu.vis_last > 0) {
+          boff = a.m.beacon_off[slot]; woff = a.m.window_off[slot];
+          table = a.m.page_table + (int64_t)slot * a.m.max_pages_per_seq;
+        }
+        lseen = seen_of(lu.vis_last, lu.P, lu.nb, lu.w, align);
+      }
+      ti.h = lu.h;
+      ti.qrow = fresh ? a.cu_q[lu.i] + lu.t * tokens : -1;
+#pragma unroll
+      for (int c = 0; c < KP; ++c) {
+        const int p = lane + 32 * c, v = ln * kTile + p * R;   // first virtual row of the copy
+        int pos = -1, col = 0;
+        if (p < copies) {
+          if (v < lseen.p) pos = v;
+          else if (v >= lseen.b0 && v < lseen.b0 + lseen.b) { pos = v - lseen.b0; col = boff; }
+          else if (v >= lseen.w0 && v < lseen.w0 + lseen.w) { pos = v - lseen.w0; col = woff; }
+        }
+        ti.valid[c] = __ballot_sync(0xffffffffu, pos >= 0);
+        ti.page[c] = 0; ti.rem[c] = 0;
+        if (pos >= 0) {
+          const int pg = pos / a.page_size;
+          col += pg;
+          ti.rem[c] = pos - pg * a.page_size;
+          if (a.m.debug && (unsigned)col >= (unsigned)a.m.max_pages_per_seq) { debug_note(a.m, col); col = 0; }
+          ti.page[c] = table[col];
+        }
+      }
+      fresh = false;
+      ++lx;
+      if (++ln == lu.n1 && lx < x_end) {
+        lu = next_unit(it, lu, x_end - lx, Hkv, tokens, align);
+        ln = lu.n0;
+        fresh = true;
+      }
+      return ti;
+    };
+    const uint32_t q_bytes = (uint32_t)(box_rows * D * 2);
+    auto copy_bytes = [&](const TileIssue<KP>& ti) {
+      int c = 0;
+#pragma unroll
+      for (int k = 0; k < KP; ++k) c += __popc(ti.valid[k]);
+      return (uint32_t)(c * R * D * 2);
+    };
+    auto issue_q = [&](const TileIssue<KP>& ti, uint32_t bar) {   // one lane
+#pragma unroll
+      for (int s = 0; s < kHalves; ++s) tma_3d(sQ + s * kHalfBytes, &q_map, s * 64, ti.h * G, ti.qrow, bar);
+    };
+    auto issue_kv = [&](const TileIssue<KP>& ti, int which, uint32_t dst, uint32_t bar) {   // every lane its copies
+#pragma unroll
+      for (int c = 0; c < KP; ++c) {
+        if (ti.valid[c] >> lane & 1) {
+          const int p = lane + 32 * c;
+          int page = ti.page[c];
+          if (a.m.debug && (unsigned)page >= (unsigned)a.m.num_pages) { debug_note(a.m, page); page = 0; }
+#pragma unroll
+          for (int s = 0; s < kHalves; ++s)
+            tma_pool(dst + s * kHalfBytes + p * R * 128, &pool_map, (which * Hkv + ti.h) * kHalves + s, page * a.page_size + ti.rem[c], a.layer, bar);
+        }
+      }
+      __syncwarp();
+    };
+    const uint64_t dQ = umma_desc(sQ), dK = umma_desc(sK), dV = umma_desc_nmajor(sV);
+    auto qk = [&]() {
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
+        umma(tS, dQ + off, dK + off, kk > 0);
+      }
+    };
+    auto wait_all = [&](uint32_t bar, uint32_t parity) {
+      const bool ok1 = mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit);
+      return __all_sync(0xffffffffu, ok1);
+    };
+    long long x = x_begin;
+    TileIssue<KP> cur = look(), nxt = {};
+    if (elect_one()) {
+      mbar_expect_tx(bar_k, q_bytes + copy_bytes(cur));
+      issue_q(cur, bar_k);
+    }
+    __syncwarp();
+    issue_kv(cur, 0, sK, bar_k);
+    if (elect_one()) mbar_expect_tx(bar_in, copy_bytes(cur));
+    __syncwarp();
+    issue_kv(cur, 1, sV, bar_in);
+    if (x + 1 < x_end) nxt = look();
+    bool first_out = true, in_open = true, products_issued = false;
+    uint32_t n_in = 1;
+    uint32_t ph_o = 0, t = 0, e = 0;
+    bool ok = wait_all(bar_k, 0);
+    if (ok) first_out = false;
+    if (ok) {
+      products_issued = true;
+      tc_fence_after();
+      if (elect_one()) { qk(); umma_commit(bar_s); }
+      __syncwarp();
+    }
+    Unit u = u0;
+    for (; ok; ++e) {
+      const Seen seen = seen_of(u.vis_last, u.P, u.nb, u.w, align);
+      for (int n = u.n0; n < u.n1 && ok; ++n, ++t, ++x) {
+        ok = wait_all(bar_s, t & 1u);                                        // S exists: the K buffer is free
+        if (!ok) break;
+        const bool last = n + 1 == u.n1, more = x + 1 < x_end;
+        TileIssue<KP> ahead = {};
+        if (more) {
+          if (elect_one()) {
+            mbar_expect_tx(bar_in, copy_bytes(nxt) + (nxt.qrow >= 0 ? q_bytes : 0u));
+            if (nxt.qrow >= 0) issue_q(nxt, bar_in);                          // the last product with this Q is done
+          }
+          __syncwarp();
+          issue_kv(nxt, 0, sK, bar_in);
+          if (x + 2 < x_end) ahead = look();
+        } else if (elect_one()) {
+          mbar_arrive_cta(bar_in);
+        }
+        __syncwarp();
+        in_open = false;
+        ok = wait_all(bar_in, t & 1u);
+        if (ok) {
+          // V rows of the tile that hold no entry the unit can see (unwritten entries of the last page, gaps between
+          // segments, rows that no copy wrote): cleared, since a weight of 0 does not cancel a NaN
+          uint32_t mask[4];
+          tile_mask(mask, seen, n * kTile);
+          if ((mask[0] & mask[1] & mask[2] & mask[3]) != 0xffffffffu) {
+            for (int idx = lane; idx < kTile * (D / 8); idx += 32) {
+              const int row = idx / (D / 8);
+              const uint32_t word = row < 64 ? (row < 32 ? mask[0] : mask[1]) : (row < 96 ? mask[2] : mask[3]);
+              if (!(word >> (row & 31) & 1)) st_zero16(sV + swz(row, idx % (D / 8)));
+            }
+            proxy_fence();
+            __syncwarp();
+          }
+        }
+        if (ok && n == u.n0 && e > 0) ok = wait_all(bar_e, (e - 1) & 1u);     // the rows have read the last O
+        ok = ok && wait_all(bar_p, t & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            umma_ts<kIdescPV>(tO, tP + (uint32_t)(kk * 8), dV + (uint64_t)((kk * 16 * 128) >> 4), (n > u.n0 || kk > 0) ? 1u : 0u);
+          if (last) umma_commit(bar_f);
+          if (more) {
+            umma_commit(bar_o);
+            qk();
+            umma_commit(bar_s);
+          }
+        }
+        __syncwarp();
+        if (more) {
+          ok = wait_all(bar_o, ph_o);                                         // the V buffer is free
+          ph_o ^= 1;
+          if (!ok) break;
+          if (elect_one()) mbar_expect_tx(bar_in, copy_bytes(nxt));
+          __syncwarp();
+          issue_kv(nxt, 1, sV, bar_in);
+          in_open = true; ++n_in;
+          cur = nxt; nxt = ahead;
+        }
+      }
+      if (!ok || x >= x_end) break;
+      u = next_unit(it, u, x_end - x, Hkv, tokens, align);
+    }
+    if (!ok) {
+      // Giving up: wait, with the full limit, for the copies and the products in flight (as in bc_mask_attn.cu).
+      *s_fail = 1;
+      __syncwarp();
+      if (elect_one()) {
+        int never = 0;
+        if (in_open) mbar_arrive_cta(bar_in);
+        if (first_out) mbar_wait_or_fail<false>(bar_k, 0, &never, kWaitLimit);
+        mbar_wait_or_fail<false>(bar_in, (n_in - 1) & 1u, &never, kWaitLimit);
+        if (products_issued) {
+          umma_commit(bar_d);
+          mbar_wait_or_fail<false>(bar_d, 0, &never, kWaitLimit);
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ========================================= row threads ==========================================
+    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    const int my_local = tid / G, my_head = tid % G;
+    constexpr float kMaxSlack = 8.f;                          // as in bc_mask_attn.cu
+    bool failed = false;
+    uint32_t t = 0, e = 0, ph_r = 0;
+    auto rows_sync = [&]() {
+      mbar_arrive_cta(bar_r);
+      const bool ok = mbar_wait_or_fail<SHORTW>(bar_r, ph_r, s_fail, a.wait_limit);
+      ph_r ^= 1;
+      return (bool)__all_sync(0xffffffffu, ok);
+    };
+    long long x = x_begin;
+    Unit u = u0;
+    for (;; ++e) {
+      const bool row_valid = tid < u.count * G;
+      const bool warp_live = warp * 32 < u.count * G;         // a warp without a row only keeps the barriers' count
+      const int vis = row_valid ? clamp_vis(u.base, my_local, u.P + u.nb + u.w) : 0;
+      const Seen seen = seen_of(vis, u.P, u.nb, u.w, align);
+      const int out_row = a.cu_q[u.i] + u.t * tokens + my_local;
+      float m_ref = -INFINITY, l_run = 0.f;
+      for (int n = u.n0; n < u.n1; ++n, ++t) {
+        const bool ok = mbar_wait_or_fail<SHORTW>(bar_s, t & 1u, s_fail, a.wait_limit);
+        if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+        if (warp_live) {
+          tc_fence_after();
+          const int k0 = n * kTile;
+          const bool whole = !row_valid || k0 + kTile <= seen.p || (k0 >= seen.b0 && k0 + kTile <= seen.b0 + seen.b) ||
+                             (k0 >= seen.w0 && k0 + kTile <= seen.w0 + seen.w);
+          const bool all_visible = __all_sync(0xffffffffu, whole);
+          float s[kTile];
+#pragma unroll
+          for (int cb = 0; cb < 4; ++cb) tmem_ld32_async(tS + lane_base + cb * 32, s + cb * 32);
+          tmem_wait_ld();
+          if (!all_visible) {
+            uint32_t mask[4];
+            tile_mask(mask, seen, k0);
+#pragma unroll
+            for (int j = 0; j < kTile; ++j)
+              if (!(mask[j >> 5] >> (j & 31) & 1)) s[j] = -INFINITY;
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < kTile; j += 8) {
+            mx[0] = max3(mx[0], s[j], s[j + 1]); mx[1] = max3(mx[1], s[j + 2], s[j + 3]);
+            mx[2] = max3(mx[2], s[j + 4], s[j + 5]); mx[3] = max3(mx[3], s[j + 6], s[j + 7]);
+          }
+          const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;   // the scale is positive
+          float alpha = 1.f;
+          const bool raise = tile_max > m_ref + kMaxSlack || (m_ref == -INFINITY && tile_max > -INFINITY);
+          if (raise) {
+            alpha = fast_exp2(m_ref - tile_max);
+            m_ref = tile_max;
+            l_run *= alpha;
+          }
+          const float m_safe = m_ref == -INFINITY ? 0.f : m_ref;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int cb = 0; cb < 4; ++cb) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float p0 = fast_exp2(fmaf(s[cb * 32 + j], a.scale_log2, -m_safe));
+              const float p1 = fast_exp2(fmaf(s[cb * 32 + j + 1], a.scale_log2, -m_safe));
+              sum[(j >> 1) & 3] += p0 + p1;
+              const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: 2^-9 per weight
+              pk[j >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
+            }
+            tmem_st16(tP + lane_base + cb * 16, pk);
+          }
+          l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          if (n > u.n0 && __any_sync(0xffffffffu, raise)) {
+#pragma unroll 1
+            for (int cb = 0; cb < D / 32; ++cb) {
+              float v[32];
+              tmem_ld32_async(tO + lane_base + cb * 32, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) v[j] *= alpha;
+              tmem_st32(tO + lane_base + cb * 32, v);
+            }
+          }
+          tmem_wait_st();
+          tc_fence_before();
+        }
+        mbar_arrive_cta(bar_p);
+      }
+      if (failed) break;
+
+      // ---- the piece's result ---------------------------------------------------------------------------------------
+      const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
+      if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+      const bool complete = u.n0 == 0 && u.n1 == u.N;
+      auto store4 = [&](int64_t at, float x0, float x1, float x2, float x3, float x4, float x5, float x6, float x7) {
+        // eight results at element `at` of the output
+        if (a.out_f32) {
+          float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
+          dst[0] = make_float4(x0, x1, x2, x3);
+          dst[1] = make_float4(x4, x5, x6, x7);
+        } else {
+          const __nv_bfloat162 b0 = __floats2bfloat162_rn(x0, x1), b1 = __floats2bfloat162_rn(x2, x3), b2 = __floats2bfloat162_rn(x4, x5),
+                               b3 = __floats2bfloat162_rn(x6, x7);
+          *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) =
+              make_uint4(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1), *reinterpret_cast<const uint32_t*>(&b2),
+                         *reinterpret_cast<const uint32_t*>(&b3));
+        }
+      };
+      float o[D];
+      if (warp_live) {
+        tc_fence_after();
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + lane_base + cb * 32, o + cb * 32);
+        tmem_wait_ld();
+        tc_fence_before();
+      }
+      mbar_arrive_cta(bar_e);
+      if (complete) {
+        if (row_valid) {
+          const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);   // NaN stays NaN
+          const int64_t at = ((int64_t)out_row * Hq + u.h * G + my_head) * D;
+#pragma unroll
+          for (int d = 0; d < D; d += 8)
+            store4(at + d, o[d] * inv, o[d + 1] * inv, o[d + 2] * inv, o[d + 3] * inv, o[d + 4] * inv, o[d + 5] * inv, o[d + 6] * inv, o[d + 7] * inv);
+        }
+      } else {
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (u.n0 == 0 ? 1 : 0);
+        if (row_valid) {
+          float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (D / 4) * kTile + tid;
+#pragma unroll
+          for (int d = 0; d < D / 4; ++d) po[d * kTile] = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
+          a.part_ml[(slot * 2) * kTile + tid] = m_ref;
+          a.part_ml[(slot * 2 + 1) * kTile + tid] = l_run;
+        }
+        __threadfence();
+        if (!rows_sync()) { failed = true; break; }
+        // the unit's first block and number of pieces, from its place on the line
+        const long long x0 = x - u.n0;
+        const int b0 = (int)(x0 / it.span), pieces = (int)((x0 + u.N - 1) / it.span) - b0 + 1;
+        if (tid == 0) {
+          const int got = atomicAdd(a.tickets + b0, 1);
+          if (got == pieces - 1) a.tickets[b0] = 0;            // all have come: zero again for the next launch
+          s_ticket = got;
+        }
+        if (!rows_sync()) { failed = true; break; }
+        if (s_ticket == pieces - 1) {
+          __threadfence();
+          // the last to come joins the pieces, in the order of the keys: threads are spread over the rows there are
+          // and, where these are few, over the head's coordinates
+          const int rows = u.count * G;
+          int rows2 = 4;
+          while (rows2 < rows) rows2 <<= 1;                    // 4 .. 128
+          const int row = tid & (rows2 - 1), part = tid / rows2, parts = kRowThreads / rows2;
+          if (row < rows) {
+            auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
+            float m_all = -INFINITY;
+#pragma unroll 4
+            for (int j = 0; j < pieces; ++j) m_all = fmaxf(m_all, __ldcg(a.part_ml + (slot_of(j) * 2) * kTile + row));
+            const float m_safe = m_all == -INFINITY ? 0.f : m_all;
+            float l_all = 0.f;
+#pragma unroll 4
+            for (int j = 0; j < pieces; ++j)
+              l_all += __ldcg(a.part_ml + (slot_of(j) * 2 + 1) * kTile + row) * fast_exp2(__ldcg(a.part_ml + (slot_of(j) * 2) * kTile + row) - m_safe);
+            const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);
+            const int64_t at = ((int64_t)(a.cu_q[u.i] + u.t * tokens + row / G) * Hq + u.h * G + row % G) * D;
+            for (int d8 = part; d8 < D / 8; d8 += parts) {
+              float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
+#pragma unroll 4
+              for (int j = 0; j < pieces; ++j) {
+                const float f = fast_exp2(__ldcg(a.part_ml + (slot_of(j) * 2) * kTile + row) - m_safe);
+                const float4* po = reinterpret_cast<const float4*>(a.part_o) + (slot_of(j) * (D / 4) + 2 * d8) * kTile + row;
+                const float4 p = __ldcg(po), q = __ldcg(po + kTile);
+                lo.x = fmaf(p.x, f, lo.x); lo.y = fmaf(p.y, f, lo.y); lo.z = fmaf(p.z, f, lo.z); lo.w = fmaf(p.w, f, lo.w);
+                hi.x = fmaf(q.x, f, hi.x); hi.y = fmaf(q.y, f, hi.y); hi.z = fmaf(q.z, f, hi.z); hi.w = fmaf(q.w, f, hi.w);
+              }
+              store4(at + d8 * 8, lo.x * inv, lo.y * inv, lo.z * inv, lo.w * inv, hi.x * inv, hi.y * inv, hi.z * inv, hi.w * inv);
+            }
+          }
+        }
+      }
+      x += u.n1 - u.n0;
+      if (x >= x_end) break;
+      u = next_unit(it, u, x_end - x, Hkv, tokens, align);
+    }
+    if (failed) *s_fail = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (*s_fail && tid == 0) atomicCAS(a.m.status, 0, BC_ERR_TIMEOUT);
+  if (warp == 0) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256) : "memory");
+  }
+}
+
+template <int D, int KP, bool SHORTW>
+cudaError_t launch(const ChunkParams& p, const CUtensorMap& q_map, const CUtensorMap& pool_map, int grid, cudaStream_t s) {
+  const int smem = 3 * kTile * D * 2 + 1024 + (int)sizeof(Items);
+  const cudaError_t e = cudaFuncSetAttribute(k_chunk_attn<D, KP, SHORTW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  k_chunk_attn<D, KP, SHORTW><<<grid, kThreads, smem, s>>>(p, q_map, pool_map);
+  return cudaGetLastError();
+}
+
+// Entries per copy: the largest power of two up to 16 that divides the page size.
+int copy_height(int page_size) {
+  int r = 1;
+  while (r < 16 && page_size % (2 * r) == 0) r *= 2;
+  return r;
+}
+
+}  // namespace
+
+size_t bc_chunk_part_o_bytes(int head_dim) { return (size_t)2 * BC_MAX_CHUNK_CTAS * head_dim * kTile * 4; }
+size_t bc_chunk_part_ml_bytes() { return (size_t)2 * BC_MAX_CHUNK_CTAS * 2 * kTile * 4; }
+
+// Tensor map of the whole pool: (64 coordinates, K|V x head x half, row, layer), unswizzled: the store's own chunk
+// permutation is the swizzle.
+bool bc_chunk_pool_map(const BcGeom& g, int layers, int64_t rows, void* pool, CUtensorMap* map) {
+  if (!encode_tiled()) return false;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)(g.entry_bytes / 128), (cuuint64_t)rows, (cuuint64_t)layers};
+  const cuuint64_t strides[3] = {128, (cuuint64_t)g.entry_bytes, (cuuint64_t)g.layer_bytes};
+  const cuuint32_t box[4] = {64, 1, (cuuint32_t)copy_height(g.page_size), 1}, es[4] = {1, 1, 1, 1};
+  return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                        CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t bc_launch_chunk_reference(const BcMeta& m, const BcGeom& g, const BcChunkArgs& a, cudaStream_t s) {
+  k_chunk_reference<<<dim3(a.total_q, g.q_heads), 32, 0, s>>>(m, g, a);
+  return cudaGetLastError();
+}
+
+cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs& a, const CUtensorMap& pool_map, int sms, cudaStream_t s) {
+  ChunkParams p;
+  p.m = m;
+  p.slots = a.slots; p.first = a.first; p.cu_q = a.cu_q; p.n = a.n; p.total_q = a.total_q;
+  p.out = a.out; p.out_f32 = a.out_f32; p.layer = a.layer;
+  p.part_o = a.part_o; p.part_ml = a.part_ml; p.tickets = a.tickets;
+  p.Hq = g.q_heads; p.Hkv = g.kv_heads; p.G = g.q_heads / g.kv_heads; p.page_size = g.page_size;
+  p.tokens = kTile / p.G;
+  p.R = copy_height(g.page_size);
+  p.align = p.R > 8 ? p.R : 8;
+  p.min_span = 1;
+  p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
+  p.scale_log2 = a.sm_scale * 1.4426950408889634f;
+  if (!encode_tiled()) return cudaErrorNotSupported;
+  CUtensorMap q_map;
+  const cuuint64_t dims[3] = {(cuuint64_t)g.head_dim, (cuuint64_t)g.q_heads, (cuuint64_t)a.total_q};
+  const cuuint64_t strides[2] = {(cuuint64_t)g.head_dim * 2, (cuuint64_t)g.q_heads * g.head_dim * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tokens}, es[3] = {1, 1, 1};
+  if (encode_tiled()(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  const int grid = a.ctas > 0 ? a.ctas : (2 * sms < BC_MAX_CHUNK_CTAS ? 2 * sms : BC_MAX_CHUNK_CTAS);   // two resident blocks per SM
+  const bool wide = p.R >= 4;
+  if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
+    if (g.head_dim != 128) return cudaErrorNotSupported;
+    return wide ? launch<128, 1, true>(p, q_map, pool_map, grid, s) : launch<128, 4, true>(p, q_map, pool_map, grid, s);
+  }
+  if (g.head_dim == 128) return wide ? launch<128, 1, false>(p, q_map, pool_map, grid, s) : launch<128, 4, false>(p, q_map, pool_map, grid, s);
+  return wide ? launch<64, 1, false>(p, q_map, pool_map, grid, s) : launch<64, 4, false>(p, q_map, pool_map, grid, s);
+}

@@ -2,6 +2,7 @@
 // store layout helpers and the kernel launch wrappers implemented in the .cu files.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -11,6 +12,7 @@
 // Upper bounds the workspace is sized for.
 #define BC_MAX_ATTN_CTAS 304   // thread blocks of the decode-attention kernel
 #define BC_MAX_ATTN_BATCH 512  // sequences per bc_decode_attn call
+#define BC_MAX_CHUNK_CTAS 304  // thread blocks of the chunk-attention kernel
 #define BC_MERGE_ELEMS 4096    // q_heads * head_dim that fits the in-block merge buffer
 // The attention plan the append bookkeeping can leave for the fused decode step: BC_PLAN_HEADER ints
 // {n, total tiles, log2(rows per tile), -}, then seven arrays of BC_MAX_ATTN_BATCH (+1 for the last) ints:
@@ -92,7 +94,8 @@ cudaError_t bc_launch_restore_rows(const BcMeta& m, const BcGeom& g, uint8_t* po
                                    const int32_t* bea, const int32_t* cu, int n, int total_tokens, int total_beacons,
                                    const void* tok_k, const void* tok_v, const void* bea_k, const void* bea_v, cudaStream_t s);
 cudaError_t bc_launch_prefill(const BcMeta& m, const BcGeom& g, uint8_t* pool_layer, const int32_t* slots,
-                              const int32_t* cu, int n, int total, const void* k, const void* v, cudaStream_t s);
+                              const int32_t* cu, int n, int total, const void* k, const void* v, cudaStream_t s,
+                              const int32_t* first = nullptr);   // first: item i's rows go to prompt positions first[i] ...
 cudaError_t bc_launch_export(const BcMeta& m, const BcGeom& g, const uint8_t* pool_layer, int slot, void* k_out,
                              void* v_out, int capacity, cudaStream_t s);
 
@@ -144,6 +147,26 @@ struct BcFusedAppend {
 // the same launch appends the step's new entries first.  *launches gets the number of kernels.
 cudaError_t bc_launch_attn(const BcMeta& m, const BcGeom& g, const BcAttnArgs& a, const BcFusedAppend* fused,
                            cudaStream_t s, cudaEvent_t ev_start, cudaEvent_t ev_stop, int* launches);
+// ---- attention of a chunk of new tokens (bc_chunk.cu) ---------------------------------------------------------------
+struct BcChunkArgs {
+  uint8_t* pool_layer;
+  int32_t layer;
+  const int32_t *slots, *first, *cu_q;   // first: NULL = the item's last live entries
+  int32_t n, total_q;
+  const void* q;
+  void* out;
+  int32_t out_f32;
+  float sm_scale;
+  float *part_o, *part_ml;               // bc_chunk_part_o_bytes, bc_chunk_part_ml_bytes
+  int32_t* tickets;                      // [BC_MAX_CHUNK_CTAS], zero between launches
+  int32_t ctas;                          // 0: two per SM
+  uint32_t wait_limit;                   // 0: the default
+};
+size_t bc_chunk_part_o_bytes(int head_dim);
+size_t bc_chunk_part_ml_bytes();
+bool bc_chunk_pool_map(const BcGeom& g, int layers, int64_t rows, void* pool, CUtensorMap* map);
+cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs& a, const CUtensorMap& pool_map, int sms, cudaStream_t s);
+cudaError_t bc_launch_chunk_reference(const BcMeta& m, const BcGeom& g, const BcChunkArgs& a, cudaStream_t s);
 // Decoder-layer operators around the cache calls (bc_model_ops.cu).
 cudaError_t bc_launch_add_rmsnorm(const void* h, const void* delta, const void* weight, int n, int hidden, float eps, void* h_out,
                                   void* normed, cudaStream_t s);

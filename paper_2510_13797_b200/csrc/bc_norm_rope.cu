@@ -1,0 +1,336 @@
+// Norms of the query and key heads with the rotation in the same pass, and the gradient of both.
+//
+// Models that normalise every query and key head before the rotation put, between the QKV projection and the
+// attention, for each head x of D coordinates (bf16 in, fp32 arithmetic, ONE rounding to bf16 at the end):
+//     y = x / sqrt(mean(x^2) + eps) * w                (w: D weights shared by all query heads, D by all key heads)
+//     out = R(pos) y                                   (half-split rotation by pos * theta^(-2j/D), as bc_rope_split)
+// and the gradient, with g = d loss / d out, r = 1 / sqrt(mean(x^2) + eps):
+//     dy = R(pos)^T g,   dx = r (w dy - x r^2 mean(x w dy)),   dw = sum over rows and heads of x r dy.
+// Everything is bound by memory: the packed rows are read once and q, k, v written once (the gradient reads x and
+// g of the rotated heads and writes dx; v's gradient is a copy).
+//
+// A head is held by D / 16 lanes, each with 8 coordinates of the lower half and the 8 that they are paired with, so
+// the rotation needs no exchange and the norm D / 16 lanes' shuffles; a warp works on 32 / (D / 16) heads at a time.
+// A warp takes a whole row (or, while there are few rows, a share of its heads) and computes the row's D / 2 angles
+// itself, D / 64 per lane: the position times the frequency in turns, reduced to a fraction of a turn in double
+// precision (pos * theta^(-2j/D) reaches 10^5 radians, where single precision has lost the angle), then the sine and
+// cosine of that fraction in fp32.
+#include "bc_common.cuh"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
+  f[0] = bf_lo(v.x); f[1] = bf_hi(v.x); f[2] = bf_lo(v.y); f[3] = bf_hi(v.y);
+  f[4] = bf_lo(v.z); f[5] = bf_hi(v.z); f[6] = bf_lo(v.w); f[7] = bf_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// sum over the D / 16 lanes that hold a head
+template <int D>
+__device__ __forceinline__ float head_sum(float x) {
+#pragma unroll
+  for (int d = D / 32; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+  return x;
+}
+
+// Frequencies (in turns per position) of the angles this lane computes: D / 64 consecutive ones.
+template <int D>
+__device__ __forceinline__ void lane_frequencies(double log2_theta, double* f) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const int j = (int)(threadIdx.x & 31) * (D / 64) + i;
+    f[i] = exp2(-2.0 * (double)j / (double)D * log2_theta) * 0.15915494309189535;   // 1 / (2 pi)
+  }
+}
+// cos and sin of the eight angles that belong to this lane's coordinates, for the position of the warp's row
+template <int D>
+__device__ __forceinline__ void row_angles(int pos, const double* f, float* c, float* s) {
+  float cs[D / 64], sn[D / 64];
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const double turns = (double)pos * f[i];
+    sincospif(2.f * (float)(turns - rint(turns)), &sn[i], &cs[i]);
+  }
+  const int piece = (int)(threadIdx.x & 31) & (D / 16 - 1);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {   // angle piece * 8 + i was computed by lane (piece * 8 + i) / (D / 64)
+    const int src = (piece * 8 + i) / (D / 64);
+    c[i] = __shfl_sync(0xffffffffu, cs[i % (D / 64)], src);
+    s[i] = __shfl_sync(0xffffffffu, sn[i % (D / 64)], src);
+  }
+}
+
+struct NormRopeArgs {
+  const uint8_t* qkv;
+  int64_t row_bytes;
+  const int32_t* positions;
+  const uint4 *q_weight, *k_weight;   // NULL: ones
+  uint4 *q_out, *k_out, *v_out;
+  int64_t units;                      // rows * split
+  int q_heads, kv_heads, split;       // split: warps that share a row's heads
+  double log2_theta;
+  float eps;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads) k_norm_rope(const NormRopeArgs a) {
+  constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;   // lanes per head, heads per warp pass, 16-byte pieces per head
+  const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes;
+  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  const uint4 wq0 = a.q_weight ? a.q_weight[piece] : ones, wq1 = a.q_weight ? a.q_weight[kLanes + piece] : ones;
+  const uint4 wk0 = a.k_weight ? a.k_weight[piece] : ones, wk1 = a.k_weight ? a.k_weight[kLanes + piece] : ones;
+  double freq[D / 64];
+  lane_frequencies<D>(a.log2_theta, freq);
+  const int rot = a.q_heads + a.kv_heads, heads = rot + a.kv_heads;
+  const int64_t step = (int64_t)gridDim.x * kWarps;
+  for (int64_t u = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); u < a.units; u += step) {
+    const int64_t row = u / a.split;
+    const int part = (int)(u - row * a.split);
+    float c[8], s[8];
+    row_angles<D>(a.positions[row], freq, c, s);
+    const uint4* in = reinterpret_cast<const uint4*>(a.qkv + row * a.row_bytes);
+    for (int h0 = part * kHeads; h0 < heads; h0 += a.split * kHeads) {
+      const int h = h0 + sub;
+      const bool live = h < heads;
+      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+      if (live) { lo = in[h * kChunks + piece]; hi = in[h * kChunks + kLanes + piece]; }
+      float x[8], y[8];
+      unpack8(lo, x); unpack8(hi, y);
+      float sq = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+      const float r = rsqrtf(head_sum<D>(sq) * (1.f / D) + a.eps);
+      if (h < rot) {
+        const bool is_q = h < a.q_heads;
+        float w0[8], w1[8];
+        unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float p = x[i] * r * w0[i], q = y[i] * r * w1[i];
+          x[i] = fmaf(p, c[i], -q * s[i]);
+          y[i] = fmaf(q, c[i], p * s[i]);
+        }
+        uint4* dst = is_q ? a.q_out + (row * a.q_heads + h) * kChunks : a.k_out + (row * a.kv_heads + (h - a.q_heads)) * kChunks;
+        dst[piece] = pack8(x);
+        dst[kLanes + piece] = pack8(y);
+      } else if (live) {
+        uint4* dst = a.v_out + (row * a.kv_heads + (h - rot)) * kChunks;
+        dst[piece] = lo;
+        dst[kLanes + piece] = hi;
+      }
+    }
+  }
+}
+
+struct NormRopeGradArgs {
+  const uint8_t* qkv;
+  int64_t row_bytes;
+  const int32_t* positions;
+  const uint4 *q_weight, *k_weight;
+  const uint4 *dq, *dk, *dv;
+  uint4* dqkv;          // [rows][q_heads + 2 kv_heads][D], contiguous
+  float* partial;       // [blocks][2][D]
+  int64_t units;
+  int q_heads, kv_heads, split;
+  double log2_theta;
+  float eps;
+};
+
+// The weight gradients: every lane adds up its 16 coordinates over the rows and heads it meets (fp32, a few dozen
+// to a few hundred terms), the block's lanes are joined in a fixed order and a second kernel adds the blocks', also
+// in a fixed order, so that results are reproducible.
+template <int D>
+__global__ void __launch_bounds__(kThreads) k_norm_rope_grad(const NormRopeGradArgs a) {
+  constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;
+  const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes, warp = threadIdx.x >> 5;
+  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  const uint4 wq0 = a.q_weight ? a.q_weight[piece] : ones, wq1 = a.q_weight ? a.q_weight[kLanes + piece] : ones;
+  const uint4 wk0 = a.k_weight ? a.k_weight[piece] : ones, wk1 = a.k_weight ? a.k_weight[kLanes + piece] : ones;
+  double freq[D / 64];
+  lane_frequencies<D>(a.log2_theta, freq);
+  const int rot = a.q_heads + a.kv_heads, heads = rot + a.kv_heads;
+  float dwq[16], dwk[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) dwq[i] = dwk[i] = 0.f;
+  const int64_t step = (int64_t)gridDim.x * kWarps;
+  for (int64_t u = (int64_t)blockIdx.x * kWarps + warp; u < a.units; u += step) {
+    const int64_t row = u / a.split;
+    const int part = (int)(u - row * a.split);
+    float c[8], s[8];
+    row_angles<D>(a.positions[row], freq, c, s);
+    const uint4* in = reinterpret_cast<const uint4*>(a.qkv + row * a.row_bytes);
+    uint4* out = a.dqkv + row * heads * kChunks;
+    for (int h0 = part * kHeads; h0 < heads; h0 += a.split * kHeads) {
+      const int h = h0 + sub;
+      const bool turned = h < rot, is_q = h < a.q_heads;
+      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo, glo = lo, ghi = lo;
+      if (h < heads) {
+        const uint4* g = is_q ? a.dq + (row * a.q_heads + h) * kChunks
+                              : (turned ? a.dk + (row * a.kv_heads + (h - a.q_heads)) * kChunks : a.dv + (row * a.kv_heads + (h - rot)) * kChunks);
+        glo = g[piece]; ghi = g[kLanes + piece];
+        if (turned) { lo = in[h * kChunks + piece]; hi = in[h * kChunks + kLanes + piece]; }
+      }
+      float x[8], y[8], p[8], q[8], w0[8], w1[8];
+      unpack8(lo, x); unpack8(hi, y); unpack8(glo, p); unpack8(ghi, q);
+      unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
+      float sq = 0.f, dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d0 = fmaf(p[i], c[i], q[i] * s[i]), d1 = fmaf(q[i], c[i], -p[i] * s[i]);   // the rotation taken back
+        p[i] = d0; q[i] = d1;
+        sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+        dot = fmaf(x[i] * w0[i], d0, fmaf(y[i] * w1[i], d1, dot));
+      }
+      sq = head_sum<D>(sq); dot = head_sum<D>(dot);
+      const float r = rsqrtf(sq * (1.f / D) + a.eps), k = r * r * dot * (1.f / D);
+      if (turned) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float xr = x[i] * r, yr = y[i] * r;
+          if (is_q) { dwq[i] = fmaf(xr, p[i], dwq[i]); dwq[8 + i] = fmaf(yr, q[i], dwq[8 + i]); }
+          else { dwk[i] = fmaf(xr, p[i], dwk[i]); dwk[8 + i] = fmaf(yr, q[i], dwk[8 + i]); }
+          x[i] = r * fmaf(w0[i], p[i], -x[i] * k);
+          y[i] = r * fmaf(w1[i], q[i], -y[i] * k);
+        }
+        out[h * kChunks + piece] = pack8(x);
+        out[h * kChunks + kLanes + piece] = pack8(y);
+      } else if (h < heads) {
+        out[h * kChunks + piece] = glo;
+        out[h * kChunks + kLanes + piece] = ghi;
+      }
+    }
+  }
+  __shared__ float sh[kWarps][2][D];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float vq = dwq[i], vk = dwk[i];
+#pragma unroll
+    for (int d = kLanes; d < 32; d <<= 1) { vq += __shfl_xor_sync(0xffffffffu, vq, d); vk += __shfl_xor_sync(0xffffffffu, vk, d); }
+    if (sub == 0) {
+      const int col = (i >> 3) * (D / 2) + piece * 8 + (i & 7);
+      sh[warp][0][col] = vq;
+      sh[warp][1][col] = vk;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 2 * D) {
+    const float* col = &sh[0][0][0] + threadIdx.x;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) t += col[w * 2 * D];
+    a.partial[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = t;
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(1024) k_norm_rope_weights(const float* __restrict__ partial, int blocks, float* __restrict__ dq_weight,
+                                                           float* __restrict__ dk_weight) {
+  constexpr int kGroups = 1024 / (2 * D);
+  __shared__ float sh[kGroups][2 * D];
+  const int col = threadIdx.x % (2 * D), grp = threadIdx.x / (2 * D);
+  float t = 0.f;
+#pragma unroll 8
+  for (int b = grp; b < blocks; b += kGroups) t += partial[(int64_t)b * 2 * D + col];
+  sh[grp][col] = t;
+  __syncthreads();
+  if (grp == 0) {
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) t += sh[g][col];
+    float* dst = col < D ? dq_weight : dk_weight;
+    if (dst != nullptr) dst[col % D] = t;
+  }
+}
+
+constexpr int kMaxGradBlocks = 148 * 2;
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Few rows: several warps share a row's heads, down to one pass each, until there are about 16 warps per SM.
+int row_split(int64_t n, int heads, int head_dim) {
+  const int passes = (heads * (head_dim / 16) + 31) / 32;
+  int split = 1;
+  while (split < passes && n * split < 148 * 16) split *= 2;
+  return split < passes ? split : passes;
+}
+
+bc_status check(int64_t n, int q_heads, int kv_heads, int head_dim, const void* qkv, int64_t row_stride, const int32_t* positions,
+                float theta, const void* q_weight, const void* k_weight, float eps) {
+  if (n <= 0 || q_heads < 1 || kv_heads < 1 || !qkv || !positions || !(theta > 1.f) || !(eps >= 0.f)) return BC_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return BC_ERR_UNSUPPORTED;
+  if ((int64_t)q_heads + 2 * (int64_t)kv_heads > (1 << 20)) return BC_ERR_UNSUPPORTED;
+  if (row_stride < (int64_t)(q_heads + 2 * kv_heads) * head_dim || row_stride % 8) return BC_ERR_INVALID_ARG;
+  if (!aligned16(qkv) || (reinterpret_cast<uintptr_t>(positions) & 3) || !aligned16(q_weight) || !aligned16(k_weight)) return BC_ERR_INVALID_ARG;
+  return BC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+bc_status bc_norm_rope_split(int32_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* qkv, int64_t row_stride,
+                             const int32_t* positions, float theta, const void* q_weight, const void* k_weight, float eps,
+                             void* q_out, void* k_out, void* v_out, void* stream) {
+  const bc_status st = check(n, q_heads, kv_heads, head_dim, qkv, row_stride, positions, theta, q_weight, k_weight, eps);
+  if (st) return st;
+  if (!q_out || !k_out || !v_out || !aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out)) return BC_ERR_INVALID_ARG;
+  NormRopeArgs a;
+  a.qkv = (const uint8_t*)qkv; a.row_bytes = row_stride * 2; a.positions = positions;
+  a.q_weight = (const uint4*)q_weight; a.k_weight = (const uint4*)k_weight;
+  a.q_out = (uint4*)q_out; a.k_out = (uint4*)k_out; a.v_out = (uint4*)v_out;
+  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim);
+  a.units = (int64_t)n * a.split; a.log2_theta = log2((double)theta); a.eps = eps;
+  const int64_t want = (a.units + kWarps - 1) / kWarps;
+  const int blocks = (int)(want < 148 * 4 ? want : 148 * 4);
+  if (head_dim == 64) k_norm_rope<64><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
+  else k_norm_rope<128><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
+  return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+
+bc_status bc_norm_rope_query_bytes(int32_t head_dim, size_t* workspace_bytes) {
+  if (!workspace_bytes) return BC_ERR_INVALID_ARG;
+  if (head_dim != 64 && head_dim != 128) return BC_ERR_UNSUPPORTED;
+  *workspace_bytes = (size_t)kMaxGradBlocks * 2 * head_dim * sizeof(float);
+  return BC_OK;
+}
+
+bc_status bc_norm_rope_split_backward(int32_t n, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const void* qkv,
+                                      int64_t row_stride, const int32_t* positions, float theta, const void* q_weight,
+                                      const void* k_weight, float eps, const void* dq, const void* dk, const void* dv, void* dqkv,
+                                      float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes, void* stream) {
+  const bc_status st = check(n, q_heads, kv_heads, head_dim, qkv, row_stride, positions, theta, q_weight, k_weight, eps);
+  if (st) return st;
+  if (!dq || !dk || !dv || !dqkv || !workspace || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(dqkv) ||
+      !aligned16(workspace) || ((reinterpret_cast<uintptr_t>(dq_weight) | reinterpret_cast<uintptr_t>(dk_weight)) & 3))
+    return BC_ERR_INVALID_ARG;
+  if (workspace_bytes < (size_t)kMaxGradBlocks * 2 * head_dim * sizeof(float)) return BC_ERR_INVALID_ARG;
+  NormRopeGradArgs a;
+  a.qkv = (const uint8_t*)qkv; a.row_bytes = row_stride * 2; a.positions = positions;
+  a.q_weight = (const uint4*)q_weight; a.k_weight = (const uint4*)k_weight;
+  a.dq = (const uint4*)dq; a.dk = (const uint4*)dk; a.dv = (const uint4*)dv; a.dqkv = (uint4*)dqkv;
+  a.partial = (float*)workspace;
+  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim);
+  a.units = (int64_t)n * a.split; a.log2_theta = log2((double)theta); a.eps = eps;
+  const int64_t want = (a.units + kWarps - 1) / kWarps;
+  const int blocks = (int)(want < kMaxGradBlocks ? want : kMaxGradBlocks);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (head_dim == 64) k_norm_rope_grad<64><<<blocks, kThreads, 0, s>>>(a);
+  else k_norm_rope_grad<128><<<blocks, kThreads, 0, s>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return BC_ERR_CUDA;
+  if (dq_weight == nullptr && dk_weight == nullptr) return BC_OK;
+  if (head_dim == 64) k_norm_rope_weights<64><<<1, 1024, 0, s>>>(a.partial, blocks, dq_weight, dk_weight);
+  else k_norm_rope_weights<128><<<1, 1024, 0, s>>>(a.partial, blocks, dq_weight, dk_weight);
+  return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+
+}  // extern "C"
