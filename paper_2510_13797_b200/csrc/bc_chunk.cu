@@ -645,14 +645,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
                          *reinterpret_cast<const uint32_t*>(&b3));
         }
       };
-      float o[D];
-      if (warp_live) {
-        tc_fence_after();
+      tc_fence_after();
+      float o[D];                                             // a warp without a row reads it too: under a condition it would be spilled
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + lane_base + cb * 32, o + cb * 32);
-        tmem_wait_ld();
-        tc_fence_before();
-      }
+      for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + lane_base + cb * 32, o + cb * 32);
+      tmem_wait_ld();
+      tc_fence_before();
       mbar_arrive_cta(bar_e);
       if (complete) {
         if (row_valid) {
