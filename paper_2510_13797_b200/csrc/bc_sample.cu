@@ -34,13 +34,11 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kCluster = 8;
 constexpr int kBins = 512;
+constexpr int kList = 256;             // elements of a bin that are ordered directly
 constexpr int kMaxVocab = 1 << 18;     // 2^18 weights of at most 2^45 add up in 63 bits
 constexpr int kWeightBits = 45;
-static_assert(kBins == 2 * kThreads, "a thread scans two bins");
 
 struct Sum2 {   // a mass and a count, added up together
   u64 mass;
@@ -49,7 +47,9 @@ struct Sum2 {   // a mass and a count, added up together
 __device__ __forceinline__ Sum2 operator+(const Sum2& a, const Sum2& b) { return {a.mass + b.mass, a.count + b.count}; }
 
 // Exclusive prefix over the block's threads; *total gets the block's sum.  All threads call.
+template <int THREADS>
 __device__ __forceinline__ Sum2 block_scan(Sum2 x, Sum2* total) {
+  constexpr int kWarps = THREADS / 32;
   __shared__ u64 sh_mass[kWarps];
   __shared__ uint32_t sh_count[kWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -84,6 +84,13 @@ template <> struct Raw<__nv_bfloat16> {
     return f == f ? f + 0.f : -INFINITY;   // + 0: the two zeros are one value
   }
   __device__ static __forceinline__ __nv_bfloat16 none() { return __ushort_as_bfloat16(0xff80); }
+  typedef __nv_bfloat162 Max;               // running maximum; the maximum of a number and a NaN is the number
+  __device__ static __forceinline__ Max start() { return __halves2bfloat162(none(), none()); }
+  __device__ static __forceinline__ void fold(Max& m, const uint4& v) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+    m = __hmax2(m, __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+  }
+  __device__ static __forceinline__ float value(const Max& m) { return fmaxf(__low2float(m), __high2float(m)) + 0.f; }
 };
 template <> struct Raw<float> {
   static constexpr int kVec = 4;
@@ -92,6 +99,12 @@ template <> struct Raw<float> {
     return f == f ? f + 0.f : -INFINITY;
   }
   __device__ static __forceinline__ float none() { return -INFINITY; }
+  typedef float Max;
+  __device__ static __forceinline__ Max start() { return -INFINITY; }
+  __device__ static __forceinline__ void fold(Max& m, const uint4& v) {
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))));
+  }
+  __device__ static __forceinline__ float value(Max m) { return m + 0.f; }
 };
 
 // order-preserving key of a float (no NaN, one zero), and back
@@ -103,106 +116,155 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^
 
 struct Scale {
   float top;      // the row's maximum
+  double dtop;
   double c;       // log2(e) / T
   float bins;     // 11 bins per octave
-  double min_p;
-  // e(x) in double precision; 0 where it is far below the weights' resolution
-  __device__ __forceinline__ double e(float x) const {
-    if (x == top) return 1.0;
-    const double t = ((double)top - (double)x) * c;
-    return t < (double)(kWeightBits + 2) ? exp2(-t) : 0.0;    // also 0 for inf * 0
+  double min_w;   // 2^45 min_p
+  // 2^45 e(x), in double precision: 2^-t for t = (top - x) log2(e) / T octaves, t = n - f with |f| <= 1/2, 2^f by its Taylor
+  // series to the tenth power (the rest is below 0.35^11 / 11! = 2^-42 of the value).  0 where it would round to 0.
+  __device__ __forceinline__ double scaled(float x) const {
+    constexpr double kMagic = 6755399441055744.0;              // 1.5 * 2^52: adding it rounds to an integer
+    const double t = (dtop - (double)x) * c;
+    const double m = t + kMagic;
+    const int n = __double2loint(m);
+    const double f = (m - kMagic) - t;
+    double p = 7.054911620801121e-09;                         // ln(2)^10 / 10!
+    p = fma(p, f, 1.0178086009239696e-07);
+    p = fma(p, f, 1.3215486790144305e-06);
+    p = fma(p, f, 1.5252733804059838e-05);
+    p = fma(p, f, 1.5403530393381606e-04);
+    p = fma(p, f, 1.3333558146428441e-03);
+    p = fma(p, f, 9.618129107628477e-03);
+    p = fma(p, f, 5.5504108664821576e-02);
+    p = fma(p, f, 2.402265069591007e-01);
+    p = fma(p, f, 6.931471805599453e-01);
+    p = fma(p, f, 1.0);
+    const double v = __hiloint2double(__double2hiint(p) + ((kWeightBits - n) << 20), __double2loint(p));
+    if (x == top) return (double)(1ull << kWeightBits);        // also where top is infinite
+    return t < (double)(kWeightBits + 1) ? v : 0.0;            // also 0 for a t that is not a number (inf * 0)
   }
-  __device__ __forceinline__ u64 fixed(double e) const { return __double2ull_rn(e * (double)(1ull << kWeightBits)); }
-  __device__ __forceinline__ u64 weight(float x) const { return fixed(e(x)); }
+  // a double of at most 2^46 to the nearest integer
+  __device__ __forceinline__ static u64 rounded(double v) {
+    return (u64)__double_as_longlong(v + 4503599627370496.0) & 0xfffffffffffffull;
+  }
+  __device__ __forceinline__ u64 weight(float x) const { return rounded(scaled(x)); }
   __device__ __forceinline__ u64 kept_weight(float x) const {   // 0 below min_p
-    const double v = e(x);
-    return v >= min_p ? fixed(v) : 0;
+    const double v = scaled(x);
+    return v >= min_w ? rounded(v) : 0;
   }
-  __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)((top - x) * bins)); }
+  __device__ __forceinline__ float depth(float x) const { return x == top ? 0.f : (top - x) * bins; }   // NaN for weights of 0 only
+  __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)depth(x)); }
+  __device__ __forceinline__ bool in_bin(float x, int b) const {
+    const float d = depth(x);
+    return d >= (float)b && (d < (float)(b + 1) || b == kBins - 1);
+  }
 };
 
 struct Shared {
   u64 mass[2][kBins];            // histograms: two, used in turn (one may still be read by other blocks)
   uint32_t count[2][kBins];
   uint32_t key_lo[2], key_hi[2];
-  float best;                    // this block's maximum and its lowest index
-  int at;
+  uint32_t list[2][kList];       // this block's elements of a bin, likewise
+  int n_list[2];
+  uint32_t keys[kList];          // all blocks' elements of a bin, and their weights
+  u64 weights[kList];
+  float best;                    // this block's maximum
+  int at;                        // its lowest index (greedy rows)
   Sum2 part;                     // this block's mass above the threshold and number of elements at it
   // results of a search, for the whole block
   int cross_bin;
   Sum2 cross_before, cross_in;
+  uint32_t thr;
   int owner;
-  u64 owner_skip;
-  uint32_t owner_ties;
+  u64 owner_skip, owner_ties;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logits, int64_t row_stride, int vocab,
-                                                     const float* __restrict__ temperature, const int32_t* __restrict__ top_k,
-                                                     const float* __restrict__ top_p, const float* __restrict__ min_p,
-                                                     const float* __restrict__ uniform, long long* __restrict__ out) {
-  constexpr int kVec = Raw<T>::kVec;
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __restrict__ logits, int64_t row_stride, int vocab,
+                                                                   const float* __restrict__ temperature, const int32_t* __restrict__ top_k,
+                                                                   const float* __restrict__ top_p, const float* __restrict__ min_p,
+                                                                   const float* __restrict__ uniform, long long* __restrict__ out) {
+  constexpr int kVec = Raw<T>::kVec, kWarps = THREADS / 32, kPer = kBins / THREADS;   // kPer: bins a thread adds up
   extern __shared__ uint4 slice[];
   __shared__ Shared sh;
+  __shared__ float warp_best[kWarps];
   cg::cluster_group cluster = cg::this_cluster();
   const int part = (int)cluster.block_rank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t r = blockIdx.x / kCluster;
   const T* row = logits + r * row_stride;
 
-  // ---- the slice: elements [first, first + cnt) of the row, kept at their 16-byte phase ---------------------------
+  // ---- the slice: elements [first, first + cnt) of the row, kept at their 16-byte phase; its maximum --------------
   const int per = (vocab + kCluster * kVec - 1) / (kCluster * kVec) * kVec;
   const int first = min(part * per, vocab), cnt = min(vocab - first, per);
   const int phase = (int)((reinterpret_cast<uintptr_t>(row + first) & 15) / sizeof(T));
   const int pieces = cnt > 0 ? (phase + cnt + kVec - 1) / kVec : 0;
   T* flat = reinterpret_cast<T*>(slice);
-  float best = -INFINITY;
-  int at = 0x7fffffff;
-  auto take = [&](float v, int i) { if (v > best || (v == best && i < at)) { best = v; at = i; } };
-  for (int p = tid; p < pieces; p += kThreads) {
-    const int e0 = p * kVec - phase;               // element of the slice in which the piece begins
-    uint4 v;
-    if (e0 >= 0 && e0 + kVec <= cnt) {
-      v = __ldcs(reinterpret_cast<const uint4*>(row + first + e0));
-      slice[p] = v;
-    } else {                                       // the row's ends: only what belongs to it is read
-      for (int i = 0; i < kVec; ++i) flat[p * kVec + i] = e0 + i >= 0 && e0 + i < cnt ? row[first + e0 + i] : Raw<T>::none();
-      v = slice[p];
+  typename Raw<T>::Max run_max = Raw<T>::start();
+  const int whole0 = phase > 0 ? 1 : 0, whole1 = (phase + cnt) / kVec;          // pieces that lie in the slice entirely
+  const uint4* aligned = reinterpret_cast<const uint4*>(row + first - phase);   // piece p at aligned + p
+#pragma unroll 4
+  for (int p = whole0 + tid; p < whole1; p += THREADS) {
+    const uint4 v = __ldcs(aligned + p);
+    slice[p] = v;
+    Raw<T>::fold(run_max, v);
+  }
+  if (tid < 2 && pieces > 0) {                                                    // the ends: only what belongs to the row is read
+    const int p = tid == 0 ? 0 : pieces - 1;
+    if ((p < whole0 || p >= whole1) && !(tid == 1 && pieces == 1)) {
+      for (int i = 0; i < kVec; ++i) {
+        const int e = p * kVec - phase + i;
+        flat[p * kVec + i] = e >= 0 && e < cnt ? row[first + e] : Raw<T>::none();
+      }
+      Raw<T>::fold(run_max, slice[p]);
     }
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (e0 + i >= 0 && e0 + i < cnt) take(Raw<T>::get(v, i), first + e0 + i);
   }
+  float best = Raw<T>::value(run_max);
+  if (!(best == best)) best = -INFINITY;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const float v = __shfl_xor_sync(0xffffffffu, best, d);
-    const int i = __shfl_xor_sync(0xffffffffu, at, d);
-    take(v, i);
-  }
-  __shared__ float warp_best[kWarps];
-  __shared__ int warp_at[kWarps];
-  if (lane == 0) { warp_best[warp] = best; warp_at[warp] = at; }
+  for (int d = 16; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
+  if (lane == 0) warp_best[warp] = best;
+  for (int b = tid; b < kBins; b += THREADS) { sh.mass[0][b] = 0; sh.count[0][b] = 0; }
+  if (tid == 0) sh.at = 0x7fffffff;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kWarps; ++w) take(warp_best[w], warp_at[w]);
-    sh.best = best; sh.at = at;
+  if (warp == 0) {
+    best = lane < kWarps ? warp_best[lane] : -INFINITY;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
+    if (lane == 0) sh.best = best;
   }
-  for (int b = tid; b < kBins; b += kThreads) { sh.mass[0][b] = 0; sh.count[0][b] = 0; }
   cluster.sync();
-  best = -INFINITY; at = 0x7fffffff;
-  for (int b = 0; b < kCluster; ++b) take(*cluster.map_shared_rank(&sh.best, b), *cluster.map_shared_rank(&sh.at, b));
+  best = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < kCluster; ++b) best = fmaxf(best, *cluster.map_shared_rank(&sh.best, b));
 
   const float temp = temperature != nullptr ? temperature[r] : 1.f;
   if (!(temp > 0.f) || best == -INFINITY) {        // greedy; a row without a finite element: its first index, as bc_argmax
-    if (part == 0 && tid == 0) out[r] = at == 0x7fffffff ? 0 : at;
+    int at = 0x7fffffff;
+    for (int q = tid; q < pieces; q += THREADS) {
+      const uint4 v = slice[q];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int e = q * kVec - phase + i;
+        if (Raw<T>::get(v, i) == best && e >= 0 && e < cnt) at = min(at, first + e);
+      }
+    }
+    at = __reduce_min_sync(0xffffffffu, at);
+    if (lane == 0) atomicMin(&sh.at, at);
+    cluster.sync();
+    if (part == 0 && tid == 0) {
+      for (int b = 0; b < kCluster; ++b) at = min(at, *cluster.map_shared_rank(&sh.at, b));
+      out[r] = at == 0x7fffffff ? 0 : at;
+    }
     cluster.sync();                                // no block leaves while its shared memory may still be read
     return;
   }
   Scale sc;
   sc.top = best;
+  sc.dtop = (double)best;
   sc.c = 1.4426950408889634 / (double)temp;
   sc.bins = (float)(11.0 * sc.c);
   const float mp = min_p != nullptr ? min_p[r] : 0.f;
-  sc.min_p = mp > 0.f ? fmin((double)mp, 1.0) : 0.0;   // at most 1: the largest element is always kept
+  sc.min_w = mp > 0.f ? fmin((double)mp, 1.0) * (double)(1ull << kWeightBits) : 0.0;   // at most 1: the largest element is always kept
   const int k = top_k != nullptr ? top_k[r] : 0;
   const float p = top_p != nullptr ? top_p[r] : 1.f;
   const bool by_count = k > 0 && k < vocab, by_mass = p < 1.f;
@@ -210,31 +272,38 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
   // ---- threshold: keep every key above thr and the first `ties` elements (in index order) that equal it ------------
   uint32_t thr = 0;
   u64 ties = 0;                                     // with no limit: every key is above 0, the key no float has
-  int round = 0;                                    // histograms filled so far, which of the two is next
-  // Adds the cluster's histograms up (this thread: bins 2 tid, 2 tid + 1).
-  auto totals = [&](int which, Sum2* b0, Sum2* b1) {
-    *b0 = {0, 0}; *b1 = {0, 0};
+  int round = 1;                                    // which of the two histograms and lists is next
+  auto val = [](const Sum2& s, bool count) { return count ? (u64)s.count : s.mass; };
+  // Adds the cluster's histograms up (this thread: bins kPer tid ...).
+  auto totals = [&](int which, Sum2 (&b)[kPer]) {
 #pragma unroll
-    for (int b = 0; b < kCluster; ++b) {
-      const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(cluster.map_shared_rank(&sh.mass[which][2 * tid], b));
-      const uint2 c = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sh.count[which][2 * tid], b));
-      b0->mass += m.x; b1->mass += m.y; b0->count += c.x; b1->count += c.y;
+    for (int i = 0; i < kPer; ++i) {
+      b[i] = {0, 0};
+#pragma unroll
+      for (int o = 0; o < kCluster; ++o) {
+        b[i].mass += *cluster.map_shared_rank(&sh.mass[which][kPer * tid + i], o);
+        b[i].count += *cluster.map_shared_rank(&sh.count[which][kPer * tid + i], o);
+      }
     }
   };
   // The bin in which the running count (or mass), largest keys first, reaches `limit`: false if it never does.
-  auto cross = [&](const Sum2& b0, const Sum2& b1, const Sum2& before0, bool count, u64 limit, Sum2* all) {
+  auto cross = [&](const Sum2 (&b)[kPer], const Sum2& before0, bool count, u64 limit, Sum2* all) {
     if (tid == 0) sh.cross_bin = -1;
-    Sum2 e0 = block_scan(b0 + b1, all);             // its barriers order the store above
-    e0 = e0 + before0;
-    const Sum2 e1 = e0 + b0, e2 = e1 + b1;
-    auto val = [&](const Sum2& s) { return count ? (u64)s.count : s.mass; };
-    if (val(e0) < limit && limit <= val(e1)) { sh.cross_bin = 2 * tid; sh.cross_before = e0; sh.cross_in = b0; }
-    if (val(e1) < limit && limit <= val(e2)) { sh.cross_bin = 2 * tid + 1; sh.cross_before = e1; sh.cross_in = b1; }
+    Sum2 mine = b[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) mine = mine + b[i];
+    Sum2 e = block_scan<THREADS>(mine, all) + before0;   // its barriers order the store above
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const Sum2 n = e + b[i];
+      if (val(e, count) < limit && limit <= val(n, count)) { sh.cross_bin = kPer * tid + i; sh.cross_before = e; sh.cross_in = b[i]; }
+      e = n;
+    }
     __syncthreads();
     return sh.cross_bin >= 0;
   };
   if (by_count || by_mass) {
-    for (int q = tid; q < pieces; q += kThreads) {
+    for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
@@ -248,29 +317,29 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
       }
     }
     cluster.sync();
-    Sum2 l0, l1, all;
-    totals(0, &l0, &l1);
-    round = 1;
-    // From the bin that cross() found to the key: histograms over the bits in which the bin's keys differ.
-    auto refine = [&](bool count, u64 limit, Sum2* before, Sum2* in) {
+    Sum2 bins[kPer], all;
+    totals(0, bins);
+    // From the bin that cross() found to the key: while the bin holds many elements, histograms over the bits in which its
+    // keys differ; then its elements are gathered and ordered by counting.  Returns the key, *before: what lies above it.
+    auto refine = [&](bool count, u64 limit, Sum2* before) {
       const int bin = sh.cross_bin;
       *before = sh.cross_before;
-      *in = sh.cross_in;
+      uint32_t in = sh.cross_in.count;
       uint32_t lo = 0, hi = 0xffffffffu;
-      for (;;) {
+      for (; in > kList; ++round) {
         uint32_t mn = 0xffffffffu, mx = 0;
-        for (int q = tid; q < pieces; q += kThreads) {
+        for (int q = tid; q < pieces; q += THREADS) {
           const uint4 v = slice[q];
 #pragma unroll
           for (int i = 0; i < kVec; ++i) {
             const float x = Raw<T>::get(v, i);
             const uint32_t key = key_of(x);
-            if (key >= lo && key <= hi && sc.bin(x) == bin && sc.weight(x)) { mn = min(mn, key); mx = max(mx, key); }
+            if (key >= lo && key <= hi && sc.in_bin(x, bin) && sc.weight(x)) { mn = min(mn, key); mx = max(mx, key); }
           }
         }
         const int which = round & 1;
         if (tid == 0) { sh.key_lo[which] = 0xffffffffu; sh.key_hi[which] = 0; }
-        for (int b = tid; b < kBins; b += kThreads) { sh.mass[which][b] = 0; sh.count[which][b] = 0; }
+        for (int b = tid; b < kBins; b += THREADS) { sh.mass[which][b] = 0; sh.count[which][b] = 0; }
         __syncthreads();
         if (mn <= mx) { atomicMin(&sh.key_lo[which], mn); atomicMax(&sh.key_hi[which], mx); }
         cluster.sync();
@@ -282,13 +351,13 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
         }
         if (mn >= mx) { ++round; return mx; }        // one key: the threshold
         const int shift = max(0, 32 - __clz(mx - mn) - 9);   // (mx - mn) >> shift is below 512
-        for (int q = tid; q < pieces; q += kThreads) {
+        for (int q = tid; q < pieces; q += THREADS) {
           const uint4 v = slice[q];
 #pragma unroll
           for (int i = 0; i < kVec; ++i) {
             const float x = Raw<T>::get(v, i);
             const uint32_t key = key_of(x);
-            if (key >= mn && key <= mx && sc.bin(x) == bin) {
+            if (key >= mn && key <= mx && sc.in_bin(x, bin)) {
               const u64 w = sc.weight(x);
               if (w) {
                 const int b = (int)((mx - key) >> shift);
@@ -299,37 +368,85 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
           }
         }
         cluster.sync();
-        Sum2 b0, b1, sub;
-        totals(which, &b0, &b1);
-        ++round;
-        cross(b0, b1, *before, count, limit, &sub);
+        Sum2 sub[kPer], unused;
+        totals(which, sub);
+        cross(sub, *before, count, limit, &unused);
         *before = sh.cross_before;
-        *in = sh.cross_in;
+        in = sh.cross_in.count;
         const uint32_t b = (uint32_t)sh.cross_bin;
         hi = mx - (b << shift);
         lo = max(mn, hi - ((1u << shift) - 1u));
         __syncthreads();                             // sh.cross_* have been read
       }
+      const int which = round & 1;
+      ++round;
+      if (tid == 0) sh.n_list[which] = 0;
+      __syncthreads();
+      for (int q = tid; q < pieces; q += THREADS) {
+        const uint4 v = slice[q];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const float x = Raw<T>::get(v, i);
+          const uint32_t key = key_of(x);
+          if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) sh.list[which][atomicAdd(&sh.n_list[which], 1)] = key;
+        }
+      }
+      cluster.sync();
+      if (tid < kList) {                              // all blocks' lists, one behind the other
+        int j = tid, o = 0, len = 0;
+        for (; o < kCluster; ++o) {
+          len = *cluster.map_shared_rank(&sh.n_list[which], o);
+          if (j < len) break;
+          j -= len;
+        }
+        if (o < kCluster) {
+          const uint32_t key = *cluster.map_shared_rank(&sh.list[which][j], o);
+          sh.keys[tid] = key;
+          sh.weights[tid] = sc.weight(of_key(key));
+        }
+      }
+      __syncthreads();
+      if (tid < (int)in) {
+        const uint32_t key = sh.keys[tid];
+        const u64 w = sh.weights[tid];
+        Sum2 above = *before;
+        uint32_t same = 0;
+        for (int j = 0; j < (int)in; ++j) {
+          const uint32_t o = sh.keys[j];
+          if (o > key) { above.mass += sh.weights[j]; ++above.count; }
+          same += o == key;
+        }
+        if (val(above, count) < limit && limit <= val(above + Sum2{same * w, same}, count)) { sh.thr = key; sh.cross_before = above; }
+      }
+      __syncthreads();
+      *before = sh.cross_before;
+      return sh.thr;
     };
     bool cut = false;
-    Sum2 before, in;
+    Sum2 before;
     u64 mass = 0;
     if (by_count) {
-      cut = cross(l0, l1, Sum2{0, 0}, true, (u64)k, &all);
+      cut = cross(bins, Sum2{0, 0}, true, (u64)k, &all);
       mass = all.mass;
       if (cut) {
-        thr = refine(true, (u64)k, &before, &in);
+        thr = refine(true, (u64)k, &before);
         ties = (u64)k - before.count;
         mass = before.mass + ties * sc.weight(of_key(thr));
       }
     }
     if (by_mass) {
       __syncthreads();
-      if (!cut) { block_scan(l0 + l1, &all); mass = all.mass; }
+      if (!cut) {
+        Sum2 mine = bins[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) mine = mine + bins[i];
+        block_scan<THREADS>(mine, &all);
+        mass = all.mass;
+      }
       const double want = ceil((double)p * (double)mass);
       const u64 limit = want >= 1.0 ? (u64)want : 1;   // the largest element is always kept; NaN never comes here
-      if (cross(l0, l1, Sum2{0, 0}, false, limit, &all)) {
-        thr = refine(false, limit, &before, &in);
+      if (cross(bins, Sum2{0, 0}, false, limit, &all)) {
+        thr = refine(false, limit, &before);
         const u64 w = sc.weight(of_key(thr));
         ties = (limit - before.mass + w - 1) / w;
       }
@@ -339,24 +456,25 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
   // ---- the draw ---------------------------------------------------------------------------------------------------
   // Thread t takes a run of consecutive pieces, so that threads are in index order; an odd run keeps the 16-byte
   // reads of neighbouring threads off one another's banks.
-  const int run = ((per / kVec + 1 + kThreads - 1) / kThreads) | 1;
+  const int run = ((per / kVec + 1 + THREADS - 1) / THREADS) | 1;
   const u64 tie_weight = thr != 0 ? sc.kept_weight(of_key(thr)) : 0;
+  const float floor_x = thr != 0 ? of_key(thr) : -INFINITY;      // nothing below it is kept
   Sum2 mine = {0, 0};                                // mass above the threshold, elements at it
   for (int q = tid * run; q < min(pieces, (tid + 1) * run); ++q) {
     const uint4 v = slice[q];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       const float x = Raw<T>::get(v, i);
-      const uint32_t key = key_of(x);
-      if (key > thr) mine.mass += sc.kept_weight(x);
-      mine.count += key == thr;
+      if (x > floor_x) mine.mass += sc.kept_weight(x);
+      mine.count += x == floor_x;
     }
   }
+  if (thr == 0) mine.count = 0;
   Sum2 block_all;
-  const Sum2 mine_before = block_scan(mine, &block_all);
+  const Sum2 mine_before = block_scan<THREADS>(mine, &block_all);
   if (tid == 0) sh.part = block_all;
   cluster.sync();
-  u64 skip = 0, all_mass = 0, my_skip = 0, my_mass = 0, my_tied = 0, tied = 0;
+  u64 all_mass = 0, my_skip = 0, my_mass = 0, my_tied = 0, tied = 0;
   for (int b = 0; b < kCluster; ++b) {
     const Sum2* o = cluster.map_shared_rank(&sh.part, b);
     const u64 here = o->count, kept = tied >= ties ? 0 : (here < ties - tied ? here : ties - tied);
@@ -372,45 +490,43 @@ __global__ void __launch_bounds__(kThreads) k_sample(const T* __restrict__ logit
     // mass of the threads before this one in the block, ties kept lowest index first
     auto kept_ties = [&](u64 t0, u64 t1) { return min(t1, ties) - min(t0, ties); };
     const u64 t0 = my_tied + mine_before.count, t1 = t0 + mine.count;
-    skip = my_skip + mine_before.mass + kept_ties(my_tied, t0) * tie_weight;
+    const u64 skip = my_skip + mine_before.mass + kept_ties(my_tied, t0) * tie_weight;
     const u64 own = mine.mass + kept_ties(t0, t1) * tie_weight;
-    if (point >= skip && point < skip + own) { sh.owner = tid; sh.owner_skip = skip; sh.cross_before.mass = t0; }
+    if (point >= skip && point < skip + own) { sh.owner = tid; sh.owner_skip = skip; sh.owner_ties = t0; }
     __syncthreads();
     const int owner = sh.owner;
-    skip = sh.owner_skip;
-    const u64 tie0 = sh.cross_before.mass;
-    // the owner's run, one element per thread (a run has at most 17 pieces of 8 or 33 of 4 elements)
+    // the owner's run, one element per thread (with 256 threads a run has at most 17 pieces of 8 or 33 of 4 elements)
     const int e = owner * run * kVec + tid, end = min(pieces, (owner + 1) * run) * kVec;
     Sum2 one = {0, 0};
     if (e < end) {
       const float x = Raw<T>::get(slice[e / kVec], e % kVec);
-      const uint32_t key = key_of(x);
-      if (key > thr) one.mass = sc.kept_weight(x);
-      one.count = key == thr;
+      if (x > floor_x) one.mass = sc.kept_weight(x);
+      one.count = thr != 0 && x == floor_x;
     }
     Sum2 unused;
-    const Sum2 b = block_scan(one, &unused);
-    const u64 from = skip + b.mass + kept_ties(tie0, tie0 + b.count) * tie_weight;
+    const Sum2 b = block_scan<THREADS>(one, &unused);
+    const u64 tie0 = sh.owner_ties;
+    const u64 from = sh.owner_skip + b.mass + kept_ties(tie0, tie0 + b.count) * tie_weight;
     const u64 width = one.mass + kept_ties(tie0 + b.count, tie0 + b.count + one.count) * tie_weight;
     if (point >= from && point < from + width) out[r] = first + e - phase;
   }
   cluster.sync();   // no block leaves while its shared memory may still be read
 }
 
-template <typename T>
+template <typename T, int THREADS>
 cudaError_t launch(const void* logits, int64_t row_stride, int n, int vocab, const float* temperature, const int32_t* top_k,
                    const float* top_p, const float* min_p, const float* uniform, int64_t* out, cudaStream_t s) {
   constexpr int kVec = Raw<T>::kVec;
   const int per = (vocab + kCluster * kVec - 1) / (kCluster * kVec);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)n * kCluster); cfg.blockDim = dim3(kThreads); cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)n * kCluster); cfg.blockDim = dim3(THREADS); cfg.stream = s;
   cfg.dynamicSmemBytes = (size_t)(per + 1) * 16;     // one more piece: a slice that does not begin on a 16-byte boundary
-  if (cudaError_t e = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)) return e;
+  if (cudaError_t e = cudaFuncSetAttribute(k_sample<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)) return e;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = kCluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_sample<T>, (const T*)logits, row_stride, vocab, temperature, top_k, top_p, min_p, uniform,
+  return cudaLaunchKernelEx(&cfg, k_sample<T, THREADS>, (const T*)logits, row_stride, vocab, temperature, top_k, top_p, min_p, uniform,
                             reinterpret_cast<long long*>(out));
 }
 
@@ -425,8 +541,9 @@ extern "C" bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t r
   if ((words & 3) || (reinterpret_cast<uintptr_t>(out) & 7) || (reinterpret_cast<uintptr_t>(logits) & (logits_f32 ? 3 : 1)))
     return BC_ERR_INVALID_ARG;
   if (vocab > kMaxVocab || n > 0x7fffffff / kCluster) return BC_ERR_UNSUPPORTED;
-  const cudaError_t e = logits_f32 ? launch<float>(logits, row_stride, n, vocab, temperature, top_k, top_p, min_p, uniform, out, (cudaStream_t)stream)
-                                   : launch<__nv_bfloat16>(logits, row_stride, n, vocab, temperature, top_k, top_p, min_p, uniform, out,
-                                                           (cudaStream_t)stream);
+  // Few rows leave SMs idle: a block then takes twice the threads.
+  const auto f = n * kCluster <= 2 * 148 ? (logits_f32 ? launch<float, 512> : launch<__nv_bfloat16, 512>)
+                                         : (logits_f32 ? launch<float, 256> : launch<__nv_bfloat16, 256>);
+  const cudaError_t e = f(logits, row_stride, n, vocab, temperature, top_k, top_p, min_p, uniform, out, (cudaStream_t)stream);
   return e == cudaSuccess ? BC_OK : BC_ERR_CUDA;
 }
