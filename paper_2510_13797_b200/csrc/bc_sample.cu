@@ -36,7 +36,8 @@ typedef unsigned long long u64;
 
 constexpr int kCluster = 8;
 constexpr int kBins = 512;
-constexpr int kList = 256;             // elements of a bin that are ordered directly
+constexpr int kList = 512;             // elements that are ordered directly, by counting
+constexpr int kFew = 256;              // first guess at a limit: so many of the threads' maxima
 constexpr int kMaxVocab = 1 << 18;     // 2^18 weights of at most 2^45 add up in 63 bits
 constexpr int kWeightBits = 45;
 
@@ -77,12 +78,12 @@ __device__ __forceinline__ Sum2 block_scan(Sum2 x, Sum2* total) {
 template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> {
   static constexpr int kVec = 8;
-  // element i of a 16-byte piece, NaN read as -inf
+  // element i of a 16-byte piece (a NaN compares below everything that is asked for)
   __device__ static __forceinline__ float get(const uint4& v, int i) {
     const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[i >> 1];
-    const float f = __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
-    return f == f ? f + 0.f : -INFINITY;   // + 0: the two zeros are one value
+    return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
   }
+  __device__ static __forceinline__ __nv_bfloat16 of(float x) { return __float2bfloat16_rn(x); }
   __device__ static __forceinline__ __nv_bfloat16 none() { return __ushort_as_bfloat16(0xff80); }
   typedef __nv_bfloat162 Max;               // running maximum; the maximum of a number and a NaN is the number
   __device__ static __forceinline__ Max start() { return __halves2bfloat162(none(), none()); }
@@ -95,9 +96,9 @@ template <> struct Raw<__nv_bfloat16> {
 template <> struct Raw<float> {
   static constexpr int kVec = 4;
   __device__ static __forceinline__ float get(const uint4& v, int i) {
-    const float f = __uint_as_float(reinterpret_cast<const uint32_t*>(&v)[i]);
-    return f == f ? f + 0.f : -INFINITY;
+    return __uint_as_float(reinterpret_cast<const uint32_t*>(&v)[i]);
   }
+  __device__ static __forceinline__ float of(float x) { return x; }
   __device__ static __forceinline__ float none() { return -INFINITY; }
   typedef float Max;
   __device__ static __forceinline__ Max start() { return -INFINITY; }
@@ -107,29 +108,29 @@ template <> struct Raw<float> {
   __device__ static __forceinline__ float value(Max m) { return m + 0.f; }
 };
 
-// order-preserving key of a float (no NaN, one zero), and back
+// order-preserving key of a float that is not a NaN, and back
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x);
+  const uint32_t b = __float_as_uint(x + 0.f);   // the two zeros are one value
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
 struct Scale {
-  float top;      // the row's maximum
+  float top;      // the row's maximum, finite
   double dtop;
   double c;       // log2(e) / T
   float bins;     // 11 bins per octave
+  float low;      // elements up to here have a weight of 0 (-inf at least)
   double min_w;   // 2^45 min_p
-  // 2^45 e(x), in double precision: 2^-t for t = (top - x) log2(e) / T octaves, t = n - f with |f| <= 1/2, 2^f by its Taylor
-  // series to the tenth power (the rest is below 0.35^11 / 11! = 2^-42 of the value).  0 where it would round to 0.
+  // 2^45 e(x) for x > low, in double precision: 2^-t for t = (top - x) log2(e) / T octaves, t = n - f with |f| <= 1/2, 2^f by its
+  // Taylor series to the ninth power (the rest is below 0.35^10 / 10! = 2^-37 of the value).
   __device__ __forceinline__ double scaled(float x) const {
     constexpr double kMagic = 6755399441055744.0;              // 1.5 * 2^52: adding it rounds to an integer
-    const double t = (dtop - (double)x) * c;
-    const double m = t + kMagic;
+    const double d = dtop - (double)x;
+    const double m = fma(d, c, kMagic);
     const int n = __double2loint(m);
-    const double f = (m - kMagic) - t;
-    double p = 7.054911620801121e-09;                         // ln(2)^10 / 10!
-    p = fma(p, f, 1.0178086009239696e-07);
+    const double f = fma(-d, c, m - kMagic);
+    double p = 1.0178086009239696e-07;                         // ln(2)^9 / 9!
     p = fma(p, f, 1.3215486790144305e-06);
     p = fma(p, f, 1.5252733804059838e-05);
     p = fma(p, f, 1.5403530393381606e-04);
@@ -139,41 +140,57 @@ struct Scale {
     p = fma(p, f, 2.402265069591007e-01);
     p = fma(p, f, 6.931471805599453e-01);
     p = fma(p, f, 1.0);
-    const double v = __hiloint2double(__double2hiint(p) + ((kWeightBits - n) << 20), __double2loint(p));
-    if (x == top) return (double)(1ull << kWeightBits);        // also where top is infinite
-    return t < (double)(kWeightBits + 1) ? v : 0.0;            // also 0 for a t that is not a number (inf * 0)
+    return __hiloint2double(__double2hiint(p) + ((kWeightBits - n) << 20), __double2loint(p));
   }
-  // a double of at most 2^46 to the nearest integer
-  __device__ __forceinline__ static u64 rounded(double v) {
-    return (u64)__double_as_longlong(v + 4503599627370496.0) & 0xfffffffffffffull;
-  }
-  __device__ __forceinline__ u64 weight(float x) const { return rounded(scaled(x)); }
+  // a double of at most 2^46, rounded to an integer, as the low 52 bits of its sum with 2^52
+  static constexpr u64 kBias = 0x4330000000000000ull;
+  __device__ __forceinline__ static u64 biased(double v) { return (u64)__double_as_longlong(v + 4503599627370496.0); }
+  __device__ __forceinline__ u64 weight(float x) const { return x > low ? biased(scaled(x)) - kBias : 0; }
   __device__ __forceinline__ u64 kept_weight(float x) const {   // 0 below min_p
+    if (!(x > low)) return 0;
     const double v = scaled(x);
-    return v >= min_w ? rounded(v) : 0;
+    return v >= min_w ? biased(v) - kBias : 0;
   }
-  __device__ __forceinline__ float depth(float x) const { return x == top ? 0.f : (top - x) * bins; }   // NaN for weights of 0 only
+  __device__ __forceinline__ float depth(float x) const { return (top - x) * bins; }   // in bins
   __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)depth(x)); }
+  // of an element above low; the last bin has no lower end
   __device__ __forceinline__ bool in_bin(float x, int b) const {
     const float d = depth(x);
     return d >= (float)b && (d < (float)(b + 1) || b == kBins - 1);
   }
 };
 
+struct Cross {                   // where a search ended
+  Sum2 before, all;
+  int bin;
+  uint32_t in;
+};
+
+// A histogram, or a list of candidates: one search step has one or the other.  Small, because a slice of 150,000 bf16 logits
+// leaves room for four blocks on an SM only while all of this stays below 18 KB.
+union Work {
+  // A mass is three sums of 32 bits, of the weights' bits 0 .. 15, 16 .. 31 and 32 .. 45 (at most 2^15 elements of a block):
+  // shared memory adds 64 bits ten times slower.
+  struct { uint32_t mass[3][kBins], count[kBins]; } h;
+  struct {
+    uint32_t list[kList];        // this block's candidates
+    uint32_t keys[kList];        // all blocks' candidates, and their weights
+    u64 weights[kList];
+  } c;
+};
+
 struct Shared {
-  u64 mass[2][kBins];            // histograms: two, used in turn (one may still be read by other blocks)
-  uint32_t count[2][kBins];
+  Work work[2];                  // used in turn: one may still be read by other blocks
   uint32_t key_lo[2], key_hi[2];
-  uint32_t list[2][kList];       // this block's elements of a bin, likewise
   int n_list[2];
-  uint32_t keys[kList];          // all blocks' elements of a bin, and their weights
-  u64 weights[kList];
-  float best;                    // this block's maximum
+  float best, row_best;          // this block's maximum, the row's
   int at;                        // its lowest index (greedy rows)
   Sum2 part;                     // this block's mass above the threshold and number of elements at it
-  // results of a search, for the whole block
-  int cross_bin;
-  Sum2 cross_before, cross_in;
+  Sum2 parts[kCluster];          // every block's
+  int offset[kCluster + 1];
+  Cross cross;
+  Sum2 above;
+  int found;
   uint32_t thr;
   int owner;
   u64 owner_skip, owner_ties;
@@ -198,7 +215,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   const int first = min(part * per, vocab), cnt = min(vocab - first, per);
   const int phase = (int)((reinterpret_cast<uintptr_t>(row + first) & 15) / sizeof(T));
   const int pieces = cnt > 0 ? (phase + cnt + kVec - 1) / kVec : 0;
-  T* flat = reinterpret_cast<T*>(slice);
   typename Raw<T>::Max run_max = Raw<T>::start();
   const int whole0 = phase > 0 ? 1 : 0, whole1 = (phase + cnt) / kVec;          // pieces that lie in the slice entirely
   const uint4* aligned = reinterpret_cast<const uint4*>(row + first - phase);   // piece p at aligned + p
@@ -211,20 +227,25 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   if (tid < 2 && pieces > 0) {                                                    // the ends: only what belongs to the row is read
     const int p = tid == 0 ? 0 : pieces - 1;
     if ((p < whole0 || p >= whole1) && !(tid == 1 && pieces == 1)) {
+      T e[kVec];
       for (int i = 0; i < kVec; ++i) {
-        const int e = p * kVec - phase + i;
-        flat[p * kVec + i] = e >= 0 && e < cnt ? row[first + e] : Raw<T>::none();
+        const int at = p * kVec - phase + i;
+        e[i] = at >= 0 && at < cnt ? row[first + at] : Raw<T>::none();
       }
-      Raw<T>::fold(run_max, slice[p]);
+      uint4 v;
+      memcpy(&v, e, 16);
+      slice[p] = v;
+      Raw<T>::fold(run_max, v);
     }
   }
-  float best = Raw<T>::value(run_max);
-  if (!(best == best)) best = -INFINITY;
+  float thread_best = Raw<T>::value(run_max);
+  if (!(thread_best == thread_best)) thread_best = -INFINITY;
+  float best = thread_best;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
   if (lane == 0) warp_best[warp] = best;
-  for (int b = tid; b < kBins; b += THREADS) { sh.mass[0][b] = 0; sh.count[0][b] = 0; }
-  if (tid == 0) sh.at = 0x7fffffff;
+  for (int b = tid; b < kBins; b += THREADS) sh.work[0].h.mass[0][b] = sh.work[0].h.mass[1][b] = sh.work[0].h.mass[2][b] = sh.work[0].h.count[b] = sh.work[1].h.count[b] = 0;
+  if (tid == 0) { sh.at = 0x7fffffff; sh.n_list[0] = 0; }
   __syncthreads();
   if (warp == 0) {
     best = lane < kWarps ? warp_best[lane] : -INFINITY;
@@ -233,9 +254,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     if (lane == 0) sh.best = best;
   }
   cluster.sync();
-  best = -INFINITY;
+  if (warp == 0) {                                 // one warp asks the other blocks, lane b block b
+    best = *cluster.map_shared_rank(&sh.best, lane & (kCluster - 1));
 #pragma unroll
-  for (int b = 0; b < kCluster; ++b) best = fmaxf(best, *cluster.map_shared_rank(&sh.best, b));
+    for (int d = kCluster / 2; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
+    if (lane == 0) sh.row_best = best;
+  }
+  __syncthreads();
+  best = sh.row_best;
 
   const float temp = temperature != nullptr ? temperature[r] : 1.f;
   if (!(temp > 0.f) || best == -INFINITY) {        // greedy; a row without a finite element: its first index, as bc_argmax
@@ -258,11 +284,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     cluster.sync();                                // no block leaves while its shared memory may still be read
     return;
   }
+  if (best == INFINITY) {                          // infinite logits share the mass: 0 in a row of -inf
+    for (int q = tid; q < pieces; q += THREADS) {
+      T e[kVec];
+      for (int i = 0; i < kVec; ++i) e[i] = Raw<T>::get(slice[q], i) == INFINITY ? Raw<T>::of(0.f) : Raw<T>::none();
+      memcpy(&slice[q], e, 16);
+    }
+    best = 0.f;
+    thread_best = thread_best == INFINITY ? 0.f : -INFINITY;
+    __syncthreads();
+  }
   Scale sc;
   sc.top = best;
   sc.dtop = (double)best;
-  sc.c = 1.4426950408889634 / (double)temp;
-  sc.bins = (float)(11.0 * sc.c);
+  sc.c = fmax(1.4426950408889634 / (double)temp, 1e-300);   // not 0 for an infinite temperature: 0 * inf
+  sc.bins = (float)fmin(11.0 * sc.c, 1e38);                 // finite: 0 * inf again
+  sc.low = fminf((float)(sc.dtop - (kWeightBits + 1) / sc.c), nextafterf(best, -INFINITY));
   const float mp = min_p != nullptr ? min_p[r] : 0.f;
   sc.min_w = mp > 0.f ? fmin((double)mp, 1.0) * (double)(1ull << kWeightBits) : 0.0;   // at most 1: the largest element is always kept
   const int k = top_k != nullptr ? top_k[r] : 0;
@@ -274,35 +311,171 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   u64 ties = 0;                                     // with no limit: every key is above 0, the key no float has
   int round = 1;                                    // which of the two histograms and lists is next
   auto val = [](const Sum2& s, bool count) { return count ? (u64)s.count : s.mass; };
-  // Adds the cluster's histograms up (this thread: bins kPer tid ...).
-  auto totals = [&](int which, Sum2 (&b)[kPer]) {
+  auto add = [&](int which, int b, u64 w) {
+    atomicAdd(&sh.work[which].h.count[b], 1u);
+    atomicAdd(&sh.work[which].h.mass[0][b], (uint32_t)w & 0xffffu);
+    if (w >> 16) atomicAdd(&sh.work[which].h.mass[1][b], (uint32_t)(w >> 16) & 0xffffu);
+    if (w >> 32) atomicAdd(&sh.work[which].h.mass[2][b], (uint32_t)(w >> 32));
+  };
+  // Block 0 adds the cluster's histograms up, thread t its bins kPer t ... (`masses`: the masses too), and searches them for
+  // the cluster: all blocks together would read eight times as much of one another's memory.
+  auto totals = [&](int which, bool masses, Sum2 (&b)[kPer]) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       b[i] = {0, 0};
+      if (part == 0) {
 #pragma unroll
-      for (int o = 0; o < kCluster; ++o) {
-        b[i].mass += *cluster.map_shared_rank(&sh.mass[which][kPer * tid + i], o);
-        b[i].count += *cluster.map_shared_rank(&sh.count[which][kPer * tid + i], o);
+        for (int o = 0; o < kCluster; ++o) {
+          b[i].count += *cluster.map_shared_rank(&sh.work[which].h.count[kPer * tid + i], o);
+          if (masses)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) b[i].mass += (u64)*cluster.map_shared_rank(&sh.work[which].h.mass[j][kPer * tid + i], o) << (16 * j);
+        }
       }
     }
   };
-  // The bin in which the running count (or mass), largest keys first, reaches `limit`: false if it never does.
+  auto mass_limit = [&](u64 mass) {                  // the largest element is always kept; NaN never comes here
+    const double want = ceil((double)p * (double)mass);
+    return want >= 1.0 ? (u64)want : (u64)1;
+  };
+  // The bin in which the running count (or mass), largest keys first, reaches `limit`: false if it never does.  *all: the sum of
+  // the bins.  Block 0 searches its totals, the others take over what it finds.  limit 0: the top-p limit of
+  // the sum.
   auto cross = [&](const Sum2 (&b)[kPer], const Sum2& before0, bool count, u64 limit, Sum2* all) {
-    if (tid == 0) sh.cross_bin = -1;
-    Sum2 mine = b[0];
+    if (part == 0) {
+      if (tid == 0) sh.cross.bin = -1;
+      Sum2 mine = b[0];
 #pragma unroll
-    for (int i = 1; i < kPer; ++i) mine = mine + b[i];
-    Sum2 e = block_scan<THREADS>(mine, all) + before0;   // its barriers order the store above
+      for (int i = 1; i < kPer; ++i) mine = mine + b[i];
+      Sum2 sum;
+      Sum2 e = block_scan<THREADS>(mine, &sum) + before0;   // its barriers order the store above
+      if (limit == 0) limit = mass_limit(sum.mass);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const Sum2 n = e + b[i];
-      if (val(e, count) < limit && limit <= val(n, count)) { sh.cross_bin = kPer * tid + i; sh.cross_before = e; sh.cross_in = b[i]; }
-      e = n;
+      for (int i = 0; i < kPer; ++i) {
+        const Sum2 n = e + b[i];
+        if (val(e, count) < limit && limit <= val(n, count)) { sh.cross.bin = kPer * tid + i; sh.cross.before = e; sh.cross.in = b[i].count; }
+        e = n;
+      }
+      if (tid == 0) sh.cross.all = sum;
+    }
+    cluster.sync();
+    if (warp == 0 && part != 0) {
+      const uint32_t* from = reinterpret_cast<const uint32_t*>(cluster.map_shared_rank(&sh.cross, 0));
+      if (lane < (int)(sizeof(Cross) / 4)) reinterpret_cast<uint32_t*>(&sh.cross)[lane] = from[lane];
     }
     __syncthreads();
-    return sh.cross_bin >= 0;
+    *all = sh.cross.all;
+    return sh.cross.bin >= 0;
   };
-  if (by_count || by_mass) {
+  // The lengths of all blocks' lists, as offsets; their sum.
+  auto offsets = [&](int which) {
+    if (warp == 0) {
+      int x = lane < kCluster ? *cluster.map_shared_rank(&sh.n_list[which], lane) : 0;
+#pragma unroll
+      for (int d = 1; d < kCluster; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (lane < kCluster) sh.offset[lane + 1] = x;
+      if (lane == 0) sh.offset[0] = 0;
+    }
+    __syncthreads();
+    return sh.offset[kCluster];
+  };
+  // All blocks' candidate lists, one behind the other, with their weights, in this block's memory.
+  auto gather = [&](int which) {
+    for (int at = tid; at < min(kList, sh.offset[kCluster]); at += THREADS) {
+      int o = 0;
+#pragma unroll
+      for (int b = 1; b < kCluster; ++b) o += at >= sh.offset[b];
+      const uint32_t key = *cluster.map_shared_rank(&sh.work[which].c.list[at - sh.offset[o]], o);
+      sh.work[which].c.keys[at] = key;
+      sh.work[which].c.weights[at] = sc.weight(of_key(key));
+    }
+    __syncthreads();
+  };
+  // Among `len` gathered candidates, with `before` above them: the key at which the running count (or mass) reaches `limit`, and
+  // what lies above that key (false if the limit is not reached).  Every candidate counts what is above itself.
+  auto select = [&](int which, int len, bool count, u64 limit, Sum2* before, uint32_t* key_out) {
+    const uint32_t* keys = sh.work[which].c.keys;
+    const u64* weights = sh.work[which].c.weights;
+    if (tid == 0) sh.found = 0;
+    __syncthreads();
+    for (int at = tid; at < len; at += THREADS) {
+      const uint32_t key = keys[at];
+      Sum2 above = *before;
+      uint32_t same = 0;
+#pragma unroll 4
+      for (int j = 0; j < len; ++j) {
+        const uint32_t o = keys[j];
+        if (o > key) { above.mass += weights[j]; ++above.count; }
+        same += o == key;
+      }
+      if (val(above, count) < limit && limit <= val(above + Sum2{same * weights[at], same}, count)) {
+        sh.found = 1; sh.thr = key; sh.above = above;   // equal keys write equal values
+      }
+    }
+    __syncthreads();
+    *before = sh.above;
+    *key_out = sh.thr;
+    const bool found = sh.found != 0;
+    __syncthreads();
+    return found;
+  };
+  // A small top-k: the elements no deeper than the kFew-th largest of the threads' maxima are few (unless the large ones are
+  // neighbours) and hold the limit.  One atomic per thread instead of several per element, and no weights but theirs.
+  bool open = by_count || by_mass;                    // the threshold is still to be found
+  if (by_count && k <= kFew) {
+    if (thread_best > sc.low) atomicAdd(&sh.work[1].h.count[sc.bin(thread_best)], 1u);
+    cluster.sync();
+    Sum2 bins[kPer], all;
+    totals(1, false, bins);
+    const int last = cross(bins, Sum2{0, 0}, true, (u64)kFew, &all) ? sh.cross.bin : kBins - 1;
+    const float reach = last == kBins - 1 ? INFINITY : (float)(last + 1);
+    for (int q = tid; q < pieces; q += THREADS) {
+      const uint4 v = slice[q];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float x = Raw<T>::get(v, i);
+        if (x > sc.low && sc.depth(x) < reach) {
+          const int at = atomicAdd(&sh.n_list[0], 1);
+          if (at < kList) sh.work[0].c.list[at] = key_of(x);
+        }
+      }
+    }
+    cluster.sync();
+    const int len = offsets(0);
+    if (len <= kList) {
+      gather(0);
+      Sum2 before = {0, 0};
+      uint32_t key = 0;
+      u64 mass;
+      open = false;
+      if (select(0, len, true, (u64)k, &before, &key)) {
+        thr = key;
+        ties = (u64)k - before.count;
+        mass = before.mass + ties * sc.weight(of_key(thr));
+      } else {                                        // fewer than k elements have a weight, and all of them are here
+        block_scan<THREADS>(Sum2{(tid < len ? sh.work[0].c.weights[tid] : 0) + (THREADS < kList && tid + THREADS < len ? sh.work[0].c.weights[tid + THREADS] : 0), 0}, &all);
+        mass = all.mass;
+      }
+      if (by_mass) {
+        const u64 limit = mass_limit(mass);
+        before = {0, 0};
+        if (select(0, len, false, limit, &before, &key)) {
+          thr = key;
+          const u64 w = sc.weight(of_key(thr));
+          ties = (limit - before.mass + w - 1) / w;
+        }
+      }
+    }
+  }
+  if (open) {
+    if (by_count && k <= kFew) {                      // the list of the first try lies where the histogram goes
+      for (int b = tid; b < kBins; b += THREADS) sh.work[0].h.mass[0][b] = sh.work[0].h.mass[1][b] = sh.work[0].h.mass[2][b] = sh.work[0].h.count[b] = 0;
+      __syncthreads();
+    }
+    // The general search.  Counts and masses of all elements by bins of depth:
     for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
 #pragma unroll
@@ -311,20 +484,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
         const u64 w = sc.weight(x);
         if (w) {
           const int b = sc.bin(x);
-          atomicAdd(&sh.mass[0][b], w);
-          atomicAdd(&sh.count[0][b], 1u);
+          add(0, b, w);
         }
       }
     }
     cluster.sync();
     Sum2 bins[kPer], all;
-    totals(0, bins);
+    totals(0, true, bins);
     // From the bin that cross() found to the key: while the bin holds many elements, histograms over the bits in which its
-    // keys differ; then its elements are gathered and ordered by counting.  Returns the key, *before: what lies above it.
+    // keys differ; then its elements are gathered and ordered.  Returns the key, *before: what lies above it.
     auto refine = [&](bool count, u64 limit, Sum2* before) {
-      const int bin = sh.cross_bin;
-      *before = sh.cross_before;
-      uint32_t in = sh.cross_in.count;
+      const int bin = sh.cross.bin;
+      *before = sh.cross.before;
+      uint32_t in = sh.cross.in;
       uint32_t lo = 0, hi = 0xffffffffu;
       for (; in > kList; ++round) {
         uint32_t mn = 0xffffffffu, mx = 0;
@@ -334,12 +506,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
           for (int i = 0; i < kVec; ++i) {
             const float x = Raw<T>::get(v, i);
             const uint32_t key = key_of(x);
-            if (key >= lo && key <= hi && sc.in_bin(x, bin) && sc.weight(x)) { mn = min(mn, key); mx = max(mx, key); }
+            if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) { mn = min(mn, key); mx = max(mx, key); }
           }
         }
         const int which = round & 1;
         if (tid == 0) { sh.key_lo[which] = 0xffffffffu; sh.key_hi[which] = 0; }
-        for (int b = tid; b < kBins; b += THREADS) { sh.mass[which][b] = 0; sh.count[which][b] = 0; }
+        for (int b = tid; b < kBins; b += THREADS) sh.work[which].h.mass[0][b] = sh.work[which].h.mass[1][b] = sh.work[which].h.mass[2][b] = sh.work[which].h.count[b] = 0;
         __syncthreads();
         if (mn <= mx) { atomicMin(&sh.key_lo[which], mn); atomicMax(&sh.key_hi[which], mx); }
         cluster.sync();
@@ -357,26 +529,25 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
           for (int i = 0; i < kVec; ++i) {
             const float x = Raw<T>::get(v, i);
             const uint32_t key = key_of(x);
-            if (key >= mn && key <= mx && sc.in_bin(x, bin)) {
+            if (sc.in_bin(x, bin) && key >= mn && key <= mx) {
               const u64 w = sc.weight(x);
               if (w) {
                 const int b = (int)((mx - key) >> shift);
-                atomicAdd(&sh.mass[which][b], w);
-                atomicAdd(&sh.count[which][b], 1u);
+                add(which, b, w);
               }
             }
           }
         }
         cluster.sync();
         Sum2 sub[kPer], unused;
-        totals(which, sub);
+        totals(which, true, sub);
         cross(sub, *before, count, limit, &unused);
-        *before = sh.cross_before;
-        in = sh.cross_in.count;
-        const uint32_t b = (uint32_t)sh.cross_bin;
+        *before = sh.cross.before;
+        in = sh.cross.in;
+        const uint32_t b = (uint32_t)sh.cross.bin;
         hi = mx - (b << shift);
         lo = max(mn, hi - ((1u << shift) - 1u));
-        __syncthreads();                             // sh.cross_* have been read
+        __syncthreads();                             // sh.cross has been read
       }
       const int which = round & 1;
       ++round;
@@ -388,46 +559,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
         for (int i = 0; i < kVec; ++i) {
           const float x = Raw<T>::get(v, i);
           const uint32_t key = key_of(x);
-          if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) sh.list[which][atomicAdd(&sh.n_list[which], 1)] = key;
+          if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) sh.work[which].c.list[atomicAdd(&sh.n_list[which], 1)] = key;
         }
       }
       cluster.sync();
-      if (tid < kList) {                              // all blocks' lists, one behind the other
-        int j = tid, o = 0, len = 0;
-        for (; o < kCluster; ++o) {
-          len = *cluster.map_shared_rank(&sh.n_list[which], o);
-          if (j < len) break;
-          j -= len;
-        }
-        if (o < kCluster) {
-          const uint32_t key = *cluster.map_shared_rank(&sh.list[which][j], o);
-          sh.keys[tid] = key;
-          sh.weights[tid] = sc.weight(of_key(key));
-        }
-      }
-      __syncthreads();
-      if (tid < (int)in) {
-        const uint32_t key = sh.keys[tid];
-        const u64 w = sh.weights[tid];
-        Sum2 above = *before;
-        uint32_t same = 0;
-        for (int j = 0; j < (int)in; ++j) {
-          const uint32_t o = sh.keys[j];
-          if (o > key) { above.mass += sh.weights[j]; ++above.count; }
-          same += o == key;
-        }
-        if (val(above, count) < limit && limit <= val(above + Sum2{same * w, same}, count)) { sh.thr = key; sh.cross_before = above; }
-      }
-      __syncthreads();
-      *before = sh.cross_before;
-      return sh.thr;
+      offsets(which);
+      gather(which);
+      uint32_t key = 0;
+      select(which, (int)in, count, limit, before, &key);
+      return key;
     };
     bool cut = false;
     Sum2 before;
     u64 mass = 0;
     if (by_count) {
       cut = cross(bins, Sum2{0, 0}, true, (u64)k, &all);
-      mass = all.mass;
       if (cut) {
         thr = refine(true, (u64)k, &before);
         ties = (u64)k - before.count;
@@ -435,17 +581,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       }
     }
     if (by_mass) {
-      __syncthreads();
-      if (!cut) {
-        Sum2 mine = bins[0];
-#pragma unroll
-        for (int i = 1; i < kPer; ++i) mine = mine + bins[i];
-        block_scan<THREADS>(mine, &all);
-        mass = all.mass;
-      }
-      const double want = ceil((double)p * (double)mass);
-      const u64 limit = want >= 1.0 ? (u64)want : 1;   // the largest element is always kept; NaN never comes here
-      if (cross(bins, Sum2{0, 0}, false, limit, &all)) {
+      cluster.sync();                                // the other blocks have taken over what the search before found
+      const bool found = cross(bins, Sum2{0, 0}, false, cut ? mass_limit(mass) : 0, &all);
+      const u64 limit = mass_limit(cut ? mass : all.mass);
+      if (found) {
         thr = refine(false, limit, &before);
         const u64 w = sc.weight(of_key(thr));
         ties = (limit - before.mass + w - 1) / w;
@@ -458,27 +597,43 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   // reads of neighbouring threads off one another's banks.
   const int run = ((per / kVec + 1 + THREADS - 1) / THREADS) | 1;
   const u64 tie_weight = thr != 0 ? sc.kept_weight(of_key(thr)) : 0;
-  const float floor_x = thr != 0 ? of_key(thr) : -INFINITY;      // nothing below it is kept
+  const float floor_x = thr != 0 ? of_key(thr) : sc.low;         // nothing below it is kept
   Sum2 mine = {0, 0};                                // mass above the threshold, elements at it
-  for (int q = tid * run; q < min(pieces, (tid + 1) * run); ++q) {
-    const uint4 v = slice[q];
+  const T* flat = reinterpret_cast<const T*>(slice);
+  const int run_end = min(pieces, (tid + 1) * run);
+  for (int q = tid * run; q < run_end; q += 32 / kVec) {
+    // 32 elements at a time: first which of them are kept, then their weights, so that a warp whose lanes keep few
+    // elements evaluates few
+    uint32_t above = 0;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const float x = Raw<T>::get(v, i);
-      if (x > floor_x) mine.mass += sc.kept_weight(x);
-      mine.count += x == floor_x;
+    for (int o = 0; o < 32 / kVec; ++o) {
+      if (q + o < run_end) {
+        const uint4 v = slice[q + o];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const float x = Raw<T>::get(v, i);
+          above |= (x > floor_x ? 1u : 0u) << (o * kVec + i);
+          mine.count += x == floor_x;
+        }
+      }
     }
+    for (; above; above &= above - 1) mine.mass += sc.kept_weight((float)flat[q * kVec + __ffs(above) - 1]);
   }
   if (thr == 0) mine.count = 0;
   Sum2 block_all;
   const Sum2 mine_before = block_scan<THREADS>(mine, &block_all);
   if (tid == 0) sh.part = block_all;
   cluster.sync();
+  if (tid < kCluster) {
+    const Sum2* o = cluster.map_shared_rank(&sh.part, tid);
+    sh.parts[tid] = *o;
+  }
+  __syncthreads();
   u64 all_mass = 0, my_skip = 0, my_mass = 0, my_tied = 0, tied = 0;
+#pragma unroll
   for (int b = 0; b < kCluster; ++b) {
-    const Sum2* o = cluster.map_shared_rank(&sh.part, b);
-    const u64 here = o->count, kept = tied >= ties ? 0 : (here < ties - tied ? here : ties - tied);
-    const u64 m = o->mass + kept * tie_weight;
+    const u64 here = sh.parts[b].count, kept = tied >= ties ? 0 : (here < ties - tied ? here : ties - tied);
+    const u64 m = sh.parts[b].mass + kept * tie_weight;
     if (b == part) { my_skip = all_mass; my_tied = tied; my_mass = m; }
     all_mass += m;
     tied += here;
@@ -541,8 +696,9 @@ extern "C" bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t r
   if ((words & 3) || (reinterpret_cast<uintptr_t>(out) & 7) || (reinterpret_cast<uintptr_t>(logits) & (logits_f32 ? 3 : 1)))
     return BC_ERR_INVALID_ARG;
   if (vocab > kMaxVocab || n > 0x7fffffff / kCluster) return BC_ERR_UNSUPPORTED;
-  // Few rows leave SMs idle: a block then takes twice the threads.
-  const auto f = n * kCluster <= 2 * 148 ? (logits_f32 ? launch<float, 512> : launch<__nv_bfloat16, 512>)
+  // 512 threads where only two blocks fit an SM in any case: few rows, or slices too large for four.
+  const bool wide = n * kCluster <= 2 * 148 || (int64_t)vocab * (logits_f32 ? 4 : 2) > (int64_t)kCluster * 38 * 1024;
+  const auto f = wide ? (logits_f32 ? launch<float, 512> : launch<__nv_bfloat16, 512>)
                                          : (logits_f32 ? launch<float, 256> : launch<__nv_bfloat16, 256>);
   const cudaError_t e = f(logits, row_stride, n, vocab, temperature, top_k, top_p, min_p, uniform, out, (cudaStream_t)stream);
   return e == cudaSuccess ? BC_OK : BC_ERR_CUDA;
