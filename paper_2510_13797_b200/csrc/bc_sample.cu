@@ -75,7 +75,14 @@ __device__ __forceinline__ Sum2 block_scan(Sum2 x, Sum2* total) {
   return {before.mass + incl.mass - x.mass, before.count + incl.count - x.count};
 }
 
-template <typename T> struct Raw;
+// order-preserving key of a float that is not a NaN, and back
+__device__ __forceinline__ uint32_t key32(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);   // the two zeros are one value
+  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float of_key32(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
+
+template <typename T> struct Raw;   // key, of_key: the same for the type's values, as small numbers (bf16: 16 bits)
 template <> struct Raw<__nv_bfloat16> {
   static constexpr int kVec = 8;
   // element i of a 16-byte piece (a NaN compares below everything that is asked for)
@@ -83,6 +90,8 @@ template <> struct Raw<__nv_bfloat16> {
     const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[i >> 1];
     return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
   }
+  __device__ static __forceinline__ uint32_t key(float x) { return key32(x) >> 16; }   // of any float: rounded down
+  __device__ static __forceinline__ float of_key(uint32_t k) { return of_key32(k << 16 | (k < 0x8000u ? 0xffffu : 0u)); }
   __device__ static __forceinline__ __nv_bfloat16 of(float x) { return __float2bfloat16_rn(x); }
   __device__ static __forceinline__ __nv_bfloat16 none() { return __ushort_as_bfloat16(0xff80); }
   typedef __nv_bfloat162 Max;               // running maximum; the maximum of a number and a NaN is the number
@@ -98,6 +107,8 @@ template <> struct Raw<float> {
   __device__ static __forceinline__ float get(const uint4& v, int i) {
     return __uint_as_float(reinterpret_cast<const uint32_t*>(&v)[i]);
   }
+  __device__ static __forceinline__ uint32_t key(float x) { return key32(x); }
+  __device__ static __forceinline__ float of_key(uint32_t k) { return of_key32(k); }
   __device__ static __forceinline__ float of(float x) { return x; }
   __device__ static __forceinline__ float none() { return -INFINITY; }
   typedef float Max;
@@ -107,13 +118,6 @@ template <> struct Raw<float> {
   }
   __device__ static __forceinline__ float value(Max m) { return m + 0.f; }
 };
-
-// order-preserving key of a float that is not a NaN, and back
-__device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.f);   // the two zeros are one value
-  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
 
 struct Scale {
   float top;      // the row's maximum, finite
@@ -181,8 +185,8 @@ union Work {
 
 struct Shared {
   Work work[2];                  // used in turn: one may still be read by other blocks
-  uint32_t key_lo[2], key_hi[2];
   int n_list[2];
+  u64 rest, row_rest;            // mass of the elements that the histogram leaves out: this block's, the row's
   float best, row_best;          // this block's maximum, the row's
   int at;                        // its lowest index (greedy rows)
   Sum2 part;                     // this block's mass above the threshold and number of elements at it
@@ -311,8 +315,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   u64 ties = 0;                                     // with no limit: every key is above 0, the key no float has
   int round = 1;                                    // which of the two histograms and lists is next
   auto val = [](const Sum2& s, bool count) { return count ? (u64)s.count : s.mass; };
-  auto add = [&](int which, int b, u64 w) {
-    atomicAdd(&sh.work[which].h.count[b], 1u);
+  auto add = [&](int which, int b, u64 w, bool count, bool mass) {
+    if (count) atomicAdd(&sh.work[which].h.count[b], 1u);
+    if (!mass) return;
     atomicAdd(&sh.work[which].h.mass[0][b], (uint32_t)w & 0xffffu);
     if (w >> 16) atomicAdd(&sh.work[which].h.mass[1][b], (uint32_t)(w >> 16) & 0xffffu);
     if (w >> 32) atomicAdd(&sh.work[which].h.mass[2][b], (uint32_t)(w >> 32));
@@ -349,7 +354,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       for (int i = 1; i < kPer; ++i) mine = mine + b[i];
       Sum2 sum;
       Sum2 e = block_scan<THREADS>(mine, &sum) + before0;   // its barriers order the store above
-      if (limit == 0) limit = mass_limit(sum.mass);
+      if (limit == 0) { sum.mass += sh.row_rest; limit = mass_limit(sum.mass); }
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const Sum2 n = e + b[i];
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       for (int b = 1; b < kCluster; ++b) o += at >= sh.offset[b];
       const uint32_t key = *cluster.map_shared_rank(&sh.work[which].c.list[at - sh.offset[o]], o);
       sh.work[which].c.keys[at] = key;
-      sh.work[which].c.weights[at] = sc.weight(of_key(key));
+      sh.work[which].c.weights[at] = sc.weight(Raw<T>::of_key(key));
     }
     __syncthreads();
   };
@@ -439,7 +444,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
         const float x = Raw<T>::get(v, i);
         if (x > sc.low && sc.depth(x) < reach) {
           const int at = atomicAdd(&sh.n_list[0], 1);
-          if (at < kList) sh.work[0].c.list[at] = key_of(x);
+          if (at < kList) sh.work[0].c.list[at] = Raw<T>::key(x);
         }
       }
     }
@@ -454,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       if (select(0, len, true, (u64)k, &before, &key)) {
         thr = key;
         ties = (u64)k - before.count;
-        mass = before.mass + ties * sc.weight(of_key(thr));
+        mass = before.mass + ties * sc.weight(Raw<T>::of_key(thr));
       } else {                                        // fewer than k elements have a weight, and all of them are here
         block_scan<THREADS>(Sum2{(tid < len ? sh.work[0].c.weights[tid] : 0) + (THREADS < kList && tid + THREADS < len ? sh.work[0].c.weights[tid + THREADS] : 0), 0}, &all);
         mass = all.mass;
@@ -464,7 +469,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
         before = {0, 0};
         if (select(0, len, false, limit, &before, &key)) {
           thr = key;
-          const u64 w = sc.weight(of_key(thr));
+          const u64 w = sc.weight(Raw<T>::of_key(thr));
           ties = (limit - before.mass + w - 1) / w;
         }
       }
@@ -475,66 +480,64 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       for (int b = tid; b < kBins; b += THREADS) sh.work[0].h.mass[0][b] = sh.work[0].h.mass[1][b] = sh.work[0].h.mass[2][b] = sh.work[0].h.count[b] = 0;
       __syncthreads();
     }
-    // The general search.  Counts and masses of all elements by bins of depth:
+    // The general search.  Counts and masses of the elements by bins of depth.  Without a top-k the elements of
+    // log2(vocab / (1 - top_p)) octaves and more are left out: all of them together are less than (1 - top_p) of the largest
+    // weight, so the limit is reached before them; they are most of a row at low temperatures.
+    const bool masses = by_mass;
+    const float deep = by_count ? INFINITY : 11.f * (log2f((float)vocab / (1.f - fmaxf(p, 0.f))) + 1.f);
+    u64 rest = 0;
     for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         const float x = Raw<T>::get(v, i);
-        const u64 w = sc.weight(x);
-        if (w) {
-          const int b = sc.bin(x);
-          add(0, b, w);
+        if (x > sc.low) {
+          const u64 w = sc.weight(x);
+          if (sc.depth(x) >= deep) rest += w;
+          else if (w) add(0, sc.bin(x), w, by_count, masses);
         }
       }
     }
-    cluster.sync();
     Sum2 bins[kPer], all;
-    totals(0, true, bins);
-    // From the bin that cross() found to the key: while the bin holds many elements, histograms over the bits in which its
-    // keys differ; then its elements are gathered and ordered.  Returns the key, *before: what lies above it.
+    {
+      Sum2 sum;
+      block_scan<THREADS>(Sum2{rest, 0}, &sum);
+      if (tid == 0) sh.rest = sum.mass;
+    }
+    cluster.sync();
+    totals(0, masses, bins);
+    if (part == 0 && warp == 0) {
+      u64 m = lane < kCluster ? *cluster.map_shared_rank(&sh.rest, lane) : 0;
+#pragma unroll
+      for (int d = kCluster / 2; d > 0; d >>= 1) m += __shfl_xor_sync(0xffffffffu, m, d);
+      if (lane == 0) sh.row_rest = m;
+    }
+    // From the bin that cross() found to the key: a histogram over the keys of the bin (over their upper bits while they are too
+    // many for one: the next step then takes the keys of one of its entries), or, once the elements are few, all of them ordered.
+    // Returns the key, *before: what lies above it.
     auto refine = [&](bool count, u64 limit, Sum2* before) {
       const int bin = sh.cross.bin;
       *before = sh.cross.before;
-      uint32_t in = sh.cross.in;
-      uint32_t lo = 0, hi = 0xffffffffu;
-      for (; in > kList; ++round) {
-        uint32_t mn = 0xffffffffu, mx = 0;
-        for (int q = tid; q < pieces; q += THREADS) {
-          const uint4 v = slice[q];
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) {
-            const float x = Raw<T>::get(v, i);
-            const uint32_t key = key_of(x);
-            if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) { mn = min(mn, key); mx = max(mx, key); }
-          }
-        }
+      uint32_t in = count ? sh.cross.in : 0xffffffffu;
+      // keys the bin can hold: its ends, rounded outwards
+      const float x1 = (float)bin / sc.bins, x0 = (float)(bin + 1) / sc.bins, slack = (fabsf(sc.top) + x0) * 4e-7f;
+      const float high = sc.top - x1 + slack, low = bin == kBins - 1 ? sc.low : sc.top - x0 - slack;
+      uint32_t lo = 0, hi = Raw<T>::key(sc.top);
+      if (high >= low) { lo = Raw<T>::key(fmaxf(low, sc.low)); hi = min(hi, Raw<T>::key(high)); }
+      for (; in > kList && lo != hi; ++round) {
         const int which = round & 1;
-        if (tid == 0) { sh.key_lo[which] = 0xffffffffu; sh.key_hi[which] = 0; }
         for (int b = tid; b < kBins; b += THREADS) sh.work[which].h.mass[0][b] = sh.work[which].h.mass[1][b] = sh.work[which].h.mass[2][b] = sh.work[which].h.count[b] = 0;
         __syncthreads();
-        if (mn <= mx) { atomicMin(&sh.key_lo[which], mn); atomicMax(&sh.key_hi[which], mx); }
-        cluster.sync();
-        mn = 0xffffffffu; mx = 0;
-#pragma unroll
-        for (int b = 0; b < kCluster; ++b) {
-          mn = min(mn, *cluster.map_shared_rank(&sh.key_lo[which], b));
-          mx = max(mx, *cluster.map_shared_rank(&sh.key_hi[which], b));
-        }
-        if (mn >= mx) { ++round; return mx; }        // one key: the threshold
-        const int shift = max(0, 32 - __clz(mx - mn) - 9);   // (mx - mn) >> shift is below 512
+        const int shift = max(0, 32 - __clz(hi - lo) - 9);   // (hi - lo) >> shift is below 512
         for (int q = tid; q < pieces; q += THREADS) {
           const uint4 v = slice[q];
 #pragma unroll
           for (int i = 0; i < kVec; ++i) {
             const float x = Raw<T>::get(v, i);
-            const uint32_t key = key_of(x);
-            if (sc.in_bin(x, bin) && key >= mn && key <= mx) {
-              const u64 w = sc.weight(x);
-              if (w) {
-                const int b = (int)((mx - key) >> shift);
-                add(which, b, w);
-              }
+            if (x > sc.low && sc.in_bin(x, bin)) {
+              const uint32_t key = Raw<T>::key(x);
+              const u64 w = key >= lo && key <= hi ? sc.weight(x) : 0;
+              if (w) add(which, (int)((hi - key) >> shift), w, true, true);
             }
           }
         }
@@ -544,11 +547,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
         cross(sub, *before, count, limit, &unused);
         *before = sh.cross.before;
         in = sh.cross.in;
-        const uint32_t b = (uint32_t)sh.cross.bin;
-        hi = mx - (b << shift);
-        lo = max(mn, hi - ((1u << shift) - 1u));
+        hi -= (uint32_t)sh.cross.bin << shift;
+        lo = max(lo, hi - ((1u << shift) - 1u));
         __syncthreads();                             // sh.cross has been read
       }
+      if (lo == hi) return lo;
       const int which = round & 1;
       ++round;
       if (tid == 0) sh.n_list[which] = 0;
@@ -558,8 +561,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
           const float x = Raw<T>::get(v, i);
-          const uint32_t key = key_of(x);
-          if (sc.in_bin(x, bin) && key >= lo && key <= hi && sc.weight(x)) sh.work[which].c.list[atomicAdd(&sh.n_list[which], 1)] = key;
+          if (x > sc.low && sc.in_bin(x, bin)) {
+            const uint32_t key = Raw<T>::key(x);
+            if (key >= lo && key <= hi && sc.weight(x)) sh.work[which].c.list[atomicAdd(&sh.n_list[which], 1)] = key;
+          }
         }
       }
       cluster.sync();
@@ -577,7 +582,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       if (cut) {
         thr = refine(true, (u64)k, &before);
         ties = (u64)k - before.count;
-        mass = before.mass + ties * sc.weight(of_key(thr));
+        mass = before.mass + ties * sc.weight(Raw<T>::of_key(thr));
       }
     }
     if (by_mass) {
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       const u64 limit = mass_limit(cut ? mass : all.mass);
       if (found) {
         thr = refine(false, limit, &before);
-        const u64 w = sc.weight(of_key(thr));
+        const u64 w = sc.weight(Raw<T>::of_key(thr));
         ties = (limit - before.mass + w - 1) / w;
       }
     }
@@ -596,8 +601,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   // Thread t takes a run of consecutive pieces, so that threads are in index order; an odd run keeps the 16-byte
   // reads of neighbouring threads off one another's banks.
   const int run = ((per / kVec + 1 + THREADS - 1) / THREADS) | 1;
-  const u64 tie_weight = thr != 0 ? sc.kept_weight(of_key(thr)) : 0;
-  const float floor_x = thr != 0 ? of_key(thr) : sc.low;         // nothing below it is kept
+  const u64 tie_weight = thr != 0 ? sc.kept_weight(Raw<T>::of_key(thr)) : 0;
+  const float floor_x = thr != 0 ? Raw<T>::of_key(thr) : sc.low;         // nothing below it is kept
   Sum2 mine = {0, 0};                                // mass above the threshold, elements at it
   const T* flat = reinterpret_cast<const T*>(slice);
   const int run_end = min(pieces, (tid + 1) * run);
