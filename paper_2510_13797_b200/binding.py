@@ -140,15 +140,35 @@ def _require(ok, where):
         raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
 
 
-def _on(where, ref, dtypes, stream):
-    """Checks that the tensors (name -> (tensor or None, dtype, shape)) are contiguous, of that dtype and shape, on the device of
-    `ref`; returns that device's guard, its stream, and whether memory allocated for the call must be tied to that stream."""
-    _require(ref.is_cuda, where)
-    for t, dtype, shape in dtypes:
-        _require(t is None or (t.device == ref.device and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous()), where)
-    own = torch.cuda.current_stream(ref.device)
-    s = own if stream is None else stream
-    return torch.cuda.device(ref.device), s, s != own
+def _on(where, ref, tensors, stream):
+    """Checks that the tensors (tensor or None, dtype, shape) are contiguous, of that dtype and shape, and on the CUDA device of
+    `ref`.  Returns that device's index, the raw stream, and the torch stream if one other than the device's current one was given
+    (memory allocated for the call must then be tied to it).  Kept short: it is most of a small call's time."""
+    dev = ref.get_device()
+    if dev < 0:
+        raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    for t, dtype, shape in tensors:
+        if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous()):
+            raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    raw = torch._C._cuda_getCurrentRawStream(dev)
+    if stream is None:
+        return dev, raw, None
+    return dev, stream.cuda_stream, stream if stream.cuda_stream != raw else None
+
+
+def _call(where, dev, fn, *args):
+    """A library call with the tensors' device current (a stream belongs to a device)."""
+    if torch._C._cuda_getDevice() == dev:
+        status = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args)
+    if status != BC_OK:
+        raise BreadcrumbsError(status, where)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 class Cache:
@@ -235,33 +255,32 @@ class Cache:
 
     def bc_norm_rope_decode_step(self, layer, slots, qkv, positions, theta, q_weight, k_weight, eps, out, sm_scale, stream=None):
         """bc_norm_rope_split + bc_decode_step: a layer's decode step straight from the packed QKV projection."""
-        n, d = slots.numel(), self.cfg.head_dim
-        guard, s, _ = _on("bc_norm_rope_decode_step", self.pool, [
-            (slots, torch.int32, (n,)), (positions, torch.int32, (n,)), (qkv, torch.bfloat16, (n, (self.cfg.q_heads + 2 * self.cfg.kv_heads) * d)),
-            (q_weight, torch.bfloat16, (d,)), (k_weight, torch.bfloat16, (d,)), (out, self.out_dtype, (n, self.cfg.q_heads, d))], stream)
-        with guard:
-            _check(lib().bc_norm_rope_decode_step(self.handle, layer, _ptr(slots), n, _ptr(qkv), _ptr(positions), theta, _ptr(q_weight),
-                                                  _ptr(k_weight), eps, _ptr(out), sm_scale, _stream(s)), "bc_norm_rope_decode_step")
+        where, n, cfg = "bc_norm_rope_decode_step", slots.numel(), self.cfg
+        d = cfg.head_dim
+        dev, s, _ = _on(where, self.pool, (
+            (slots, torch.int32, (n,)), (positions, torch.int32, (n,)), (qkv, torch.bfloat16, (n, (cfg.q_heads + 2 * cfg.kv_heads) * d)),
+            (q_weight, torch.bfloat16, (d,)), (k_weight, torch.bfloat16, (d,)), (out, self.out_dtype, (n, cfg.q_heads, d))), stream)
+        _call(where, dev, lib().bc_norm_rope_decode_step, self.handle, layer, _at(slots), n, _at(qkv), _at(positions), theta, _at(q_weight),
+              _at(k_weight), eps, _at(out), sm_scale, s)
 
     def bc_chunk_attn(self, layer, slots, cu_q, total_q, q, out, sm_scale, first=None, stream=None):
         """Attention of a ragged chunk of queries per sequence (breadcrumbs.h); first None: the sequences' last entries."""
-        n, shape = slots.numel(), (total_q, self.cfg.q_heads, self.cfg.head_dim)
-        guard, s, _ = _on("bc_chunk_attn", self.pool, [
+        where, n = "bc_chunk_attn", slots.numel()
+        shape = (total_q, self.cfg.q_heads, self.cfg.head_dim)
+        dev, s, _ = _on(where, self.pool, (
             (slots, torch.int32, (n,)), (cu_q, torch.int32, (n + 1,)), (first, torch.int32, (n,)), (q, torch.bfloat16, shape),
-            (out, self.out_dtype, shape)], stream)
-        with guard:
-            _check(lib().bc_chunk_attn(self.handle, layer, _ptr(slots), _ptr(first), _ptr(cu_q), n, total_q, _ptr(q), _ptr(out), sm_scale,
-                                       _stream(s)), "bc_chunk_attn")
+            (out, self.out_dtype, shape)), stream)
+        _call(where, dev, lib().bc_chunk_attn, self.handle, layer, _at(slots), _at(first), _at(cu_q), n, total_q, _at(q), _at(out), sm_scale, s)
 
     def bc_prefill_chunk(self, layer, slots, first, cu_chunk, total, q, k, v, out, sm_scale, stream=None):
         """Stores a chunk of every prompt at positions first[i] ... and attends with its queries (breadcrumbs.h)."""
-        n, shape, kv = slots.numel(), (total, self.cfg.q_heads, self.cfg.head_dim), (total, self.cfg.kv_heads, self.cfg.head_dim)
-        guard, s, _ = _on("bc_prefill_chunk", self.pool, [
+        where, n, cfg = "bc_prefill_chunk", slots.numel(), self.cfg
+        shape, kv = (total, cfg.q_heads, cfg.head_dim), (total, cfg.kv_heads, cfg.head_dim)
+        dev, s, _ = _on(where, self.pool, (
             (slots, torch.int32, (n,)), (cu_chunk, torch.int32, (n + 1,)), (first, torch.int32, (n,)), (q, torch.bfloat16, shape),
-            (k, torch.bfloat16, kv), (v, torch.bfloat16, kv), (out, self.out_dtype, shape)], stream)
-        with guard:
-            _check(lib().bc_prefill_chunk(self.handle, layer, _ptr(slots), _ptr(first), _ptr(cu_chunk), n, total, _ptr(q), _ptr(k), _ptr(v),
-                                          _ptr(out), sm_scale, _stream(s)), "bc_prefill_chunk")
+            (k, torch.bfloat16, kv), (v, torch.bfloat16, kv), (out, self.out_dtype, shape)), stream)
+        _call(where, dev, lib().bc_prefill_chunk, self.handle, layer, _at(slots), _at(first), _at(cu_chunk), n, total, _at(q), _at(k), _at(v),
+              _at(out), sm_scale, s)
 
     def bc_decode_attn_static(self, layer, slots, q, out, sm_scale, extra_k=None, extra_v=None, stream=None):
         """bc_decode_attn with the split-K scratch taken from the array built into the library, for callers
@@ -417,10 +436,12 @@ def bc_distill_loss(cu_rows, student_logits, teacher_idx, teacher_logprob, with_
 
 
 def _norm_rope_shapes(qkv, q_heads, kv_heads, where):
-    _require(qkv.dim() == 2 and qkv.is_cuda and qkv.dtype == torch.bfloat16 and qkv.stride(1) == 1 and q_heads > 0 and kv_heads > 0
-             and qkv.shape[1] % (q_heads + 2 * kv_heads) == 0, where)
-    n, d = qkv.shape[0], qkv.shape[1] // (q_heads + 2 * kv_heads)
-    return n, d, qkv.stride(0) if n > 1 else max(qkv.stride(0), qkv.shape[1]), (n, q_heads, d), (n, kv_heads, d)
+    heads = q_heads + 2 * kv_heads
+    if qkv.dim() != 2 or qkv.dtype is not torch.bfloat16 or q_heads < 1 or kv_heads < 1 or qkv.shape[1] % heads or qkv.stride(1) != 1:
+        raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    n, width = qkv.shape
+    d = width // heads
+    return n, d, qkv.stride(0) if n > 1 else max(qkv.stride(0), width), (n, q_heads, d), (n, kv_heads, d)
 
 
 def bc_norm_rope_split(qkv, positions, theta, q_weight, k_weight, eps, q_heads, kv_heads, q_out=None, k_out=None, v_out=None, stream=None):
@@ -428,56 +449,58 @@ def bc_norm_rope_split(qkv, positions, theta, q_weight, k_weight, eps, q_heads, 
 
     qkv: [n, (q_heads + 2 kv_heads) * head_dim] bf16, rows may be strided; q_weight, k_weight: [head_dim] bf16 or None; q_out,
     k_out, v_out are allocated when not given."""
-    where = "bc_norm_rope_split"
+    where, bf16 = "bc_norm_rope_split", torch.bfloat16
     n, d, row_stride, qs, ks = _norm_rope_shapes(qkv, q_heads, kv_heads, where)
-    guard, s, tie = _on(where, qkv, [(positions, torch.int32, (n,)), (q_weight, torch.bfloat16, (d,)), (k_weight, torch.bfloat16, (d,)),
-                                     (q_out, torch.bfloat16, qs), (k_out, torch.bfloat16, ks), (v_out, torch.bfloat16, ks)], stream)
-    with guard:
-        outs = [torch.empty(sh, dtype=torch.bfloat16, device=qkv.device) if o is None else o for o, sh in ((q_out, qs), (k_out, ks), (v_out, ks))]
-        _check(lib().bc_norm_rope_split(n, q_heads, kv_heads, d, _ptr(qkv), row_stride, _ptr(positions), theta, _ptr(q_weight), _ptr(k_weight),
-                                        eps, *[_ptr(o) for o in outs], _stream(s)), where)
-    if tie:
-        for o in outs:
-            o.record_stream(s)
-    return tuple(outs)
+    dev, s, other = _on(where, qkv, ((positions, torch.int32, (n,)), (q_weight, bf16, (d,)), (k_weight, bf16, (d,)), (q_out, bf16, qs),
+                                     (k_out, bf16, ks), (v_out, bf16, ks)), stream)
+    q = qkv.new_empty(qs) if q_out is None else q_out
+    k = qkv.new_empty(ks) if k_out is None else k_out
+    v = qkv.new_empty(ks) if v_out is None else v_out
+    if other is not None:
+        for t in (q, k, v):
+            t.record_stream(other)
+    _call(where, dev, lib().bc_norm_rope_split, n, q_heads, kv_heads, d, qkv.data_ptr(), row_stride, positions.data_ptr(), theta, _at(q_weight),
+          _at(k_weight), eps, q.data_ptr(), k.data_ptr(), v.data_ptr(), s)
+    return q, k, v
 
 
 def bc_norm_rope_split_backward(qkv, positions, theta, q_weight, k_weight, eps, dq, dk, dv, weight_grads=True, stream=None):
     """Gradient of bc_norm_rope_split (breadcrumbs.h): returns (dqkv [n, ...] bf16, dq_weight, dk_weight [head_dim] fp32 or None)."""
-    where = "bc_norm_rope_split_backward"
+    where, bf16 = "bc_norm_rope_split_backward", torch.bfloat16
     _require(dq.dim() == 3 and dk.dim() == 3, where)
-    n, d, row_stride, qs, ks = _norm_rope_shapes(qkv, dq.shape[1], dk.shape[1], where)
-    guard, s, tie = _on(where, qkv, [(positions, torch.int32, (n,)), (q_weight, torch.bfloat16, (d,)), (k_weight, torch.bfloat16, (d,)),
-                                     (dq, torch.bfloat16, qs), (dk, torch.bfloat16, ks), (dv, torch.bfloat16, ks)], stream)
+    q_heads, kv_heads = dq.shape[1], dk.shape[1]
+    n, d, row_stride, qs, ks = _norm_rope_shapes(qkv, q_heads, kv_heads, where)
+    dev, s, other = _on(where, qkv, ((positions, torch.int32, (n,)), (q_weight, bf16, (d,)), (k_weight, bf16, (d,)), (dq, bf16, qs), (dk, bf16, ks),
+                                     (dv, bf16, ks)), stream)
     size = C.c_size_t()
     _check(lib().bc_norm_rope_query_bytes(d, C.byref(size)), "bc_norm_rope_query_bytes")
-    with guard:
-        dqkv = torch.empty((n, qkv.shape[1]), dtype=torch.bfloat16, device=qkv.device)
-        dqw, dkw = [torch.empty(d, dtype=torch.float32, device=qkv.device) if weight_grads else None for _ in range(2)]
-        ws = torch.empty(size.value, dtype=torch.uint8, device=qkv.device)
-        _check(lib().bc_norm_rope_split_backward(n, dq.shape[1], dk.shape[1], d, _ptr(qkv), row_stride, _ptr(positions), theta, _ptr(q_weight),
-                                                 _ptr(k_weight), eps, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dqkv), _ptr(dqw), _ptr(dkw), _ptr(ws),
-                                                 size.value, _stream(s)), where)
-    if tie:
-        for t in (dqkv, dqw, dkw, ws):
-            if t is not None:
-                t.record_stream(s)
-    return dqkv, dqw, dkw
+    dqkv = qkv.new_empty((n, qkv.shape[1]))
+    # the weights' gradients and the scratch in one allocation
+    ws = torch.empty(size.value // 4 + 2 * d, dtype=torch.float32, device=qkv.device)
+    if other is not None:
+        dqkv.record_stream(other)
+        ws.record_stream(other)
+    at = ws.data_ptr()
+    _call(where, dev, lib().bc_norm_rope_split_backward, n, q_heads, kv_heads, d, qkv.data_ptr(), row_stride, positions.data_ptr(), theta,
+          _at(q_weight), _at(k_weight), eps, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dqkv.data_ptr(), at if weight_grads else None,
+          at + 4 * d if weight_grads else None, at + 8 * d, size.value, s)
+    return (dqkv, ws[:d], ws[d:2 * d]) if weight_grads else (dqkv, None, None)
 
 
 def bc_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, out=None, stream=None):
     """One token per row of bf16 or fp32 logits [n, vocab] (rows may be strided) from one uniform number per row, with the
     row's temperature, top-k, top-p and min-p (breadcrumbs.h): returns int64 [n]."""
-    where = "bc_sample"
-    _require(logits.dim() == 2 and logits.dtype in (torch.bfloat16, torch.float32) and logits.stride(1) in (1, logits.stride(0)), where)
+    where, f32 = "bc_sample", torch.float32
+    if logits.dim() != 2 or (logits.dtype is not torch.bfloat16 and logits.dtype is not f32):
+        raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
     n, vocab = logits.shape
-    _require(logits.stride(1) == 1 or vocab == 1, where)
-    guard, s, tie = _on(where, logits, [(uniform, torch.float32, (n,)), (temperature, torch.float32, (n,)), (top_k, torch.int32, (n,)),
-                                        (top_p, torch.float32, (n,)), (min_p, torch.float32, (n,)), (out, torch.int64, (n,))], stream)
-    with guard:
-        res = torch.empty(n, dtype=torch.int64, device=logits.device) if out is None else out
-        _check(lib().bc_sample(_ptr(logits), int(logits.dtype == torch.float32), max(logits.stride(0), vocab) if n == 1 else logits.stride(0), n, vocab,
-                               _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(res), _stream(s)), where)
-    if tie:
-        res.record_stream(s)
+    row_stride = logits.stride(0)
+    _require(vocab == 1 or logits.stride(1) == 1, where)
+    dev, s, other = _on(where, logits, ((uniform, f32, (n,)), (temperature, f32, (n,)), (top_k, torch.int32, (n,)), (top_p, f32, (n,)),
+                                        (min_p, f32, (n,)), (out, torch.int64, (n,))), stream)
+    res = torch.empty(n, dtype=torch.int64, device=logits.device) if out is None else out
+    if other is not None:
+        res.record_stream(other)
+    _call(where, dev, lib().bc_sample, logits.data_ptr(), 1 if logits.dtype is f32 else 0, row_stride if n > 1 else max(row_stride, vocab), n, vocab,
+          _at(temperature), _at(top_k), _at(top_p), _at(min_p), uniform.data_ptr(), res.data_ptr(), s)
     return res
