@@ -6,11 +6,10 @@
 // zeros where that is nothing.  That is the attention of a prompt chunk behind the entries stored before it, and of
 // the last m_i entries of a window (several guessed tokens checked at once).
 //
-// k_chunk_attn runs on the tcgen05 tensor cores.  A thread block (one per SM) works on units of 256 query rows, two
-// groups of floor(128 / G) tokens times the G query heads of a KV head, against tiles of 128 keys that both groups share:
-// S = Q K^T into tensor memory, softmax by one thread per row, P as bf16 back into tensor memory, O += P V; one group's
-// softmax runs beside the other's products.  In a unit with rows for one group only ("solo") the two groups take the key
-// tiles in turn, with an accumulator each, which the group that had the first tile joins at the end.
+// k_chunk_attn runs on the tcgen05 tensor cores.  A thread block (two per SM) works on units of 128 query rows,
+// floor(128 / G) tokens times the G query heads of a KV head, against tiles of 128 keys: S = Q K^T into tensor memory,
+// softmax by one thread per row, P as bf16 back into tensor memory, O += P V; while one block's rows work on S the
+// products of the SM's other block run.
 //   * Keys come from pages.  The live entries lie in a virtual row space, prompt from 0, beacons and window each from
 //     the next multiple of the copy height, so that (row & 7) equals the entry's position in its segment modulo 8:
 //     the store's chunk permutation IS the 128-byte swizzle of the product's operand layout, and unswizzled tensor
@@ -23,9 +22,10 @@
 //     prompt chunk ends everywhere at the same time.
 //   * Every block works the line out from the lengths on the device by itself: no host copy of a length, no plan
 //     kernel, and the call can be captured.
-//   * K and V tiles run through rings of kStages buffers each; the stream of tiles goes on across units.
-// Bounds: at many rows per key the tensor pipe and the exponentials, at few rows the reads of the cache; a tile is 64 KB
-// of K and V for 16.8 MFLOP (two groups).
+//   * The copies, the products and the rows' softmax each have warps of their own, and the stream of tiles goes on across
+//     units.
+// Bounds: at many rows per key the tensor pipe, the exponentials and the waits between them, at few rows the reads of the
+// cache; a tile is 64 KB of K and V for 8.4 MFLOP.
 //
 // Entries that no row of a query tile can see are not read into a product: their scores are overwritten with -inf, and
 // V rows that are past the last visible entry of the tile are cleared in shared memory, so that whatever the
@@ -42,9 +42,10 @@ namespace {
 #include "bc_tc.cuh"
 #include "bc_book_device.cuh"
 
-constexpr int kGroup = 128;                    // rows, and row threads, of a group
-constexpr int kThreads = 2 * kGroup + 64;      // two groups, the product warp and the copy warp
+constexpr int kRowThreads = 128;               // one per query row
+constexpr int kThreads = kRowThreads + 64;     // and the product warp and the copy warp
 constexpr int kMaxItems = BC_MAX_ATTN_BATCH;
+constexpr int kTmemColumns = 256;              // S and O; what is allocated and what is given back
 
 // ---- the simple form -----------------------------------------------------------------------------------------------
 // item of packed row `row`: the largest i with cu[i] <= row; false if the row belongs to none
@@ -104,6 +105,21 @@ __global__ void k_chunk_reference(BcMeta m, BcGeom g, BcChunkArgs a) {
   }
 }
 
+// n / d for 0 <= n < 2^31 by a product and a shift: mul = floor(2^32 (2^l - d) / d) + 1 with l = ceil(log2 d) (Granlund and
+// Montgomery's round-up method).
+struct FastDiv {
+  uint32_t mul, shift1, shift2;
+  __device__ __forceinline__ int operator()(int n) const {
+    const uint32_t t = __umulhi(mul, (uint32_t)n);
+    return (int)((t + (((uint32_t)n - t) >> shift1)) >> shift2);
+  }
+};
+FastDiv make_fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return {d > 1 ? (uint32_t)(((1ull << 32) * ((1ull << l) - d)) / d + 1) : 1u, l > 0 ? 1u : 0u, l > 0 ? l - 1 : 0u};
+}
+
 // ---- the tensor-core form ------------------------------------------------------------------------------------------
 struct ChunkParams {
   BcMeta m;
@@ -111,12 +127,12 @@ struct ChunkParams {
   int32_t n, total_q;
   void* out;
   int32_t out_f32, layer;
-  float* part_o;      // [2 grid][2][D / 4][128] float4: a block's partial results
-  float* part_ml;     // [2 grid][2][2][128]
-  int32_t* tickets;   // [grid][2], by the block that begins the unit; zero between launches
+  float* part_o;      // [2 grid][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
+  float* part_ml;     // [2 grid][2][128]
+  int32_t* tickets;   // [grid], by the block that begins the unit; zero between launches
   int32_t Hq, Hkv, G, page_size;
-  int32_t half;       // tokens of a group: 128 / G
-  int32_t tokens;     // of a unit: two groups
+  FastDiv by_page;
+  int32_t tokens;     // per unit: 128 / G
   int32_t R;          // entries per copy, a power of two
   int32_t align;      // segment starts in the virtual row space: max(8, R)
   int32_t min_span;   // key tiles a block works on at least
@@ -127,23 +143,19 @@ struct ChunkParams {
 // Lengths of the items, in shared memory (structure of arrays).
 struct Items {
   int m[kMaxItems], first[kMaxItems], P[kMaxItems], nb[kMaxItems], w[kMaxItems];
-  int cu[kMaxItems], slot[kMaxItems], boff[kMaxItems], woff[kMaxItems];
   long long before[kMaxItems + 1];   // key tiles of one KV head in the items before
   int large[64], n_large;            // items whose tiles all threads count together
-  float2 other[kGroup];              // a solo unit: (m, l) of the group that had the second tile
   long long total, span;
   int item0, head0, tile0;           // where this block's span begins
   int n0;
 };
 
-// One unit: the query tile `t` (two groups) of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
+// One unit: the query tile `t` of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
 struct Unit {
   int i, h, t;
   int count, vis_last;     // tokens in the tile; entries its last token sees
   int P, nb, w, base;      // lengths of the sequence; base: entries the tile's first token sees, minus 1
   int n0, n1, N;
-  int start;               // a solo unit's group of tile n0 (the other takes n0 + 1, and so on in turn)
-  bool two;                // rows for both groups
 };
 // Entries `vis` of a sequence as intervals of the virtual row space: [0, p), [b0, b0 + b), [w0, w0 + w).
 struct Seen {
@@ -167,7 +179,7 @@ __device__ __forceinline__ int key_tiles(const Items& it, int i, int t, int toke
   const int vis = clamp_vis(it.first[i], last, it.P[i] + it.nb[i] + it.w[i]);
   return max(1, (virtual_end(seen_of(vis, it.P[i], it.nb[i], it.w[i], align)) + kTile - 1) / kTile);
 }
-__device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, int n0, long long left, int tokens, int align, int start) {
+__device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, int n0, long long left, int tokens, int align) {
   Unit u;
   u.i = i; u.h = h; u.t = t; u.n0 = n0;
   u.P = it.P[i]; u.nb = it.nb[i]; u.w = it.w[i];
@@ -177,8 +189,6 @@ __device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, 
   u.base = it.first[i] + t * tokens;
   u.N = key_tiles(it, i, t, tokens, align);
   u.n1 = (int)min((long long)u.N, n0 + left);
-  u.two = 2 * u.count > tokens;
-  u.start = u.two ? 0 : start;
   return u;
 }
 // The unit behind u on the line (there is one: the caller knows how many key tiles are left).
@@ -191,9 +201,13 @@ __device__ __forceinline__ Unit next_unit(const Items& it, const Unit& u, long l
       do ++i; while (it.m[i] == 0);
     }
   }
-  return make_unit(it, i, h, t, 0, left, tokens, align, u.two ? 0 : (u.start + u.n1 - u.n0) & 1);
+  return make_unit(it, i, h, t, 0, left, tokens, align);
 }
 
+// the tile at k0 lies in one interval entirely
+__device__ __forceinline__ bool inside(const Seen& s, int k0) {
+  return k0 + kTile <= s.p || (k0 >= s.b0 && k0 + kTile <= s.b0 + s.b) || (k0 >= s.w0 && k0 + kTile <= s.w0 + s.w);
+}
 // 128-bit mask (bit j of word j / 32: column j of the tile) of the tile's columns inside [lo, hi) of the virtual space
 __device__ __forceinline__ void add_range(uint32_t (&mask)[4], int lo, int hi) {
 #pragma unroll
@@ -216,7 +230,7 @@ struct TileIssue {
   int page[KP], rem[KP];     // page id and first entry inside the page
   uint32_t valid[KP];        // ballots: which copies there are
   int h, qrow;               // KV head; packed row of the unit's first token
-  bool fresh, two;           // the unit's first tile here; rows for two groups
+  bool fresh;                // the unit's first tile here
 };
 
 __device__ __forceinline__ void tma_pool(uint32_t dst, const CUtensorMap* map, int head_half, int row, int layer, uint32_t bar) {
@@ -226,56 +240,52 @@ __device__ __forceinline__ void tma_pool(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// Shared memory of a block: the groups' Q, the rings of K and V, the items.
+// Shared memory of a block: Q, the rings of K and V (one buffer each where two blocks leave room for no more), the items.
 template <int D>
 struct Smem {
-  static constexpr int kStages = D == 64 ? 4 : 2;
+  static constexpr int kStages = D == 64 ? 2 : 1;
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = kTile * 128;            // 128 rows of 64 coordinates
   static constexpr int kOperand = kHalves * kHalfBytes;
-  static constexpr int kBytes = (2 + 2 * kStages) * kOperand + 1024 + (int)sizeof(Items);
+  static constexpr int kBytes = (1 + 2 * kStages) * kOperand + 1024 + (int)sizeof(Items);
 };
 
 // D: head_dim.  KP: copies per lane, tensor and tile (1 for pages that are a multiple of 4 entries, else 4).
 //
-// Roles: warps 0 .. 3 are group 0's row threads, warps 4 .. 7 group 1's, warp 8 issues the products, warp 9 the copies.
-//
-// A task is one group's products with one key tile.  The tasks of a unit alternate between the groups: (tile n, group 0),
-// (n, 1), (n + 1, 0) ... of a unit with two groups of rows, (n, g), (n + 1, 1 - g) ... of a solo unit.  S = Q K^T of a task is
-// issued as soon as its group's S is free, which is behind the product with P of the group's task before it (a block's
-// products run in the order of issue); so while a group works on its S the other group's products run.
+// Roles: warps 0 .. 3 are the row threads, warp 4 issues the products, warp 5 the copies.
+// S of the next tile is issued right behind the product with P of the last one, whose P it overwrites: one thread issues both,
+// and they run in that order.
 // Barriers (single-phase mbarriers, parity = completions & 1):
 //   bar_kin[s], bar_vin[s]: K, V of ring buffer s have landed     bar_ke[s], bar_ve[s]: they have been read
 //   bar_q: Q of a unit has landed                                 bar_qe: it has been read
-//   bar_s[g]: S of group g is ready                               bar_p[g]: its 128 row threads have stored P
-//   bar_f[g]: its O of the unit is final                          bar_e[g]: its rows have read O
-//   bar_r[g]: its row threads among themselves (bounded, unlike a block barrier)
-//   bar_j: the other group's sums of a solo unit are in shared memory
+//   bar_s: S of a tile is ready                                   bar_p: the 128 row threads have stored P
+//   bar_f: O of a unit is final                                   bar_e: the rows have read O
+//   bar_r: the row threads among themselves (bounded, unlike a block barrier)
 template <int D, int KP, bool SHORTW>
-__global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
+__global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
                                                            const __grid_constant__ CUtensorMap pool_map) {
   constexpr int kHalves = Smem<D>::kHalves, kHalfBytes = Smem<D>::kHalfBytes, kOperand = Smem<D>::kOperand, kStages = Smem<D>::kStages;
   constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sQ = smem_addr(smem), sK = sQ + 2 * kOperand, sV = sK + kStages * kOperand;
-  Items& it = *reinterpret_cast<Items*>(smem + (2 + 2 * kStages) * kOperand);
-  __shared__ __align__(8) uint64_t s_bars[4 * kStages + 14];
+  const uint32_t sQ = smem_addr(smem), sK = sQ + kOperand, sV = sK + kStages * kOperand;
+  Items& it = *reinterpret_cast<Items*>(smem + (1 + 2 * kStages) * kOperand);
+  __shared__ __align__(8) uint64_t s_bars[4 * kStages + 8];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_fail_word, s_ticket[2];
+  __shared__ int s_fail_word, s_ticket;
   volatile int* s_fail = &s_fail_word;
   const uint32_t bars = smem_addr(s_bars);
-  const uint32_t bar_kin = bars, bar_vin = bars + 8 * kStages, bar_ke = bars + 16 * kStages, bar_ve = bars + 24 * kStages,
-                 bar_q = bars + 32 * kStages, bar_qe = bar_q + 8, bar_s = bar_qe + 8, bar_p = bar_s + 16, bar_f = bar_p + 16, bar_e = bar_f + 16, bar_r = bar_e + 16, bar_d = bar_r + 16, bar_j = bar_d + 8;
+  const uint32_t bar_kin = bars, bar_vin = bars + 8 * kStages, bar_ke = bars + 16 * kStages, bar_ve = bars + 24 * kStages, bar_q = bars + 32 * kStages,
+                 bar_qe = bar_q + 8, bar_s = bar_q + 16, bar_p = bar_q + 24, bar_f = bar_q + 32, bar_e = bar_q + 40, bar_r = bar_q + 48, bar_d = bar_q + 56;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = a.G, Hq = a.Hq, Hkv = a.Hkv, half = a.half, tokens = a.tokens, align = a.align;
+  const int G = a.G, Hq = a.Hq, Hkv = a.Hkv, tokens = a.tokens, align = a.align;
 
   if (tid == 0) {
     auto init = [&](uint32_t bar, int count, uint32_t arrivals) {
       for (int i = 0; i < count; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + i * 8), "r"(arrivals) : "memory");
     };
-    init(bar_kin, 4 * kStages, 1); init(bar_q, 1, 1); init(bar_qe, 1, 1); init(bar_s, 2, 1); init(bar_p, 2, kGroup);
-    init(bar_f, 2, 1); init(bar_e, 2, kGroup); init(bar_r, 2, kGroup); init(bar_d, 1, 1); init(bar_j, 1, kGroup);
+    init(bar_kin, 4 * kStages + 3, 1);                      // kin, vin, ke, ve, q, qe, s
+    init(bar_p, 1, kRowThreads); init(bar_f, 1, 1); init(bar_e, 2, kRowThreads); init(bar_d, 1, 1);   // e and r
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
     it.n_large = 0;
@@ -285,15 +295,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
   // ---- the line: every item's lengths, its key tiles per KV head, and where this block's span begins ------------------
   for (int i = tid; i < a.n; i += kThreads) {
     const int slot = a.slots[i], c0 = a.cu_q[i], c1 = a.cu_q[i + 1];
-    int P = 0, nb = 0, w = 0, boff = 0, woff = 0;
-    if (slot >= 0 && slot < a.m.max_seqs && a.m.open[slot]) {
-      P = a.m.prompt_len[slot]; nb = a.m.n_beacons[slot]; w = a.m.window_len[slot];
-      boff = a.m.beacon_off[slot]; woff = a.m.window_off[slot];
-    }
+    int P = 0, nb = 0, w = 0;
+    if (slot >= 0 && slot < a.m.max_seqs && a.m.open[slot]) { P = a.m.prompt_len[slot]; nb = a.m.n_beacons[slot]; w = a.m.window_len[slot]; }
     const int m = c0 < 0 || c0 > a.total_q ? 0 : max(0, min(c1, a.total_q) - c0);
     const int first = a.first != nullptr ? a.first[i] : P + nb + w - m;
     it.m[i] = m; it.first[i] = min(max(first, -(1 << 30)), 1 << 30); it.P[i] = P; it.nb[i] = nb; it.w[i] = w;
-    it.cu[i] = c0; it.slot[i] = slot; it.boff[i] = boff; it.woff[i] = woff;
     const int tiles = (m + tokens - 1) / tokens;
     long long cost = 0;
     bool mine = true;
@@ -367,29 +373,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
   if (x_begin >= x_end) return;                             // nothing to do: no tensor memory has been taken yet
 
   if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(kTmemColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // Rows of the Q buffers that no tensor copy writes (only when G does not divide 128) stay zero.
-  const int box_rows = half * G;
-  for (int idx = tid; idx < 2 * (kTile - box_rows) * (D / 8); idx += kThreads) {
-    const int r = idx / (D / 8), g = r >= kTile - box_rows ? 1 : 0;
-    st_zero16(sQ + g * kOperand + swz(box_rows + r - g * (kTile - box_rows), idx % (D / 8)));
-  }
+  // Rows of the Q buffer that no tensor copy writes (only when G does not divide 128) stay zero.
+  const int box_rows = tokens * G;
+  for (int idx = tid; idx < (kTile - box_rows) * (D / 8); idx += kThreads) st_zero16(sQ + swz(box_rows + idx / (D / 8), idx % (D / 8)));
   proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  // columns: S (then P, in its first 64) of the groups at 0 and 128, O at 256 and 256 + D
-  const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align, 0);
+  const uint32_t tS = tmem, tO = tmem + kTile;              // columns [0, 128): S, then P in its first 64; [128, 128 + D): O
+  const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align);
 
   auto wait_all = [&](uint32_t bar, uint32_t parity) {       // every lane polls, a vote joins the answers
     const bool ok1 = mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit);
     return (bool)__all_sync(0xffffffffu, ok1);
   };
-  if (warp == 2 * kGroup / 32 + 1) {
-    // ======================================== copy warp =============================================
+  if (warp == kRowThreads / 32 + 1) {
+    // ========================================= copy warp ============================================
     const int R = a.R, copies = kTile / R;
     // cursor of the look-ahead: the tile whose copies are worked out next
     Unit lu = u0;
@@ -405,12 +408,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       if (fresh) {
         // of a slot that is not open no entry is seen: no copy is valid and nothing below is read
         if (lu.vis_last > 0) {
-          boff = it.boff[lu.i]; woff = it.woff[lu.i];
-          table = a.m.page_table + (int64_t)it.slot[lu.i] * a.m.max_pages_per_seq;
+          const int seq = a.slots[lu.i];
+          table = a.m.page_table + (int64_t)seq * a.m.max_pages_per_seq;
+          if (lu.vis_last > lu.P) { boff = a.m.beacon_off[seq]; woff = a.m.window_off[seq]; }
         }
         lseen = seen_of(lu.vis_last, lu.P, lu.nb, lu.w, align);
-        ti.qrow = it.cu[lu.i] + lu.t * tokens;
-        ti.two = lu.two;
+        ti.qrow = a.cu_q[lu.i] + lu.t * tokens;
         fresh = false;
       }
       ti.h = lu.h;
@@ -426,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
         ti.valid[c] = __ballot_sync(0xffffffffu, pos >= 0);
         ti.page[c] = 0; ti.rem[c] = 0;
         if (pos >= 0) {
-          const int pg = pos / a.page_size;
+          const int pg = a.by_page(pos);
           col += pg;
           ti.rem[c] = pos - pg * a.page_size;
           if (a.m.debug && (unsigned)col >= (unsigned)a.m.max_pages_per_seq) { debug_note(a.m, col); col = 0; }
@@ -441,8 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       }
       return ti;
     };
-    // K (which 0) or V (which 1) of a tile into ring buffer `slot`
-    auto issue_kv = [&](const TileIssue<KP>& ti, int which, int slot) {
+    auto issue = [&](const TileIssue<KP>& ti, int which, int slot) {   // K (0) or V (1) of a tile into ring buffer `slot`
       const uint32_t dst = (which ? sV : sK) + slot * kOperand, bar = (which ? bar_vin : bar_kin) + slot * 8;
       int c = 0;
 #pragma unroll
@@ -465,31 +467,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
     const uint32_t T = (uint32_t)(x_end - x_begin);          // tiles of the span (far below 2^31)
     uint32_t nk = 0, nv = 0, nq = 0;                          // copies of K and V tiles and of Q issued so far
     bool ok = true;
-    TileIssue<KP> next = look();
+    TileIssue<KP> ti = look();
     for (uint32_t j = 0; j < T; ++j) {
-      const TileIssue<KP> ti = next;
-      if (j + 1 < T) next = look();
       const int slot = (int)(j % kStages);
       const uint32_t old = (j / kStages - 1) & 1u;             // phase in which the buffer's last tile was read
-      if (j >= (uint32_t)kStages) ok = wait_all(bar_ke + slot * 8, old);
-      if (!ok) break;
-      issue_kv(ti, 0, slot); ++nk;
       if (ti.fresh) {                                          // the unit's Q, once the last unit's has been read
         if (nq > 0) ok = wait_all(bar_qe, (nq - 1) & 1u);
         if (!ok) break;
         if (elect_one()) {
-          const int groups = ti.two ? 2 : 1;
-          mbar_expect_tx(bar_q, (uint32_t)(groups * box_rows * D * 2));
-          for (int g = 0; g < groups; ++g)
+          mbar_expect_tx(bar_q, (uint32_t)(box_rows * D * 2));
 #pragma unroll
-            for (int s = 0; s < kHalves; ++s) tma_3d(sQ + g * kOperand + s * kHalfBytes, &q_map, s * 64, ti.h * G, ti.qrow + g * half, bar_q);
+          for (int s = 0; s < kHalves; ++s) tma_3d(sQ + s * kHalfBytes, &q_map, s * 64, ti.h * G, ti.qrow, bar_q);
         }
         __syncwarp();
         ++nq;
       }
+      if (j >= (uint32_t)kStages) ok = wait_all(bar_ke + slot * 8, old);
+      if (!ok) break;
+      issue(ti, 0, slot); ++nk;
       if (j >= (uint32_t)kStages) ok = wait_all(bar_ve + slot * 8, old);
       if (!ok) break;
-      issue_kv(ti, 1, slot); ++nv;
+      issue(ti, 1, slot); ++nv;
+      if (j + 1 < T) ti = look();                              // its page ids arrive while the warp waits for the next buffer
     }
     if (!ok) {
       // Giving up: no copy may still be on its way into this block's shared memory when the block leaves.  Wait, with the full
@@ -506,101 +505,83 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       }
     }
     __syncwarp();
-  } else if (warp == 2 * kGroup / 32) {
-    // ======================================= product warp ===========================================
+  } else if (warp == kRowThreads / 32) {
+    // ======================================== product warp ==========================================
     // All 32 lanes walk the loop and the waits together; one elected lane issues the products.
     const uint64_t dQ = umma_desc(sQ), dK = umma_desc(sK), dV = umma_desc_nmajor(sV);
-    struct Task {
-      Unit u;
-      int n, g;              // key tile, group
-      uint32_t j;            // index of the tile in the block's stream
-    };
-    auto advance = [&](Task& t) {                              // to the next task; the caller knows that there is one
-      if (t.u.two && t.g == 0) { t.g = 1; return; }
-      t.g ^= 1;
-      ++t.j;
-      if (++t.n == t.u.n1 && x_begin + t.j < x_end) {
-        t.u = next_unit(it, t.u, x_end - (x_begin + t.j), Hkv, tokens, align);
-        t.n = t.u.n0;
-        t.g = t.u.start;
-      }
-    };
     const uint32_t T = (uint32_t)(x_end - x_begin);
-    Task q = {u0, u0.n0, u0.start, 0}, p = q;                   // the next task to get its S, the next one to get its O
-    bool pending[2] = {false, false};                          // S of the group belongs to a task whose O is still to come
-    uint32_t q_used = 0, p_cnt[2] = {0, 0}, o_cnt[2] = {0, 0};  // units' Q used; per group: tasks done, units begun
+    Unit u = u0;
+    uint32_t j = 0, units = 0;                                  // tiles and units so far
     bool ok = true, products = false;
-    auto fill = [&]() {                                        // S of every task whose group is free
-      while (ok && q.j < T && !pending[q.g]) {
-        const int slot = (int)(q.j % kStages);
-        const bool new_tile = !q.u.two || q.g == 0, last_of_tile = !q.u.two || q.g == 1;
-        if (new_tile) {
-          if (q.n == q.u.n0) { ok = wait_all(bar_q, q_used & 1u); ++q_used; }
-          ok = ok && wait_all(bar_kin + slot * 8, (q.j / kStages) & 1u);
-          if (!ok) return;
-        }
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t dq = dQ + (uint64_t)((q.u.two ? q.g : 0) * kOperand >> 4), dk = dK + (uint64_t)(slot * kOperand >> 4);
+    auto qk = [&](uint32_t tile, bool last) {                   // S of the block's tile number `tile`; last: of its unit
+      const int slot = (int)(tile % kStages);
+      ok = ok && wait_all(bar_kin + slot * 8, (tile / kStages) & 1u);
+      if (!ok) return;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t k = dK + (uint64_t)(slot * kOperand >> 4);
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {                 // descriptor start addresses advance in 16-byte units
-            const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
-            umma(tmem + q.g * kTile, dq + off, dk + off, kk > 0);
-          }
-          umma_commit(bar_s + q.g * 8);
-          if (last_of_tile) umma_commit(bar_ke + slot * 8);
-          if (last_of_tile && q.n + 1 == q.u.n1) umma_commit(bar_qe);
+        for (int kk = 0; kk < D / 16; ++kk) {                   // descriptor start addresses advance in 16-byte units
+          const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
+          umma(tS, dQ + off, k + off, kk > 0);
         }
-        __syncwarp();
-        products = true;
-        pending[q.g] = true;
-        advance(q);
+        umma_commit(bar_s);
+        umma_commit(bar_ke + slot * 8);
+        if (last) umma_commit(bar_qe);
       }
+      __syncwarp();
+      products = true;
     };
-    fill();
-    while (ok && p.j < T) {
-      const int slot = (int)(p.j % kStages), g = p.g;
-      const bool new_tile = !p.u.two || g == 0, last_of_tile = !p.u.two || g == 1;
-      const int lag = p.u.two ? 0 : g ^ p.u.start;              // the group's first tile of the unit is n0 + lag
-      const bool begins = p.n == p.u.n0 + lag, ends = p.u.two ? p.n + 1 == p.u.n1 : p.n + 2 >= p.u.n1;
-      if (new_tile) {
-        ok = wait_all(bar_vin + slot * 8, (p.j / kStages) & 1u);
+    ok = wait_all(bar_q, 0);
+    qk(0, u.n0 + 1 == u.n1);
+    while (ok) {
+      const Seen seen = seen_of(u.vis_last, u.P, u.nb, u.w, align);
+      Unit next = u;
+      for (int n = u.n0; ok && n < u.n1; ++n, ++j) {
+        const int slot = (int)(j % kStages);
+        ok = wait_all(bar_vin + slot * 8, (j / kStages) & 1u);
         if (!ok) break;
         // V rows of the tile that hold no entry the unit can see (unwritten entries of the last page, gaps between
-        // segments, rows that no copy wrote): cleared, since a weight of 0 does not cancel a NaN
-        const Seen seen = seen_of(p.u.vis_last, p.u.P, p.u.nb, p.u.w, align);
-        uint32_t mask[4];
-        tile_mask(mask, seen, p.n * kTile);
-        if ((mask[0] & mask[1] & mask[2] & mask[3]) != 0xffffffffu) {
+        // segments, rows that no copy wrote) are cleared, since a weight of 0 does not cancel a NaN.
+        const int k0 = n * kTile;
+        if (!inside(seen, k0)) {
           const uint32_t dst = sV + slot * kOperand;
-          for (int idx = lane; idx < kTile * (D / 8); idx += 32) {
-            const int row = idx / (D / 8);
-            const uint32_t word = row < 64 ? (row < 32 ? mask[0] : mask[1]) : (row < 96 ? mask[2] : mask[3]);
-            if (!(word >> (row & 31) & 1)) st_zero16(dst + swz(row, idx % (D / 8)));
-          }
+          auto clear = [&](int from, int to) {                  // rows of the virtual space
+            from = max(from - k0, 0); to = min(to - k0, kTile);
+#pragma unroll
+            for (int s = 0; s < kHalves; ++s)
+#pragma unroll 4
+              for (int at = from * 128 + lane * 16; at < to * 128; at += 512) st_zero16(dst + s * kHalfBytes + at);
+          };
+          clear(seen.p, seen.b > 0 ? seen.b0 : (seen.w > 0 ? seen.w0 : k0 + kTile));
+          if (seen.b > 0) clear(seen.b0 + seen.b, seen.w > 0 ? seen.w0 : k0 + kTile);
+          if (seen.w > 0) clear(seen.w0 + seen.w, k0 + kTile);
           proxy_fence();   // the product reads shared memory through the asynchronous proxy
           __syncwarp();
         }
-      }
-      if (begins && o_cnt[g] > 0) ok = wait_all(bar_e + g * 8, (o_cnt[g] - 1) & 1u);   // the rows have read the last O
-      ok = ok && wait_all(bar_p + g * 8, p_cnt[g] & 1u);
-      if (!ok) break;
-      ++p_cnt[g];
-      if (begins) ++o_cnt[g];
-      tc_fence_after();
-      if (elect_one()) {
-        const uint64_t dv = dV + (uint64_t)(slot * kOperand >> 4);
+        const bool ends = n + 1 == u.n1, more = j + 1 < T;
+        if (ends && more) next = next_unit(it, u, x_end - (x_begin + j + 1), Hkv, tokens, align);
+        if (n == u.n0 && units > 0) ok = wait_all(bar_e, (units - 1) & 1u);   // the rows have read the last unit's O
+        ok = ok && wait_all(bar_p, j & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t v = dV + (uint64_t)(slot * kOperand >> 4);
 #pragma unroll
-        for (int kk = 0; kk < kTile / 16; ++kk)                 // 16 keys at a time
-          umma_ts<kIdescPV>(tmem + 2 * kTile + g * D, tmem + g * kTile + (uint32_t)(kk * 8), dv + (uint64_t)((kk * 16 * 128) >> 4),
-                            (!begins || kk > 0) ? 1u : 0u);
-        if (ends) umma_commit(bar_f + g * 8);
-        if (last_of_tile) umma_commit(bar_ve + slot * 8);
+          for (int kk = 0; kk < kTile / 16; ++kk)               // 16 keys at a time
+            umma_ts<kIdescPV>(tO, tS + (uint32_t)(kk * 8), v + (uint64_t)((kk * 16 * 128) >> 4), (n > u.n0 || kk > 0) ? 1u : 0u);
+          if (ends) umma_commit(bar_f);
+          umma_commit(bar_ve + slot * 8);
+        }
+        __syncwarp();
+        if (more) {
+          if (ends) ok = wait_all(bar_q, (units + 1) & 1u);
+          qk(j + 1, ends ? next.n0 + 1 == next.n1 : n + 2 == u.n1);
+        }
       }
-      __syncwarp();
-      pending[g] = false;
-      advance(p);
-      fill();
+      if (!ok || j >= T) break;
+      u = next;
+      ++units;
     }
     if (!ok) {   // giving up: every product issued so far ends before the block leaves (one more commit arrives when all have)
       *s_fail = 1;
@@ -614,157 +595,123 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
     __syncwarp();
   } else {
     // ========================================= row threads ==========================================
-    const int grp = warp >> 2, row = tid & (kGroup - 1);        // group, row inside it
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + grp * kTile + lane_base, tO = tmem + 2 * kTile + grp * D + lane_base;
-    const uint32_t my_s = bar_s + grp * 8, my_p = bar_p + grp * 8, my_f = bar_f + grp * 8, my_e = bar_e + grp * 8, my_r = bar_r + grp * 8;
-    const int my_local = row / G, my_head = row % G;
+    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    const int my_local = tid / G, my_head = tid % G;
     constexpr float kMaxSlack = 8.f;                          // as in bc_mask_attn.cu
     bool failed = false;
-    uint32_t t = 0, e = 0, ph_r = 0, joins = 0, others = 0;   // joins: solo units joined so far; others: the other group's units
+    uint32_t t = 0, e = 0, ph_r = 0;
     auto rows_sync = [&]() {
-      mbar_arrive_cta(my_r);
-      const bool ok = mbar_wait_or_fail<SHORTW>(my_r, ph_r, s_fail, a.wait_limit);
+      mbar_arrive_cta(bar_r);
+      const bool ok = mbar_wait_or_fail<SHORTW>(bar_r, ph_r, s_fail, a.wait_limit);
       ph_r ^= 1;
       return (bool)__all_sync(0xffffffffu, ok);
     };
+    auto store8 = [&](int64_t at, const float* v, float f) {    // eight results, times f, at element `at` of the output
+      if (a.out_f32) {
+        float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
+        dst[0] = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+        dst[1] = make_float4(v[4] * f, v[5] * f, v[6] * f, v[7] * f);
+      } else {
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i] * f, v[2 * i + 1] * f);
+          b[i] = *reinterpret_cast<const uint32_t*>(&p);
+        }
+        *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) = make_uint4(b[0], b[1], b[2], b[3]);
+      }
+    };
     long long x = x_begin;
     Unit u = u0;
-    for (;;) {
-      const int mine = u.two ? min(u.count - grp * half, half) : u.count;   // tokens of this group's rows
-      const int lag = u.two ? 0 : grp ^ u.start, step = u.two ? 1 : 2;      // its tiles: n0 + lag, then every step-th
-      const int token0 = u.two ? grp * half : 0;
-      if (u.n0 + lag < u.n1) {
-        const bool row_valid = row < mine * G;
-        const bool warp_live = (warp & 3) * 32 < mine * G;      // a warp without a row only keeps the barriers' count
-        const int vis = row_valid ? clamp_vis(u.base, token0 + my_local, u.P + u.nb + u.w) : 0;
-        const Seen seen = seen_of(vis, u.P, u.nb, u.w, align);
-        float m_ref = -INFINITY, l_run = 0.f;
-        for (int n = u.n0 + lag; n < u.n1; n += step, ++t) {
-          const bool ok = mbar_wait_or_fail<SHORTW>(my_s, t & 1u, s_fail, a.wait_limit);
-          if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-          if (warp_live) {
-            tc_fence_after();
-            const int k0 = n * kTile;
-            const bool whole = !row_valid || k0 + kTile <= seen.p || (k0 >= seen.b0 && k0 + kTile <= seen.b0 + seen.b) ||
-                               (k0 >= seen.w0 && k0 + kTile <= seen.w0 + seen.w);
-            const bool all_visible = __all_sync(0xffffffffu, whole);
-            float s[kTile];
-#pragma unroll
-            for (int cb = 0; cb < 4; ++cb) tmem_ld32_async(tS + cb * 32, s + cb * 32);
-            tmem_wait_ld();
-            if (!all_visible) {
-              uint32_t mask[4];
-              tile_mask(mask, seen, k0);
-#pragma unroll
-              for (int j = 0; j < kTile; ++j)
-                if (!(mask[j >> 5] >> (j & 31) & 1)) s[j] = -INFINITY;
-            }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int j = 0; j < kTile; j += 8) {
-              mx[0] = max3(mx[0], s[j], s[j + 1]); mx[1] = max3(mx[1], s[j + 2], s[j + 3]);
-              mx[2] = max3(mx[2], s[j + 4], s[j + 5]); mx[3] = max3(mx[3], s[j + 6], s[j + 7]);
-            }
-            const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;   // the scale is positive
-            float alpha = 1.f;
-            const bool raise = tile_max > m_ref + kMaxSlack || (m_ref == -INFINITY && tile_max > -INFINITY);
-            if (raise) {
-              alpha = fast_exp2(m_ref - tile_max);
-              m_ref = tile_max;
-              l_run *= alpha;
-            }
-            const float m_safe = m_ref == -INFINITY ? 0.f : m_ref;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int cb = 0; cb < 4; ++cb) {
-              uint32_t pk[16];
-#pragma unroll
-              for (int j = 0; j < 32; j += 2) {
-                const float p0 = fast_exp2(fmaf(s[cb * 32 + j], a.scale_log2, -m_safe));
-                const float p1 = fast_exp2(fmaf(s[cb * 32 + j + 1], a.scale_log2, -m_safe));
-                sum[(j >> 1) & 3] += p0 + p1;
-                const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: 2^-9 per weight
-                pk[j >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
-              }
-              tmem_st16(tS + cb * 16, pk);
-            }
-            l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            // the rows whose reference has moved are rescaled (S of this tile exists, so every product into O before it is done)
-            if (n > u.n0 + lag && __any_sync(0xffffffffu, raise)) {
-#pragma unroll 1
-              for (int cb = 0; cb < D / 32; ++cb) {
-                float v[32];
-                tmem_ld32_async(tO + cb * 32, v);
-                tmem_wait_ld();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= alpha;
-                tmem_st32(tO + cb * 32, v);
-              }
-            }
-            tmem_wait_st();
-            tc_fence_before();
-          }
-          mbar_arrive_cta(my_p);
-        }
-        if (failed) break;
-
-        // ---- the piece's result ---------------------------------------------------------------------------------------
-        const bool ok = mbar_wait_or_fail<SHORTW>(my_f, e & 1u, s_fail, a.wait_limit);
+    for (;; ++e) {
+      const int rows = u.count * G;
+      const bool row_valid = tid < rows;
+      const bool warp_live = warp * 32 < rows;                // a warp without a row only keeps the barriers' count
+      const int vis = row_valid ? clamp_vis(u.base, my_local, u.P + u.nb + u.w) : 0;
+      const Seen seen = seen_of(vis, u.P, u.nb, u.w, align);
+      const int row0 = a.cu_q[u.i] + u.t * tokens;            // packed row of the unit's first token
+      float m_ref = -INFINITY, l_run = 0.f;
+      for (int n = u.n0; n < u.n1; ++n, ++t) {
+        const bool ok = mbar_wait_or_fail<SHORTW>(bar_s, t & 1u, s_fail, a.wait_limit);
         if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-        ++e;
-        const bool joined = !u.two && u.n1 - u.n0 > 1;          // a solo unit of which the other group has a share
-        if (joined && lag == 1) {                               // hand over; the first tile's group reads this one's O
-          it.other[row] = make_float2(m_ref, l_run);
-          mbar_arrive_cta(bar_j);
-        } else {
-          float o[D];                                           // a warp without a row reads it too: under a condition it would be spilled
+        if (warp_live) {
           tc_fence_after();
+          const int k0 = n * kTile;
+          const bool all_visible = __all_sync(0xffffffffu, !row_valid || inside(seen, k0));
+          float s[kTile];
 #pragma unroll
-          for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + cb * 32, o + cb * 32);
+          for (int cb = 0; cb < 4; ++cb) tmem_ld32_async(tS + lane_base + cb * 32, s + cb * 32);
           tmem_wait_ld();
-          if (joined) {
-            // the other group has waited for its O before it wrote its sums; this wait makes that O readable here too
-            bool ok2 = mbar_wait_or_fail<SHORTW>(bar_j, joins & 1u, s_fail, a.wait_limit);
-            ok2 = ok2 && mbar_wait_or_fail<SHORTW>(bar_f + (grp ^ 1) * 8, others & 1u, s_fail, a.wait_limit);
-            if (!__all_sync(0xffffffffu, ok2)) { failed = true; break; }
-            tc_fence_after();
-            const float2 ml = it.other[row];
-            const float m_all = fmaxf(m_ref, ml.x), m_safe = m_all == -INFINITY ? 0.f : m_all;
-            const float f = fast_exp2(m_ref - m_safe), f2 = fast_exp2(ml.x - m_safe);
-            l_run = l_run * f + ml.y * f2;
-            m_ref = m_all;
-            const uint32_t tO2 = tmem + 2 * kTile + (grp ^ 1) * D + lane_base;
+          if (!all_visible) {
+            uint32_t mask[4];
+            tile_mask(mask, seen, k0);
 #pragma unroll
+            for (int j = 0; j < kTile; ++j)
+              if (!(mask[j >> 5] >> (j & 31) & 1)) s[j] = -INFINITY;
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < kTile; j += 8) {
+            mx[0] = max3(mx[0], s[j], s[j + 1]); mx[1] = max3(mx[1], s[j + 2], s[j + 3]);
+            mx[2] = max3(mx[2], s[j + 4], s[j + 5]); mx[3] = max3(mx[3], s[j + 6], s[j + 7]);
+          }
+          const float tile_max = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;   // the scale is positive
+          float alpha = 1.f;
+          const bool raise = tile_max > m_ref + kMaxSlack || (m_ref == -INFINITY && tile_max > -INFINITY);
+          if (raise) {
+            alpha = fast_exp2(m_ref - tile_max);
+            m_ref = tile_max;
+            l_run *= alpha;
+          }
+          const float m_safe = m_ref == -INFINITY ? 0.f : m_ref;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int cb = 0; cb < 4; ++cb) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float p0 = fast_exp2(fmaf(s[cb * 32 + j], a.scale_log2, -m_safe));
+              const float p1 = fast_exp2(fmaf(s[cb * 32 + j + 1], a.scale_log2, -m_safe));
+              sum[(j >> 1) & 3] += p0 + p1;
+              const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: 2^-9 per weight
+              pk[j >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
+            }
+            tmem_st16(tS + lane_base + cb * 16, pk);
+          }
+          l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          // the rows whose reference has moved are rescaled (S of this tile exists, so every product into O before it is done)
+          if (n > u.n0 && __any_sync(0xffffffffu, raise)) {
+#pragma unroll 1
             for (int cb = 0; cb < D / 32; ++cb) {
               float v[32];
-              tmem_ld32_async(tO2 + cb * 32, v);
+              tmem_ld32_async(tO + lane_base + cb * 32, v);
               tmem_wait_ld();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[cb * 32 + j] = o[cb * 32 + j] * f + v[j] * f2;
+              for (int j = 0; j < 32; ++j) v[j] *= alpha;
+              tmem_st32(tO + lane_base + cb * 32, v);
             }
-            tc_fence_before();
-            mbar_arrive_cta(bar_e + (grp ^ 1) * 8);
           }
+          tmem_wait_st();
           tc_fence_before();
-          mbar_arrive_cta(my_e);
-          const bool complete = u.n0 == 0 && u.n1 == u.N;
-          const int row0 = it.cu[u.i] + u.t * tokens + token0;    // packed row of the group's first token
-          auto store8 = [&](int64_t at, const float* v, float f) {    // eight results, times f, at element `at` of the output
-            if (a.out_f32) {
-              float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
-              dst[0] = make_float4(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-              dst[1] = make_float4(v[4] * f, v[5] * f, v[6] * f, v[7] * f);
-            } else {
-              uint32_t b[4];
+        }
+        mbar_arrive_cta(bar_p);
+      }
+      if (failed) break;
+
+      // ---- the piece's result -----------------------------------------------------------------------------------------
+      const bool complete = u.n0 == 0 && u.n1 == u.N;
+      auto po_of = [&](int64_t slot) { return reinterpret_cast<float4*>(a.part_o) + slot * (D / 4) * kTile; };
+      auto ml_of = [&](int64_t slot) { return a.part_ml + slot * 2 * kTile; };
+      if (warp_live) {
+        const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
+        if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+        tc_fence_after();
+        float o[D];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i] * f, v[2 * i + 1] * f);
-                b[i] = *reinterpret_cast<const uint32_t*>(&p);
-              }
-              *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) = make_uint4(b[0], b[1], b[2], b[3]);
-            }
-          };
+        for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + lane_base + cb * 32, o + cb * 32);
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive_cta(bar_e);
         if (complete) {
           if (row_valid) {
             const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);   // NaN stays NaN
@@ -773,69 +720,66 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
             for (int d = 0; d < D; d += 8) store8(at + d, o + d, inv);
           }
         } else {
-          // partial results: slot 0 of the block continues a unit, slot 1 begins one; in it a half per group of rows
-          const int my_half = u.two ? grp : 0;
-          auto po_of = [&](int64_t slot) { return reinterpret_cast<float4*>(a.part_o) + (slot * 2 + my_half) * (D / 4) * kTile; };
-          auto ml_of = [&](int64_t slot) { return a.part_ml + (slot * 2 + my_half) * 2 * kTile; };
           const int64_t slot = 2 * (int64_t)blockIdx.x + (u.n0 == 0 ? 1 : 0);
           if (row_valid) {
-            float4* po = po_of(slot) + row;
+            float4* po = po_of(slot) + tid;
 #pragma unroll
             for (int d = 0; d < D / 4; ++d) po[d * kTile] = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
-            ml_of(slot)[row] = m_ref;
-            ml_of(slot)[kTile + row] = l_run;
+            ml_of(slot)[tid] = m_ref;
+            ml_of(slot)[kTile + tid] = l_run;
           }
           __threadfence();
-          if (!rows_sync()) { failed = true; break; }
-          // the unit's first block and number of pieces, from its place on the line
-          const long long x0 = x - u.n0;
-          const int b0 = (int)(x0 / it.span), pieces = (int)((x0 + u.N - 1) / it.span) - b0 + 1;
-          int32_t* ticket = a.tickets + 2 * b0 + my_half;
-          if (row == 0) {
-            const int got = atomicAdd(ticket, 1);
-            if (got == pieces - 1) *ticket = 0;                   // all have come: zero again for the next launch
-            s_ticket[grp] = got;
-          }
-          if (!rows_sync()) { failed = true; break; }
-          if (s_ticket[grp] == pieces - 1) {
-            __threadfence();
-            // the last to come joins them, always in the same order: threads are spread over the rows there are and, where
-            // these are few, over the head's coordinates
-            const int rows = mine * G;
-            int rows2 = 8;
-            while (rows2 < rows) rows2 <<= 1;                    // 8 .. 128
-            const int r = row & (rows2 - 1), part = row / rows2, parts = kGroup / rows2;
-            if (r < rows) {
-              auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
-              float m_all = -INFINITY;
+        }
+      } else {
+        // the barrier's every completion is waited for (a parity tells two of them apart, no more)
+        const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
+        if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
+        mbar_arrive_cta(bar_e);
+      }
+      if (!complete) {
+        if (!rows_sync()) { failed = true; break; }
+        // the unit's first block and number of pieces, from its place on the line
+        const long long x0 = x - u.n0;
+        const int b0 = (int)(x0 / it.span), pieces = (int)((x0 + u.N - 1) / it.span) - b0 + 1;
+        if (tid == 0) {
+          const int got = atomicAdd(a.tickets + b0, 1);
+          if (got == pieces - 1) a.tickets[b0] = 0;            // all have come: zero again for the next launch
+          s_ticket = got;
+        }
+        if (!rows_sync()) { failed = true; break; }
+        if (s_ticket == pieces - 1) {
+          __threadfence();
+          // the last to come joins them, in the order of the keys: threads are spread over the rows there are and, where these
+          // are few, over the head's coordinates
+          int rows2 = 8;
+          while (rows2 < rows) rows2 <<= 1;                    // 8 .. 128
+          const int r = tid & (rows2 - 1), part = tid / rows2, parts = kRowThreads / rows2;
+          if (r < rows) {
+            auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
+            float m_all = -INFINITY;
 #pragma unroll 8
-              for (int j = 0; j < pieces; ++j) m_all = fmaxf(m_all, __ldcg(ml_of(slot_of(j)) + r));
-              const float m_safe = m_all == -INFINITY ? 0.f : m_all;
-              float l_all = 0.f;
+            for (int j = 0; j < pieces; ++j) m_all = fmaxf(m_all, __ldcg(ml_of(slot_of(j)) + r));
+            const float m_safe = m_all == -INFINITY ? 0.f : m_all;
+            float l_all = 0.f;
 #pragma unroll 8
-              for (int j = 0; j < pieces; ++j) l_all += __ldcg(ml_of(slot_of(j)) + kTile + r) * fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
-              const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);
-              const int64_t at = ((int64_t)(row0 + r / G) * Hq + u.h * G + r % G) * D;
-              for (int d8 = part; d8 < D / 8; d8 += parts) {
-                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < pieces; ++j) l_all += __ldcg(ml_of(slot_of(j)) + kTile + r) * fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
+            const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);
+            const int64_t at = ((int64_t)(row0 + r / G) * Hq + u.h * G + r % G) * D;
+            for (int d8 = part; d8 < D / 8; d8 += parts) {
+              float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-                for (int j = 0; j < pieces; ++j) {
-                  const float f = fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
-                  const float4* po = po_of(slot_of(j)) + 2 * d8 * kTile + r;
-                  const float4 p = __ldcg(po), q = __ldcg(po + kTile);
-                  v[0] = fmaf(p.x, f, v[0]); v[1] = fmaf(p.y, f, v[1]); v[2] = fmaf(p.z, f, v[2]); v[3] = fmaf(p.w, f, v[3]);
-                  v[4] = fmaf(q.x, f, v[4]); v[5] = fmaf(q.y, f, v[5]); v[6] = fmaf(q.z, f, v[6]); v[7] = fmaf(q.w, f, v[7]);
-                }
-                store8(at + d8 * 8, v, inv);
+              for (int j = 0; j < pieces; ++j) {
+                const float f = fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
+                const float4* po = po_of(slot_of(j)) + 2 * d8 * kTile + r;
+                const float4 p = __ldcg(po), q = __ldcg(po + kTile);
+                v[0] = fmaf(p.x, f, v[0]); v[1] = fmaf(p.y, f, v[1]); v[2] = fmaf(p.z, f, v[2]); v[3] = fmaf(p.w, f, v[3]);
+                v[4] = fmaf(q.x, f, v[4]); v[5] = fmaf(q.y, f, v[5]); v[6] = fmaf(q.z, f, v[6]); v[7] = fmaf(q.w, f, v[7]);
               }
+              store8(at + d8 * 8, v, inv);
             }
           }
         }
-        }
-        joins += joined ? 1u : 0u;
       }
-      // units of the other group so far: it has a share of every unit but a solo one whose only tile is this group's
-      if (u.two || u.n0 + (lag ^ 1) < u.n1) ++others;
       x += u.n1 - u.n0;
       if (x >= x_end) break;
       u = next_unit(it, u, x_end - x, Hkv, tokens, align);
@@ -847,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
   if (*s_fail && tid == 0) atomicCAS(a.m.status, 0, BC_ERR_TIMEOUT);
   if (warp == 0) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");
   }
 }
 
@@ -869,9 +813,9 @@ int copy_height(int page_size) {
 
 }  // namespace
 
-// two pieces per block, two groups each
-size_t bc_chunk_part_o_bytes(int head_dim) { return (size_t)4 * BC_MAX_CHUNK_CTAS * head_dim * kTile * 4; }
-size_t bc_chunk_part_ml_bytes() { return (size_t)4 * BC_MAX_CHUNK_CTAS * 2 * kTile * 4; }
+// two pieces per block
+size_t bc_chunk_part_o_bytes(int head_dim) { return (size_t)2 * BC_MAX_CHUNK_CTAS * head_dim * kTile * 4; }
+size_t bc_chunk_part_ml_bytes() { return (size_t)2 * BC_MAX_CHUNK_CTAS * 2 * kTile * 4; }
 
 // Tensor map of the whole pool: (64 coordinates, K|V x head x half, row, layer), unswizzled: the store's own chunk
 // permutation is the swizzle.
@@ -896,8 +840,8 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.out = a.out; p.out_f32 = a.out_f32; p.layer = a.layer;
   p.part_o = a.part_o; p.part_ml = a.part_ml; p.tickets = a.tickets;
   p.Hq = g.q_heads; p.Hkv = g.kv_heads; p.G = g.q_heads / g.kv_heads; p.page_size = g.page_size;
-  p.half = kTile / p.G;
-  p.tokens = 2 * p.half;
+  p.by_page = make_fast_div((uint32_t)g.page_size);
+  p.tokens = kTile / p.G;
   p.R = copy_height(g.page_size);
   p.align = p.R > 8 ? p.R : 8;
   p.min_span = 4;
@@ -907,11 +851,11 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   CUtensorMap q_map;
   const cuuint64_t dims[3] = {(cuuint64_t)g.head_dim, (cuuint64_t)g.q_heads, (cuuint64_t)a.total_q};
   const cuuint64_t strides[2] = {(cuuint64_t)g.head_dim * 2, (cuuint64_t)g.q_heads * g.head_dim * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.half}, es[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tokens}, es[3] = {1, 1, 1};
   if (encode_tiled()(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  const int want = a.ctas > 0 ? a.ctas : sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // one resident block per SM
+  const int want = a.ctas > 0 ? a.ctas : 2 * sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // two resident blocks per SM
   if (a.ctas > 0) p.min_span = 1;   // a given number of blocks is for the cuts it makes
   const bool wide = p.R >= 4;
   if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
