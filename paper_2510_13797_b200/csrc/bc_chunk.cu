@@ -129,13 +129,15 @@ struct ChunkParams {
   int32_t out_f32, layer;
   float* part_o;      // [2 grid][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
   float* part_ml;     // [2 grid][2][128]
-  int32_t* tickets;   // [grid], by the block that begins the unit; zero between launches
+  // [3][BC_MAX_CHUNK_CTAS], zero between launches.  Sixteen pieces count themselves at the block of their first one, in row 0 where
+  // that one begins the unit and in row 1 where it continues it (a block has one of either kind at most); row 2: the sixteens of a unit.
+  int32_t* tickets;
   int32_t Hq, Hkv, G, page_size;
   FastDiv by_page;
   int32_t tokens;     // per unit: 128 / G
   int32_t R;          // entries per copy, a power of two
   int32_t align;      // segment starts in the virtual row space: max(8, R)
-  int32_t min_span;   // key tiles a block works on at least
+  int32_t min_tiles;  // key tiles of a piece at least
   uint32_t wait_limit;
   float scale_log2;
 };
@@ -145,9 +147,9 @@ struct Items {
   int m[kMaxItems], first[kMaxItems], P[kMaxItems], nb[kMaxItems], w[kMaxItems];
   long long before[kMaxItems + 1];   // key tiles of one KV head in the items before
   int large[64], n_large;            // items whose tiles all threads count together
-  long long total, span;
-  int item0, head0, tile0;           // where this block's span begins
-  int n0;
+  long long total, units, span;      // weight of the line, number of units, weight per block
+  int item0, head0, tile0, n0, tiles;   // where this block's span begins, and its tiles
+  int b0, pieces;                    // where units are cut into pieces: first block and number of pieces of this block's unit
 };
 
 // One unit: the query tile `t` of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
@@ -233,6 +235,9 @@ struct TileIssue {
   bool fresh;                // the unit's first tile here
 };
 
+template <int N>
+struct Width { static constexpr int value = N; };
+
 __device__ __forceinline__ void tma_pool(uint32_t dst, const CUtensorMap* map, int head_half, int row, int layer, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
@@ -288,9 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     init(bar_p, 1, kRowThreads); init(bar_f, 1, 1); init(bar_e, 2, kRowThreads); init(bar_d, 1, 1);   // e and r
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
-    it.n_large = 0;
   }
-  __syncthreads();
 
   // ---- the line: every item's lengths, its key tiles per KV head, and where this block's span begins ------------------
   for (int i = tid; i < a.n; i += kThreads) {
@@ -300,44 +303,73 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     const int m = c0 < 0 || c0 > a.total_q ? 0 : max(0, min(c1, a.total_q) - c0);
     const int first = a.first != nullptr ? a.first[i] : P + nb + w - m;
     it.m[i] = m; it.first[i] = min(max(first, -(1 << 30)), 1 << 30); it.P[i] = P; it.nb[i] = nb; it.w[i] = w;
-    const int tiles = (m + tokens - 1) / tokens;
-    long long cost = 0;
-    bool mine = true;
-    if (tiles > 8) {                                        // a long chunk: counted by all threads below
-      const int at = atomicAdd(&it.n_large, 1);
-      if (at < 64) { it.large[at] = i; mine = false; }
-    }
-    if (mine)
-      for (int t = 0; t < tiles; ++t) cost += key_tiles(it, i, t, tokens, align);
-    it.before[i + 1] = cost;
   }
-  __syncthreads();
-  const int n_large = min(it.n_large, 64);
-  for (int x = 0; x < n_large; ++x) {
-    const int i = it.large[x], tiles = (it.m[i] + tokens - 1) / tokens;
-    long long cost = 0;
-    for (int t = tid; t < tiles; t += kThreads) cost += key_tiles(it, i, t, tokens, align);
-    atomicAdd(reinterpret_cast<unsigned long long*>(&it.before[i + 1]), (unsigned long long)cost);
-  }
-  if (n_large) __syncthreads();
-  if (warp == 0) {
-    long long carry = 0;
-    for (int i0 = 0; i0 < a.n; i0 += 32) {
-      const int i = i0 + lane;
-      long long x = i < a.n ? it.before[i + 1] : 0;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
+  // pieces of a unit of N tiles, where there are `units` units (fewer than blocks) of `total` tiles together
+  auto pieces_of = [&](int N, long long units, long long total) {
+    const long long share = ((long long)gridDim.x - units) * N / total;
+    return (int)max(1ll, min((long long)(N / a.min_tiles), share));
+  };
+  // before[i + 1] = sum over the items up to i of their tiles' weights: key tiles, or (units > 0) pieces
+  auto line = [&](long long units, long long total) {
+    auto weight = [&](int i, int t) {
+      const int N = key_tiles(it, i, t, tokens, align);
+      return units > 0 ? pieces_of(N, units, total) : N;
+    };
+    __syncthreads();
+    if (tid == 0) it.n_large = 0;
+    __syncthreads();
+    for (int i = tid; i < a.n; i += kThreads) {
+      const int tiles = (it.m[i] + tokens - 1) / tokens;
+      long long cost = 0;
+      bool mine = true;
+      if (tiles > 8) {                                      // a long chunk: counted by all threads below
+        const int at = atomicAdd(&it.n_large, 1);
+        if (at < 64) { it.large[at] = i; mine = false; }
       }
-      if (i < a.n) it.before[i + 1] = carry + x;
-      carry += __shfl_sync(0xffffffffu, x, 31);
+      if (mine)
+        for (int t = 0; t < tiles; ++t) cost += weight(i, t);
+      it.before[i + 1] = cost;
     }
-    const long long total = carry * Hkv;
-    long long span = (total + gridDim.x - 1) / gridDim.x;
-    if (span < a.min_span) span = a.min_span;
-    if (lane == 0) { it.before[0] = 0; it.total = total; it.span = span; }
-    __syncwarp();
+    __syncthreads();
+    const int n_large = min(it.n_large, 64);
+    for (int x = 0; x < n_large; ++x) {
+      const int i = it.large[x], tiles = (it.m[i] + tokens - 1) / tokens;
+      long long cost = 0;
+      for (int t = tid; t < tiles; t += kThreads) cost += weight(i, t);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&it.before[i + 1]), (unsigned long long)cost);
+    }
+    if (n_large) __syncthreads();
+    if (warp == 0) {
+      long long carry = 0, tiles = 0;
+      for (int i0 = 0; i0 < a.n; i0 += 32) {
+        const int i = i0 + lane;
+        long long x = i < a.n ? it.before[i + 1] : 0;
+        if (i < a.n) tiles += (it.m[i] + tokens - 1) / tokens;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long y = __shfl_up_sync(0xffffffffu, x, d);
+          if (lane >= d) x += y;
+        }
+        if (i < a.n) it.before[i + 1] = carry + x;
+        carry += __shfl_sync(0xffffffffu, x, 31);
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, d);
+      if (lane == 0) { it.before[0] = 0; it.total = carry * Hkv; it.units = tiles * Hkv; }
+    }
+    __syncthreads();
+  };
+  line(0, 1);
+  const long long all_units = it.units, all_tiles = it.total;
+  const bool by_unit = all_units < (long long)gridDim.x;     // every block has (at most) one piece of one unit
+  if (by_unit && all_units > 0) line(all_units, all_tiles);
+  if (warp == 0) {
+    const long long total = it.total;
+    long long span = 1;
+    if (!by_unit) {
+      span = (total + gridDim.x - 1) / gridDim.x;
+      if (span < a.min_tiles) span = a.min_tiles;
+    }
     const long long x0 = (long long)blockIdx.x * span;
     if (x0 < total) {
       int lo = 0, hi = a.n;                                 // the item: largest i with before[i] * Hkv <= x0 (a non-empty one)
@@ -348,7 +380,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
       int t = 0;                                            // the query tile: 32 at a time
       for (;; t += 32) {
         const int tt = t + lane;
-        int x = tt * tokens < it.m[lo] ? key_tiles(it, lo, tt, tokens, align) : 0;
+        int x = 0;
+        if (tt * tokens < it.m[lo]) {
+          x = key_tiles(it, lo, tt, tokens, align);
+          if (by_unit) x = pieces_of(x, all_units, all_tiles);
+        }
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
           const int y = __shfl_up_sync(0xffffffffu, x, d);
@@ -364,13 +400,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         }
         in_head -= __shfl_sync(0xffffffffu, x, 31);
       }
-      if (lane == 0) { it.item0 = lo; it.head0 = head; it.tile0 = t; it.n0 = (int)in_head; }
+      if (lane == 0) {
+        it.item0 = lo; it.head0 = head; it.tile0 = t; it.n0 = (int)in_head;
+        it.tiles = (int)min(span, total - x0);
+        if (by_unit) {                                      // piece number in_head of the unit's `pieces`
+          const int N = key_tiles(it, lo, t, tokens, align), c = pieces_of(N, all_units, all_tiles);
+          it.n0 = (int)(in_head * N / c);
+          it.tiles = (int)((in_head + 1) * N / c) - it.n0;
+          it.pieces = c;
+          it.b0 = (int)(blockIdx.x - in_head);
+        }
+      }
+    } else if (lane == 0) {
+      it.tiles = 0;
     }
+    if (lane == 0) it.span = span;
   }
   __syncthreads();
-  const long long x_begin = (long long)blockIdx.x * it.span;
-  const long long x_end = min(it.total, x_begin + it.span);
-  if (x_begin >= x_end) return;                             // nothing to do: no tensor memory has been taken yet
+  const long long x_begin = (long long)blockIdx.x * it.span;  // by_unit: a number without a meaning on the line
+  const long long x_end = x_begin + it.tiles;
+  if (it.tiles == 0) return;                                // nothing to do: no tensor memory has been taken yet
 
   if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(kTmemColumns) : "memory");
@@ -738,46 +787,91 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
       }
       if (!complete) {
         if (!rows_sync()) { failed = true; break; }
-        // the unit's first block and number of pieces, from its place on the line
+        // the unit's first block and number of pieces: from its place on the line, where units are not cut one by one
         const long long x0 = x - u.n0;
-        const int b0 = (int)(x0 / it.span), pieces = (int)((x0 + u.N - 1) / it.span) - b0 + 1;
-        if (tid == 0) {
-          const int got = atomicAdd(a.tickets + b0, 1);
-          if (got == pieces - 1) a.tickets[b0] = 0;            // all have come: zero again for the next launch
-          s_ticket = got;
-        }
-        if (!rows_sync()) { failed = true; break; }
-        if (s_ticket == pieces - 1) {
-          __threadfence();
-          // the last to come joins them, in the order of the keys: threads are spread over the rows there are and, where these
-          // are few, over the head's coordinates
-          int rows2 = 8;
-          while (rows2 < rows) rows2 <<= 1;                    // 8 .. 128
-          const int r = tid & (rows2 - 1), part = tid / rows2, parts = kRowThreads / rows2;
+        const int b0 = by_unit ? it.b0 : (int)(x0 / it.span);
+        const int pieces = by_unit ? it.pieces : (int)((x0 + u.N - 1) / it.span) - b0 + 1;
+        auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
+        // true for the last of `count` callers
+        auto last_of = [&](int32_t* ticket, int count, bool* is_last) {
+          if (tid == 0) {
+            const int got = atomicAdd(ticket, 1);
+            if (got == count - 1) *ticket = 0;                  // all have come: zero again for the next launch
+            s_ticket = got;
+          }
+          if (!rows_sync()) return false;
+          *is_last = s_ticket == count - 1;
+          if (*is_last) __threadfence();
+          return true;
+        };
+        // Joins pieces j0, j0 + step, ... (`count`, at most 32) in this order, into the output or into the first one's place.
+        // Threads are spread over the rows there are and, where these are few, over the head's coordinates.
+        int rows2 = 8;
+        while (rows2 < rows) rows2 <<= 1;                      // 8 .. 128
+        const int r = tid & (rows2 - 1), part = tid / rows2, parts = kRowThreads / rows2;
+        auto join = [&](int j0, int step, int count, bool final) {
+          float m_all = -INFINITY, l_all = 0.f;
           if (r < rows) {
-            auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
-            float m_all = -INFINITY;
 #pragma unroll 8
-            for (int j = 0; j < pieces; ++j) m_all = fmaxf(m_all, __ldcg(ml_of(slot_of(j)) + r));
-            const float m_safe = m_all == -INFINITY ? 0.f : m_all;
-            float l_all = 0.f;
+            for (int j = 0; j < count; ++j) m_all = fmaxf(m_all, __ldcg(ml_of(slot_of(j0 + j * step)) + r));
+          }
+          const float m_safe = m_all == -INFINITY ? 0.f : m_all;
+          if (r < rows) {
 #pragma unroll 8
-            for (int j = 0; j < pieces; ++j) l_all += __ldcg(ml_of(slot_of(j)) + kTile + r) * fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
-            const float inv = l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all);
-            const int64_t at = ((int64_t)(row0 + r / G) * Hq + u.h * G + r % G) * D;
-            for (int d8 = part; d8 < D / 8; d8 += parts) {
-              float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-              for (int j = 0; j < pieces; ++j) {
-                const float f = fast_exp2(__ldcg(ml_of(slot_of(j)) + r) - m_safe);
-                const float4* po = po_of(slot_of(j)) + 2 * d8 * kTile + r;
-                const float4 p = __ldcg(po), q = __ldcg(po + kTile);
-                v[0] = fmaf(p.x, f, v[0]); v[1] = fmaf(p.y, f, v[1]); v[2] = fmaf(p.z, f, v[2]); v[3] = fmaf(p.w, f, v[3]);
-                v[4] = fmaf(q.x, f, v[4]); v[5] = fmaf(q.y, f, v[5]); v[6] = fmaf(q.z, f, v[6]); v[7] = fmaf(q.w, f, v[7]);
-              }
-              store8(at + d8 * 8, v, inv);
+            for (int j = 0; j < count; ++j) {
+              const float* ml = ml_of(slot_of(j0 + j * step));
+              l_all += __ldcg(ml + kTile + r) * fast_exp2(__ldcg(ml + r) - m_safe);
             }
           }
+          const float inv = final ? (l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all)) : 1.f;
+          const int64_t at = ((int64_t)(row0 + r / G) * Hq + u.h * G + r % G) * D;
+          const int each = max(1, D / 8 / parts);              // groups of eight coordinates per thread
+          auto some = [&](int d8, auto width) {                // `width` of them at a time
+            constexpr int kWidth = decltype(width)::value;
+            float v[8 * kWidth];
+#pragma unroll
+            for (int i = 0; i < 8 * kWidth; ++i) v[i] = 0.f;
+#pragma unroll (kWidth == 1 ? 8 : 2)
+            for (int j = 0; j < count; ++j) {
+              const int64_t slot = slot_of(j0 + j * step);
+              const float f = fast_exp2(__ldcg(ml_of(slot) + r) - m_safe);
+              const float4* po = po_of(slot) + 2 * d8 * kTile + r;
+#pragma unroll
+              for (int i = 0; i < 2 * kWidth; ++i) {
+                const float4 p = __ldcg(po + i * kTile);
+                v[4 * i] = fmaf(p.x, f, v[4 * i]); v[4 * i + 1] = fmaf(p.y, f, v[4 * i + 1]);
+                v[4 * i + 2] = fmaf(p.z, f, v[4 * i + 2]); v[4 * i + 3] = fmaf(p.w, f, v[4 * i + 3]);
+              }
+            }
+            if (final) {
+#pragma unroll
+              for (int i = 0; i < kWidth; ++i) store8(at + (d8 + i) * 8, v + 8 * i, inv);
+            } else {
+              float4* po = po_of(slot_of(j0)) + 2 * d8 * kTile + r;
+#pragma unroll
+              for (int i = 0; i < 2 * kWidth; ++i) po[i * kTile] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+          };
+          if (r < rows) {
+            const int d0 = part * each, d1 = min(D / 8, d0 + each);
+            if (each >= 4) for (int d8 = d0; d8 < d1; d8 += 4) some(d8, Width<4>());
+            else for (int d8 = d0; d8 < d1; ++d8) some(d8, Width<1>());
+          }
+          if (final) return true;
+          if (!rows_sync()) return false;                      // everybody has read the first one's (m, l)
+          if (r < rows && part == 0) { ml_of(slot_of(j0))[r] = m_all; ml_of(slot_of(j0))[kTile + r] = l_all; }
+          __threadfence();
+          return rows_sync();
+        };
+        constexpr int kFan = 16;
+        const int mine = by_unit ? (int)blockIdx.x - b0 : (int)(x / it.span) - b0;   // number of this piece
+        const int group = mine / kFan, groups = (pieces + kFan - 1) / kFan, in_group = min(kFan, pieces - group * kFan);
+        bool last = false;
+        if (!last_of(a.tickets + (group > 0 ? BC_MAX_CHUNK_CTAS : 0) + b0 + group * kFan, in_group, &last)) { failed = true; break; }
+        if (last && groups == 1) join(0, 1, pieces, true);
+        if (last && groups > 1) {
+          if (!join(group * kFan, 1, in_group, false) || !last_of(a.tickets + 2 * BC_MAX_CHUNK_CTAS + b0, groups, &last)) { failed = true; break; }
+          if (last) join(0, kFan, groups, true);
         }
       }
       x += u.n1 - u.n0;
@@ -844,7 +938,8 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.tokens = kTile / p.G;
   p.R = copy_height(g.page_size);
   p.align = p.R > 8 ? p.R : 8;
-  p.min_span = 4;
+  // pieces of units with many rows are joined slower: 128 rows' partial results are 64 KB each
+  p.min_tiles = (int64_t)a.total_q * p.G >= (int64_t)a.n * 32 ? 8 : 2;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
   p.scale_log2 = a.sm_scale * 1.4426950408889634f;
   if (!encode_tiled()) return cudaErrorNotSupported;
@@ -856,7 +951,7 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   const int want = a.ctas > 0 ? a.ctas : 2 * sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // two resident blocks per SM
-  if (a.ctas > 0) p.min_span = 1;   // a given number of blocks is for the cuts it makes
+  if (a.ctas > 0) p.min_tiles = 1;   // a given number of blocks is for the cuts it makes
   const bool wide = p.R >= 4;
   if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
     if (g.head_dim != 128) return cudaErrorNotSupported;

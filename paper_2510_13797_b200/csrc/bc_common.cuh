@@ -158,7 +158,7 @@ struct BcChunkArgs {
   int32_t out_f32;
   float sm_scale;
   float *part_o, *part_ml;               // bc_chunk_part_o_bytes, bc_chunk_part_ml_bytes
-  int32_t* tickets;                      // [BC_MAX_CHUNK_CTAS], zero between launches
+  int32_t* tickets;                      // [3 BC_MAX_CHUNK_CTAS], zero between launches
   int32_t ctas;                          // 0: two per SM
   uint32_t wait_limit;                   // 0: the default
 };

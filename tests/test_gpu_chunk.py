@@ -116,6 +116,24 @@ def test_spans_of_any_number_of_blocks(Hkv, G, D, ps, c, plens, gens, ms, ctas):
         _run(pair, slots, ms, g)
 
 
+@pytest.mark.parametrize("ctas", [0, 64, 304])
+def test_one_long_cache_between_many_short_ones(ctas):
+    """Spans much shorter than the longest unit: a unit in many more pieces than are joined at once, between units that are not cut."""
+    plens = [40] * 30 + [30000] + [40] * 41
+    pair, slots, g = _cache(4, 2, 64, 16, 1, plens, [0] * len(plens), seed=21)
+    pair.gpu.bc_set_attn_ctas(ctas)
+    for ms in ([1] * len(plens), [1 + i % 3 for i in range(len(plens))]):
+        _run(pair, slots, ms, g)
+
+
+def test_few_units_in_many_pieces():
+    """Fewer units than thread blocks: one sequence over hundreds of key tiles, few rows and many."""
+    pair, slots, g = _cache(1, 6, 128, 16, 1, [40000], [0], seed=22)
+    _run(pair, slots, [1], g)
+    _run(pair, slots, [30], g)
+    _run(pair, slots, [7], g, first=[20000])
+
+
 def test_results_do_not_change_from_call_to_call():
     pair, slots, g = _cache(2, 6, 128, 16, 1, [5000, 1200], [40, 10], seed=7)
     q, out = _run(pair, slots, [33, 10], g)
