@@ -137,7 +137,7 @@ struct ChunkParams {
   int32_t tokens;     // per unit: 128 / G
   int32_t R;          // entries per copy, a power of two
   int32_t align;      // segment starts in the virtual row space: max(8, R)
-  int32_t min_tiles;  // key tiles of a piece at least
+  int32_t min_shift;  // log2 of the key tiles of a piece, at least
   uint32_t wait_limit;
   float scale_log2;
 };
@@ -304,18 +304,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     const int first = a.first != nullptr ? a.first[i] : P + nb + w - m;
     it.m[i] = m; it.first[i] = min(max(first, -(1 << 30)), 1 << 30); it.P[i] = P; it.nb[i] = nb; it.w[i] = w;
   }
-  // pieces of a unit of N tiles, where there are `units` units (fewer than blocks) of `total` tiles together
-  auto pieces_of = [&](int N, long long units, long long total) {
-    const long long share = ((long long)gridDim.x - units) * N / total;
-    return (int)max(1ll, min((long long)(N / a.min_tiles), share));
-  };
-  // before[i + 1] = sum over the items up to i of their tiles' weights: key tiles, or (units > 0) pieces
-  auto line = [&](long long units, long long total) {
+  // Pieces of a unit of N tiles, where units are fewer than blocks; share: blocks left over per key tile
+  // (together at most as many as blocks: a piece each, and the rest of the blocks by shares rounded down)
+  auto pieces_of = [&](int N, float share) { return max(1, min(N >> a.min_shift, (int)((float)N * share))); };
+  // First before[i + 1] = the key tiles of one KV head in the items up to i; then, where there are fewer units than blocks, the
+  // same in pieces (one loop for both: its instructions come from memory in most calls).
+  bool by_unit = false;                                      // every block has (at most) one piece of one unit
+  float share = 0.f;
+#pragma unroll 1
+  for (;;) {
     auto weight = [&](int i, int t) {
       const int N = key_tiles(it, i, t, tokens, align);
-      return units > 0 ? pieces_of(N, units, total) : N;
+      return by_unit ? pieces_of(N, share) : N;
     };
-    __syncthreads();
     if (tid == 0) it.n_large = 0;
     __syncthreads();
     for (int i = tid; i < a.n; i += kThreads) {
@@ -327,20 +328,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         if (at < 64) { it.large[at] = i; mine = false; }
       }
       if (mine)
+#pragma unroll 1
         for (int t = 0; t < tiles; ++t) cost += weight(i, t);
       it.before[i + 1] = cost;
     }
     __syncthreads();
     const int n_large = min(it.n_large, 64);
+#pragma unroll 1
     for (int x = 0; x < n_large; ++x) {
       const int i = it.large[x], tiles = (it.m[i] + tokens - 1) / tokens;
       long long cost = 0;
+#pragma unroll 1
       for (int t = tid; t < tiles; t += kThreads) cost += weight(i, t);
       atomicAdd(reinterpret_cast<unsigned long long*>(&it.before[i + 1]), (unsigned long long)cost);
     }
     if (n_large) __syncthreads();
     if (warp == 0) {
       long long carry = 0, tiles = 0;
+#pragma unroll 1
       for (int i0 = 0; i0 < a.n; i0 += 32) {
         const int i = i0 + lane;
         long long x = i < a.n ? it.before[i + 1] : 0;
@@ -358,17 +363,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
       if (lane == 0) { it.before[0] = 0; it.total = carry * Hkv; it.units = tiles * Hkv; }
     }
     __syncthreads();
-  };
-  line(0, 1);
-  const long long all_units = it.units, all_tiles = it.total;
-  const bool by_unit = all_units < (long long)gridDim.x;     // every block has (at most) one piece of one unit
-  if (by_unit && all_units > 0) line(all_units, all_tiles);
+    if (by_unit || it.units >= (long long)gridDim.x || it.total == 0) break;
+    by_unit = true;
+    // blocks left over per key tile, a little less so that the rounding cannot hand out one block too many
+    share = (float)((long long)gridDim.x - it.units) / (float)it.total * 0.9999f;
+    __syncthreads();                                        // it.total has been read
+  }
   if (warp == 0) {
     const long long total = it.total;
     long long span = 1;
     if (!by_unit) {
       span = (total + gridDim.x - 1) / gridDim.x;
-      if (span < a.min_tiles) span = a.min_tiles;
+      if (span < (1 << a.min_shift)) span = 1 << a.min_shift;
     }
     const long long x0 = (long long)blockIdx.x * span;
     if (x0 < total) {
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         int x = 0;
         if (tt * tokens < it.m[lo]) {
           x = key_tiles(it, lo, tt, tokens, align);
-          if (by_unit) x = pieces_of(x, all_units, all_tiles);
+          if (by_unit) x = pieces_of(x, share);
         }
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -404,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         it.item0 = lo; it.head0 = head; it.tile0 = t; it.n0 = (int)in_head;
         it.tiles = (int)min(span, total - x0);
         if (by_unit) {                                      // piece number in_head of the unit's `pieces`
-          const int N = key_tiles(it, lo, t, tokens, align), c = pieces_of(N, all_units, all_tiles);
+          const int N = key_tiles(it, lo, t, tokens, align), c = pieces_of(N, share);
           it.n0 = (int)(in_head * N / c);
           it.tiles = (int)((in_head + 1) * N / c) - it.n0;
           it.pieces = c;
@@ -755,25 +761,29 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
         if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
         tc_fence_after();
-        float o[D];
+        const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);   // NaN stays NaN
+        const int64_t at = ((int64_t)(row0 + my_local) * Hq + u.h * G + my_head) * D;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (u.n0 == 0 ? 1 : 0);
+        float4* po = po_of(slot) + tid;
+        // 32 columns at a time, not unrolled: this runs once per unit, and its instructions come from memory the first time
+#pragma unroll 1
+        for (int cb = 0; cb < D / 32; ++cb) {
+          float o[32];
+          tmem_ld32_async(tO + lane_base + cb * 32, o);
+          tmem_wait_ld();
+          if (row_valid && complete) {
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) tmem_ld32_async(tO + lane_base + cb * 32, o + cb * 32);
-        tmem_wait_ld();
+            for (int d = 0; d < 32; d += 8) store8(at + cb * 32 + d, o + d, inv);
+          }
+          if (row_valid && !complete) {
+#pragma unroll
+            for (int d = 0; d < 8; ++d) po[(cb * 8 + d) * kTile] = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
+          }
+        }
         tc_fence_before();
         mbar_arrive_cta(bar_e);
-        if (complete) {
+        if (!complete) {
           if (row_valid) {
-            const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);   // NaN stays NaN
-            const int64_t at = ((int64_t)(row0 + my_local) * Hq + u.h * G + my_head) * D;
-#pragma unroll
-            for (int d = 0; d < D; d += 8) store8(at + d, o + d, inv);
-          }
-        } else {
-          const int64_t slot = 2 * (int64_t)blockIdx.x + (u.n0 == 0 ? 1 : 0);
-          if (row_valid) {
-            float4* po = po_of(slot) + tid;
-#pragma unroll
-            for (int d = 0; d < D / 4; ++d) po[d * kTile] = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
             ml_of(slot)[tid] = m_ref;
             ml_of(slot)[kTile + tid] = l_run;
           }
@@ -812,17 +822,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         auto join = [&](int j0, int step, int count, bool final) {
           float m_all = -INFINITY, l_all = 0.f;
           if (r < rows) {
-#pragma unroll 8
-            for (int j = 0; j < count; ++j) m_all = fmaxf(m_all, __ldcg(ml_of(slot_of(j0 + j * step)) + r));
-          }
-          const float m_safe = m_all == -INFINITY ? 0.f : m_all;
-          if (r < rows) {
-#pragma unroll 8
+#pragma unroll 4
             for (int j = 0; j < count; ++j) {
               const float* ml = ml_of(slot_of(j0 + j * step));
-              l_all += __ldcg(ml + kTile + r) * fast_exp2(__ldcg(ml + r) - m_safe);
+              const float m = __ldcg(ml + r), l = __ldcg(ml + kTile + r), to = fmaxf(m_all, m), safe = to == -INFINITY ? 0.f : to;
+              l_all = l_all * fast_exp2(m_all - safe) + l * fast_exp2(m - safe);
+              m_all = to;
             }
           }
+          const float m_safe = m_all == -INFINITY ? 0.f : m_all;
           const float inv = final ? (l_all > 0.f ? 1.f / l_all : (l_all == 0.f ? 0.f : l_all)) : 1.f;
           const int64_t at = ((int64_t)(row0 + r / G) * Hq + u.h * G + r % G) * D;
           const int each = max(1, D / 8 / parts);              // groups of eight coordinates per thread
@@ -831,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
             float v[8 * kWidth];
 #pragma unroll
             for (int i = 0; i < 8 * kWidth; ++i) v[i] = 0.f;
-#pragma unroll (kWidth == 1 ? 8 : 2)
+#pragma unroll (kWidth == 1 ? 4 : 2)
             for (int j = 0; j < count; ++j) {
               const int64_t slot = slot_of(j0 + j * step);
               const float f = fast_exp2(__ldcg(ml_of(slot) + r) - m_safe);
@@ -866,13 +874,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         constexpr int kFan = 16;
         const int mine = by_unit ? (int)blockIdx.x - b0 : (int)(x / it.span) - b0;   // number of this piece
         const int group = mine / kFan, groups = (pieces + kFan - 1) / kFan, in_group = min(kFan, pieces - group * kFan);
+        int32_t* ticket = a.tickets + (group > 0 ? BC_MAX_CHUNK_CTAS : 0) + b0 + group * kFan;
+        int j0 = group * kFan, step = 1, count = in_group;
         bool last = false;
-        if (!last_of(a.tickets + (group > 0 ? BC_MAX_CHUNK_CTAS : 0) + b0 + group * kFan, in_group, &last)) { failed = true; break; }
-        if (last && groups == 1) join(0, 1, pieces, true);
-        if (last && groups > 1) {
-          if (!join(group * kFan, 1, in_group, false) || !last_of(a.tickets + 2 * BC_MAX_CHUNK_CTAS + b0, groups, &last)) { failed = true; break; }
-          if (last) join(0, kFan, groups, true);
+#pragma unroll 1
+        for (bool final = groups == 1;; final = true) {         // first these sixteen, then the sixteens
+          failed = !last_of(ticket, count, &last);
+          if (failed || !last) break;
+          failed = !join(j0, step, count, final);
+          if (failed || final) break;
+          ticket = a.tickets + 2 * BC_MAX_CHUNK_CTAS + b0;
+          j0 = 0; step = kFan; count = groups;
         }
+        if (failed) break;
       }
       x += u.n1 - u.n0;
       if (x >= x_end) break;
@@ -938,8 +952,7 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.tokens = kTile / p.G;
   p.R = copy_height(g.page_size);
   p.align = p.R > 8 ? p.R : 8;
-  // pieces of units with many rows are joined slower: 128 rows' partial results are 64 KB each
-  p.min_tiles = (int64_t)a.total_q * p.G >= (int64_t)a.n * 32 ? 8 : 2;
+  p.min_shift = 2;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
   p.scale_log2 = a.sm_scale * 1.4426950408889634f;
   if (!encode_tiled()) return cudaErrorNotSupported;
@@ -951,7 +964,7 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   const int want = a.ctas > 0 ? a.ctas : 2 * sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // two resident blocks per SM
-  if (a.ctas > 0) p.min_tiles = 1;   // a given number of blocks is for the cuts it makes
+  if (a.ctas > 0) p.min_shift = 0;   // a given number of blocks is for the cuts it makes
   const bool wide = p.R >= 4;
   if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
     if (g.head_dim != 128) return cudaErrorNotSupported;
