@@ -83,9 +83,13 @@ struct NormRopeArgs {
   float eps;
 };
 
+// The heads a warp has of a row are worked on in passes of kHeads; kAhead passes' loads are in flight at once (two blocks per SM
+// of 4 KB per warp: 64 KB, a little more than the memory's latency times its rate takes), the row's angles are computed behind the
+// first of them.
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_norm_rope(const NormRopeArgs a) {
-  constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;   // lanes per head, heads per warp pass, 16-byte pieces per head
+__global__ void __launch_bounds__(kThreads, 2) k_norm_rope(const NormRopeArgs a) {
+  constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;   // lanes per head, heads per pass, 16-byte pieces per head
+  constexpr int kAhead = 4;
   const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes;
   const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   const uint4 wq0 = a.q_weight ? a.q_weight[piece] : ones, wq1 = a.q_weight ? a.q_weight[kLanes + piece] : ones;
@@ -97,37 +101,46 @@ __global__ void __launch_bounds__(kThreads) k_norm_rope(const NormRopeArgs a) {
   for (int64_t u = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); u < a.units; u += step) {
     const int64_t row = u / a.split;
     const int part = (int)(u - row * a.split);
-    float c[8], s[8];
-    row_angles<D>(a.positions[row], freq, c, s);
+    const int pos = a.positions[row];
     const uint4* in = reinterpret_cast<const uint4*>(a.qkv + row * a.row_bytes);
-    for (int h0 = part * kHeads; h0 < heads; h0 += a.split * kHeads) {
-      const int h = h0 + sub;
-      const bool live = h < heads;
-      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-      if (live) { lo = in[h * kChunks + piece]; hi = in[h * kChunks + kLanes + piece]; }
-      float x[8], y[8];
-      unpack8(lo, x); unpack8(hi, y);
-      float sq = 0.f;
+    float c[8], s[8];
+    for (int h0 = part * kHeads; h0 < heads; h0 += kAhead * a.split * kHeads) {
+      uint4 lo[kAhead], hi[kAhead];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-      const float r = rsqrtf(head_sum<D>(sq) * (1.f / D) + a.eps);
-      if (h < rot) {
-        const bool is_q = h < a.q_heads;
-        float w0[8], w1[8];
-        unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
+      for (int k = 0; k < kAhead; ++k) {
+        const int h = h0 + k * a.split * kHeads + sub;
+        lo[k] = hi[k] = make_uint4(0, 0, 0, 0);
+        if (h < heads) { lo[k] = __ldcs(in + h * kChunks + piece); hi[k] = __ldcs(in + h * kChunks + kLanes + piece); }
+      }
+      if (h0 == part * kHeads) row_angles<D>(pos, freq, c, s);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float p = x[i] * r * w0[i], q = y[i] * r * w1[i];
-          x[i] = fmaf(p, c[i], -q * s[i]);
-          y[i] = fmaf(q, c[i], p * s[i]);
+      for (int k = 0; k < kAhead; ++k) {
+        const int h = h0 + k * a.split * kHeads + sub;
+        if (h0 + k * a.split * kHeads >= heads) break;             // uniform over the warp
+        float x[8], y[8];
+        unpack8(lo[k], x); unpack8(hi[k], y);
+        float sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+        const float r = rsqrtf(head_sum<D>(sq) * (1.f / D) + a.eps);
+        if (h < rot) {
+          const bool is_q = h < a.q_heads;
+          float w0[8], w1[8];
+          unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float p = x[i] * r * w0[i], q = y[i] * r * w1[i];
+            x[i] = fmaf(p, c[i], -q * s[i]);
+            y[i] = fmaf(q, c[i], p * s[i]);
+          }
+          uint4* dst = is_q ? a.q_out + (row * a.q_heads + h) * kChunks : a.k_out + (row * a.kv_heads + (h - a.q_heads)) * kChunks;
+          dst[piece] = pack8(x);
+          dst[kLanes + piece] = pack8(y);
+        } else if (h < heads) {
+          uint4* dst = a.v_out + (row * a.kv_heads + (h - rot)) * kChunks;
+          dst[piece] = lo[k];
+          dst[kLanes + piece] = hi[k];
         }
-        uint4* dst = is_q ? a.q_out + (row * a.q_heads + h) * kChunks : a.k_out + (row * a.kv_heads + (h - a.q_heads)) * kChunks;
-        dst[piece] = pack8(x);
-        dst[kLanes + piece] = pack8(y);
-      } else if (live) {
-        uint4* dst = a.v_out + (row * a.kv_heads + (h - rot)) * kChunks;
-        dst[piece] = lo;
-        dst[kLanes + piece] = hi;
       }
     }
   }
@@ -137,7 +150,7 @@ struct NormRopeGradArgs {
   const uint8_t* qkv;
   int64_t row_bytes;
   const int32_t* positions;
-  const uint4 *q_weight, *k_weight;
+  const __nv_bfloat16 *q_weight, *k_weight;
   const uint4 *dq, *dk, *dv;
   uint4* dqkv;          // [rows][q_heads + 2 kv_heads][D], contiguous
   float* partial;       // [blocks][2][D]
@@ -147,74 +160,107 @@ struct NormRopeGradArgs {
   float eps;
 };
 
-// The weight gradients: every lane adds up its 16 coordinates over the rows and heads it meets (fp32, a few dozen
-// to a few hundred terms), the block's lanes are joined in a fixed order and a second kernel adds the blocks', also
-// in a fixed order, so that results are reproducible.
+// The weight gradients: every lane adds up its 16 coordinates over the rows and heads it meets (fp32, a few dozen to a
+// few hundred terms; the query heads' sums in registers, the key heads', which are fewer, in a place of the lane's own in
+// shared memory), the block's lanes are joined in a fixed order and a second kernel adds the blocks', also in a fixed order, so
+// that results are reproducible.
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_norm_rope_grad(const NormRopeGradArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGradArgs a) {
   constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;
+  constexpr int kAhead = 2;
+  __shared__ __align__(16) float weights[2][D];
+  __shared__ __align__(16) float dwk[kWarps][4][32][4];           // a lane's 16 sums: 16 bytes apart from its neighbours'
   const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes, warp = threadIdx.x >> 5;
-  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-  const uint4 wq0 = a.q_weight ? a.q_weight[piece] : ones, wq1 = a.q_weight ? a.q_weight[kLanes + piece] : ones;
-  const uint4 wk0 = a.k_weight ? a.k_weight[piece] : ones, wk1 = a.k_weight ? a.k_weight[kLanes + piece] : ones;
+  for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
+    const __nv_bfloat16* w = i < D ? a.q_weight : a.k_weight;
+    weights[i / D][i % D] = w ? __bfloat162float(w[i % D]) : 1.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dwk[warp][i][lane]) = make_float4(0.f, 0.f, 0.f, 0.f);
+  __syncthreads();
   double freq[D / 64];
   lane_frequencies<D>(a.log2_theta, freq);
   const int rot = a.q_heads + a.kv_heads, heads = rot + a.kv_heads;
-  float dwq[16], dwk[16];
+  float dwq[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) dwq[i] = dwk[i] = 0.f;
+  for (int i = 0; i < 16; ++i) dwq[i] = 0.f;
   const int64_t step = (int64_t)gridDim.x * kWarps;
   for (int64_t u = (int64_t)blockIdx.x * kWarps + warp; u < a.units; u += step) {
     const int64_t row = u / a.split;
     const int part = (int)(u - row * a.split);
-    float c[8], s[8];
-    row_angles<D>(a.positions[row], freq, c, s);
+    const int pos = a.positions[row];
     const uint4* in = reinterpret_cast<const uint4*>(a.qkv + row * a.row_bytes);
+    const uint4* gq = a.dq + row * a.q_heads * kChunks;               // + h: the gradient of head h of the row, of its kind
+    const uint4* gk = a.dk + (row * a.kv_heads - a.q_heads) * kChunks;
+    const uint4* gv = a.dv + (row * a.kv_heads - rot) * kChunks;
     uint4* out = a.dqkv + row * heads * kChunks;
-    for (int h0 = part * kHeads; h0 < heads; h0 += a.split * kHeads) {
-      const int h = h0 + sub;
-      const bool turned = h < rot, is_q = h < a.q_heads;
-      uint4 lo = make_uint4(0, 0, 0, 0), hi = lo, glo = lo, ghi = lo;
-      if (h < heads) {
-        const uint4* g = is_q ? a.dq + (row * a.q_heads + h) * kChunks
-                              : (turned ? a.dk + (row * a.kv_heads + (h - a.q_heads)) * kChunks : a.dv + (row * a.kv_heads + (h - rot)) * kChunks);
-        glo = g[piece]; ghi = g[kLanes + piece];
-        if (turned) { lo = in[h * kChunks + piece]; hi = in[h * kChunks + kLanes + piece]; }
-      }
-      float x[8], y[8], p[8], q[8], w0[8], w1[8];
-      unpack8(lo, x); unpack8(hi, y); unpack8(glo, p); unpack8(ghi, q);
-      unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
-      float sq = 0.f, dot = 0.f;
+    float c[8], s[8];
+    for (int h0 = part * kHeads; h0 < heads; h0 += kAhead * a.split * kHeads) {
+      uint4 xlo[kAhead], xhi[kAhead], glo[kAhead], ghi[kAhead];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d0 = fmaf(p[i], c[i], q[i] * s[i]), d1 = fmaf(q[i], c[i], -p[i] * s[i]);   // the rotation taken back
-        p[i] = d0; q[i] = d1;
-        sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-        dot = fmaf(x[i] * w0[i], d0, fmaf(y[i] * w1[i], d1, dot));
+      for (int k = 0; k < kAhead; ++k) {
+        const int h = h0 + k * a.split * kHeads + sub;
+        xlo[k] = xhi[k] = glo[k] = ghi[k] = make_uint4(0, 0, 0, 0);
+        if (h < rot) { xlo[k] = __ldcs(in + h * kChunks + piece); xhi[k] = __ldcs(in + h * kChunks + kLanes + piece); }
+        if (h < heads) {
+          const uint4* g = (h < a.q_heads ? gq : (h < rot ? gk : gv)) + h * kChunks;
+          glo[k] = __ldcs(g + piece); ghi[k] = __ldcs(g + kLanes + piece);
+        }
       }
-      sq = head_sum<D>(sq); dot = head_sum<D>(dot);
-      const float r = rsqrtf(sq * (1.f / D) + a.eps), k = r * r * dot * (1.f / D);
-      if (turned) {
+      if (h0 == part * kHeads) row_angles<D>(pos, freq, c, s);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int h = h0 + k * a.split * kHeads + sub;
+        if (h0 + k * a.split * kHeads >= heads) break;             // uniform over the warp
+        const bool is_q = h < a.q_heads;
+        const float* w = weights[is_q ? 0 : 1] + piece * 8;
+        float x[8], y[8], p[8], q[8];
+        unpack8(xlo[k], x); unpack8(xhi[k], y); unpack8(glo[k], p); unpack8(ghi[k], q);
+        float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float xr = x[i] * r, yr = y[i] * r;
-          if (is_q) { dwq[i] = fmaf(xr, p[i], dwq[i]); dwq[8 + i] = fmaf(yr, q[i], dwq[8 + i]); }
-          else { dwk[i] = fmaf(xr, p[i], dwk[i]); dwk[8 + i] = fmaf(yr, q[i], dwk[8 + i]); }
-          x[i] = r * fmaf(w0[i], p[i], -x[i] * k);
-          y[i] = r * fmaf(w1[i], q[i], -y[i] * k);
+          const float d0 = fmaf(p[i], c[i], q[i] * s[i]), d1 = fmaf(q[i], c[i], -p[i] * s[i]);   // the rotation taken back
+          p[i] = d0; q[i] = d1;
+          sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+          dot = fmaf(x[i] * w[i], d0, fmaf(y[i] * w[D / 2 + i], d1, dot));
         }
-        out[h * kChunks + piece] = pack8(x);
-        out[h * kChunks + kLanes + piece] = pack8(y);
-      } else if (h < heads) {
-        out[h * kChunks + piece] = glo;
-        out[h * kChunks + kLanes + piece] = ghi;
+        sq = head_sum<D>(sq); dot = head_sum<D>(dot);
+        const float r = rsqrtf(sq * (1.f / D) + a.eps), t = r * r * dot * (1.f / D);
+        if (h < rot) {
+          if (is_q) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { dwq[i] = fmaf(x[i] * r, p[i], dwq[i]); dwq[8 + i] = fmaf(y[i] * r, q[i], dwq[8 + i]); }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float4* at = reinterpret_cast<float4*>(dwk[warp][j][lane]);
+              float4 v = *at;
+              const float* xx = j < 2 ? x + 4 * j : y + 4 * (j - 2);
+              const float* pp = j < 2 ? p + 4 * j : q + 4 * (j - 2);
+              v.x = fmaf(xx[0] * r, pp[0], v.x); v.y = fmaf(xx[1] * r, pp[1], v.y);
+              v.z = fmaf(xx[2] * r, pp[2], v.z); v.w = fmaf(xx[3] * r, pp[3], v.w);
+              *at = v;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] = r * fmaf(w[i], p[i], -x[i] * t);
+            y[i] = r * fmaf(w[D / 2 + i], q[i], -y[i] * t);
+          }
+          out[h * kChunks + piece] = pack8(x);
+          out[h * kChunks + kLanes + piece] = pack8(y);
+        } else if (h < heads) {
+          out[h * kChunks + piece] = glo[k];
+          out[h * kChunks + kLanes + piece] = ghi[k];
+        }
       }
     }
   }
+  if (a.partial == nullptr) return;
   __shared__ float sh[kWarps][2][D];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float vq = dwq[i], vk = dwk[i];
+    float vq = dwq[i], vk = dwk[warp][i >> 2][lane][i & 3];
 #pragma unroll
     for (int d = kLanes; d < 32; d <<= 1) { vq += __shfl_xor_sync(0xffffffffu, vq, d); vk += __shfl_xor_sync(0xffffffffu, vk, d); }
     if (sub == 0) {
@@ -228,25 +274,25 @@ __global__ void __launch_bounds__(kThreads) k_norm_rope_grad(const NormRopeGradA
     const float* col = &sh[0][0][0] + threadIdx.x;
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) t += col[w * 2 * D];
+    for (int v = 0; v < kWarps; ++v) t += col[v * 2 * D];
     a.partial[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = t;
   }
 }
 
-template <int D>
-__global__ void __launch_bounds__(1024) k_norm_rope_weights(const float* __restrict__ partial, int blocks, float* __restrict__ dq_weight,
+// Adds the blocks' sums: a block has 32 of the 2 D columns, 32 threads per column.
+__global__ void __launch_bounds__(1024) k_norm_rope_weights(const float* __restrict__ partial, int blocks, int D, float* __restrict__ dq_weight,
                                                            float* __restrict__ dk_weight) {
-  constexpr int kGroups = 1024 / (2 * D);
-  __shared__ float sh[kGroups][2 * D];
-  const int col = threadIdx.x % (2 * D), grp = threadIdx.x / (2 * D);
+  asm volatile("griddepcontrol.wait;" ::: "memory");           // the launch may begin while the kernel ahead ends
+  __shared__ float sh[32][33];
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + lane;
   float t = 0.f;
-#pragma unroll 8
-  for (int b = grp; b < blocks; b += kGroups) t += partial[(int64_t)b * 2 * D + col];
-  sh[grp][col] = t;
+#pragma unroll 10
+  for (int b = grp; b < blocks; b += 32) t += partial[(int64_t)b * 2 * D + col];
+  sh[grp][lane] = t;
   __syncthreads();
   if (grp == 0) {
 #pragma unroll
-    for (int g = 1; g < kGroups; ++g) t += sh[g][col];
+    for (int g = 1; g < 32; ++g) t += sh[g][lane];
     float* dst = col < D ? dq_weight : dk_weight;
     if (dst != nullptr) dst[col % D] = t;
   }
@@ -256,11 +302,11 @@ constexpr int kMaxGradBlocks = 148 * 2;
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Few rows: several warps share a row's heads, down to one pass each, until there are about 16 warps per SM.
-int row_split(int64_t n, int heads, int head_dim) {
+// Few rows: several warps share a row's heads, down to one pass each, until there are about `warps` of them.
+int row_split(int64_t n, int heads, int head_dim, int64_t warps) {
   const int passes = (heads * (head_dim / 16) + 31) / 32;
   int split = 1;
-  while (split < passes && n * split < 148 * 16) split *= 2;
+  while (split < passes && n * split < warps) split *= 2;
   return split < passes ? split : passes;
 }
 
@@ -288,10 +334,10 @@ bc_status bc_norm_rope_split(int32_t n, int32_t q_heads, int32_t kv_heads, int32
   a.qkv = (const uint8_t*)qkv; a.row_bytes = row_stride * 2; a.positions = positions;
   a.q_weight = (const uint4*)q_weight; a.k_weight = (const uint4*)k_weight;
   a.q_out = (uint4*)q_out; a.k_out = (uint4*)k_out; a.v_out = (uint4*)v_out;
-  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim);
+  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 148 * 16);
   a.units = (int64_t)n * a.split; a.log2_theta = log2((double)theta); a.eps = eps;
   const int64_t want = (a.units + kWarps - 1) / kWarps;
-  const int blocks = (int)(want < 148 * 4 ? want : 148 * 4);
+  const int blocks = (int)(want < 148 * 2 ? want : 148 * 2);   // two resident blocks per SM
   if (head_dim == 64) k_norm_rope<64><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
   else k_norm_rope<128><<<blocks, kThreads, 0, (cudaStream_t)stream>>>(a);
   return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
@@ -316,21 +362,28 @@ bc_status bc_norm_rope_split_backward(int32_t n, int32_t q_heads, int32_t kv_hea
   if (workspace_bytes < (size_t)kMaxGradBlocks * 2 * head_dim * sizeof(float)) return BC_ERR_INVALID_ARG;
   NormRopeGradArgs a;
   a.qkv = (const uint8_t*)qkv; a.row_bytes = row_stride * 2; a.positions = positions;
-  a.q_weight = (const uint4*)q_weight; a.k_weight = (const uint4*)k_weight;
+  a.q_weight = (const __nv_bfloat16*)q_weight; a.k_weight = (const __nv_bfloat16*)k_weight;
   a.dq = (const uint4*)dq; a.dk = (const uint4*)dk; a.dv = (const uint4*)dv; a.dqkv = (uint4*)dqkv;
-  a.partial = (float*)workspace;
-  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim);
-  a.units = (int64_t)n * a.split; a.log2_theta = log2((double)theta); a.eps = eps;
+  const bool weights = dq_weight != nullptr || dk_weight != nullptr;
+  a.partial = weights ? (float*)workspace : nullptr;
+  a.q_heads = q_heads; a.kv_heads = kv_heads; a.log2_theta = log2((double)theta); a.eps = eps;
+  a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 148 * 16);
+  a.units = (int64_t)n * a.split;
   const int64_t want = (a.units + kWarps - 1) / kWarps;
   const int blocks = (int)(want < kMaxGradBlocks ? want : kMaxGradBlocks);
   cudaStream_t s = (cudaStream_t)stream;
   if (head_dim == 64) k_norm_rope_grad<64><<<blocks, kThreads, 0, s>>>(a);
   else k_norm_rope_grad<128><<<blocks, kThreads, 0, s>>>(a);
   if (cudaGetLastError() != cudaSuccess) return BC_ERR_CUDA;
-  if (dq_weight == nullptr && dk_weight == nullptr) return BC_OK;
-  if (head_dim == 64) k_norm_rope_weights<64><<<1, 1024, 0, s>>>(a.partial, blocks, dq_weight, dk_weight);
-  else k_norm_rope_weights<128><<<1, 1024, 0, s>>>(a.partial, blocks, dq_weight, dk_weight);
-  return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+  if (!weights) return BC_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * head_dim / 32)); cfg.blockDim = dim3(1024); cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k_norm_rope_weights, (const float*)a.partial, blocks, (int)head_dim, dq_weight, dk_weight);
+  return e == cudaSuccess ? BC_OK : BC_ERR_CUDA;
 }
 
 }  // extern "C"
