@@ -28,12 +28,39 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-  f[0] = bf_lo(v.x); f[1] = bf_hi(v.x); f[2] = bf_lo(v.y); f[3] = bf_hi(v.y);
-  f[4] = bf_lo(v.z); f[5] = bf_hi(v.z); f[6] = bf_lo(v.w); f[7] = bf_hi(v.w);
+
+// Pairs of fp32 numbers in one register pair: one instruction for both (Blackwell's packed fp32 arithmetic).
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+__device__ __forceinline__ void split(F2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack8(const uint4& v, F2* f) {
+  f[0] = pair(bf_lo(v.x), bf_hi(v.x)); f[1] = pair(bf_lo(v.y), bf_hi(v.y));
+  f[2] = pair(bf_lo(v.z), bf_hi(v.z)); f[3] = pair(bf_lo(v.w), bf_hi(v.w));
+}
+__device__ __forceinline__ uint32_t pack_bf16(F2 v) {
+  float a, b;
+  split(v, &a, &b);
+  return pack_bf16(a, b);
+}
+__device__ __forceinline__ uint4 pack8(const F2* f) { return make_uint4(pack_bf16(f[0]), pack_bf16(f[1]), pack_bf16(f[2]), pack_bf16(f[3])); }
+__device__ __forceinline__ float sum_of(F2 v) {
+  float a, b;
+  split(v, &a, &b);
+  return a + b;
 }
 
 // sum over the D / 16 lanes that hold a head
@@ -55,7 +82,8 @@ __device__ __forceinline__ void lane_frequencies(double log2_theta, double* f) {
 }
 // cos and sin of the eight angles that belong to this lane's coordinates, for the position of the warp's row
 template <int D>
-__device__ __forceinline__ void row_angles(int pos, const double* f, float* c, float* s) {
+__device__ __forceinline__ void row_angles(int pos, const double* f, F2* c2, F2* s2) {
+  float c[8], s[8];
   float cs[D / 64], sn[D / 64];
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
@@ -69,6 +97,8 @@ __device__ __forceinline__ void row_angles(int pos, const double* f, float* c, f
     c[i] = __shfl_sync(0xffffffffu, cs[i % (D / 64)], src);
     s[i] = __shfl_sync(0xffffffffu, sn[i % (D / 64)], src);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { c2[i] = pair(c[2 * i], c[2 * i + 1]); s2[i] = pair(s[2 * i], s[2 * i + 1]); }
 }
 
 struct NormRopeArgs {
@@ -103,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope(const NormRopeArgs a)
     const int part = (int)(u - row * a.split);
     const int pos = a.positions[row];
     const uint4* in = reinterpret_cast<const uint4*>(a.qkv + row * a.row_bytes);
-    float c[8], s[8];
+    F2 c[4], s[4];
     for (int h0 = part * kHeads; h0 < heads; h0 += kAhead * a.split * kHeads) {
       uint4 lo[kAhead], hi[kAhead];
 #pragma unroll
@@ -117,21 +147,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope(const NormRopeArgs a)
       for (int k = 0; k < kAhead; ++k) {
         const int h = h0 + k * a.split * kHeads + sub;
         if (h0 + k * a.split * kHeads >= heads) break;             // uniform over the warp
-        float x[8], y[8];
+        F2 x[4], y[4], sq = pair(0.f, 0.f);
         unpack8(lo[k], x); unpack8(hi[k], y);
-        float sq = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-        const float r = rsqrtf(head_sum<D>(sq) * (1.f / D) + a.eps);
+        for (int i = 0; i < 4; ++i) sq = fma2(x[i], x[i], fma2(y[i], y[i], sq));
+        const float r = rsqrtf(head_sum<D>(sum_of(sq)) * (1.f / D) + a.eps);
         if (h < rot) {
           const bool is_q = h < a.q_heads;
-          float w0[8], w1[8];
+          F2 w0[4], w1[4];
           unpack8(is_q ? wq0 : wk0, w0); unpack8(is_q ? wq1 : wk1, w1);
+          const F2 r2 = pair(r, r), minus = pair(-1.f, -1.f);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float p = x[i] * r * w0[i], q = y[i] * r * w1[i];
-            x[i] = fmaf(p, c[i], -q * s[i]);
-            y[i] = fmaf(q, c[i], p * s[i]);
+          for (int i = 0; i < 4; ++i) {
+            const F2 p = mul2(mul2(x[i], r2), w0[i]), q = mul2(mul2(y[i], r2), w1[i]);
+            x[i] = fma2(p, c[i], mul2(mul2(q, minus), s[i]));
+            y[i] = fma2(q, c[i], mul2(p, s[i]));
           }
           uint4* dst = is_q ? a.q_out + (row * a.q_heads + h) * kChunks : a.k_out + (row * a.kv_heads + (h - a.q_heads)) * kChunks;
           dst[piece] = pack8(x);
@@ -168,6 +198,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGradArgs a) {
   constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;
   constexpr int kAhead = 2;
+  if (a.partial != nullptr) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel that adds the blocks' sums waits for this one's end
   __shared__ __align__(16) float weights[2][D];
   __shared__ __align__(16) float dwk[kWarps][4][32][4];           // a lane's 16 sums: 16 bytes apart from its neighbours'
   const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes, warp = threadIdx.x >> 5;
@@ -181,9 +212,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
   double freq[D / 64];
   lane_frequencies<D>(a.log2_theta, freq);
   const int rot = a.q_heads + a.kv_heads, heads = rot + a.kv_heads;
-  float dwq[16];
+  F2 dwq[8];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) dwq[i] = 0.f;
+  for (int i = 0; i < 8; ++i) dwq[i] = pair(0.f, 0.f);
   const int64_t step = (int64_t)gridDim.x * kWarps;
   for (int64_t u = (int64_t)blockIdx.x * kWarps + warp; u < a.units; u += step) {
     const int64_t row = u / a.split;
@@ -194,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
     const uint4* gk = a.dk + (row * a.kv_heads - a.q_heads) * kChunks;
     const uint4* gv = a.dv + (row * a.kv_heads - rot) * kChunks;
     uint4* out = a.dqkv + row * heads * kChunks;
-    float c[8], s[8];
+    F2 c[4], s[4];
     for (int h0 = part * kHeads; h0 < heads; h0 += kAhead * a.split * kHeads) {
       uint4 xlo[kAhead], xhi[kAhead], glo[kAhead], ghi[kAhead];
 #pragma unroll
@@ -213,39 +244,46 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
         const int h = h0 + k * a.split * kHeads + sub;
         if (h0 + k * a.split * kHeads >= heads) break;             // uniform over the warp
         const bool is_q = h < a.q_heads;
-        const float* w = weights[is_q ? 0 : 1] + piece * 8;
-        float x[8], y[8], p[8], q[8];
-        unpack8(xlo[k], x); unpack8(xhi[k], y); unpack8(glo[k], p); unpack8(ghi[k], q);
-        float sq = 0.f, dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float d0 = fmaf(p[i], c[i], q[i] * s[i]), d1 = fmaf(q[i], c[i], -p[i] * s[i]);   // the rotation taken back
-          p[i] = d0; q[i] = d1;
-          sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-          dot = fmaf(x[i] * w[i], d0, fmaf(y[i] * w[D / 2 + i], d1, dot));
+        F2 w0[4], w1[4];
+        {
+          const float4* w = reinterpret_cast<const float4*>(weights[is_q ? 0 : 1] + piece * 8);
+          const float4 v0 = w[0], v1 = w[1], v2 = w[D / 8], v3 = w[D / 8 + 1];
+          w0[0] = pair(v0.x, v0.y); w0[1] = pair(v0.z, v0.w); w0[2] = pair(v1.x, v1.y); w0[3] = pair(v1.z, v1.w);
+          w1[0] = pair(v2.x, v2.y); w1[1] = pair(v2.z, v2.w); w1[2] = pair(v3.x, v3.y); w1[3] = pair(v3.z, v3.w);
         }
-        sq = head_sum<D>(sq); dot = head_sum<D>(dot);
+        F2 x[4], y[4], p[4], q[4], sq2 = pair(0.f, 0.f), dot2 = sq2;
+        const F2 minus = pair(-1.f, -1.f);
+        unpack8(xlo[k], x); unpack8(xhi[k], y); unpack8(glo[k], p); unpack8(ghi[k], q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const F2 d0 = fma2(p[i], c[i], mul2(q[i], s[i])), d1 = fma2(q[i], c[i], mul2(mul2(p[i], minus), s[i]));   // the rotation taken back
+          p[i] = d0; q[i] = d1;
+          sq2 = fma2(x[i], x[i], fma2(y[i], y[i], sq2));
+          dot2 = fma2(mul2(x[i], w0[i]), d0, fma2(mul2(y[i], w1[i]), d1, dot2));
+        }
+        const float sq = head_sum<D>(sum_of(sq2)), dot = head_sum<D>(sum_of(dot2));
         const float r = rsqrtf(sq * (1.f / D) + a.eps), t = r * r * dot * (1.f / D);
+        const F2 r2 = pair(r, r), t2 = pair(-t, -t);
         if (h < rot) {
           if (is_q) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { dwq[i] = fmaf(x[i] * r, p[i], dwq[i]); dwq[8 + i] = fmaf(y[i] * r, q[i], dwq[8 + i]); }
+            for (int i = 0; i < 4; ++i) { dwq[i] = fma2(mul2(x[i], r2), p[i], dwq[i]); dwq[4 + i] = fma2(mul2(y[i], r2), q[i], dwq[4 + i]); }
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              float4* at = reinterpret_cast<float4*>(dwk[warp][j][lane]);
-              float4 v = *at;
-              const float* xx = j < 2 ? x + 4 * j : y + 4 * (j - 2);
-              const float* pp = j < 2 ? p + 4 * j : q + 4 * (j - 2);
-              v.x = fmaf(xx[0] * r, pp[0], v.x); v.y = fmaf(xx[1] * r, pp[1], v.y);
-              v.z = fmaf(xx[2] * r, pp[2], v.z); v.w = fmaf(xx[3] * r, pp[3], v.w);
+              ulonglong2* at = reinterpret_cast<ulonglong2*>(dwk[warp][j][lane]);
+              ulonglong2 v = *at;
+              const F2* xx = j < 2 ? x + 2 * j : y + 2 * (j - 2);
+              const F2* pp = j < 2 ? p + 2 * j : q + 2 * (j - 2);
+              v.x = fma2(mul2(xx[0], r2), pp[0], v.x);
+              v.y = fma2(mul2(xx[1], r2), pp[1], v.y);
               *at = v;
             }
           }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[i] = r * fmaf(w[i], p[i], -x[i] * t);
-            y[i] = r * fmaf(w[D / 2 + i], q[i], -y[i] * t);
+          for (int i = 0; i < 4; ++i) {
+            x[i] = mul2(r2, fma2(x[i], t2, mul2(w0[i], p[i])));
+            y[i] = mul2(r2, fma2(y[i], t2, mul2(w1[i], q[i])));
           }
           out[h * kChunks + piece] = pack8(x);
           out[h * kChunks + kLanes + piece] = pack8(y);
@@ -260,7 +298,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
   __shared__ float sh[kWarps][2][D];
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float vq = dwq[i], vk = dwk[warp][i >> 2][lane][i & 3];
+    float even, odd;
+    split(dwq[i >> 1], &even, &odd);
+    float vq = (i & 1) ? odd : even, vk = dwk[warp][i >> 2][lane][i & 3];
 #pragma unroll
     for (int d = kLanes; d < 32; d <<= 1) { vq += __shfl_xor_sync(0xffffffffu, vq, d); vk += __shfl_xor_sync(0xffffffffu, vk, d); }
     if (sub == 0) {
@@ -302,11 +342,13 @@ constexpr int kMaxGradBlocks = 148 * 2;
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Few rows: several warps share a row's heads, down to one pass each, until there are about `warps` of them.
-int row_split(int64_t n, int heads, int head_dim, int64_t warps) {
+// Few rows: several warps share a row's heads, down to one pass each, until there is a unit for each of the 16 warps per SM;
+// and while that leaves `ahead` passes per unit, until there are about six, so that the last round of units is a small part
+// of the whole (8192 rows of 48 heads, the gradient: 64 us in 3.5 rounds, 57 us in 6.9).
+int row_split(int64_t n, int heads, int head_dim, int ahead) {
   const int passes = (heads * (head_dim / 16) + 31) / 32;
   int split = 1;
-  while (split < passes && n * split < warps) split *= 2;
+  while (split < passes && (n * split < 148 * 16 || (n * split < 148 * 16 * 6 && passes >= 2 * split * ahead))) split *= 2;
   return split < passes ? split : passes;
 }
 
@@ -334,7 +376,7 @@ bc_status bc_norm_rope_split(int32_t n, int32_t q_heads, int32_t kv_heads, int32
   a.qkv = (const uint8_t*)qkv; a.row_bytes = row_stride * 2; a.positions = positions;
   a.q_weight = (const uint4*)q_weight; a.k_weight = (const uint4*)k_weight;
   a.q_out = (uint4*)q_out; a.k_out = (uint4*)k_out; a.v_out = (uint4*)v_out;
-  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 148 * 16);
+  a.q_heads = q_heads; a.kv_heads = kv_heads; a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 4);
   a.units = (int64_t)n * a.split; a.log2_theta = log2((double)theta); a.eps = eps;
   const int64_t want = (a.units + kWarps - 1) / kWarps;
   const int blocks = (int)(want < 148 * 2 ? want : 148 * 2);   // two resident blocks per SM
@@ -367,7 +409,7 @@ bc_status bc_norm_rope_split_backward(int32_t n, int32_t q_heads, int32_t kv_hea
   const bool weights = dq_weight != nullptr || dk_weight != nullptr;
   a.partial = weights ? (float*)workspace : nullptr;
   a.q_heads = q_heads; a.kv_heads = kv_heads; a.log2_theta = log2((double)theta); a.eps = eps;
-  a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 148 * 16);
+  a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 2);
   a.units = (int64_t)n * a.split;
   const int64_t want = (a.units + kWarps - 1) / kWarps;
   const int blocks = (int)(want < kMaxGradBlocks ? want : kMaxGradBlocks);
