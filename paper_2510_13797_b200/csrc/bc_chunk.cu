@@ -126,7 +126,8 @@ struct ChunkParams {
   const int32_t *slots, *first, *cu_q;
   int32_t n, total_q;
   void* out;
-  int32_t out_f32, layer;
+  int32_t out_f32, layer, entry_bytes;
+  const uint8_t* pool_layer;
   float* part_o;      // [2 grid][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
   float* part_ml;     // [2 grid][2][128]
   // [3][BC_MAX_CHUNK_CTAS], zero between launches.  Sixteen pieces count themselves at the block of their first one, in row 0 where
@@ -135,7 +136,7 @@ struct ChunkParams {
   int32_t Hq, Hkv, G, page_size;
   FastDiv by_page;
   int32_t tokens;     // per unit: 128 / G
-  int32_t R;          // entries per copy, a power of two
+  int32_t R;          // entries per copy: 8, 16 or 32, or 1 (row by row)
   int32_t align;      // segment starts in the virtual row space: max(8, R)
   int32_t min_shift;  // log2 of the key tiles of a piece, at least
   uint32_t wait_limit;
@@ -235,6 +236,10 @@ struct TileIssue {
   bool fresh;                // the unit's first tile here
 };
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 template <int N>
 struct Width { static constexpr int value = N; };
 
@@ -255,7 +260,8 @@ struct Smem {
   static constexpr int kBytes = (1 + 2 * kStages) * kOperand + 1024 + (int)sizeof(Items);
 };
 
-// D: head_dim.  KP: copies per lane, tensor and tile (1 for pages that are a multiple of 4 entries, else 4).
+// D: head_dim.  ROWS: the page size has no power of two from 8 up: a tensor copy would hold one entry or a few, and a warp issues
+// one in some 70 cycles, so the copy warp's lanes copy the rows 16 bytes each.
 //
 // Roles: warps 0 .. 3 are the row threads, warp 4 issues the products, warp 5 the copies.
 // S of the next tile is issued right behind the product with P of the last one, whose P it overwrites: one thread issues both,
@@ -266,9 +272,10 @@ struct Smem {
 //   bar_s: S of a tile is ready                                   bar_p: the 128 row threads have stored P
 //   bar_f: O of a unit is final                                   bar_e: the rows have read O
 //   bar_r: the row threads among themselves (bounded, unlike a block barrier)
-template <int D, int KP, bool SHORTW>
+template <int D, bool ROWS, bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
                                                            const __grid_constant__ CUtensorMap pool_map) {
+  constexpr int KP = ROWS ? 4 : 1;                          // copies per lane, tensor and tile
   constexpr int kHalves = Smem<D>::kHalves, kHalfBytes = Smem<D>::kHalfBytes, kOperand = Smem<D>::kOperand, kStages = Smem<D>::kStages;
   constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -501,20 +508,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     };
     auto issue = [&](const TileIssue<KP>& ti, int which, int slot) {   // K (0) or V (1) of a tile into ring buffer `slot`
       const uint32_t dst = (which ? sV : sK) + slot * kOperand, bar = (which ? bar_vin : bar_kin) + slot * 8;
-      int c = 0;
+      if constexpr (ROWS) {
+        constexpr int kPieces = D / 8, kRows = 32 / kPieces;     // 16-byte pieces of a row, rows per instruction
+        const int piece = lane % kPieces;
+        const uint8_t* src = a.pool_layer + (int64_t)(which * Hkv + ti.h) * (D * 2) + piece * 16;
+        const uint32_t at = dst + (piece >> 3) * kHalfBytes + (piece & 7) * 16;
 #pragma unroll
-      for (int k = 0; k < KP; ++k) c += __popc(ti.valid[k]);
-      if (elect_one()) mbar_expect_tx(bar, (uint32_t)(c * R * D * 2));
-      __syncwarp();
-#pragma unroll
-      for (int k = 0; k < KP; ++k) {
-        if (ti.valid[k] >> lane & 1) {
-          const int p = lane + 32 * k;
+        for (int k = 0; k < KP; ++k) {
           int page = ti.page[k];
+          if (a.m.debug && (ti.valid[k] >> lane & 1) && (unsigned)page >= (unsigned)a.m.num_pages) { debug_note(a.m, page); page = 0; }
+          const int own = page * a.page_size + ti.rem[k];        // pool row of the tile's row 32 k + lane
+#pragma unroll 4
+          for (int i = 0; i < 32 / kRows; ++i) {
+            const int r = i * kRows + lane / kPieces, from = __shfl_sync(0xffffffffu, own, r);
+            if (ti.valid[k] >> r & 1) cp_async16(at + (32 * k + r) * 128, src + (int64_t)from * a.entry_bytes);
+          }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        proxy_fence();   // the product reads shared memory through the asynchronous proxy
+        __syncwarp();
+        if (elect_one()) mbar_arrive_cta(bar);
+      } else {
+        if (elect_one()) mbar_expect_tx(bar, (uint32_t)(__popc(ti.valid[0]) * R * D * 2));
+        __syncwarp();
+        if (ti.valid[0] >> lane & 1) {
+          int page = ti.page[0];
           if (a.m.debug && (unsigned)page >= (unsigned)a.m.num_pages) { debug_note(a.m, page); page = 0; }
 #pragma unroll
           for (int s = 0; s < kHalves; ++s)
-            tma_pool(dst + s * kHalfBytes + p * R * 128, &pool_map, (which * Hkv + ti.h) * kHalves + s, page * a.page_size + ti.rem[k], a.layer, bar);
+            tma_pool(dst + s * kHalfBytes + lane * R * 128, &pool_map, (which * Hkv + ti.h) * kHalves + s, page * a.page_size + ti.rem[0], a.layer, bar);
         }
       }
       __syncwarp();
@@ -903,12 +925,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
   }
 }
 
-template <int D, int KP, bool SHORTW>
+template <int D, bool ROWS, bool SHORTW>
 cudaError_t launch(const ChunkParams& p, const CUtensorMap& q_map, const CUtensorMap& pool_map, int grid, cudaStream_t s) {
   const int smem = Smem<D>::kBytes;
-  const cudaError_t e = cudaFuncSetAttribute(k_chunk_attn<D, KP, SHORTW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = cudaFuncSetAttribute(k_chunk_attn<D, ROWS, SHORTW>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  k_chunk_attn<D, KP, SHORTW><<<grid, kThreads, smem, s>>>(p, q_map, pool_map);
+  k_chunk_attn<D, ROWS, SHORTW><<<grid, kThreads, smem, s>>>(p, q_map, pool_map);
   return cudaGetLastError();
 }
 
@@ -945,12 +967,14 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   ChunkParams p;
   p.m = m;
   p.slots = a.slots; p.first = a.first; p.cu_q = a.cu_q; p.n = a.n; p.total_q = a.total_q;
-  p.out = a.out; p.out_f32 = a.out_f32; p.layer = a.layer;
+  p.out = a.out; p.out_f32 = a.out_f32; p.layer = a.layer; p.entry_bytes = g.entry_bytes; p.pool_layer = a.pool_layer;
   p.part_o = a.part_o; p.part_ml = a.part_ml; p.tickets = a.tickets;
   p.Hq = g.q_heads; p.Hkv = g.kv_heads; p.G = g.q_heads / g.kv_heads; p.page_size = g.page_size;
   p.by_page = make_fast_div((uint32_t)g.page_size);
   p.tokens = kTile / p.G;
-  p.R = copy_height(g.page_size);
+  const int height = copy_height(g.page_size);
+  const bool rows = height < 8;
+  p.R = rows ? 1 : height;
   p.align = p.R > 8 ? p.R : 8;
   p.min_shift = 2;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
@@ -965,11 +989,10 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
     return cudaErrorInvalidValue;
   const int want = a.ctas > 0 ? a.ctas : 2 * sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // two resident blocks per SM
   if (a.ctas > 0) p.min_shift = 0;   // a given number of blocks is for the cuts it makes
-  const bool wide = p.R >= 4;
   if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
     if (g.head_dim != 128) return cudaErrorNotSupported;
-    return wide ? launch<128, 1, true>(p, q_map, pool_map, grid, s) : launch<128, 4, true>(p, q_map, pool_map, grid, s);
+    return rows ? launch<128, true, true>(p, q_map, pool_map, grid, s) : launch<128, false, true>(p, q_map, pool_map, grid, s);
   }
-  if (g.head_dim == 128) return wide ? launch<128, 1, false>(p, q_map, pool_map, grid, s) : launch<128, 4, false>(p, q_map, pool_map, grid, s);
-  return wide ? launch<64, 1, false>(p, q_map, pool_map, grid, s) : launch<64, 4, false>(p, q_map, pool_map, grid, s);
+  if (g.head_dim == 128) return rows ? launch<128, true, false>(p, q_map, pool_map, grid, s) : launch<128, false, false>(p, q_map, pool_map, grid, s);
+  return rows ? launch<64, true, false>(p, q_map, pool_map, grid, s) : launch<64, false, false>(p, q_map, pool_map, grid, s);
 }
