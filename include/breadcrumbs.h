@@ -346,7 +346,7 @@ BC_API bc_status bc_norm_rope_decode_step(bc_cache* cache, int32_t layer, const 
  * rows is exactly 0).
  * The call changes no bookkeeping and may be issued at any point of the layer order; it uses scratch in the
  * cache's workspace (one call at a time per cache, like every call).  One launch; it completes before
- * any later kernel of the stream starts.  bc_set_attn_ctas sets its number of thread blocks too (0 = two per SM),
+ * any later kernel of the stream starts.  bc_set_attn_ctas sets its number of thread blocks too (0 = one per SM, 160 at most),
  * bc_set_wait_limit its waits' limit, and a wait that runs out is reported as there. */
 BC_API bc_status bc_chunk_attn(bc_cache* cache, int32_t layer, const int32_t* slots, const int32_t* first,
                                const int32_t* cu_q, int32_t n, int32_t total_q, const void* q, void* out, float sm_scale,

@@ -75,7 +75,7 @@ WorkLayout work_layout(const bc_config& c) {
     l.stage_out2[b] = take(max_n * c.q_heads * c.head_dim * 4);
   }
   l.rope_stage = take(max_n * (c.q_heads + 2 * c.kv_heads) * c.head_dim * 2);   // bc_rope_decode_step: q | k | v
-  l.chunk_tickets = take(3 * BC_MAX_CHUNK_CTAS * 4);
+  l.chunk_tickets = take(6 * BC_MAX_CHUNK_CTAS * 4);
   l.chunk_ml = take(bc_chunk_part_ml_bytes());
   l.chunk_o = take(bc_chunk_part_o_bytes(c.head_dim));
   l.total = o;
@@ -425,7 +425,7 @@ bc_status bc_cache_create(const bc_config* cfg, void* pool, void* meta, void* wo
   if (e == cudaSuccess) e = bc_launch_init(c->meta, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.tickets, 0, (size_t)BC_MAX_ATTN_BATCH * 4 * c->cfg.layers, (cudaStream_t)stream);
   if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.book_flag, 0, 4, (cudaStream_t)stream);
-  if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, 3 * BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, 6 * BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream);
   if (e != cudaSuccess) { delete c; return BC_ERR_CUDA; }
   c->launches += 1;
   *out = c;
@@ -1276,7 +1276,7 @@ bc_status bc_clear_error(bc_cache* c, void* stream) {
   BC_CUDA(c, cudaMemsetAsync(c->meta.status, 0, 16, (cudaStream_t)stream));
   // an attention launch that gave up (BC_ERR_TIMEOUT) may have left ticket counters non-zero
   BC_CUDA(c, cudaMemsetAsync(c->work + c->wl.tickets, 0, (size_t)BC_MAX_ATTN_BATCH * 4 * c->cfg.layers, (cudaStream_t)stream));
-  BC_CUDA(c, cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, 3 * BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream));
+  BC_CUDA(c, cudaMemsetAsync(c->work + c->wl.chunk_tickets, 0, 6 * BC_MAX_CHUNK_CTAS * 4, (cudaStream_t)stream));
   // The counters of the built-in array are shared by every cache of the process: they are touched
   // only when THIS cache has used the static entry point since its last clear (a launch of its own
   // may have left them non-zero), never on behalf of a cache that did not.

@@ -6,26 +6,30 @@
 // zeros where that is nothing.  That is the attention of a prompt chunk behind the entries stored before it, and of
 // the last m_i entries of a window (several guessed tokens checked at once).
 //
-// k_chunk_attn runs on the tcgen05 tensor cores.  A thread block (two per SM) works on units of 128 query rows,
-// floor(128 / G) tokens times the G query heads of a KV head, against tiles of 128 keys: S = Q K^T into tensor memory,
-// softmax by one thread per row, P as bf16 back into tensor memory, O += P V; while one block's rows work on S the
-// products of the SM's other block run.
+// k_chunk_attn runs on the tcgen05 tensor cores.  A thread block (one per SM) works on units of 256 query rows, two
+// groups of floor(128 / G) tokens times the G query heads of a KV head, against tiles of 64 keys that both groups share:
+// S = Q K^T into tensor memory, softmax by one thread per row, P as bf16 back into tensor memory, O += P V.  S of a group
+// has two places, used in turn, so that the next tile's S is there when the rows have finished one.  Sharing K and V halves
+// what a block reads: with a block per group the reads' latency was the bound (4 x 2048 rows over 8192 entries, 32 / 8 heads:
+// 1.07 ms).  A unit with rows for one group only ("solo") belongs to one of the groups, taken in turn, so that one writes
+// its results while the other begins.
 //   * Keys come from pages.  The live entries lie in a virtual row space, prompt from 0, beacons and window each from
 //     the next multiple of the copy height, so that (row & 7) equals the entry's position in its segment modulo 8:
 //     the store's chunk permutation IS the 128-byte swizzle of the product's operand layout, and unswizzled tensor
 //     copies of up to 32 entries of one page (64 of the head's coordinates each) put a tile together, K and V alike.
 //     The copy height R is the largest power of two up to that which divides the page size, so no copy crosses a page.
 //   * The key tiles of all (sequence, KV head, query tile) units form one line that is cut into equal spans, one per
-//     thread block: a unit that is cut leaves unnormalised partial results (m, l, O) per row in the workspace,
-//     and the group that takes the unit's last ticket joins them in the order of the keys, so results do not depend
-//     on which block that is.  Few rows over a long cache are spread over all SMs this way, and a large
-//     prompt chunk ends everywhere at the same time.
+//     thread block, so that a large prompt chunk ends everywhere at the same time; where there are fewer units than
+//     blocks, each unit is cut into equal pieces instead, as many as its share of the blocks, of at least 8 tiles (joining
+//     pieces takes about as long as four to eight tiles).  A unit that is cut leaves unnormalised partial results (m, l, O)
+//     per row in the workspace, and the block that takes its last ticket joins them in the order of the keys, sixteen at a
+//     time, so results do not depend on which block that is.
 //   * Every block works the line out from the lengths on the device by itself: no host copy of a length, no plan
 //     kernel, and the call can be captured.
 //   * The copies, the products and the rows' softmax each have warps of their own, and the stream of tiles goes on across
 //     units.
 // Bounds: at many rows per key the tensor pipe, the exponentials and the waits between them, at few rows the reads of the
-// cache; a tile is 64 KB of K and V for 8.4 MFLOP.
+// cache; a tile is 32 KB of K and V for 4.2 MFLOP.
 //
 // Entries that no row of a query tile can see are not read into a product: their scores are overwritten with -inf, and
 // V rows that are past the last visible entry of the tile are cleared in shared memory, so that whatever the
@@ -42,10 +46,11 @@ namespace {
 #include "bc_tc.cuh"
 #include "bc_book_device.cuh"
 
-constexpr int kRowThreads = 128;               // one per query row
-constexpr int kThreads = kRowThreads + 64;     // and the product warp and the copy warp
+constexpr int kGroup = 128;                    // rows, and row threads, of a group
+constexpr int kThreads = 2 * kGroup + 128;     // two groups, a product warp for each and two copy warps
+constexpr int kKeys = 64;                      // keys per tile
 constexpr int kMaxItems = BC_MAX_ATTN_BATCH;
-constexpr int kTmemColumns = 256;              // S and O; what is allocated and what is given back
+constexpr int kTmemColumns = 512;              // S and O; what is allocated and what is given back
 
 // ---- the simple form -----------------------------------------------------------------------------------------------
 // item of packed row `row`: the largest i with cu[i] <= row; false if the row belongs to none
@@ -128,14 +133,16 @@ struct ChunkParams {
   void* out;
   int32_t out_f32, layer, entry_bytes;
   const uint8_t* pool_layer;
-  float* part_o;      // [2 grid][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
-  float* part_ml;     // [2 grid][2][128]
-  // [3][BC_MAX_CHUNK_CTAS], zero between launches.  Sixteen pieces count themselves at the block of their first one, in row 0 where
-  // that one begins the unit and in row 1 where it continues it (a block has one of either kind at most); row 2: the sixteens of a unit.
+  float* part_o;      // [2 grid][2 groups][D / 4][128] float4: a block's partial results, slot 0 continues a unit, slot 1 begins one
+  float* part_ml;     // [2 grid][2 groups][2][128]
+  // [3][BC_MAX_CHUNK_CTAS][2 groups], zero between launches.  Sixteen pieces count themselves at the block of their first one, in row
+  // 0 where that one begins the unit and in row 1 where it continues it (a block has one of either kind at most); row 2: the
+  // sixteens of a unit.
   int32_t* tickets;
   int32_t Hq, Hkv, G, page_size;
   FastDiv by_page;
-  int32_t tokens;     // per unit: 128 / G
+  int32_t half;       // tokens of a group: 128 / G
+  int32_t tokens;     // of a unit: two groups
   int32_t R;          // entries per copy: 8, 16 or 32, or 1 (row by row)
   int32_t align;      // segment starts in the virtual row space: max(8, R)
   int32_t min_shift;  // log2 of the key tiles of a piece, at least
@@ -153,12 +160,13 @@ struct Items {
   int b0, pieces;                    // where units are cut into pieces: first block and number of pieces of this block's unit
 };
 
-// One unit: the query tile `t` of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
+// One unit: the query tile `t` (two groups) of item `i` for KV head `h`, and the key tiles [n0, n1) of its N that this block does.
 struct Unit {
   int i, h, t;
   int count, vis_last;     // tokens in the tile; entries its last token sees
   int P, nb, w, base;      // lengths of the sequence; base: entries the tile's first token sees, minus 1
   int n0, n1, N;
+  int solo;                // -1: rows for both groups; else the group that has the rows
 };
 // Entries `vis` of a sequence as intervals of the virtual row space: [0, p), [b0, b0 + b), [w0, w0 + w).
 struct Seen {
@@ -180,9 +188,9 @@ __device__ __forceinline__ int clamp_vis(int first, int r, int live) {   // entr
 __device__ __forceinline__ int key_tiles(const Items& it, int i, int t, int tokens, int align) {
   const int last = min((t + 1) * tokens, it.m[i]) - 1;
   const int vis = clamp_vis(it.first[i], last, it.P[i] + it.nb[i] + it.w[i]);
-  return max(1, (virtual_end(seen_of(vis, it.P[i], it.nb[i], it.w[i], align)) + kTile - 1) / kTile);
+  return max(1, (virtual_end(seen_of(vis, it.P[i], it.nb[i], it.w[i], align)) + kKeys - 1) / kKeys);
 }
-__device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, int n0, long long left, int tokens, int align) {
+__device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, int n0, long long left, int tokens, int align, int solo) {
   Unit u;
   u.i = i; u.h = h; u.t = t; u.n0 = n0;
   u.P = it.P[i]; u.nb = it.nb[i]; u.w = it.w[i];
@@ -192,6 +200,7 @@ __device__ __forceinline__ Unit make_unit(const Items& it, int i, int h, int t, 
   u.base = it.first[i] + t * tokens;
   u.N = key_tiles(it, i, t, tokens, align);
   u.n1 = (int)min((long long)u.N, n0 + left);
+  u.solo = 2 * u.count > tokens ? -1 : solo;
   return u;
 }
 // The unit behind u on the line (there is one: the caller knows how many key tiles are left).
@@ -204,35 +213,34 @@ __device__ __forceinline__ Unit next_unit(const Items& it, const Unit& u, long l
       do ++i; while (it.m[i] == 0);
     }
   }
-  return make_unit(it, i, h, t, 0, left, tokens, align);
+  return make_unit(it, i, h, t, 0, left, tokens, align, u.solo < 0 ? 0 : u.solo ^ 1);
 }
 
 // the tile at k0 lies in one interval entirely
 __device__ __forceinline__ bool inside(const Seen& s, int k0) {
-  return k0 + kTile <= s.p || (k0 >= s.b0 && k0 + kTile <= s.b0 + s.b) || (k0 >= s.w0 && k0 + kTile <= s.w0 + s.w);
+  return k0 + kKeys <= s.p || (k0 >= s.b0 && k0 + kKeys <= s.b0 + s.b) || (k0 >= s.w0 && k0 + kKeys <= s.w0 + s.w);
 }
-// 128-bit mask (bit j of word j / 32: column j of the tile) of the tile's columns inside [lo, hi) of the virtual space
-__device__ __forceinline__ void add_range(uint32_t (&mask)[4], int lo, int hi) {
+// 64-bit mask (bit j of word j / 32: column j of the tile) of the tile's columns inside [lo, hi) of the virtual space
+__device__ __forceinline__ void add_range(uint32_t (&mask)[2], int lo, int hi) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < 2; ++q) {
     const int l = min(max(lo - 32 * q, 0), 32), e = min(max(hi - 32 * q, 0), 32);
     if (e > l) mask[q] |= (e - l == 32 ? 0xffffffffu : ((1u << (e - l)) - 1u)) << l;
   }
 }
-__device__ __forceinline__ void tile_mask(uint32_t (&mask)[4], const Seen& s, int k0) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) mask[q] = 0;
+__device__ __forceinline__ void tile_mask(uint32_t (&mask)[2], const Seen& s, int k0) {
+  mask[0] = mask[1] = 0;
   add_range(mask, -k0, s.p - k0);
   add_range(mask, s.b0 - k0, s.b0 + s.b - k0);
   add_range(mask, s.w0 - k0, s.w0 + s.w - k0);
 }
 
-// What the control warp needs to issue a tile's copies.  Lane l holds the copies l, l + 32, ... of the tile's 128 / R.
+// What the control warp needs to issue a tile's copies.  Lane l holds the copies l, l + 32, ... of the tile's 64 / R.
 template <int KP>
 struct TileIssue {
   int page[KP], rem[KP];     // page id and first entry inside the page
   uint32_t valid[KP];        // ballots: which copies there are
-  int h, qrow;               // KV head; packed row of the unit's first token
+  int h, qrow, solo;         // KV head; packed row of the unit's first token; the unit's group
   bool fresh;                // the unit's first tile here
 };
 
@@ -250,54 +258,63 @@ __device__ __forceinline__ void tma_pool(uint32_t dst, const CUtensorMap* map, i
       : "memory");
 }
 
-// Shared memory of a block: Q, the rings of K and V (one buffer each where two blocks leave room for no more), the items.
+// Shared memory of a block: the groups' Q, the rings of K and V, the items.
 template <int D>
 struct Smem {
-  static constexpr int kStages = D == 64 ? 2 : 1;
+  static constexpr int kStages = D == 64 ? 8 : 4;
   static constexpr int kHalves = D / 64;
-  static constexpr int kHalfBytes = kTile * 128;            // 128 rows of 64 coordinates
-  static constexpr int kOperand = kHalves * kHalfBytes;
-  static constexpr int kBytes = (1 + 2 * kStages) * kOperand + 1024 + (int)sizeof(Items);
+  static constexpr int kQHalf = kTile * 128;                // 128 rows of 64 coordinates
+  static constexpr int kHalf = kKeys * 128;                 // 64 rows of 64 coordinates
+  static constexpr int kQ = kHalves * kQHalf;
+  static constexpr int kOperand = kHalves * kHalf;
+  static constexpr int kBytes = 2 * kQ + 2 * kStages * kOperand + 1024 + (int)sizeof(Items);
 };
 
 // D: head_dim.  ROWS: the page size has no power of two from 8 up: a tensor copy would hold one entry or a few, and a warp issues
 // one in some 70 cycles, so the copy warp's lanes copy the rows 16 bytes each.
 //
-// Roles: warps 0 .. 3 are the row threads, warp 4 issues the products, warp 5 the copies.
-// S of the next tile is issued right behind the product with P of the last one, whose P it overwrites: one thread issues both,
-// and they run in that order.
-// Barriers (single-phase mbarriers, parity = completions & 1):
-//   bar_kin[s], bar_vin[s]: K, V of ring buffer s have landed     bar_ke[s], bar_ve[s]: they have been read
-//   bar_q: Q of a unit has landed                                 bar_qe: it has been read
-//   bar_s: S of a tile is ready                                   bar_p: the 128 row threads have stored P
-//   bar_f: O of a unit is final                                   bar_e: the rows have read O
-//   bar_r: the row threads among themselves (bounded, unlike a block barrier)
+// Roles: warps 0 .. 3 are group 0's row threads, warps 4 .. 7 group 1's, warps 8 and 9 issue the products of the two groups,
+// warp 10 the copies of Q and K, warp 11 those of V.
+// S of a group's tile t + 2 is issued right behind the product with P of its tile t, whose place it takes: one thread issues
+// both, and they run in that order.
+// Barriers (single-phase mbarriers, parity = completions & 1), [g] per group, t counting the group's own tiles:
+//   bar_kin[s], bar_vin[s]: K, V of ring buffer s have landed     bar_ke[s], bar_ve[s]: both groups are done with them
+//     Both product warps wait for every K and V, also for what only the other group multiplies with, and then say so: a parity
+//     tells two completions apart and no more, so no waiter may fall behind or skip one.
+//   bar_q[g]: Q of the group's unit has landed                    bar_qe[g]: it has been read
+//   bar_s[g][t & 1]: S of tile t is ready                         bar_p[g][t & 1]: the 128 row threads have stored its P
+//   bar_o[g][t & 1]: the product with P of tile t is done         bar_f[g]: O of the unit is final
+//   bar_e[g]: the rows have read O                                bar_r[g]: the row threads among themselves (bounded, unlike
+//                                                                 a block barrier)
 template <int D, bool ROWS, bool SHORTW>
-__global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
+__global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a, const __grid_constant__ CUtensorMap q_map,
                                                            const __grid_constant__ CUtensorMap pool_map) {
-  constexpr int KP = ROWS ? 4 : 1;                          // copies per lane, tensor and tile
-  constexpr int kHalves = Smem<D>::kHalves, kHalfBytes = Smem<D>::kHalfBytes, kOperand = Smem<D>::kOperand, kStages = Smem<D>::kStages;
+  constexpr int KP = ROWS ? 2 : 1;                          // copies per lane, tensor and tile
+  constexpr int kHalves = Smem<D>::kHalves, kHalf = Smem<D>::kHalf, kQ = Smem<D>::kQ, kQHalf = Smem<D>::kQHalf, kOperand = Smem<D>::kOperand, kStages = Smem<D>::kStages;
+  constexpr uint32_t kIdescQK = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kKeys >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
   constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sQ = smem_addr(smem), sK = sQ + kOperand, sV = sK + kStages * kOperand;
-  Items& it = *reinterpret_cast<Items*>(smem + (1 + 2 * kStages) * kOperand);
-  __shared__ __align__(8) uint64_t s_bars[4 * kStages + 8];
+  const uint32_t sQ = smem_addr(smem), sK = sQ + 2 * kQ, sV = sK + kStages * kOperand;
+  Items& it = *reinterpret_cast<Items*>(smem + 2 * kQ + 2 * kStages * kOperand);
+  __shared__ __align__(8) uint64_t s_bars[4 * kStages + 24];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_fail_word, s_ticket;
+  __shared__ int s_fail_word, s_ticket[2];
   volatile int* s_fail = &s_fail_word;
   const uint32_t bars = smem_addr(s_bars);
   const uint32_t bar_kin = bars, bar_vin = bars + 8 * kStages, bar_ke = bars + 16 * kStages, bar_ve = bars + 24 * kStages, bar_q = bars + 32 * kStages,
-                 bar_qe = bar_q + 8, bar_s = bar_q + 16, bar_p = bar_q + 24, bar_f = bar_q + 32, bar_e = bar_q + 40, bar_r = bar_q + 48, bar_d = bar_q + 56;
+                 bar_qe = bar_q + 16, bar_s = bar_q + 32, bar_o = bar_q + 64, bar_f = bar_q + 96, bar_d = bar_q + 112, bar_p = bar_q + 128,
+                 bar_e = bar_q + 160, bar_r = bar_q + 176;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = a.G, Hq = a.Hq, Hkv = a.Hkv, tokens = a.tokens, align = a.align;
+  const int G = a.G, Hq = a.Hq, Hkv = a.Hkv, half = a.half, tokens = a.tokens, align = a.align;
 
   if (tid == 0) {
     auto init = [&](uint32_t bar, int count, uint32_t arrivals) {
       for (int i = 0; i < count; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + i * 8), "r"(arrivals) : "memory");
     };
-    init(bar_kin, 4 * kStages + 3, 1);                      // kin, vin, ke, ve, q, qe, s
-    init(bar_p, 1, kRowThreads); init(bar_f, 1, 1); init(bar_e, 2, kRowThreads); init(bar_d, 1, 1);   // e and r
+    init(bar_kin, 2 * kStages, 1); init(bar_ke, 2 * kStages, 2);
+    init(bar_q, 16, 1);                                     // q, qe (two each), s, o (four each), f, d (two each)
+    init(bar_p, 8, kGroup);                                 // p (four), e, r (two each)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
   }
@@ -438,24 +455,29 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(kTmemColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // Rows of the Q buffer that no tensor copy writes (only when G does not divide 128) stay zero.
-  const int box_rows = tokens * G;
-  for (int idx = tid; idx < (kTile - box_rows) * (D / 8); idx += kThreads) st_zero16(sQ + swz(box_rows + idx / (D / 8), idx % (D / 8)));
+  // Rows of the Q buffers that no tensor copy writes (only when G does not divide 128) stay zero.
+  const int box_rows = half * G;
+  for (int idx = tid; idx < 2 * (kTile - box_rows) * (D / 8); idx += kThreads) {
+    const int r = idx / (D / 8), g = r >= kTile - box_rows ? 1 : 0;
+    st_zero16(sQ + g * kQ + swz(box_rows + r - g * (kTile - box_rows), idx % (D / 8)));
+  }
   proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  const uint32_t tS = tmem, tO = tmem + kTile;              // columns [0, 128): S, then P in its first 64; [128, 128 + D): O
-  const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align);
+  // columns: S (then P, in its first 32) of the groups at 0 and 64, 128 and 192, O at 256 and 256 + D
+  const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align, 0);
 
   auto wait_all = [&](uint32_t bar, uint32_t parity) {       // every lane polls, a vote joins the answers
     const bool ok1 = mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit);
     return (bool)__all_sync(0xffffffffu, ok1);
   };
-  if (warp == kRowThreads / 32 + 1) {
-    // ========================================= copy warp ============================================
-    const int R = a.R, copies = kTile / R;
+  if (warp > 2 * kGroup / 32 + 1) {
+    // ======================================== copy warps ============================================
+    // The first one copies Q and the K tiles, the second one the V tiles.
+    const int which = warp - 2 * kGroup / 32 - 2;
+    const int R = a.R, copies = kKeys / R;
     // cursor of the look-ahead: the tile whose copies are worked out next
     Unit lu = u0;
     int ln = u0.n0;
@@ -476,12 +498,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         }
         lseen = seen_of(lu.vis_last, lu.P, lu.nb, lu.w, align);
         ti.qrow = a.cu_q[lu.i] + lu.t * tokens;
+        ti.solo = lu.solo;
         fresh = false;
       }
       ti.h = lu.h;
 #pragma unroll
       for (int c = 0; c < KP; ++c) {
-        const int p = lane + 32 * c, v = ln * kTile + p * R;   // first virtual row of the copy
+        const int p = lane + 32 * c, v = ln * kKeys + p * R;   // first virtual row of the copy
         int pos = -1, col = 0;
         if (p < copies) {
           if (v < lseen.p) pos = v;
@@ -506,13 +529,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
       }
       return ti;
     };
-    auto issue = [&](const TileIssue<KP>& ti, int which, int slot) {   // K (0) or V (1) of a tile into ring buffer `slot`
-      const uint32_t dst = (which ? sV : sK) + slot * kOperand, bar = (which ? bar_vin : bar_kin) + slot * 8;
+    const uint32_t ring = which ? sV : sK, bar_in = which ? bar_vin : bar_kin, bar_read = which ? bar_ve : bar_ke;
+    auto issue = [&](const TileIssue<KP>& ti, int slot) {       // a tile into ring buffer `slot`
+      const uint32_t dst = ring + slot * kOperand, bar = bar_in + slot * 8;
       if constexpr (ROWS) {
         constexpr int kPieces = D / 8, kRows = 32 / kPieces;     // 16-byte pieces of a row, rows per instruction
         const int piece = lane % kPieces;
         const uint8_t* src = a.pool_layer + (int64_t)(which * Hkv + ti.h) * (D * 2) + piece * 16;
-        const uint32_t at = dst + (piece >> 3) * kHalfBytes + (piece & 7) * 16;
+        const uint32_t at = dst + (piece >> 3) * kHalf + (piece & 7) * 16;
 #pragma unroll
         for (int k = 0; k < KP; ++k) {
           int page = ti.page[k];
@@ -536,35 +560,36 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
           if (a.m.debug && (unsigned)page >= (unsigned)a.m.num_pages) { debug_note(a.m, page); page = 0; }
 #pragma unroll
           for (int s = 0; s < kHalves; ++s)
-            tma_pool(dst + s * kHalfBytes + lane * R * 128, &pool_map, (which * Hkv + ti.h) * kHalves + s, page * a.page_size + ti.rem[0], a.layer, bar);
+            tma_pool(dst + s * kHalf + lane * R * 128, &pool_map, (which * Hkv + ti.h) * kHalves + s, page * a.page_size + ti.rem[0], a.layer, bar);
         }
       }
       __syncwarp();
     };
     const uint32_t T = (uint32_t)(x_end - x_begin);          // tiles of the span (far below 2^31)
-    uint32_t nk = 0, nv = 0, nq = 0;                          // copies of K and V tiles and of Q issued so far
+    uint32_t issued = 0, nq[2] = {0, 0};                      // copies of tiles and of the groups' Q issued so far
     bool ok = true;
     TileIssue<KP> ti = look();
     for (uint32_t j = 0; j < T; ++j) {
       const int slot = (int)(j % kStages);
-      const uint32_t old = (j / kStages - 1) & 1u;             // phase in which the buffer's last tile was read
-      if (ti.fresh) {                                          // the unit's Q, once the last unit's has been read
-        if (nq > 0) ok = wait_all(bar_qe, (nq - 1) & 1u);
-        if (!ok) break;
-        if (elect_one()) {
-          mbar_expect_tx(bar_q, (uint32_t)(box_rows * D * 2));
+      if (which == 0 && ti.fresh) {                            // the unit's Q, once the groups' last ones have been read
 #pragma unroll
-          for (int s = 0; s < kHalves; ++s) tma_3d(sQ + s * kHalfBytes, &q_map, s * 64, ti.h * G, ti.qrow, bar_q);
+        for (int g = 0; g < 2; ++g) {
+          if (!ok || (ti.solo >= 0 && ti.solo != g)) continue;
+          if (nq[g] > 0) ok = wait_all(bar_qe + g * 8, (nq[g] - 1) & 1u);
+          if (ok && elect_one()) {
+            mbar_expect_tx(bar_q + g * 8, (uint32_t)(box_rows * D * 2));
+#pragma unroll
+            for (int s = 0; s < kHalves; ++s)
+              tma_3d(sQ + g * kQ + s * kQHalf, &q_map, s * 64, ti.h * G, ti.qrow + (ti.solo < 0 ? g * half : 0), bar_q + g * 8);
+          }
+          __syncwarp();
+          if (ok) ++nq[g];
         }
-        __syncwarp();
-        ++nq;
+        if (!ok) break;
       }
-      if (j >= (uint32_t)kStages) ok = wait_all(bar_ke + slot * 8, old);
+      if (j >= (uint32_t)kStages) ok = wait_all(bar_read + slot * 8, (j / kStages - 1) & 1u);   // the buffer's last tile has been read
       if (!ok) break;
-      issue(ti, 0, slot); ++nk;
-      if (j >= (uint32_t)kStages) ok = wait_all(bar_ve + slot * 8, old);
-      if (!ok) break;
-      issue(ti, 1, slot); ++nv;
+      issue(ti, slot); ++issued;
       if (j + 1 < T) ti = look();                              // its page ids arrive while the warp waits for the next buffer
     }
     if (!ok) {
@@ -574,112 +599,130 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
       __syncwarp();
       if (elect_one()) {
         int never = 0;
-        if (nq > 0) mbar_wait_or_fail<false>(bar_q, (nq - 1) & 1u, &never, kWaitLimit);
-        for (uint32_t s = 0; s < (uint32_t)kStages; ++s) {
-          if (nk > s) mbar_wait_or_fail<false>(bar_kin + s * 8, ((nk - 1 - s) / kStages) & 1u, &never, kWaitLimit);
-          if (nv > s) mbar_wait_or_fail<false>(bar_vin + s * 8, ((nv - 1 - s) / kStages) & 1u, &never, kWaitLimit);
-        }
+        for (int g = 0; g < 2; ++g)
+          if (nq[g] > 0) mbar_wait_or_fail<false>(bar_q + g * 8, (nq[g] - 1) & 1u, &never, kWaitLimit);
+        for (uint32_t s = 0; s < (uint32_t)kStages; ++s)
+          if (issued > s) mbar_wait_or_fail<false>(bar_in + s * 8, ((issued - 1 - s) / kStages) & 1u, &never, kWaitLimit);
       }
     }
     __syncwarp();
-  } else if (warp == kRowThreads / 32) {
-    // ======================================== product warp ==========================================
+  } else if (warp >= 2 * kGroup / 32) {
+    // ======================================== product warps =========================================
     // All 32 lanes walk the loop and the waits together; one elected lane issues the products.
-    const uint64_t dQ = umma_desc(sQ), dK = umma_desc(sK), dV = umma_desc_nmajor(sV);
+    const int g = warp - 2 * kGroup / 32;
+    const uint64_t dQ = umma_desc(sQ + g * kQ), dK = umma_desc(sK), dV = umma_desc_nmajor(sV, kHalf);
+    const uint32_t tS = tmem + g * 2 * kKeys, tO = tmem + 4 * kKeys + g * D;
     const uint32_t T = (uint32_t)(x_end - x_begin);
     Unit u = u0;
-    uint32_t j = 0, units = 0;                                  // tiles and units so far
+    uint32_t j0 = 0, t = 0, units = 0;                          // the unit's first tile in the block's stream; tiles and units of this group so far
     bool ok = true, products = false;
-    auto qk = [&](uint32_t tile, bool last) {                   // S of the block's tile number `tile`; last: of its unit
-      const int slot = (int)(tile % kStages);
-      ok = ok && wait_all(bar_kin + slot * 8, (tile / kStages) & 1u);
-      if (!ok) return;
-      tc_fence_after();
-      if (elect_one()) {
-        const uint64_t k = dK + (uint64_t)(slot * kOperand >> 4);
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {                   // descriptor start addresses advance in 16-byte units
-          const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
-          umma(tS, dQ + off, k + off, kk > 0);
-        }
-        umma_commit(bar_s);
-        umma_commit(bar_ke + slot * 8);
-        if (last) umma_commit(bar_qe);
-      }
-      __syncwarp();
-      products = true;
-    };
-    ok = wait_all(bar_q, 0);
-    qk(0, u.n0 + 1 == u.n1);
     while (ok) {
-      const Seen seen = seen_of(u.vis_last, u.P, u.nb, u.w, align);
-      Unit next = u;
-      for (int n = u.n0; ok && n < u.n1; ++n, ++j) {
-        const int slot = (int)(j % kStages);
-        ok = wait_all(bar_vin + slot * 8, (j / kStages) & 1u);
-        if (!ok) break;
-        // V rows of the tile that hold no entry the unit can see (unwritten entries of the last page, gaps between
-        // segments, rows that no copy wrote) are cleared, since a weight of 0 does not cancel a NaN.
-        const int k0 = n * kTile;
-        if (!inside(seen, k0)) {
-          const uint32_t dst = sV + slot * kOperand;
-          auto clear = [&](int from, int to) {                  // rows of the virtual space
-            from = max(from - k0, 0); to = min(to - k0, kTile);
+      const int tiles = u.n1 - u.n0;
+      if (u.solo < 0 || u.solo == g) {
+        const Seen seen = seen_of(u.vis_last, u.P, u.nb, u.w, align);
+        auto qk = [&](int d) {                                  // S of the unit's tile d, the group's tile t + d
+          const uint32_t j = j0 + (uint32_t)d, place = (t + (uint32_t)d) & 1u;
+          const int slot = (int)(j % kStages);
+          ok = ok && wait_all(bar_kin + slot * 8, (j / kStages) & 1u);
+          if (!ok) return;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t k = dK + (uint64_t)(slot * kOperand >> 4);
 #pragma unroll
-            for (int s = 0; s < kHalves; ++s)
+            for (int kk = 0; kk < D / 16; ++kk)                 // descriptor start addresses advance in 16-byte units
+              umma<kIdescQK>(tS + place * kKeys, dQ + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
+                             k + (uint64_t)(((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kk > 0);
+            umma_commit(bar_s + g * 16 + place * 8);
+            umma_commit(bar_ke + slot * 8);
+            if (d + 1 == tiles) umma_commit(bar_qe + g * 8);
+          }
+          __syncwarp();
+          products = true;
+        };
+        ok = wait_all(bar_q + g * 8, units & 1u);
+        qk(0);
+        if (tiles > 1) qk(1);
+        for (int d = 0; ok && d < tiles; ++d) {
+          const uint32_t j = j0 + (uint32_t)d, at = t + (uint32_t)d, place = at & 1u;
+          const int slot = (int)(j % kStages);
+          ok = wait_all(bar_vin + slot * 8, (j / kStages) & 1u);
+          if (!ok) break;
+          // V rows of the tile that hold no entry the unit can see (unwritten entries of the last page, gaps between
+          // segments, rows that no copy wrote) are cleared, since a weight of 0 does not cancel a NaN.  In a unit with two groups
+          // both clear them: neither may begin before they are clear, and zeros over zeros change nothing.
+          const int k0 = (u.n0 + d) * kKeys;
+          if (!inside(seen, k0)) {
+            const uint32_t dst = sV + slot * kOperand;
+            auto clear = [&](int from, int to) {                // rows of the virtual space
+              from = max(from - k0, 0); to = min(to - k0, kKeys);
+#pragma unroll
+              for (int s = 0; s < kHalves; ++s)
 #pragma unroll 4
-              for (int at = from * 128 + lane * 16; at < to * 128; at += 512) st_zero16(dst + s * kHalfBytes + at);
-          };
-          clear(seen.p, seen.b > 0 ? seen.b0 : (seen.w > 0 ? seen.w0 : k0 + kTile));
-          if (seen.b > 0) clear(seen.b0 + seen.b, seen.w > 0 ? seen.w0 : k0 + kTile);
-          if (seen.w > 0) clear(seen.w0 + seen.w, k0 + kTile);
-          proxy_fence();   // the product reads shared memory through the asynchronous proxy
+                for (int b = from * 128 + lane * 16; b < to * 128; b += 512) st_zero16(dst + s * kHalf + b);
+            };
+            clear(seen.p, seen.b > 0 ? seen.b0 : (seen.w > 0 ? seen.w0 : k0 + kKeys));
+            if (seen.b > 0) clear(seen.b0 + seen.b, seen.w > 0 ? seen.w0 : k0 + kKeys);
+            if (seen.w > 0) clear(seen.w0 + seen.w, k0 + kKeys);
+            proxy_fence();   // the product reads shared memory through the asynchronous proxy
+            __syncwarp();
+          }
+          if (d == 0 && units > 0) ok = wait_all(bar_e + g * 8, (units - 1) & 1u);   // the rows have read the last unit's O
+          ok = ok && wait_all(bar_p + g * 16 + place * 8, (at >> 1) & 1u);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t v = dV + (uint64_t)(slot * kOperand >> 4);
+#pragma unroll
+            for (int kk = 0; kk < kKeys / 16; ++kk)             // 16 keys at a time
+              umma_ts<kIdescPV>(tO, tS + place * kKeys + (uint32_t)(kk * 8), v + (uint64_t)((kk * 16 * 128) >> 4), (d > 0 || kk > 0) ? 1u : 0u);
+            umma_commit(bar_o + g * 16 + place * 8);
+            umma_commit(bar_ve + slot * 8);
+            if (d + 1 == tiles) umma_commit(bar_f + g * 8);     // the last one: the block leaves behind it
+          }
+          __syncwarp();
+          if (d + 2 < tiles) qk(d + 2);
+        }
+        t += (uint32_t)tiles;
+        ++units;
+      } else {                                                  // the other group's unit
+        for (int d = 0; ok && d < tiles; ++d) {
+          const uint32_t j = j0 + (uint32_t)d, slot = j % kStages, parity = (j / kStages) & 1u;
+          ok = wait_all(bar_kin + slot * 8, parity);
+          if (ok && elect_one()) mbar_arrive_cta(bar_ke + slot * 8);
+          __syncwarp();
+          ok = ok && wait_all(bar_vin + slot * 8, parity);
+          if (ok && elect_one()) mbar_arrive_cta(bar_ve + slot * 8);
           __syncwarp();
         }
-        const bool ends = n + 1 == u.n1, more = j + 1 < T;
-        if (ends && more) next = next_unit(it, u, x_end - (x_begin + j + 1), Hkv, tokens, align);
-        if (n == u.n0 && units > 0) ok = wait_all(bar_e, (units - 1) & 1u);   // the rows have read the last unit's O
-        ok = ok && wait_all(bar_p, j & 1u);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t v = dV + (uint64_t)(slot * kOperand >> 4);
-#pragma unroll
-          for (int kk = 0; kk < kTile / 16; ++kk)               // 16 keys at a time
-            umma_ts<kIdescPV>(tO, tS + (uint32_t)(kk * 8), v + (uint64_t)((kk * 16 * 128) >> 4), (n > u.n0 || kk > 0) ? 1u : 0u);
-          if (ends) umma_commit(bar_f);
-          umma_commit(bar_ve + slot * 8);
-        }
-        __syncwarp();
-        if (more) {
-          if (ends) ok = wait_all(bar_q, (units + 1) & 1u);
-          qk(j + 1, ends ? next.n0 + 1 == next.n1 : n + 2 == u.n1);
-        }
       }
-      if (!ok || j >= T) break;
-      u = next;
-      ++units;
+      j0 += (uint32_t)tiles;
+      if (!ok || j0 >= T) break;
+      u = next_unit(it, u, x_end - (x_begin + j0), Hkv, tokens, align);
     }
     if (!ok) {   // giving up: every product issued so far ends before the block leaves (one more commit arrives when all have)
       *s_fail = 1;
       __syncwarp();
       if (elect_one() && products) {
         int never = 0;
-        umma_commit(bar_d);
-        mbar_wait_or_fail<false>(bar_d, 0, &never, kWaitLimit);
+        umma_commit(bar_d + g * 8);
+        mbar_wait_or_fail<false>(bar_d + g * 8, 0, &never, kWaitLimit);
       }
     }
     __syncwarp();
   } else {
     // ========================================= row threads ==========================================
-    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
-    const int my_local = tid / G, my_head = tid % G;
+    const int grp = warp >> 2, row = tid & (kGroup - 1);      // group, row inside it
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tmem + grp * 2 * kKeys + lane_base, tO = tmem + 4 * kKeys + grp * D + lane_base;
+    const uint32_t my_s = bar_s + grp * 16, my_p = bar_p + grp * 16, my_o = bar_o + grp * 16, my_f = bar_f + grp * 8, my_e = bar_e + grp * 8,
+                   my_r = bar_r + grp * 8;
+    const int my_local = row / G, my_head = row % G;
     constexpr float kMaxSlack = 8.f;                          // as in bc_mask_attn.cu
     bool failed = false;
     uint32_t t = 0, e = 0, ph_r = 0;
     auto rows_sync = [&]() {
-      mbar_arrive_cta(bar_r);
-      const bool ok = mbar_wait_or_fail<SHORTW>(bar_r, ph_r, s_fail, a.wait_limit);
+      mbar_arrive_cta(my_r);
+      const bool ok = mbar_wait_or_fail<SHORTW>(my_r, ph_r, s_fail, a.wait_limit);
       ph_r ^= 1;
       return (bool)__all_sync(0xffffffffu, ok);
     };
@@ -700,35 +743,40 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
     };
     long long x = x_begin;
     Unit u = u0;
-    for (;; ++e) {
-      const int rows = u.count * G;
-      const bool row_valid = tid < rows;
-      const bool warp_live = warp * 32 < rows;                // a warp without a row only keeps the barriers' count
-      const int vis = row_valid ? clamp_vis(u.base, my_local, u.P + u.nb + u.w) : 0;
+    for (;;) {
+      // this group's rows of the unit (none of the other group's solo units)
+      const int mine = u.solo < 0 ? min(u.count - grp * half, half) : (u.solo == grp ? u.count : 0);
+      const int token0 = u.solo < 0 ? grp * half : 0;
+      if (mine > 0) {
+      const int rows = mine * G;
+      const bool row_valid = row < rows;
+      const bool warp_live = (warp & 3) * 32 < rows;          // a warp without a row only keeps the barriers' count
+      const int vis = row_valid ? clamp_vis(u.base, token0 + my_local, u.P + u.nb + u.w) : 0;
       const Seen seen = seen_of(vis, u.P, u.nb, u.w, align);
-      const int row0 = a.cu_q[u.i] + u.t * tokens;            // packed row of the unit's first token
+      const int row0 = a.cu_q[u.i] + u.t * tokens + token0;   // packed row of the group's first token
       float m_ref = -INFINITY, l_run = 0.f;
       for (int n = u.n0; n < u.n1; ++n, ++t) {
-        const bool ok = mbar_wait_or_fail<SHORTW>(bar_s, t & 1u, s_fail, a.wait_limit);
+        const bool ok = mbar_wait_or_fail<SHORTW>(my_s + (t & 1u) * 8, (t >> 1) & 1u, s_fail, a.wait_limit);
         if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
         if (warp_live) {
           tc_fence_after();
-          const int k0 = n * kTile;
+          const int k0 = n * kKeys;
+          const uint32_t tMine = tS + (t & 1u) * kKeys;
           const bool all_visible = __all_sync(0xffffffffu, !row_valid || inside(seen, k0));
-          float s[kTile];
-#pragma unroll
-          for (int cb = 0; cb < 4; ++cb) tmem_ld32_async(tS + lane_base + cb * 32, s + cb * 32);
+          float s[kKeys];
+          tmem_ld32_async(tMine, s);
+          tmem_ld32_async(tMine + 32, s + 32);
           tmem_wait_ld();
           if (!all_visible) {
-            uint32_t mask[4];
+            uint32_t mask[2];
             tile_mask(mask, seen, k0);
 #pragma unroll
-            for (int j = 0; j < kTile; ++j)
+            for (int j = 0; j < kKeys; ++j)
               if (!(mask[j >> 5] >> (j & 31) & 1)) s[j] = -INFINITY;
           }
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < kTile; j += 8) {
+          for (int j = 0; j < kKeys; j += 8) {
             mx[0] = max3(mx[0], s[j], s[j + 1]); mx[1] = max3(mx[1], s[j + 2], s[j + 3]);
             mx[2] = max3(mx[2], s[j + 4], s[j + 5]); mx[3] = max3(mx[3], s[j + 6], s[j + 7]);
           }
@@ -743,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
           const float m_safe = m_ref == -INFINITY ? 0.f : m_ref;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int cb = 0; cb < 4; ++cb) {
+          for (int cb = 0; cb < 2; ++cb) {
             uint32_t pk[16];
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
@@ -753,45 +801,50 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
               const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: 2^-9 per weight
               pk[j >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
             }
-            tmem_st16(tS + lane_base + cb * 16, pk);
+            tmem_st16(tMine + cb * 16, pk);
           }
           l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          // the rows whose reference has moved are rescaled (S of this tile exists, so every product into O before it is done)
+          // The rows whose reference has moved are rescaled, once the product of the tile before is done.  (Its barrier's completion
+          // before that one, of tile t - 3, lies a tile back: S of tile t - 1 was issued behind that product.  So the parity tells.)
           if (n > u.n0 && __any_sync(0xffffffffu, raise)) {
+            const bool done = mbar_wait_or_fail<SHORTW>(my_o + ((t - 1) & 1u) * 8, ((t - 1) >> 1) & 1u, s_fail, a.wait_limit);
+            if (!__all_sync(0xffffffffu, done)) { failed = true; break; }
+            tc_fence_after();
 #pragma unroll 1
             for (int cb = 0; cb < D / 32; ++cb) {
               float v[32];
-              tmem_ld32_async(tO + lane_base + cb * 32, v);
+              tmem_ld32_async(tO + cb * 32, v);
               tmem_wait_ld();
 #pragma unroll
               for (int j = 0; j < 32; ++j) v[j] *= alpha;
-              tmem_st32(tO + lane_base + cb * 32, v);
+              tmem_st32(tO + cb * 32, v);
             }
           }
           tmem_wait_st();
           tc_fence_before();
         }
-        mbar_arrive_cta(bar_p);
+        mbar_arrive_cta(my_p + (t & 1u) * 8);
       }
       if (failed) break;
 
       // ---- the piece's result -----------------------------------------------------------------------------------------
       const bool complete = u.n0 == 0 && u.n1 == u.N;
-      auto po_of = [&](int64_t slot) { return reinterpret_cast<float4*>(a.part_o) + slot * (D / 4) * kTile; };
-      auto ml_of = [&](int64_t slot) { return a.part_ml + slot * 2 * kTile; };
+      const int my_half = u.solo < 0 ? grp : 0;               // of the block's partial results
+      auto po_of = [&](int64_t slot) { return reinterpret_cast<float4*>(a.part_o) + (slot * 2 + my_half) * (D / 4) * kTile; };
+      auto ml_of = [&](int64_t slot) { return a.part_ml + (slot * 2 + my_half) * 2 * kTile; };
       if (warp_live) {
-        const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
+        const bool ok = mbar_wait_or_fail<SHORTW>(my_f, e & 1u, s_fail, a.wait_limit);
         if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
         tc_fence_after();
         const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);   // NaN stays NaN
         const int64_t at = ((int64_t)(row0 + my_local) * Hq + u.h * G + my_head) * D;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (u.n0 == 0 ? 1 : 0);
-        float4* po = po_of(slot) + tid;
+        float4* po = po_of(slot) + row;
         // 32 columns at a time, not unrolled: this runs once per unit, and its instructions come from memory the first time
 #pragma unroll 1
         for (int cb = 0; cb < D / 32; ++cb) {
           float o[32];
-          tmem_ld32_async(tO + lane_base + cb * 32, o);
+          tmem_ld32_async(tO + cb * 32, o);
           tmem_wait_ld();
           if (row_valid && complete) {
 #pragma unroll
@@ -803,19 +856,19 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
           }
         }
         tc_fence_before();
-        mbar_arrive_cta(bar_e);
+        mbar_arrive_cta(my_e);
         if (!complete) {
           if (row_valid) {
-            ml_of(slot)[tid] = m_ref;
-            ml_of(slot)[kTile + tid] = l_run;
+            ml_of(slot)[row] = m_ref;
+            ml_of(slot)[kTile + row] = l_run;
           }
           __threadfence();
         }
       } else {
         // the barrier's every completion is waited for (a parity tells two of them apart, no more)
-        const bool ok = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
+        const bool ok = mbar_wait_or_fail<SHORTW>(my_f, e & 1u, s_fail, a.wait_limit);
         if (!__all_sync(0xffffffffu, ok)) { failed = true; break; }
-        mbar_arrive_cta(bar_e);
+        mbar_arrive_cta(my_e);
       }
       if (!complete) {
         if (!rows_sync()) { failed = true; break; }
@@ -826,13 +879,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         auto slot_of = [&](int j) { return 2 * (int64_t)(b0 + j) + (j == 0 ? 1 : 0); };
         // true for the last of `count` callers
         auto last_of = [&](int32_t* ticket, int count, bool* is_last) {
-          if (tid == 0) {
+          if (row == 0) {
             const int got = atomicAdd(ticket, 1);
             if (got == count - 1) *ticket = 0;                  // all have come: zero again for the next launch
-            s_ticket = got;
+            s_ticket[grp] = got;
           }
           if (!rows_sync()) return false;
-          *is_last = s_ticket == count - 1;
+          *is_last = s_ticket[grp] == count - 1;
           if (*is_last) __threadfence();
           return true;
         };
@@ -840,7 +893,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         // Threads are spread over the rows there are and, where these are few, over the head's coordinates.
         int rows2 = 8;
         while (rows2 < rows) rows2 <<= 1;                      // 8 .. 128
-        const int r = tid & (rows2 - 1), part = tid / rows2, parts = kRowThreads / rows2;
+        const int r = row & (rows2 - 1), part = row / rows2, parts = kGroup / rows2;
         auto join = [&](int j0, int step, int count, bool final) {
           float m_all = -INFINITY, l_all = 0.f;
           if (r < rows) {
@@ -896,7 +949,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
         constexpr int kFan = 16;
         const int mine = by_unit ? (int)blockIdx.x - b0 : (int)(x / it.span) - b0;   // number of this piece
         const int group = mine / kFan, groups = (pieces + kFan - 1) / kFan, in_group = min(kFan, pieces - group * kFan);
-        int32_t* ticket = a.tickets + (group > 0 ? BC_MAX_CHUNK_CTAS : 0) + b0 + group * kFan;
+        int32_t* ticket = a.tickets + 2 * ((group > 0 ? BC_MAX_CHUNK_CTAS : 0) + b0 + group * kFan) + my_half;
         int j0 = group * kFan, step = 1, count = in_group;
         bool last = false;
 #pragma unroll 1
@@ -905,10 +958,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_chunk_attn(const ChunkParams a,
           if (failed || !last) break;
           failed = !join(j0, step, count, final);
           if (failed || final) break;
-          ticket = a.tickets + 2 * BC_MAX_CHUNK_CTAS + b0;
+          ticket = a.tickets + 2 * (2 * BC_MAX_CHUNK_CTAS + b0) + my_half;
           j0 = 0; step = kFan; count = groups;
         }
         if (failed) break;
+      }
+      ++e;
       }
       x += u.n1 - u.n0;
       if (x >= x_end) break;
@@ -943,9 +998,9 @@ int copy_height(int page_size) {
 
 }  // namespace
 
-// two pieces per block
-size_t bc_chunk_part_o_bytes(int head_dim) { return (size_t)2 * BC_MAX_CHUNK_CTAS * head_dim * kTile * 4; }
-size_t bc_chunk_part_ml_bytes() { return (size_t)2 * BC_MAX_CHUNK_CTAS * 2 * kTile * 4; }
+// two pieces per block, two groups of rows each
+size_t bc_chunk_part_o_bytes(int head_dim) { return (size_t)4 * BC_MAX_CHUNK_CTAS * head_dim * kTile * 4; }
+size_t bc_chunk_part_ml_bytes() { return (size_t)4 * BC_MAX_CHUNK_CTAS * 2 * kTile * 4; }
 
 // Tensor map of the whole pool: (64 coordinates, K|V x head x half, row, layer), unswizzled: the store's own chunk
 // permutation is the swizzle.
@@ -971,23 +1026,24 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.part_o = a.part_o; p.part_ml = a.part_ml; p.tickets = a.tickets;
   p.Hq = g.q_heads; p.Hkv = g.kv_heads; p.G = g.q_heads / g.kv_heads; p.page_size = g.page_size;
   p.by_page = make_fast_div((uint32_t)g.page_size);
-  p.tokens = kTile / p.G;
+  p.half = kTile / p.G;
+  p.tokens = 2 * p.half;
   const int height = copy_height(g.page_size);
   const bool rows = height < 8;
   p.R = rows ? 1 : height;
   p.align = p.R > 8 ? p.R : 8;
-  p.min_shift = 2;
+  p.min_shift = 3;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
   p.scale_log2 = a.sm_scale * 1.4426950408889634f;
   if (!encode_tiled()) return cudaErrorNotSupported;
   CUtensorMap q_map;
   const cuuint64_t dims[3] = {(cuuint64_t)g.head_dim, (cuuint64_t)g.q_heads, (cuuint64_t)a.total_q};
   const cuuint64_t strides[2] = {(cuuint64_t)g.head_dim * 2, (cuuint64_t)g.q_heads * g.head_dim * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.tokens}, es[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, (cuuint32_t)p.G, (cuuint32_t)p.half}, es[3] = {1, 1, 1};
   if (encode_tiled()(&q_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  const int want = a.ctas > 0 ? a.ctas : 2 * sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // two resident blocks per SM
+  const int want = a.ctas > 0 ? a.ctas : sms, grid = want < BC_MAX_CHUNK_CTAS ? want : BC_MAX_CHUNK_CTAS;   // one resident block per SM
   if (a.ctas > 0) p.min_shift = 0;   // a given number of blocks is for the cuts it makes
   if (a.wait_limit) {   // bc_set_wait_limit: head_dim 128 only
     if (g.head_dim != 128) return cudaErrorNotSupported;

@@ -12,7 +12,7 @@
 // Upper bounds the workspace is sized for.
 #define BC_MAX_ATTN_CTAS 304   // thread blocks of the decode-attention kernel
 #define BC_MAX_ATTN_BATCH 512  // sequences per bc_decode_attn call
-#define BC_MAX_CHUNK_CTAS 304  // thread blocks of the chunk-attention kernel
+#define BC_MAX_CHUNK_CTAS 160  // thread blocks of the chunk-attention kernel
 #define BC_MERGE_ELEMS 4096    // q_heads * head_dim that fits the in-block merge buffer
 // The attention plan the append bookkeeping can leave for the fused decode step: BC_PLAN_HEADER ints
 // {n, total tiles, log2(rows per tile), -}, then seven arrays of BC_MAX_ATTN_BATCH (+1 for the last) ints:
@@ -158,8 +158,8 @@ struct BcChunkArgs {
   int32_t out_f32;
   float sm_scale;
   float *part_o, *part_ml;               // bc_chunk_part_o_bytes, bc_chunk_part_ml_bytes
-  int32_t* tickets;                      // [3 BC_MAX_CHUNK_CTAS], zero between launches
-  int32_t ctas;                          // 0: two per SM
+  int32_t* tickets;                      // [6 BC_MAX_CHUNK_CTAS], zero between launches
+  int32_t ctas;                          // 0: one per SM
   uint32_t wait_limit;                   // 0: the default
 };
 size_t bc_chunk_part_o_bytes(int head_dim);

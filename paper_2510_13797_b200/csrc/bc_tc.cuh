@@ -43,10 +43,10 @@ __device__ __forceinline__ uint64_t umma_desc(uint32_t saddr) {
 // The same for an N-major B operand (V as stored: 128 keys by rows of 128 bytes = 64 head dimensions,
 // the other 64 dimensions 16 KB further): 8-key groups 1024 bytes apart along K, the two 64-wide
 // halves of N kLeadBytes apart.
-__device__ __forceinline__ uint64_t umma_desc_nmajor(uint32_t saddr) {
+__device__ __forceinline__ uint64_t umma_desc_nmajor(uint32_t saddr, int half_bytes = kTile * 128) {
   uint64_t d = 0;
   d |= (uint64_t)((saddr & 0x3ffff) >> 4);
-  d |= (uint64_t)((kTile * 128) >> 4) << 16;  // leading byte offset: next 64 elements of N
+  d |= (uint64_t)(half_bytes >> 4) << 16;     // leading byte offset: next 64 elements of N
   d |= (uint64_t)(1024 >> 4) << 32;           // stride byte offset: next 8 keys
   d |= (uint64_t)1 << 46;
   d |= (uint64_t)2 << 61;
@@ -56,11 +56,12 @@ __device__ __forceinline__ uint64_t umma_desc_nmajor(uint32_t saddr) {
 constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTile >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 
 constexpr uint32_t kIdescBN = kIdesc | (1u << 16);   // B operand N-major
+template <uint32_t IDESC = kIdesc>
 __device__ __forceinline__ void umma(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "l"(a), "l"(b), "r"(kIdesc), "r"(accumulate)
+      "l"(a), "l"(b), "r"(IDESC), "r"(accumulate)
       : "memory");
 }
 __device__ __forceinline__ void umma_commit(uint32_t bar) {
