@@ -470,6 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
   const Unit u0 = make_unit(it, it.item0, it.head0, it.tile0, it.n0, x_end - x_begin, tokens, align, 0);
 
   auto wait_all = [&](uint32_t bar, uint32_t parity) {       // every lane polls, a vote joins the answers
+    if (!SHORTW && __all_sync(0xffffffffu, mbar_try(bar, parity))) return true;   // mostly so: without the loop's counts and exits
     const bool ok1 = mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit);
     return (bool)__all_sync(0xffffffffu, ok1);
   };
@@ -620,32 +621,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       const int tiles = u.n1 - u.n0;
       if (u.solo < 0 || u.solo == g) {
         const Seen seen = seen_of(u.vis_last, u.P, u.nb, u.w, align);
-        auto qk = [&](int d) {                                  // S of the unit's tile d, the group's tile t + d
-          const uint32_t j = j0 + (uint32_t)d, place = (t + (uint32_t)d) & 1u;
-          const int slot = (int)(j % kStages);
-          ok = ok && wait_all(bar_kin + slot * 8, (j / kStages) & 1u);
-          if (!ok) return;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint64_t k = dK + (uint64_t)(slot * kOperand >> 4);
+        auto k_in = [&](int d) { const uint32_t j = j0 + (uint32_t)d; return wait_all(bar_kin + (j % kStages) * 8, (j / kStages) & 1u); };
+        auto qk = [&](int d) {                                  // one lane: S of the unit's tile d, the group's tile t + d
+          const uint32_t place = (t + (uint32_t)d) & 1u, slot = (j0 + (uint32_t)d) % kStages;
+          const uint64_t k = dK + (uint64_t)(slot * kOperand >> 4);
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)                 // descriptor start addresses advance in 16-byte units
-              umma<kIdescQK>(tS + place * kKeys, dQ + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
-                             k + (uint64_t)(((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kk > 0);
-            umma_commit(bar_s + g * 16 + place * 8);
-            umma_commit(bar_ke + slot * 8);
-            if (d + 1 == tiles) umma_commit(bar_qe + g * 8);
-          }
-          __syncwarp();
-          products = true;
+          for (int kk = 0; kk < D / 16; ++kk)                   // descriptor start addresses advance in 16-byte units
+            umma<kIdescQK>(tS + place * kKeys, dQ + (uint64_t)(((kk >> 2) * kQHalf + (kk & 3) * 32) >> 4),
+                           k + (uint64_t)(((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), kk > 0);
+          umma_commit(bar_s + g * 16 + place * 8);
+          umma_commit(bar_ke + slot * 8);
+          if (d + 1 == tiles) umma_commit(bar_qe + g * 8);
         };
         ok = wait_all(bar_q + g * 8, units & 1u);
-        qk(0);
-        if (tiles > 1) qk(1);
+#pragma unroll 1
+        for (int d = 0; ok && d < min(tiles, 2); ++d) {
+          ok = k_in(d);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) qk(d);
+          __syncwarp();
+          products = true;
+        }
         for (int d = 0; ok && d < tiles; ++d) {
           const uint32_t j = j0 + (uint32_t)d, at = t + (uint32_t)d, place = at & 1u;
           const int slot = (int)(j % kStages);
+          // all that the two products need but P, so that they follow P without another wait
           ok = wait_all(bar_vin + slot * 8, (j / kStages) & 1u);
+          if (d + 2 < tiles) ok = ok && k_in(d + 2);
           if (!ok) break;
           // V rows of the tile that hold no entry the unit can see (unwritten entries of the last page, gaps between
           // segments, rows that no copy wrote) are cleared, since a weight of 0 does not cancel a NaN.  In a unit with two groups
@@ -678,9 +681,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
             umma_commit(bar_o + g * 16 + place * 8);
             umma_commit(bar_ve + slot * 8);
             if (d + 1 == tiles) umma_commit(bar_f + g * 8);     // the last one: the block leaves behind it
+            if (d + 2 < tiles) qk(d + 2);
           }
           __syncwarp();
-          if (d + 2 < tiles) qk(d + 2);
         }
         t += (uint32_t)tiles;
         ++units;

@@ -137,6 +137,11 @@ __device__ __forceinline__ bool elect_one() {   // true in exactly one lane of a
 __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 // Bounded wait that also gives up as soon as another thread of the block has reported a failure.  The
 // ordinary instantiation has a compile-time limit (with a run-time limit the polling loops cost a
 // third of the kernel's throughput); the settable limit of bc_mask_attn_set_wait_limit lives in an
