@@ -37,7 +37,7 @@ typedef unsigned long long u64;
 constexpr int kCluster = 8;
 constexpr int kBins = 512;
 constexpr int kList = 512;             // elements that are ordered directly, by counting
-constexpr int kFew = 256;              // first guess at a limit: so many of the threads' maxima
+constexpr int kFew = 256;              // a top-k up to here is looked for among the threads' maxima first
 constexpr int kMaxVocab = 1 << 18;     // 2^18 weights of at most 2^45 add up in 63 bits
 constexpr int kWeightBits = 45;
 
@@ -170,6 +170,12 @@ struct Cross {                   // where a search ended
   uint32_t in;
 };
 
+struct Pick {                    // a key that a limit falls on, and what lies above it
+  Sum2 above;
+  uint32_t key;
+  int found;
+};
+
 // A histogram, or a list of candidates: one search step has one or the other.  Small, because a slice of 150,000 bf16 logits
 // leaves room for four blocks on an SM only while all of this stays below 18 KB.
 union Work {
@@ -193,9 +199,7 @@ struct Shared {
   Sum2 parts[kCluster];          // every block's
   int offset[kCluster + 1];
   Cross cross;
-  Sum2 above;
-  int found;
-  uint32_t thr;
+  Pick pick[2];
   int owner;
   u64 owner_skip, owner_ties;
 };
@@ -249,7 +253,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   for (int d = 16; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
   if (lane == 0) warp_best[warp] = best;
   for (int b = tid; b < kBins; b += THREADS) sh.work[0].h.mass[0][b] = sh.work[0].h.mass[1][b] = sh.work[0].h.mass[2][b] = sh.work[0].h.count[b] = sh.work[1].h.count[b] = 0;
-  if (tid == 0) { sh.at = 0x7fffffff; sh.n_list[0] = 0; }
+  if (tid == 0) { sh.at = 0x7fffffff; sh.n_list[0] = 0; sh.pick[0].found = sh.pick[1].found = 0; }
   __syncthreads();
   if (warp == 0) {
     best = lane < kWarps ? warp_best[lane] : -INFINITY;
@@ -400,34 +404,46 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     __syncthreads();
   };
   // Among `len` gathered candidates, with `before` above them: the key at which the running count (or mass) reaches `limit`, and
-  // what lies above that key (false if the limit is not reached).  Every candidate counts what is above itself.
+  // what lies above that key (false if the limit is not reached).  Every candidate counts what is above itself; the blocks share
+  // the candidates, kLanes threads each, and the one that finds the key tells the others.
+  int picks = 0;                                     // two at most: by count, then by mass
   auto select = [&](int which, int len, bool count, u64 limit, Sum2* before, uint32_t* key_out) {
+    constexpr int kLanes = THREADS / (kList / kCluster);
     const uint32_t* keys = sh.work[which].c.keys;
     const u64* weights = sh.work[which].c.weights;
-    if (tid == 0) sh.found = 0;
-    __syncthreads();
-    for (int at = tid; at < len; at += THREADS) {
-      const uint32_t key = keys[at];
-      Sum2 above = *before;
-      uint32_t same = 0;
+    const int at = tid / kLanes * kCluster + part;
+    const uint32_t key = at < len ? keys[at] : 0xffffffffu;
+    Sum2 above = {0, 0};
+    uint32_t same = 0;
+    if (at < len) {
 #pragma unroll 4
-      for (int j = 0; j < len; ++j) {
+      for (int j = tid % kLanes; j < len; j += kLanes) {
         const uint32_t o = keys[j];
         if (o > key) { above.mass += weights[j]; ++above.count; }
         same += o == key;
       }
-      if (val(above, count) < limit && limit <= val(above + Sum2{same * weights[at], same}, count)) {
-        sh.found = 1; sh.thr = key; sh.above = above;   // equal keys write equal values
+    }
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) {
+      above.mass += __shfl_xor_sync(0xffffffffu, above.mass, d);
+      above.count += __shfl_xor_sync(0xffffffffu, above.count, d);
+      same += __shfl_xor_sync(0xffffffffu, same, d);
+    }
+    above = above + *before;
+    if (at < len && tid % kLanes == 0 && val(above, count) < limit && limit <= val(above + Sum2{same * weights[at], same}, count)) {
+#pragma unroll
+      for (int b = 0; b < kCluster; ++b) {           // equal keys write equal values
+        Pick* to = cluster.map_shared_rank(&sh.pick[picks], b);
+        to->found = 1; to->key = key; to->above = above;
       }
     }
-    __syncthreads();
-    *before = sh.above;
-    *key_out = sh.thr;
-    const bool found = sh.found != 0;
-    __syncthreads();
-    return found;
+    cluster.sync();
+    const Pick& got = sh.pick[picks++];
+    *before = got.above;
+    *key_out = got.key;
+    return got.found != 0;
   };
-  // A small top-k: the elements no deeper than the kFew-th largest of the threads' maxima are few (unless the large ones are
+  // A small top-k: the elements no deeper than the k-th largest of the threads' maxima are few (unless the large ones are
   // neighbours) and hold the limit.  One atomic per thread instead of several per element, and no weights but theirs.
   bool open = by_count || by_mass;                    // the threshold is still to be found
   if (by_count && k <= kFew) {
@@ -435,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     cluster.sync();
     Sum2 bins[kPer], all;
     totals(1, false, bins);
-    const int last = cross(bins, Sum2{0, 0}, true, (u64)kFew, &all) ? sh.cross.bin : kBins - 1;
+    const int last = cross(bins, Sum2{0, 0}, true, (u64)k, &all) ? sh.cross.bin : kBins - 1;
     const float reach = last == kBins - 1 ? INFINITY : (float)(last + 1);
     for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
