@@ -149,11 +149,14 @@ struct Scale {
   // a double of at most 2^46, rounded to an integer, as the low 52 bits of its sum with 2^52
   static constexpr u64 kBias = 0x4330000000000000ull;
   __device__ __forceinline__ static u64 biased(double v) { return (u64)__double_as_longlong(v + 4503599627370496.0); }
-  __device__ __forceinline__ u64 weight(float x) const { return x > low ? biased(scaled(x)) - kBias : 0; }
+  // without branches, so that the evaluations of several elements overlap
+  __device__ __forceinline__ u64 weight(float x) const {
+    const u64 w = biased(scaled(x > low ? x : top)) - kBias;
+    return x > low ? w : 0;
+  }
   __device__ __forceinline__ u64 kept_weight(float x) const {   // 0 below min_p
-    if (!(x > low)) return 0;
-    const double v = scaled(x);
-    return v >= min_w ? biased(v) - kBias : 0;
+    const double v = scaled(x > low ? x : top);
+    return x > low && v >= min_w ? biased(v) - kBias : 0;
   }
   __device__ __forceinline__ float depth(float x) const { return (top - x) * bins; }   // in bins
   __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)depth(x)); }
@@ -187,6 +190,7 @@ union Work {
     uint32_t keys[kList];        // all blocks' candidates, and their weights
     u64 weights[kList];
   } c;
+  Sum2 total[kBins];             // block 0: a histogram of the whole cluster
 };
 
 struct Shared {
@@ -323,25 +327,44 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     if (count) atomicAdd(&sh.work[which].h.count[b], 1u);
     if (!mass) return;
     atomicAdd(&sh.work[which].h.mass[0][b], (uint32_t)w & 0xffffu);
-    if (w >> 16) atomicAdd(&sh.work[which].h.mass[1][b], (uint32_t)(w >> 16) & 0xffffu);
+    atomicAdd(&sh.work[which].h.mass[1][b], (uint32_t)(w >> 16) & 0xffffu);
     if (w >> 32) atomicAdd(&sh.work[which].h.mass[2][b], (uint32_t)(w >> 32));
   };
-  // Block 0 adds the cluster's histograms up, thread t its bins kPer t ... (`masses`: the masses too), and searches them for
-  // the cluster: all blocks together would read eight times as much of one another's memory.
+  // The cluster's histograms added up, for block 0, which searches them for all (all blocks together would read eight times as much
+  // of one another's memory): thread t gets its bins kPer t ...  Counts alone it reads itself.  With masses (`masses`) each
+  // block adds up an eighth of the bins, kLanes threads a bin, and hands the sums over: a barrier more, but block 0 alone
+  // takes 3 to 6 us for what the others hold.
   auto totals = [&](int which, bool masses, Sum2 (&b)[kPer]) {
+    if (!masses) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      b[i] = {0, 0};
-      if (part == 0) {
+      for (int i = 0; i < kPer; ++i) {
+        b[i] = {0, 0};
+        if (part == 0)
 #pragma unroll
-        for (int o = 0; o < kCluster; ++o) {
-          b[i].count += *cluster.map_shared_rank(&sh.work[which].h.count[kPer * tid + i], o);
-          if (masses)
-#pragma unroll
-            for (int j = 0; j < 3; ++j) b[i].mass += (u64)*cluster.map_shared_rank(&sh.work[which].h.mass[j][kPer * tid + i], o) << (16 * j);
-        }
+          for (int o = 0; o < kCluster; ++o) b[i].count += *cluster.map_shared_rank(&sh.work[which].h.count[kPer * tid + i], o);
       }
+      return;
     }
+    constexpr int kShare = kBins / kCluster, kLanes = THREADS / kShare, kEach = kCluster / kLanes;
+    const int bin = part * kShare + tid / kLanes;
+    Sum2 sum = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int o = tid % kLanes * kEach + i;
+      sum.count += *cluster.map_shared_rank(&sh.work[which].h.count[bin], o);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) sum.mass += (u64)*cluster.map_shared_rank(&sh.work[which].h.mass[j][bin], o) << (16 * j);
+    }
+#pragma unroll
+    for (int d = kLanes / 2; d > 0; d >>= 1) {
+      sum.mass += __shfl_xor_sync(0xffffffffu, sum.mass, d);
+      sum.count += __shfl_xor_sync(0xffffffffu, sum.count, d);
+    }
+    // into the other of the two, which nobody reads any more: its readers have passed a cluster barrier since
+    if (tid % kLanes == 0) *cluster.map_shared_rank(&sh.work[which ^ 1].total[bin], 0) = sum;
+    cluster.sync();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) b[i] = part == 0 ? sh.work[which ^ 1].total[kPer * tid + i] : Sum2{0, 0};
   };
   auto mass_limit = [&](u64 mass) {                  // the largest element is always kept; NaN never comes here
     const double want = ceil((double)p * (double)mass);
@@ -505,12 +528,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const float x = Raw<T>::get(v, i);
-        if (x > sc.low) {
-          const u64 w = sc.weight(x);
-          if (sc.depth(x) >= deep) rest += w;
-          else if (w) add(0, sc.bin(x), w, by_count, masses);
+      for (int i0 = 0; i0 < kVec; i0 += 4) {            // the weights of four at a time before their branches
+        u64 w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = sc.weight(Raw<T>::get(v, i0 + i));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = Raw<T>::get(v, i0 + i);
+          const bool out = sc.depth(x) >= deep;
+          rest += out ? w[i] : 0;
+          if (w[i] && !out) add(0, sc.bin(x), w[i], by_count, masses);
         }
       }
     }
@@ -622,7 +649,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   Sum2 mine = {0, 0};                                // mass above the threshold, elements at it
   const T* flat = reinterpret_cast<const T*>(slice);
   const int run_end = min(pieces, (tid + 1) * run);
-  for (int q = tid * run; q < run_end; q += 32 / kVec) {
+  if (thr == 0) {                                    // nearly all are kept
+#pragma unroll 1
+    for (int q = tid * run; q < run_end; ++q) {
+      const uint4 v = slice[q];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) mine.mass += sc.kept_weight(Raw<T>::get(v, i));
+    }
+  }
+  for (int q = tid * run; thr != 0 && q < run_end; q += 32 / kVec) {
     // 32 elements at a time: first which of them are kept, then their weights, so that a warp whose lanes keep few
     // elements evaluates few
     uint32_t above = 0;
@@ -640,7 +675,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     }
     for (; above; above &= above - 1) mine.mass += sc.kept_weight((float)flat[q * kVec + __ffs(above) - 1]);
   }
-  if (thr == 0) mine.count = 0;
   Sum2 block_all;
   const Sum2 mine_before = block_scan<THREADS>(mine, &block_all);
   if (tid == 0) sh.part = block_all;
