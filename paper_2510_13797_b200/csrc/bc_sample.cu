@@ -158,7 +158,7 @@ struct Scale {
     const double v = scaled(x > low ? x : top);
     return x > low && v >= min_w ? biased(v) - kBias : 0;
   }
-  __device__ __forceinline__ float depth(float x) const { return (top - x) * bins; }   // in bins
+  __device__ __forceinline__ float depth(float x) const { return fminf(top - x, 3e38f) * bins; }   // in bins (finite: inf * 0 is none)
   __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)depth(x)); }
   // of an element above low; the last bin has no lower end
   __device__ __forceinline__ bool in_bin(float x, int b) const {
@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       const float high = sc.top - x1 + slack, low = bin == kBins - 1 ? sc.low : sc.top - x0 - slack;
       uint32_t lo = 0, hi = Raw<T>::key(sc.top);
       if (high >= low) { lo = Raw<T>::key(fmaxf(low, sc.low)); hi = min(hi, Raw<T>::key(high)); }
-      for (; in > kList && lo != hi; ++round) {
+      for (int left = 4; in > kList && lo != hi && left > 0; ++round, --left) {   // 9 bits of the keys' 32 at a time
         const int which = round & 1;
         for (int b = tid; b < kBins; b += THREADS) sh.work[which].h.mass[0][b] = sh.work[which].h.mass[1][b] = sh.work[which].h.mass[2][b] = sh.work[which].h.count[b] = 0;
         __syncthreads();
@@ -606,7 +606,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
           const float x = Raw<T>::get(v, i);
           if (x > sc.low && sc.in_bin(x, bin)) {
             const uint32_t key = Raw<T>::key(x);
-            if (key >= lo && key <= hi && sc.weight(x)) sh.work[which].c.list[atomicAdd(&sh.n_list[which], 1)] = key;
+            if (key >= lo && key <= hi && sc.weight(x)) {
+              const int at = atomicAdd(&sh.n_list[which], 1);
+              if (at < kList) sh.work[which].c.list[at] = key;   // always so: they are `in`
+            }
           }
         }
       }
@@ -614,7 +617,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
       offsets(which);
       gather(which);
       uint32_t key = 0;
-      select(which, (int)in, count, limit, before, &key);
+      select(which, min(kList, sh.offset[kCluster]), count, limit, before, &key);
       return key;
     };
     bool cut = false;

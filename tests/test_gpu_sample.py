@@ -112,6 +112,24 @@ def test_extreme_parameters():
            k=[-2 ** 31, 2 ** 31 - 1, 0, 1] + [3000, 3001, 3002, 2] * 2)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_infinite_temperature_over_the_whole_range(dtype):
+    """Differences beyond the largest float, and a temperature that makes all of them nothing: every finite logit weighs the same."""
+    n, v = 6, 1001
+    x = _logits(13, n, v, torch.float32)
+    x = (x / x.abs().amax() * 3.3e38).to(dtype)
+    x[:, 5] = -INF
+    x[0, :] = 3e38
+    x[1, ::2] = -3e38
+    for t in (INF, 3e38):
+        for u in (0.0, 0.3, 0.9999):
+            us, ts = [u] * n, [t] * n
+            _check(x, us, t=ts)
+            _check(x, us, t=ts, k=[300] * n)
+            _check(x, us, t=ts, p=[0.6] * n)
+            _check(x, us, t=ts, k=[600] * n, p=[0.7] * n)
+
+
 def test_frequencies_of_a_stratified_uniform():
     """4096 rows of one distribution, one uniform per cell of an even grid: every token's count is its probability within one."""
     n, v = 4096, 37
