@@ -339,7 +339,8 @@ BC_API bc_status bc_norm_rope_decode_step(bc_cache* cache, int32_t layer, const 
  * first[i] = 0 and m_i = the prompt's length it is the causal attention of a stored prompt.
  * slots, first: device int32 [n]; cu_q: device int32 [n + 1], prefix sums, cu_q[0] = 0 and cu_q[n] ==
  * total_q (host; rows at or past total_q are neither read nor written); q [total_q, q_heads, head_dim]
- * bf16; out: same shape, bf16 (fp32 with BC_FLAG_OUT_F32), not overlapping q.  n <= 512, total_q <= 2^28 (else
+ * bf16; out: same shape, bf16 (fp32 with BC_FLAG_OUT_F32), not overlapping q.  n <= 512 and max_seqs (a
+ * slot may occur more than once), total_q <= 2^28 (else
  * BC_ERR_UNSUPPORTED), sm_scale > 0.  total_q == 0 does nothing.  Accumulation in fp32, softmax
  * weights rounded to bf16 before the second product.  Entries that no row of the chunk sees are never
  * used; an entry that only later rows of the same chunk see must be finite (its weight in the earlier

@@ -28,8 +28,14 @@
 //     kernel, and the call can be captured.
 //   * The copies, the products and the rows' softmax each have warps of their own, and the stream of tiles goes on across
 //     units.
-// Bounds: at many rows per key the tensor pipe, the exponentials and the waits between them, at few rows the reads of the
-// cache; a tile is 32 KB of K and V for 4.2 MFLOP.
+// Bounds: at many rows per key the tensor pipe (for 64 keys, Q K^T reads 6 KB of operands from shared memory per 16 coordinates, by the
+// sizes half as long again as it multiplies), the exponentials and the waits between them; at few rows the reads of the cache (a tile is
+// 32 KB of K and V for 4.2 MFLOP per group) and, below some 20 us, the steps from the launch to the first tile and
+// from the last one to the joined result.  Measured, 32 / 8 heads of 128, pages of 16: 4 x 2048 rows over 8192 entries 0.87 ms (1100
+// TFLOP/s, 0.66 of the measured product rate); 64 x 5 rows over 585 entries 46 us (3.3 TB/s); 64 single rows over 2000 99 us
+// (5.3 TB/s).  12 / 2 heads: one row over 100,000 entries 39 us (2.6 TB/s), 13 rows over 512 16 us.  Tried on the large chunk:
+// a quarter of the exponentials as polynomials on the ordinary pipes (0.93 ms against 0.89: the row threads' instructions
+// count more than the exponential unit).
 //
 // Entries that no row of a query tile can see are not read into a product: their scores are overwritten with -inf, and
 // V rows that are past the last visible entry of the tile are cleared in shared memory, so that whatever the
@@ -270,8 +276,9 @@ struct Smem {
   static constexpr int kBytes = 2 * kQ + 2 * kStages * kOperand + 1024 + (int)sizeof(Items);
 };
 
-// D: head_dim.  ROWS: the page size has no power of two from 8 up: a tensor copy would hold one entry or a few, and a warp issues
-// one in some 70 cycles, so the copy warp's lanes copy the rows 16 bytes each.
+// D: head_dim.  ROWS: the page size is no multiple of 4: a tensor copy would hold one entry or two, and a warp issues one in some
+// 70 cycles, so the copy warp's lanes copy the rows 16 bytes each.  2048 rows over 8192 entries, 32 / 8 heads, by rows and by tensor
+// copies: pages of 2 0.40 and 0.52 ms, of 4 0.40 and 0.33, of 8 0.40 and 0.25.
 //
 // Roles: warps 0 .. 3 are group 0's row threads, warps 4 .. 7 group 1's, warps 8 and 9 issue the products of the two groups,
 // warp 10 the copies of Q and K, warp 11 those of V.
@@ -593,18 +600,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       issue(ti, slot); ++issued;
       if (j + 1 < T) ti = look();                              // its page ids arrive while the warp waits for the next buffer
     }
-    if (!ok) {
-      // Giving up: no copy may still be on its way into this block's shared memory when the block leaves.  Wait, with the full
-      // limit, for the last copy into every buffer (tile s + kStages * j is copy j of buffer s).
-      *s_fail = 1;
-      __syncwarp();
-      if (elect_one()) {
-        int never = 0;
-        for (int g = 0; g < 2; ++g)
-          if (nq[g] > 0) mbar_wait_or_fail<false>(bar_q + g * 8, (nq[g] - 1) & 1u, &never, kWaitLimit);
-        for (uint32_t s = 0; s < (uint32_t)kStages; ++s)
-          if (issued > s) mbar_wait_or_fail<false>(bar_in + s * 8, ((issued - 1 - s) / kStages) & 1u, &never, kWaitLimit);
-      }
+    // No copy may still be on its way into this block's shared memory when the block leaves, whichever warp gives up and when.
+    // Wait, with the full limit, for the last copy into every buffer (tile s + kStages * j is copy j of buffer s).
+    if (!ok) *s_fail = 1;
+    __syncwarp();
+    if (elect_one()) {
+      int never = 0;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        if (nq[g] > 0) mbar_wait_or_fail<false>(bar_q + g * 8, (nq[g] - 1) & 1u, &never, kWaitLimit);
+#pragma unroll 1
+      for (uint32_t s = 0; s < (uint32_t)kStages; ++s)
+        if (issued > s) mbar_wait_or_fail<false>(bar_in + s * 8, ((issued - 1 - s) / kStages) & 1u, &never, kWaitLimit);
     }
     __syncwarp();
   } else if (warp >= 2 * kGroup / 32) {
@@ -702,14 +709,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
       if (!ok || j0 >= T) break;
       u = next_unit(it, u, x_end - (x_begin + j0), Hkv, tokens, align);
     }
-    if (!ok) {   // giving up: every product issued so far ends before the block leaves (one more commit arrives when all have)
-      *s_fail = 1;
-      __syncwarp();
-      if (elect_one() && products) {
-        int never = 0;
-        umma_commit(bar_d + g * 8);
-        mbar_wait_or_fail<false>(bar_d + g * 8, 0, &never, kWaitLimit);
-      }
+    // every product issued ends before the block leaves, also where the rows give up (one more commit arrives when all have)
+    if (!ok) *s_fail = 1;
+    __syncwarp();
+    if (products && elect_one()) {
+      int never = 0;
+      umma_commit(bar_d + g * 8);
+      mbar_wait_or_fail<false>(bar_d + g * 8, 0, &never, kWaitLimit);
     }
     __syncwarp();
   } else {
@@ -1032,9 +1038,11 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.half = kTile / p.G;
   p.tokens = 2 * p.half;
   const int height = copy_height(g.page_size);
-  const bool rows = height < 8;
+  const bool rows = height < 4;
   p.R = rows ? 1 : height;
   p.align = p.R > 8 ? p.R : 8;
+  // Pieces of 8 tiles at least.  4, 8, 16: 512 rows over 1024 entries, 12 / 2 heads, 31.5, 29.0, 30.5 us; 13 rows over 512 18.2, 16.0,
+  // 15.9; 64 x 5 rows over 585, 32 / 8 heads, 49.2, 47.8, 48.1.
   p.min_shift = 3;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
   p.scale_log2 = a.sm_scale * 1.4426950408889634f;

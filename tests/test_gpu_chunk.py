@@ -116,6 +116,44 @@ def test_spans_of_any_number_of_blocks(Hkv, G, D, ps, c, plens, gens, ms, ctas):
         _run(pair, slots, ms, g)
 
 
+@pytest.mark.parametrize("Hkv,G,D", [(2, 6, 128), (1, 3, 64)])
+@pytest.mark.parametrize("ps", [2, 3, 4, 8, 12, 20, 40])
+def test_page_sizes(Hkv, G, D, ps):
+    """Tensor copies of 4 to 8 entries and copies row by row, across the three segments."""
+    pair, slots, g = _cache(Hkv, G, D, ps, 3, [70, 201, 0], [3 * 30 + 2, 1, 3 * 25], seed=21)
+    _run(pair, slots, [50, 90, 25], g)
+    _run(pair, slots, [1, 2, 0], g)
+
+
+def test_one_sequence_several_times_and_units_of_one_group():
+    """Items of the same sequence, lengths that leave a second group of rows empty, full or with one token."""
+    # a group: 32 tokens, a unit: 64; a call has at most as many items as the cache has slots
+    pair, slots, g = _cache(2, 4, 128, 16, 1, [400, 90], [0, 0], seed=22, slots=[0, 40])
+    _run(pair, [0, 40, 0, 0, 40, 0], [31, 33, 32, 65, 64, 1], g, first=[100, 3, 300, 335, 26, 399])
+    _run(pair, [0] * 40, [1, 34] * 20, g, first=[9 * i for i in range(40)])
+
+
+def test_two_caches_on_two_streams_at_once():
+    caches = [_cache(2, 6, 128, 16, 1, [700, 40], [0, 0], seed=23), _cache(1, 4, 64, 16, 4, [300], [4 * 50 + 3], seed=24)]
+    calls = []
+    for pair, slots, g in caches:
+        n = 130 if len(slots) == 2 else 3
+        ms = [n, 20][:len(slots)]
+        q = randn_bf16(g, (sum(ms), pair.Hq, pair.D), DEV)
+        alone, out = torch.empty_like(q), torch.empty_like(q)
+        args = (0, _i32(slots), _cu(ms), sum(ms), q)
+        pair.gpu.bc_chunk_attn(*args, alone, 0.1)
+        calls.append((pair, args, alone, out, torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for pair, args, _, out, s in calls:
+            pair.gpu.bc_chunk_attn(*args, out, 0.1, stream=s)
+    torch.cuda.synchronize()
+    for pair, _, alone, out, _ in calls:
+        assert torch.equal(alone, out)
+        assert pair.gpu.bc_poll_error()[0] == 0
+
+
 @pytest.mark.parametrize("ctas", [0, 64, 304])
 def test_one_long_cache_between_many_short_ones(ctas):
     """Spans much shorter than the longest unit: a unit in many more pieces than are joined at once, between units that are not cut."""
