@@ -15,6 +15,10 @@
 // itself, D / 64 per lane: the position times the frequency in turns, reduced to a fraction of a turn in double
 // precision (pos * theta^(-2j/D) reaches 10^5 radians, where single precision has lost the angle), then the sine and
 // cosine of that fraction in fp32.
+//
+// Measured (32 / 8 heads of 128, bf16): 16384 rows 66 us, 6.1 TB/s of the 403 MB moved (0.93 of a copy); the gradient with
+// the weights' of 8192 rows 61 us, 4.6 TB/s (its sums over rows and the second launch, which adds the blocks' sums up, are what
+// a copy does not have); 64 rows of 12 / 2 heads 2.6 us, a launch.
 #include "bc_common.cuh"
 
 namespace {

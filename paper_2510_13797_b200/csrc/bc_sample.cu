@@ -16,14 +16,22 @@
 // gets eight SMs).  Each block copies its slice of the row into shared memory, the only time the row is read from
 // memory, and everything after works on the slices, joined through distributed shared memory:
 //   1. maximum of the row (and its lowest index: the greedy answer);
-//   2. with top-k or top-p: the threshold key, by a histogram of counts and masses over 512 bins of (m - x) / T, 1/11
-//      octave wide (logits spread over many of them, so the atomics rarely collide), then, inside the bin in which
-//      the limit is crossed, by histograms over the keys' own bits until the bin holds one key; elements that equal
-//      the threshold are kept lowest index first, as many as the limit needs;
+//   2. with top-k or top-p: the threshold key.  For a top-k of up to 256: the k-th largest of the threads' maxima bounds it
+//      from below, the elements from there on (a few more than k) are gathered, and each counts what lies above it.
+//      Otherwise: a histogram of counts and masses over 512 bins of (m - x) / T, 1/11 octave wide (logits spread over many
+//      of them, so the atomics rarely collide), then, inside the bin in which the limit is crossed, histograms over the keys'
+//      own bits until the bin holds one key or its elements are few enough for the list.  Elements that equal the
+//      threshold are kept lowest index first, as many as the limit needs;
 //   3. the kept mass of every thread's run of elements, a prefix sum over threads and blocks, and the element in
 //      which u * mass falls.
-// Bound by the latency of these steps (two cluster barriers without top-k and top-p, about four more with one of them),
-// not by the 300 KB a row has.
+//
+// Measured (T = 0.7; 64 rows of 151,936 bf16 = 19 MB, 3 us at the copy rate): greedy 10 us, temperature alone 24, top-k 50 22,
+// top-k 50 and top-p 0.95 24, top-p 0.95 61; one row: 5, 10, 13, 14, 27 us.  Bounds: for one row the steps' latency (two cluster
+// barriers for temperature alone, five with top-k, seven with top-p, about 1 us each with what is read behind them); for many rows
+// the double-precision weights of all elements (13 us of the 24) and, with top-p alone, three shared-memory atomics for
+// each element of the first 22 octaves (about 25 us of the 61).  Tried for these: weights in single precision from 24
+// octaves on (the branch costs more than the arithmetic: 87 us); a histogram of counts alone and masses of the few bins that they leave
+// open (96 us, for the same reason).
 #include <cooperative_groups.h>
 
 #include "bc_common.cuh"
@@ -754,8 +762,10 @@ extern "C" bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t r
   if ((words & 3) || (reinterpret_cast<uintptr_t>(out) & 7) || (reinterpret_cast<uintptr_t>(logits) & (logits_f32 ? 3 : 1)))
     return BC_ERR_INVALID_ARG;
   if (vocab > kMaxVocab || n > 0x7fffffff / kCluster) return BC_ERR_UNSUPPORTED;
-  // 512 threads where only two blocks fit an SM in any case: few rows, or slices too large for four.
-  const bool wide = n * kCluster <= 2 * 148 || (int64_t)vocab * (logits_f32 ? 4 : 2) > (int64_t)kCluster * 38 * 1024;
+  // 512 threads where a block has an SM to itself: few rows (8 of 151,936 bf16, top-p: 30 us, with 256 threads 35; 32 rows: 43
+  // and 41), or slices of more than 95 KB (64 rows of 200,000 fp32, top-p: 172 and 213 us; of 151,936: 91 and 90, temperature
+  // alone 38 and 30).
+  const bool wide = n * kCluster <= 148 || (int64_t)vocab * (logits_f32 ? 4 : 2) > (int64_t)kCluster * 95 * 1024;
   const auto f = wide ? (logits_f32 ? launch<float, 512> : launch<__nv_bfloat16, 512>)
                                          : (logits_f32 ? launch<float, 256> : launch<__nv_bfloat16, 256>);
   const cudaError_t e = f(logits, row_stride, n, vocab, temperature, top_k, top_p, min_p, uniform, out, (cudaStream_t)stream);
