@@ -356,7 +356,8 @@ BC_API bc_status bc_chunk_attn(bc_cache* cache, int32_t layer, const int32_t* sl
 /* A chunk of every prompt: stores the K/V rows of item i at prompt positions first[i] .. first[i] + m_i - 1
  * (bc_prefill for part of a prompt; positions at or past the length the sequence was opened with, and items
  * whose slot is not open, are not stored), then bc_chunk_attn with the same `first`.  A prompt of any
- * length is processed by successive calls, per layer, chunks in ascending order.  k, v [total, kv_heads,
+ * length is processed by successive calls, per layer, chunks in ascending order.  No position of a sequence
+ * may be given twice in one call (which row is kept is not defined then).  k, v [total, kv_heads,
  * head_dim] bf16 packed like q; first must not be NULL.  Two launches. */
 BC_API bc_status bc_prefill_chunk(bc_cache* cache, int32_t layer, const int32_t* slots, const int32_t* first,
                                   const int32_t* cu_chunk, int32_t n, int32_t total, const void* q, const void* k,
