@@ -28,16 +28,16 @@
 //     kernel, and the call can be captured.
 //   * The copies, the products and the rows' softmax each have warps of their own, and the stream of tiles goes on across
 //     units.
-// Bounds.  At many rows per key: the product warps' round of waits and issues, 1.1 us per pair of tiles, of which the tensor pipe is
-// busy for 41 %, the exponential unit for 47 % and the issue slots for 43 % (4 x 1024 rows over 3024 entries); with half the
-// products left out the kernel gains 7 %, without exponentials 3 %.  At few rows: the reads of the cache (a tile is 32 KB of K
+// Bounds.  At many rows per key: the round S -> softmax -> P -> product -> next S of each group, 1.1 us per pair of tiles, of which
+// the tensor pipe is busy for 41 %, the exponential unit for 47 % and the issue slots for 43 % (4 x 1024 rows over 3024
+// entries); with half the products left out the kernel gains 7 %, without exponentials 3 %.  At few rows: the reads of the cache (a tile is 32 KB of K
 // and V for 4.2 MFLOP per group) and, below some 20 us, the steps from the launch to the first tile and from the last one to
 // the joined result.  Measured, 32 / 8 heads of 128, pages of 16: 4 x 2048 rows over 8192 entries 0.87 ms (1100 TFLOP/s, 0.66 of
 // the measured product rate); 64 x 5 rows over 585 entries 46 us (3.3 TB/s); 64 single rows over 2000 99 us (5.3 TB/s).
 // 12 / 2 heads: one row over 100,000 entries 38 us (2.7 TB/s), 13 rows over 512 15 us.  Tried on the large chunk (0.88 ms): a
 // quarter of the exponentials as polynomials on the ordinary pipes 0.93; one lane that waits and issues by itself, without votes,
-// 0.99 (its operands are no longer uniform over the warp); the rows' loop rehearsed before the first tile, so that its
-// instructions are there, 0.97.
+// 0.99 (its operands are no longer uniform over the warp); a warp of its own for each of the two products 0.94; the rows' loop
+// rehearsed before the first tile, so that its instructions are there, 0.97.
 //
 // Entries that no row of a query tile can see are not read into a product: their scores are overwritten with -inf, and
 // V rows that are past the last visible entry of the tile are cleared in shared memory, so that whatever the
