@@ -742,7 +742,10 @@ cudaError_t launch(const void* logits, int64_t row_stride, int n, int vocab, con
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n * kCluster); cfg.blockDim = dim3(THREADS); cfg.stream = s;
   cfg.dynamicSmemBytes = (size_t)(per + 1) * 16;     // one more piece: a slice that does not begin on a 16-byte boundary
-  if (cudaError_t e = cudaFuncSetAttribute(k_sample<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes)) return e;
+  // The limit belongs to the kernel, not to the call: always that of the largest vocabulary, so that calls of several host threads
+  // cannot lower it for one another between setting it and launching.
+  constexpr int kMaxSlice = (kMaxVocab / (kCluster * kVec) + 1) * 16;
+  if (cudaError_t e = cudaFuncSetAttribute(k_sample<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice)) return e;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = kCluster; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
