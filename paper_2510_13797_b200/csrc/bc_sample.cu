@@ -166,7 +166,8 @@ struct Scale {
     const double v = scaled(x > low ? x : top);
     return x > low && v >= min_w ? biased(v) - kBias : 0;
   }
-  __device__ __forceinline__ float depth(float x) const { return fminf(top - x, 3e38f) * bins; }   // in bins (finite: inf * 0 is none)
+  // in bins, of an element above low.  The difference is taken in halves: that of two finite numbers can be beyond the largest one.
+  __device__ __forceinline__ float depth(float x) const { return fmaf(x, -0.5f, 0.5f * top) * (2.f * bins); }
   __device__ __forceinline__ int bin(float x) const { return min(kBins - 1, (int)depth(x)); }
   // of an element above low; the last bin has no lower end
   __device__ __forceinline__ bool in_bin(float x, int b) const {
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   for (int d = 16; d > 0; d >>= 1) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
   if (lane == 0) warp_best[warp] = best;
   for (int b = tid; b < kBins; b += THREADS) sh.work[0].h.mass[0][b] = sh.work[0].h.mass[1][b] = sh.work[0].h.mass[2][b] = sh.work[0].h.count[b] = sh.work[1].h.count[b] = 0;
-  if (tid == 0) { sh.at = 0x7fffffff; sh.n_list[0] = 0; sh.pick[0].found = sh.pick[1].found = 0; }
+  if (tid == 0) { sh.at = 0x7fffffff; sh.n_list[0] = 0; sh.pick[0] = sh.pick[1] = Pick{{0, 0}, 0, 0}; }
   __syncthreads();
   if (warp == 0) {
     best = lane < kWarps ? warp_best[lane] : -INFINITY;
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   sc.top = best;
   sc.dtop = (double)best;
   sc.c = fmax(1.4426950408889634 / (double)temp, 1e-300);   // not 0 for an infinite temperature: 0 * inf
-  sc.bins = (float)fmin(11.0 * sc.c, 1e38);                 // finite: 0 * inf again
+  sc.bins = (float)fmin(11.0 * sc.c, 1e38);                 // finite, and twice as much as well: 0 * inf again
   sc.low = fminf((float)(sc.dtop - (kWeightBits + 1) / sc.c), nextafterf(best, -INFINITY));
   const float mp = min_p != nullptr ? min_p[r] : 0.f;
   sc.min_w = mp > 0.f ? fmin((double)mp, 1.0) * (double)(1ull << kWeightBits) : 0.0;   // at most 1: the largest element is always kept

@@ -1,13 +1,34 @@
-"""bc_sample where host threads could make it go wrong."""
+"""bc_sample where host threads or differences beyond the largest float could make it go wrong, against its fp64 oracle
+(oracle/sampling_oracle.py): the tokens have to be equal."""
 import threading
 
+import numpy as np
 import pytest
 import torch
 
+from oracle.sampling_oracle import sample
 from paper_2510_13797_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
+INF = float("inf")
+
+
+def _t(x, dtype=torch.float32):
+    return None if x is None else torch.tensor(x, dtype=dtype, device=DEV)
+
+
+def _check(x, u, t=None, k=None, p=None, floor=False):
+    """floor: elements of less than 2^-46 of the largest weight, which are never chosen (breadcrumbs.h), are left out of the oracle's row."""
+    n = len(x)
+    got = B.bc_sample(x, _t(u), _t(t), _t(k, torch.int32), _t(p))
+    rows = x.double().cpu().numpy()
+    for r in range(n) if floor else ():
+        rows[r][(rows[r] - rows[r].max()) / float(np.float32(t[r])) < -46 * np.log(2.0)] = -INF
+    f32 = lambda v: [1.0] * n if v is None else [float(np.float32(a)) for a in v]
+    t, p, k = f32(t), f32(p), [0] * n if k is None else k
+    want = [sample(rows[r], np.float32(u[r]), t[r], k[r], p[r]) for r in range(n)]
+    assert got.tolist() == want, [(r, g, w) for r, (g, w) in enumerate(zip(got.tolist(), want)) if g != w][:5]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -42,3 +63,24 @@ def test_large_and_small_vocabularies_from_two_threads(dtype):
     for th in threads:
         th.join()
     assert not failures
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("t", [1e37, 1e38, 3e38])
+def test_lowest_value_as_a_mask_at_temperatures_that_reach_it(dtype, t):
+    """Logits near 0 and the type's lowest value: differences of more than 3e38 that still weigh something."""
+    n, v = 4, 2000
+    g = torch.Generator(device=DEV)
+    g.manual_seed(31)
+    x = torch.full((n, v), torch.finfo(dtype).min, device=DEV, dtype=dtype)
+    for r in range(n):
+        at = torch.randperm(v, generator=g, device=DEV)[:500]
+        x[r, at] = torch.randn(500, generator=g, device=DEV).to(dtype)
+    x[2, 100], x[3, 100] = torch.finfo(dtype).max / 2, torch.finfo(dtype).max     # differences beyond the largest float
+    for u in (0.0, 0.35, 0.7, 0.9999):
+        us, ts = [u] * n, [t] * n
+        _check(x, us, t=ts, floor=True)
+        _check(x, us, t=ts, k=[600] * n, floor=True)
+        _check(x, us, t=ts, k=[1999] * n, floor=True)
+        _check(x, us, t=ts, p=[0.9] * n, floor=True)
+        _check(x, us, t=ts, k=[600] * n, p=[0.99] * n, floor=True)
