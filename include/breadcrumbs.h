@@ -407,8 +407,8 @@ BC_API bc_status bc_argmax(const void* logits, int32_t n, int32_t vocab, int64_t
  *       top_p * mass(K) -- at least one element; all of K if top_p >= 1 --,
  *   S = the elements of N with e_j >= min_p (min_p <= 0: all; values above 1 count as 1),
  *   out = the first j of S in index order with the sum of e over S up to j ABOVE uniform * mass(S).
- * T <= 0 (or NaN): the greedy choice, as bc_argmax.  A row whose maximum is -inf: its lowest index of a
- * maximum, as bc_argmax.  NaN logits count as -inf; -inf logits are never chosen beside finite ones; +inf
+ * NaN logits count as -inf.  T <= 0 (or NaN): the lowest index of the maximum, as bc_argmax.  A row without a
+ * logit above -inf: index 0.  -inf logits are never chosen beside finite ones; +inf
  * logits share the whole mass.  top_p, min_p NaN: off.  uniform below 0 or NaN counts as 0, 1 and above as the
  * largest number below 1.  Weights are evaluated in double precision and added up exactly as multiples of
  * 2^-45 (an element below that is never chosen), so the result does not depend on the order of additions.

@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
   best = sh.row_best;
 
   const float temp = temperature != nullptr ? temperature[r] : 1.f;
-  if (!(temp > 0.f) || best == -INFINITY) {        // greedy; a row without a finite element: its first index, as bc_argmax
+  if (!(temp > 0.f) || best == -INFINITY) {        // greedy; a row of -inf and NaN: its first index
     int at = 0x7fffffff;
     for (int q = tid; q < pieces; q += THREADS) {
       const uint4 v = slice[q];
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_sample(const T* __r
     cluster.sync();
     if (part == 0 && tid == 0) {
       for (int b = 0; b < kCluster; ++b) at = min(at, *cluster.map_shared_rank(&sh.at, b));
-      out[r] = at == 0x7fffffff ? 0 : at;
+      out[r] = best == -INFINITY ? 0 : at;         // NaN counts as -inf: every element is the maximum
     }
     cluster.sync();                                // no block leaves while its shared memory may still be read
     return;

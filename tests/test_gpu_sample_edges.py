@@ -1,5 +1,5 @@
-"""bc_sample where host threads or differences beyond the largest float could make it go wrong, against its fp64 oracle
-(oracle/sampling_oracle.py): the tokens have to be equal."""
+"""bc_sample where host threads, differences beyond the largest float or rows without a number could make it go wrong, against its
+fp64 oracle (oracle/sampling_oracle.py): the tokens have to be equal."""
 import threading
 
 import numpy as np
@@ -11,7 +11,7 @@ from paper_2510_13797_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
-INF = float("inf")
+INF, NAN = float("inf"), float("nan")
 
 
 def _t(x, dtype=torch.float32):
@@ -84,3 +84,19 @@ def test_lowest_value_as_a_mask_at_temperatures_that_reach_it(dtype, t):
         _check(x, us, t=ts, k=[1999] * n, floor=True)
         _check(x, us, t=ts, p=[0.9] * n, floor=True)
         _check(x, us, t=ts, k=[600] * n, p=[0.99] * n, floor=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_of_nan_and_minus_infinity_yield_their_first_element(dtype):
+    n, v = 6, 4001
+    x = torch.full((n, v), -INF, device=DEV, dtype=dtype)
+    x[0, 0] = NAN
+    x[1, :3999] = NAN
+    x[2, 1:] = NAN
+    x[3, 5] = NAN
+    x[4, :] = NAN
+    x[5, :600] = NAN
+    for t in (None, [0.0] * n, [0.7] * n):
+        _check(x, [0.5] * n, t=t)
+        _check(x, [0.5] * n, t=t, k=[3] * n, p=[0.9] * n)
+        assert B.bc_sample(x, torch.rand(n, device=DEV), _t(t)).tolist() == [0] * n
