@@ -410,8 +410,9 @@ BC_API bc_status bc_argmax(const void* logits, int32_t n, int32_t vocab, int64_t
  * NaN logits count as -inf.  T <= 0 (or NaN): the lowest index of the maximum, as bc_argmax.  A row without a
  * logit above -inf: index 0.  -inf logits are never chosen beside finite ones; +inf
  * logits share the whole mass.  top_p, min_p NaN: off.  uniform below 0 or NaN counts as 0, 1 and above as the
- * largest number below 1.  Weights are evaluated in double precision and added up exactly as multiples of
- * 2^-45 (an element below that is never chosen), so the result does not depend on the order of additions.
+ * largest number below 1.  Weights are evaluated in double precision (to 2^-48 of their value), rounded to
+ * multiples of 2^-45 (an element below 2^-46 is never chosen) and added up exactly, so the result does not depend on the
+ * order of additions.
  * logits: device, n rows of vocab elements, bf16 (logits_f32 == 0) or fp32, row i at logits + i * row_stride
  * elements (row_stride >= vocab; any value, any vocab up to 262144, else BC_ERR_UNSUPPORTED), aligned to the
  * element; temperature, top_p, min_p fp32 [n], top_k int32 [n]: device, each NULL = 1, off, off, off for all

@@ -1,5 +1,5 @@
-"""bc_sample where host threads, differences beyond the largest float or rows without a number could make it go wrong, against its
-fp64 oracle (oracle/sampling_oracle.py): the tokens have to be equal."""
+"""bc_sample where host threads, borders between elements, differences beyond the largest float or rows without a number could make
+it go wrong, against its fp64 oracle (oracle/sampling_oracle.py): the tokens have to be equal."""
 import threading
 
 import numpy as np
@@ -100,3 +100,32 @@ def test_rows_of_nan_and_minus_infinity_yield_their_first_element(dtype):
         _check(x, [0.5] * n, t=t)
         _check(x, [0.5] * n, t=t, k=[3] * n, p=[0.9] * n)
         assert B.bc_sample(x, torch.rand(n, device=DEV), _t(t)).tolist() == [0] * n
+
+
+# Pairs (d, u) of fp32 numbers: in the row (-d, 0) the first element's share e^-d / (1 + e^-d) is u, off by 2^-42 to 2^-37 of it.  From an
+# enumeration of the d whose weight lies about half-way between two powers of two.
+BORDERS = [
+    (0.3351668119430542, 0.4169839918613434), (0.3373848497867584, 0.41644486784935), (0.3393268287181854, 0.4159730076789856),
+    (0.3422203063964844, 0.41527023911476135), (0.3429049551486969, 0.4151040017604828), (0.3438277244567871, 0.4148799777030945),
+    (0.34420573711395264, 0.41478821635246277), (0.34737640619277954, 0.41401877999305725), (0.3482600748538971, 0.41380441188812256),
+    (0.3515695333480835, 0.4130018651485443), (0.3532089293003082, 0.4126044809818268), (0.35387200117111206, 0.41244378685951233),
+    (1.0292387008666992, 0.26323172450065613), (1.0367457866668701, 0.2617783844470978), (1.0469118356704712, 0.25981855392456055),
+    (1.7248982191085815, 0.15124131739139557), (1.7295488119125366, 0.15064530074596405), (1.7386198043823242, 0.14948832988739014),
+    (1.7453124523162842, 0.14863941073417664), (1.7517313957214355, 0.14782895147800446), (2.423910617828369, 0.08136747032403946),
+    (2.4285147190093994, 0.08102399110794067), (2.4351704120635986, 0.08052979409694672), (0.3349699378013611, 0.417031854391098),
+    (0.3350943624973297, 0.4170016050338745), (1.0195037126541138, 0.2651240825653076), (1.020089030265808, 0.2650100588798523),
+    (1.7169504165649414, 0.15226438641548157), (1.7193050384521484, 0.15196070075035095), (2.4052348136901855, 0.08277438580989838),
+    (2.4083049297332764, 0.08254159241914749),
+]
+
+
+def test_numbers_close_to_a_border_between_two_elements():
+    """The weights are as good as their rounding to a multiple of 2^-45: a border is where fp64 puts it, to 2^-42 of itself."""
+    d, u = np.array(BORDERS, dtype=np.float32).T
+    p = 1.0 / (1.0 + np.exp(d.astype(np.float64)))
+    off = np.abs(p / u.astype(np.float64) - 1)
+    assert off.min() > 2.0 ** -42 and off.max() < 2.0 ** -37
+    x = torch.zeros((len(d), 2), device=DEV)
+    x[:, 0] = -torch.from_numpy(d).to(DEV)
+    _check(x, u.tolist())
+    _check(x, u.tolist(), p=[0.9999] * len(d))
