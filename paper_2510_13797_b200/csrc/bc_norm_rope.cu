@@ -189,15 +189,17 @@ struct NormRopeGradArgs {
   uint4* dqkv;          // [rows][q_heads + 2 kv_heads][D], contiguous
   float* partial;       // [blocks][2][D]
   int64_t units;
-  int q_heads, kv_heads, split;
+  int q_heads, kv_heads, split, fold;
   double log2_theta;
   float eps;
 };
 
-// The weight gradients: every lane adds up its 16 coordinates over the rows and heads it meets (fp32, a few dozen to a
-// few hundred terms; the query heads' sums in registers, the key heads', which are fewer, in a place of the lane's own in
-// shared memory), the block's lanes are joined in a fixed order and a second kernel adds the blocks', also in a fixed order, so
-// that results are reproducible.
+// The weight gradients: every lane adds up its 16 coordinates over the rows and heads it meets (fp32; the query heads' sums in
+// registers, the key heads', which are fewer, in a place of the lane's own in shared memory).  After `fold` units, kFoldTerms terms or one
+// unit's, the warp's lanes are joined into the warp's sums in shared memory and begin again, so that no chain of additions grows
+// with the number of rows but that of the folds, a hundredth as long.  At the end the block's warps are joined and a second kernel adds
+// the blocks', all in a fixed order, so that results are reproducible.
+constexpr int kFoldTerms = 128;
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGradArgs a) {
   constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kChunks = D / 8;
@@ -205,11 +207,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
   if (a.partial != nullptr) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the kernel that adds the blocks' sums waits for this one's end
   __shared__ __align__(16) float weights[2][D];
   __shared__ __align__(16) float dwk[kWarps][4][32][4];           // a lane's 16 sums: 16 bytes apart from its neighbours'
+  __shared__ __align__(16) float sums[kWarps][2][D];
   const int lane = threadIdx.x & 31, piece = lane & (kLanes - 1), sub = lane / kLanes, warp = threadIdx.x >> 5;
   for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
     const __nv_bfloat16* w = i < D ? a.q_weight : a.k_weight;
     weights[i / D][i % D] = w ? __bfloat162float(w[i % D]) : 1.f;
   }
+  for (int i = threadIdx.x; i < kWarps * 2 * D / 4; i += kThreads) reinterpret_cast<float4*>(sums)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dwk[warp][i][lane]) = make_float4(0.f, 0.f, 0.f, 0.f);
   __syncthreads();
@@ -220,6 +224,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
 #pragma unroll
   for (int i = 0; i < 8; ++i) dwq[i] = pair(0.f, 0.f);
   const int64_t step = (int64_t)gridDim.x * kWarps;
+  int left = a.fold;
   for (int64_t u = (int64_t)blockIdx.x * kWarps + warp; u < a.units; u += step) {
     const int64_t row = u / a.split;
     const int part = (int)(u - row * a.split);
@@ -297,25 +302,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_norm_rope_grad(const NormRopeGr
         }
       }
     }
-  }
-  if (a.partial == nullptr) return;
-  __shared__ float sh[kWarps][2][D];
+    if (a.partial != nullptr && (--left == 0 || u + step >= a.units)) {   // the lanes' sums to the warp's
+      left = a.fold;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float even, odd;
-    split(dwq[i >> 1], &even, &odd);
-    float vq = (i & 1) ? odd : even, vk = dwk[warp][i >> 2][lane][i & 3];
+      for (int j = 0; j < 4; ++j) {               // four coordinates of q and of k
+        const float4 k4 = *reinterpret_cast<const float4*>(dwk[warp][j][lane]);
+        float v[8] = {0.f, 0.f, 0.f, 0.f, k4.x, k4.y, k4.z, k4.w};
+        split(dwq[2 * j], v, v + 1);
+        split(dwq[2 * j + 1], v + 2, v + 3);
 #pragma unroll
-    for (int d = kLanes; d < 32; d <<= 1) { vq += __shfl_xor_sync(0xffffffffu, vq, d); vk += __shfl_xor_sync(0xffffffffu, vk, d); }
-    if (sub == 0) {
-      const int col = (i >> 3) * (D / 2) + piece * 8 + (i & 7);
-      sh[warp][0][col] = vq;
-      sh[warp][1][col] = vk;
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int d = kLanes; d < 32; d <<= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+        if (sub < 2) {                            // one lane of each piece keeps the query heads' sums, one the key heads'
+          float4* at = reinterpret_cast<float4*>(&sums[warp][sub][(j >> 1) * (D / 2) + piece * 8 + (j & 1) * 4]);
+          const float4 s4 = *at;
+          *at = sub == 0 ? make_float4(s4.x + v[0], s4.y + v[1], s4.z + v[2], s4.w + v[3])
+                         : make_float4(s4.x + v[4], s4.y + v[5], s4.z + v[6], s4.w + v[7]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dwq[i] = pair(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(dwk[warp][i][lane]) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
   }
+  if (a.partial == nullptr) return;
   __syncthreads();
   if (threadIdx.x < 2 * D) {
-    const float* col = &sh[0][0][0] + threadIdx.x;
+    const float* col = &sums[0][0][0] + threadIdx.x;
     float t = 0.f;
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) t += col[v * 2 * D];
@@ -415,6 +430,8 @@ bc_status bc_norm_rope_split_backward(int32_t n, int32_t q_heads, int32_t kv_hea
   a.q_heads = q_heads; a.kv_heads = kv_heads; a.log2_theta = log2((double)theta); a.eps = eps;
   a.split = row_split(n, q_heads + 2 * kv_heads, head_dim, 2);
   a.units = (int64_t)n * a.split;
+  const int per_pass = 32 / (head_dim / 16) * a.split, terms = (q_heads + 2 * kv_heads + per_pass - 1) / per_pass;   // of a lane, per unit, at most
+  a.fold = terms < kFoldTerms ? kFoldTerms / terms : 1;
   const int64_t want = (a.units + kWarps - 1) / kWarps;
   const int blocks = (int)(want < kMaxGradBlocks ? want : kMaxGradBlocks);
   cudaStream_t s = (cudaStream_t)stream;
