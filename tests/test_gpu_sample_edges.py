@@ -129,3 +129,20 @@ def test_numbers_close_to_a_border_between_two_elements():
     x[:, 0] = -torch.from_numpy(d).to(DEV)
     _check(x, u.tolist())
     _check(x, u.tolist(), p=[0.9999] * len(d))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows_of_a_full_vocabulary(dtype):
+    """A batch that fills the device (fewer threads per block than a few rows get), every filter."""
+    n, v = 20, 151936
+    g = torch.Generator(device=DEV)
+    g.manual_seed(33)
+    x = torch.randn((n, v), generator=g, device=DEV) * 2.5
+    x.scatter_add_(1, torch.randint(0, v, (n, 8), generator=g, device=DEV), 3 + 3 * torch.randn((n, 8), generator=g, device=DEV))
+    x = x.to(dtype)
+    u = torch.rand(n, generator=g, device=DEV).tolist()
+    r = range(n)
+    t = [[1.0, 0.7, 1.3, 0.05][i % 4] for i in r]
+    _check(x, u, t=t)
+    _check(x, u, t=t, p=[[0.95, 0.5, 0.99][i % 3] for i in r])
+    _check(x, u, t=t, k=[[50, 1, 400, v, 5000][i % 5] for i in r], p=[[1.0, 0.9, 0.5][i % 3] for i in r])
