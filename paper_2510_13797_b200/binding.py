@@ -143,7 +143,7 @@ def _require(ok, where):
 def _on(where, ref, tensors, stream):
     """Checks that the tensors (tensor or None, dtype, shape) are contiguous, of that dtype and shape, and on the CUDA device of
     `ref`.  Returns that device's index, the raw stream, and the torch stream if one other than the device's current one was given
-    (memory allocated for the call must then be tied to it).  Kept short: it is most of a small call's time."""
+    (memory for the call's results is then taken from it).  Kept short: it is most of a small call's time."""
     dev = ref.get_device()
     if dev < 0:
         raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
@@ -169,6 +169,18 @@ def _call(where, dev, fn, *args):
 
 def _at(t):
     return None if t is None else t.data_ptr()
+
+
+def _new(like, shape, dtype, other):
+    """Memory for results of a call on the stream `other` (None: the current one), on the device of `like`.  It is taken from that
+    stream's memory, since a block that the current stream has freed may still be in use by work queued there; the caller may use it on
+    the current stream."""
+    if other is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(other):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream(like.device))
+    return t
 
 
 class Cache:
@@ -453,12 +465,9 @@ def bc_norm_rope_split(qkv, positions, theta, q_weight, k_weight, eps, q_heads, 
     n, d, row_stride, qs, ks = _norm_rope_shapes(qkv, q_heads, kv_heads, where)
     dev, s, other = _on(where, qkv, ((positions, torch.int32, (n,)), (q_weight, bf16, (d,)), (k_weight, bf16, (d,)), (q_out, bf16, qs),
                                      (k_out, bf16, ks), (v_out, bf16, ks)), stream)
-    q = qkv.new_empty(qs) if q_out is None else q_out
-    k = qkv.new_empty(ks) if k_out is None else k_out
-    v = qkv.new_empty(ks) if v_out is None else v_out
-    if other is not None:
-        for t in (q, k, v):
-            t.record_stream(other)
+    q = _new(qkv, qs, bf16, other) if q_out is None else q_out
+    k = _new(qkv, ks, bf16, other) if k_out is None else k_out
+    v = _new(qkv, ks, bf16, other) if v_out is None else v_out
     _call(where, dev, lib().bc_norm_rope_split, n, q_heads, kv_heads, d, qkv.data_ptr(), row_stride, positions.data_ptr(), theta, _at(q_weight),
           _at(k_weight), eps, q.data_ptr(), k.data_ptr(), v.data_ptr(), s)
     return q, k, v
@@ -474,12 +483,9 @@ def bc_norm_rope_split_backward(qkv, positions, theta, q_weight, k_weight, eps, 
                                      (dv, bf16, ks)), stream)
     size = C.c_size_t()
     _check(lib().bc_norm_rope_query_bytes(d, C.byref(size)), "bc_norm_rope_query_bytes")
-    dqkv = qkv.new_empty((n, qkv.shape[1]))
+    dqkv = _new(qkv, (n, qkv.shape[1]), bf16, other)
     # the weights' gradients and the scratch in one allocation
-    ws = torch.empty(size.value // 4 + 2 * d, dtype=torch.float32, device=qkv.device)
-    if other is not None:
-        dqkv.record_stream(other)
-        ws.record_stream(other)
+    ws = _new(qkv, size.value // 4 + 2 * d, torch.float32, other)
     at = ws.data_ptr()
     _call(where, dev, lib().bc_norm_rope_split_backward, n, q_heads, kv_heads, d, qkv.data_ptr(), row_stride, positions.data_ptr(), theta,
           _at(q_weight), _at(k_weight), eps, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dqkv.data_ptr(), at if weight_grads else None,
@@ -498,9 +504,7 @@ def bc_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=N
     _require(vocab == 1 or logits.stride(1) == 1, where)
     dev, s, other = _on(where, logits, ((uniform, f32, (n,)), (temperature, f32, (n,)), (top_k, torch.int32, (n,)), (top_p, f32, (n,)),
                                         (min_p, f32, (n,)), (out, torch.int64, (n,))), stream)
-    res = torch.empty(n, dtype=torch.int64, device=logits.device) if out is None else out
-    if other is not None:
-        res.record_stream(other)
+    res = _new(logits, n, torch.int64, other) if out is None else out
     _call(where, dev, lib().bc_sample, logits.data_ptr(), 1 if logits.dtype is f32 else 0, row_stride if n > 1 else max(row_stride, vocab), n, vocab,
           _at(temperature), _at(top_k), _at(top_p), _at(min_p), uniform.data_ptr(), res.data_ptr(), s)
     return res

@@ -1,0 +1,45 @@
+"""Results that the binding allocates itself for a call on a given stream: their memory may not be that of work still queued on the
+current stream."""
+import pytest
+import torch
+
+from paper_2510_13797_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _calls():
+    n, Hq, Hkv, D = 64, 4, 2, 64
+    qkv = torch.randn((n, (Hq + 2 * Hkv) * D), device=DEV).to(torch.bfloat16)
+    pos, w = torch.arange(n, dtype=torch.int32, device=DEV), torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    grads = [torch.randn((n, h, D), device=DEV).to(torch.bfloat16) for h in (Hq, Hkv, Hkv)]
+    x, u = torch.randn((n, 999), device=DEV), torch.rand(n, device=DEV)
+    return {
+        "sample": lambda **kw: (B.bc_sample(x, u, **kw),),
+        "split": lambda **kw: B.bc_norm_rope_split(qkv, pos, 1e4, w, w, 1e-6, Hq, Hkv, **kw),
+        "backward": lambda **kw: B.bc_norm_rope_split_backward(qkv, pos, 1e4, w, w, 1e-6, *grads, **kw),
+    }
+
+
+@pytest.mark.parametrize("name", ["sample", "split", "backward"])
+def test_results_do_not_share_memory_with_work_on_the_current_stream(name):
+    call = _calls()[name]
+    want = call()
+    sizes = [t.untyped_storage().nbytes() for t in want]
+    s = torch.cuda.Stream()
+    torch.cuda._sleep(1)                                 # kernels are loaded by their first launch, which may wait for the device
+    torch.empty(8, dtype=torch.uint8, device=DEV).fill_(0)
+    torch.cuda.synchronize()
+    blocks = [torch.empty(size, dtype=torch.uint8, device=DEV) for size in sizes for _ in range(100)]
+    torch.cuda._sleep(100_000_000)                       # some 50 ms; the writes behind it come after the call on the other stream
+    for b in blocks:
+        b.fill_(77)
+    held = blocks[::2]                                   # so that the others stay apart
+    del blocks, b                                        # free for the current stream, whose order protects them there
+    got = call(stream=s)
+    s.synchronize()
+    first = [t.clone() for t in got]
+    torch.cuda.synchronize()
+    del held
+    assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(want, got, first))
