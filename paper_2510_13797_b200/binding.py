@@ -171,6 +171,11 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _other(ref, stream):
+    """`stream`, if it is another one than the current stream of the device of `ref`."""
+    return stream if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(ref.get_device()) else None
+
+
 def _new(like, shape, dtype, other):
     """Memory for results of a call on the stream `other` (None: the current one), on the device of `like`.  It is taken from that
     stream's memory, since a block that the current stream has freed may still be in use by work queued there; the caller may use it on
@@ -347,8 +352,9 @@ class Cache:
 
     def bc_export_seq(self, layer, slot, capacity, stream=None):
         shape = (capacity, self.cfg.kv_heads, self.cfg.head_dim)
-        k = torch.zeros(shape, dtype=torch.bfloat16, device=self.device)
-        v = torch.zeros(shape, dtype=torch.bfloat16, device=self.device)
+        k, v = [_new(self.pool, shape, torch.bfloat16, _other(self.pool, stream)) for _ in range(2)]
+        with torch.cuda.stream(stream):
+            k.zero_(), v.zero_()
         _check(lib().bc_export_seq(self.handle, layer, slot, _ptr(k), _ptr(v), capacity, _stream(stream)),
                "bc_export_seq")
         return k, v
@@ -393,9 +399,10 @@ def bc_mask_attn_forward(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, 
     size = C.c_size_t()
     _check(lib().bc_mask_attn_query_bytes(n, q_heads, kv_heads, head_dim, cu_p[n], cu_t[n], total_b, C.byref(size)),
            "bc_mask_attn_query_bytes")
-    ws = torch.empty(size.value, dtype=torch.uint8, device=tok_q.device)
-    out_tok = torch.empty_like(tok_q)
-    out_bea = torch.empty((total_b, q_heads, head_dim), dtype=tok_q.dtype, device=tok_q.device)
+    other = _other(tok_q, stream)
+    ws = _new(tok_q, size.value, torch.uint8, other)
+    out_tok = _new(tok_q, tok_q.shape, tok_q.dtype, other)
+    out_bea = _new(tok_q, (total_b, q_heads, head_dim), tok_q.dtype, other)
     _check(lib().bc_mask_attn_forward(n, q_heads, kv_heads, head_dim, c, cu_p, cu_t, _ptr(prompt_k), _ptr(prompt_v),
                                       _ptr(tok_q), _ptr(tok_k), _ptr(tok_v), _ptr(beacon_q), _ptr(beacon_k),
                                       _ptr(beacon_v), _ptr(out_tok), _ptr(out_bea), sm_scale, _ptr(ws), size.value,
@@ -437,10 +444,10 @@ def bc_distill_loss(cu_rows, student_logits, teacher_idx, teacher_logprob, with_
     teacher_logprob fp32 [rows, top_k]."""
     rows, vocab = student_logits.shape
     top_k = teacher_idx.shape[1]
-    dev = student_logits.device
-    row_loss = torch.empty(rows, dtype=torch.float32, device=dev)
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    grad = torch.empty_like(student_logits) if with_grad else None
+    other = _other(student_logits, stream)
+    row_loss = _new(student_logits, rows, torch.float32, other)
+    loss = _new(student_logits, 1, torch.float32, other)
+    grad = _new(student_logits, student_logits.shape, student_logits.dtype, other) if with_grad else None
     _check(lib().bc_distill_loss(cu_rows.numel() - 1, _ptr(cu_rows), rows, vocab, top_k, _ptr(student_logits),
                                  _ptr(teacher_idx), _ptr(teacher_logprob), _ptr(row_loss), _ptr(loss), _ptr(grad),
                                  _stream(stream)), "bc_distill_loss")

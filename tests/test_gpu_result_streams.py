@@ -15,14 +15,25 @@ def _calls():
     pos, w = torch.arange(n, dtype=torch.int32, device=DEV), torch.ones(D, dtype=torch.bfloat16, device=DEV)
     grads = [torch.randn((n, h, D), device=DEV).to(torch.bfloat16) for h in (Hq, Hkv, Hkv)]
     x, u = torch.randn((n, 999), device=DEV), torch.rand(n, device=DEV)
+    cache = B.Cache(1, Hkv, Hq, D, 1, 16, max_seqs=1, num_pages=8, max_pages_per_seq=8)
+    slot, k = torch.zeros(1, dtype=torch.int32, device=DEV), torch.randn((40, Hkv, D), device=DEV).to(torch.bfloat16)
+    cache.bc_seq_open(slot, slot + 40)
+    cache.bc_prefill(0, slot, torch.tensor([0, 40], dtype=torch.int32, device=DEV), 40, k, k)
+    mq, mk = torch.randn((60, 4, 128), device=DEV).to(torch.bfloat16), torch.randn((60, 2, 128), device=DEV).to(torch.bfloat16)
+    cu, idx = torch.tensor([0, 64], dtype=torch.int32, device=DEV), torch.arange(5, dtype=torch.int32, device=DEV).repeat(64, 1)
+    logp = torch.full((64, 5), -2.0, device=DEV)
+    z = torch.randn((64, 1000), device=DEV).to(torch.bfloat16)
     return {
         "sample": lambda **kw: (B.bc_sample(x, u, **kw),),
         "split": lambda **kw: B.bc_norm_rope_split(qkv, pos, 1e4, w, w, 1e-6, Hq, Hkv, **kw),
         "backward": lambda **kw: B.bc_norm_rope_split_backward(qkv, pos, 1e4, w, w, 1e-6, *grads, **kw),
+        "export": lambda **kw: cache.bc_export_seq(0, 0, 40, **kw),
+        "mask": lambda **kw: B.bc_mask_attn_forward([0], [60], 4, None, None, mq, mk, mk, mq[:15], mk[:15], mk[:15], 0.1, check=False, **kw),
+        "distill": lambda **kw: B.bc_distill_loss(cu, z, idx, logp, with_grad=True, **kw),
     }
 
 
-@pytest.mark.parametrize("name", ["sample", "split", "backward"])
+@pytest.mark.parametrize("name", ["sample", "split", "backward", "export", "mask", "distill"])
 def test_results_do_not_share_memory_with_work_on_the_current_stream(name):
     call = _calls()[name]
     want = call()
