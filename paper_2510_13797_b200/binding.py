@@ -199,9 +199,10 @@ class Cache:
         sizes = [C.c_size_t() for _ in range(3)]
         _check(lib().bc_cache_query_bytes(C.byref(self.cfg), *[C.byref(s) for s in sizes]), "bc_cache_query_bytes")
         self.pool_bytes, self.meta_bytes, self.workspace_bytes = [s.value for s in sizes]
-        self.pool = torch.empty(self.pool_bytes, dtype=torch.uint8, device=self.device)
-        self.meta = torch.empty(self.meta_bytes, dtype=torch.uint8, device=self.device)
-        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(stream):   # which initialises it: a block of another stream may still be in use by work queued there
+            self.pool = torch.empty(self.pool_bytes, dtype=torch.uint8, device=self.device)
+            self.meta = torch.empty(self.meta_bytes, dtype=torch.uint8, device=self.device)
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
         h = C.c_void_p()
         _check(lib().bc_cache_create(C.byref(self.cfg), _ptr(self.pool), _ptr(self.meta), _ptr(self.workspace),
                                      _stream(stream), C.byref(h)), "bc_cache_create")

@@ -54,3 +54,30 @@ def test_results_do_not_share_memory_with_work_on_the_current_stream(name):
     torch.cuda.synchronize()
     del held
     assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(want, got, first))
+
+
+def test_a_cache_created_on_a_stream_does_not_share_memory_with_work_on_the_current_stream():
+    Hkv, D = 2, 64
+    make = lambda s: B.Cache(1, Hkv, 2 * Hkv, D, 1, 16, max_seqs=2, num_pages=20, max_pages_per_seq=8, stream=s)
+    first = make(None)
+    sizes = [first.pool_bytes, first.meta_bytes, first.workspace_bytes]
+    slot, cu = torch.ones(1, dtype=torch.int32, device=DEV), torch.tensor([0, 40], dtype=torch.int32, device=DEV)
+    plen, k = slot * 40, torch.randn((40, Hkv, D), device=DEV).to(torch.bfloat16)
+    s = torch.cuda.Stream()
+    torch.cuda._sleep(1)
+    torch.empty(8, dtype=torch.uint8, device=DEV).fill_(0)
+    torch.cuda.synchronize()
+    blocks = [torch.empty(size, dtype=torch.uint8, device=DEV) for size in sizes for _ in range(2)]
+    torch.cuda._sleep(100_000_000)
+    for b in blocks:
+        b.fill_(77)
+    del blocks, b
+    cache = make(s)
+    s.synchronize()
+    torch.cuda.synchronize()                             # what was queued has run; the cache is as it was made
+    assert cache.bc_get_state(0) == first.bc_get_state(0)
+    cache.bc_seq_open(slot, plen, stream=s)
+    cache.bc_prefill(0, slot, cu, 40, k, k, stream=s)
+    got = cache.bc_export_seq(0, 1, 40, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, k) for x in got) and cache.bc_poll_error()[0] == 0
