@@ -150,10 +150,9 @@ def _on(where, ref, tensors, stream):
     for t, dtype, shape in tensors:
         if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous()):
             raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
-    raw = torch._C._cuda_getCurrentRawStream(dev)
     if stream is None:
-        return dev, raw, None
-    return dev, stream.cuda_stream, stream if stream.cuda_stream != raw else None
+        return dev, torch._C._cuda_getCurrentRawStream(dev), None
+    return dev, stream.cuda_stream, _other(dev, stream)
 
 
 def _call(where, dev, fn, *args):
@@ -171,9 +170,11 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def _other(ref, stream):
-    """`stream`, if it is another one than the current stream of the device of `ref`."""
-    return stream if stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(ref.get_device()) else None
+def _other(dev, stream):
+    """`stream` (anything that holds a stream's handle as cuda_stream) as a torch stream, if it is not the device's current one."""
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(dev):
+        return None
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, torch.device("cuda", dev))
 
 
 def _new(like, shape, dtype, other):
@@ -199,7 +200,8 @@ class Cache:
         sizes = [C.c_size_t() for _ in range(3)]
         _check(lib().bc_cache_query_bytes(C.byref(self.cfg), *[C.byref(s) for s in sizes]), "bc_cache_query_bytes")
         self.pool_bytes, self.meta_bytes, self.workspace_bytes = [s.value for s in sizes]
-        with torch.cuda.stream(stream):   # which initialises it: a block of another stream may still be in use by work queued there
+        index = torch.cuda.current_device() if self.device.index is None else self.device.index
+        with torch.cuda.stream(_other(index, stream)):   # it initialises them: another stream's blocks may be in use by work queued there
             self.pool = torch.empty(self.pool_bytes, dtype=torch.uint8, device=self.device)
             self.meta = torch.empty(self.meta_bytes, dtype=torch.uint8, device=self.device)
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
@@ -353,8 +355,9 @@ class Cache:
 
     def bc_export_seq(self, layer, slot, capacity, stream=None):
         shape = (capacity, self.cfg.kv_heads, self.cfg.head_dim)
-        k, v = [_new(self.pool, shape, torch.bfloat16, _other(self.pool, stream)) for _ in range(2)]
-        with torch.cuda.stream(stream):
+        other = _other(self.pool.get_device(), stream)
+        k, v = [_new(self.pool, shape, torch.bfloat16, other) for _ in range(2)]
+        with torch.cuda.stream(other):
             k.zero_(), v.zero_()
         _check(lib().bc_export_seq(self.handle, layer, slot, _ptr(k), _ptr(v), capacity, _stream(stream)),
                "bc_export_seq")
@@ -400,7 +403,7 @@ def bc_mask_attn_forward(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, 
     size = C.c_size_t()
     _check(lib().bc_mask_attn_query_bytes(n, q_heads, kv_heads, head_dim, cu_p[n], cu_t[n], total_b, C.byref(size)),
            "bc_mask_attn_query_bytes")
-    other = _other(tok_q, stream)
+    other = _other(tok_q.get_device(), stream)
     ws = _new(tok_q, size.value, torch.uint8, other)
     out_tok = _new(tok_q, tok_q.shape, tok_q.dtype, other)
     out_bea = _new(tok_q, (total_b, q_heads, head_dim), tok_q.dtype, other)
@@ -445,7 +448,7 @@ def bc_distill_loss(cu_rows, student_logits, teacher_idx, teacher_logprob, with_
     teacher_logprob fp32 [rows, top_k]."""
     rows, vocab = student_logits.shape
     top_k = teacher_idx.shape[1]
-    other = _other(student_logits, stream)
+    other = _other(student_logits.get_device(), stream)
     row_loss = _new(student_logits, rows, torch.float32, other)
     loss = _new(student_logits, 1, torch.float32, other)
     grad = _new(student_logits, student_logits.shape, student_logits.dtype, other) if with_grad else None

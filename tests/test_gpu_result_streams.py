@@ -56,6 +56,22 @@ def test_results_do_not_share_memory_with_work_on_the_current_stream(name):
     assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(want, got, first))
 
 
+def test_any_object_with_a_stream_handle_is_a_stream():
+    class Handle:
+        def __init__(self, s):
+            self.cuda_stream = s.cuda_stream
+
+    s = torch.cuda.Stream()
+    for call in _calls().values():
+        want = call()
+        torch.cuda.synchronize()
+        got = call(stream=Handle(s))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    B.Cache(1, 2, 4, 64, 1, 16, max_seqs=1, num_pages=1, max_pages_per_seq=1, stream=Handle(s))
+    torch.cuda.synchronize()
+
+
 def test_a_cache_created_on_a_stream_does_not_share_memory_with_work_on_the_current_stream():
     Hkv, D = 2, 64
     make = lambda s: B.Cache(1, Hkv, 2 * Hkv, D, 1, 16, max_seqs=2, num_pages=20, max_pages_per_seq=8, stream=s)
