@@ -633,7 +633,7 @@ BC_API bc_status bc_set_attn_ctas(bc_cache* cache, int32_t ctas);
 BC_API bc_status bc_profile_enable(bc_cache* cache, int32_t max_launches);
 BC_API bc_status bc_profile_read(bc_cache* cache, int32_t* launches, float* total_ms);
 
-/* Poll limit of the bounded waits inside the kernels of bc_decode_attn and bc_decode_step this handle
+/* Poll limit of the bounded waits inside the kernels of bc_decode_attn, bc_decode_step, bc_chunk_attn and bc_prefill_chunk this handle
  * launches (0 = the default, about a quarter of a second; the paired form keeps the default).  The
  * settable limit lives in kernel variants of its own, built for head_dim 128 with at most 8 query
  * heads per KV head: other shapes return BC_ERR_UNSUPPORTED.  A wait that runs out makes its thread block stop issuing

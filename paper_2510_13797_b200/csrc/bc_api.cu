@@ -360,7 +360,7 @@ namespace {
 bc_status flush_pending(bc_cache* c);   // defined with the host-buffer entry points below
 }
 
-int32_t bc_version(void) { return 240; }
+int32_t bc_version(void) { return 241; }
 
 const char* bc_status_string(bc_status s) {
   switch (s) {

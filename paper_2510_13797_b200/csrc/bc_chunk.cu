@@ -14,16 +14,18 @@
 // 1.07 ms).  A unit with rows for one group only ("solo") belongs to one of the groups, taken in turn, so that one writes
 // its results while the other begins.
 //   * Keys come from pages.  The live entries lie in a virtual row space, prompt from 0, beacons and window each from
-//     the next multiple of the copy height, so that (row & 7) equals the entry's position in its segment modulo 8:
+//     the next multiple of the copy height (of 8 at least), so that (row & 7) equals the entry's position in its segment modulo 8:
 //     the store's chunk permutation IS the 128-byte swizzle of the product's operand layout, and unswizzled tensor
 //     copies of up to 32 entries of one page (64 of the head's coordinates each) put a tile together, K and V alike.
 //     The copy height R is the largest power of two up to that which divides the page size, so no copy crosses a page.
 //   * The key tiles of all (sequence, KV head, query tile) units form one line that is cut into equal spans, one per
-//     thread block, so that a large prompt chunk ends everywhere at the same time; where there are fewer units than
-//     blocks, each unit is cut into equal pieces instead, as many as its share of the blocks, of at least 8 tiles (joining
-//     pieces takes about as long as four to eight tiles).  A unit that is cut leaves unnormalised partial results (m, l, O)
-//     per row in the workspace, and the block that takes its last ticket joins them in the order of the keys, sixteen at a
-//     time, so results do not depend on which block that is.
+//     thread block, of at least 8 tiles, so that a large prompt chunk ends everywhere at the same time; where there are fewer
+//     units than blocks, each unit is cut into equal pieces instead, of at least 8 tiles (joining pieces takes about as long as four
+//     to eight tiles) and as many as its share of the blocks that are left over, at least one.  So equal units have a second piece
+//     only while they are at most a third of the blocks, 49 on 148 SMs: calls of 50 to 147 equal units leave blocks without work, and
+//     so do sequences that are much shorter than 8 tiles (20 prompts of 60 tokens, 8 KV heads: 20 blocks).  A unit that is cut
+//     leaves unnormalised partial results (m, l, O) per row in the workspace, and the block that takes its last ticket joins them in
+//     the order of the keys, sixteen at a time, so results do not depend on which block that is.
 //   * Every block works the line out from the lengths on the device by itself: no host copy of a length, no plan
 //     kernel, and the call can be captured.
 //   * The copies, the products and the rows' softmax each have warps of their own, and the stream of tiles goes on across
@@ -32,8 +34,9 @@
 // the tensor pipe is busy for 41 %, the exponential unit for 47 % and the issue slots for 43 % (4 x 1024 rows over 3024
 // entries); with half the products left out the kernel gains 7 %, without exponentials 3 %.  At few rows: the reads of the cache (a tile is 32 KB of K
 // and V for 4.2 MFLOP per group) and, below some 20 us, the steps from the launch to the first tile and from the last one to
-// the joined result.  Measured, 32 / 8 heads of 128, pages of 16: 4 x 2048 rows over 8192 entries 0.87 ms (1100 TFLOP/s, 0.66 of
-// the measured product rate); 64 x 5 rows over 585 entries 46 us (3.3 TB/s); 64 single rows over 2000 99 us (5.3 TB/s).
+// the joined result.  Measured, 32 / 8 heads of 128, pages of 16: 4 x 2048 rows over 8192 entries 0.88 ms in a short replay (1090
+// TFLOP/s, 0.66 of the measured product rate), 1.05 ms per call in a run of a second, at lower clocks (920 TFLOP/s); 64 x 5 rows over
+// 585 entries 46 us (3.3 TB/s); 64 single rows over 2000 99 us (5.3 TB/s).
 // 12 / 2 heads: one row over 100,000 entries 38 us (2.7 TB/s), 13 rows over 512 15 us.  Tried on the large chunk (0.88 ms): a
 // quarter of the exponentials as polynomials on the ordinary pipes 0.93; one lane that waits and issues by itself, without votes,
 // 0.99 (its operands are no longer uniform over the warp); a warp of its own for each of the two products 0.94; the rows' loop
@@ -151,7 +154,7 @@ struct ChunkParams {
   FastDiv by_page;
   int32_t half;       // tokens of a group: 128 / G
   int32_t tokens;     // of a unit: two groups
-  int32_t R;          // entries per copy: 8, 16 or 32, or 1 (row by row)
+  int32_t R;          // entries per copy: 4, 8, 16 or 32, or 1 (row by row)
   int32_t align;      // segment starts in the virtual row space: max(8, R)
   int32_t min_shift;  // log2 of the key tiles of a piece, at least
   uint32_t wait_limit;
@@ -243,7 +246,7 @@ __device__ __forceinline__ void tile_mask(uint32_t (&mask)[2], const Seen& s, in
   add_range(mask, s.w0 - k0, s.w0 + s.w - k0);
 }
 
-// What the control warp needs to issue a tile's copies.  Lane l holds the copies l, l + 32, ... of the tile's 64 / R.
+// What a copy warp needs to issue a tile's copies.  Lane l holds the copies l, l + 32, ... of the tile's 64 / R.
 template <int KP>
 struct TileIssue {
   int page[KP], rem[KP];     // page id and first entry inside the page
@@ -337,8 +340,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
     const int first = a.first != nullptr ? a.first[i] : P + nb + w - m;
     it.m[i] = m; it.first[i] = min(max(first, -(1 << 30)), 1 << 30); it.P[i] = P; it.nb[i] = nb; it.w[i] = w;
   }
-  // Pieces of a unit of N tiles, where units are fewer than blocks; share: blocks left over per key tile
-  // (together at most as many as blocks: a piece each, and the rest of the blocks by shares rounded down)
+  // Pieces of a unit of N tiles, where units are fewer than blocks; share: blocks left over per key tile.  (Together at most as many as
+  // blocks: a piece each, or the unit's share of the blocks left over, rounded down, where that is more.)
   auto pieces_of = [&](int N, float share) { return max(1, min(N >> a.min_shift, (int)((float)N * share))); };
   // First before[i + 1] = the key tiles of one KV head in the items up to i; then, where there are fewer units than blocks, the
   // same in pieces (one loop for both: its instructions come from memory in most calls).
@@ -809,7 +812,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_chunk_attn(const ChunkParams a,
               const float p0 = fast_exp2(fmaf(s[cb * 32 + j], a.scale_log2, -m_safe));
               const float p1 = fast_exp2(fmaf(s[cb * 32 + j + 1], a.scale_log2, -m_safe));
               sum[(j >> 1) & 3] += p0 + p1;
-              const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: 2^-9 per weight
+              const __nv_bfloat162 pb = __floats2bfloat162_rn(p0, p1);   // the second product's operand type: off by 2^-8 of the weight at most
               pk[j >> 1] = *reinterpret_cast<const uint32_t*>(&pb);
             }
             tmem_st16(tMine + cb * 16, pk);
@@ -1044,7 +1047,7 @@ cudaError_t bc_launch_chunk(const BcMeta& m, const BcGeom& g, const BcChunkArgs&
   p.R = rows ? 1 : height;
   p.align = p.R > 8 ? p.R : 8;
   // Pieces of 8 tiles at least.  4, 8, 16: 512 rows over 1024 entries, 12 / 2 heads, 31.5, 29.0, 30.5 us; 13 rows over 512 18.2, 16.0,
-  // 15.9; 64 x 5 rows over 585, 32 / 8 heads, 49.2, 47.8, 48.1.
+  // 15.9; 64 x 5 rows over 585, 32 / 8 heads, 49.2, 47.8, 48.1.  (12, 2 and 512 units: none of them between 50 and 147.)
   p.min_shift = 3;
   p.wait_limit = a.wait_limit ? a.wait_limit : kWaitLimit;
   p.scale_log2 = a.sm_scale * 1.4426950408889634f;

@@ -16,9 +16,9 @@
 // precision (pos * theta^(-2j/D) reaches 10^5 radians, where single precision has lost the angle), then the sine and
 // cosine of that fraction in fp32.
 //
-// Measured (32 / 8 heads of 128, bf16): 16384 rows 66 us, 6.1 TB/s of the 403 MB moved (0.93 of a copy); the gradient with
-// the weights' of 8192 rows 61 us, 4.6 TB/s (its sums over rows and the second launch, which adds the blocks' sums up, are what
-// a copy does not have); 64 rows of 12 / 2 heads 2.6 us, a launch.
+// Measured (32 / 8 heads of 128, bf16): 16384 rows 66 to 67 us in replays, 6.0 TB/s of the 403 MB moved (0.92 of a
+// copy), 69 us as a call; the gradient with the weights' of 8192 rows 61 us, 4.6 TB/s, 63.5 us as a call (its sums over rows and the
+// second launch, which adds the blocks' sums up, are what a copy does not have); 64 rows of 12 / 2 heads 2.5 us, a launch.
 #include "bc_common.cuh"
 
 namespace {
@@ -363,7 +363,7 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 
 // Few rows: several warps share a row's heads, down to one pass each, until there is a unit for each of the 16 warps per SM;
 // and while that leaves `ahead` passes per unit, until there are about six, so that the last round of units is a small part
-// of the whole (8192 rows of 48 heads, the gradient: 64 us in 3.5 rounds, 57 us in 6.9).
+// of the whole (8192 rows of 48 heads, the gradient: 63.7 us in 3.5 rounds, 60.8 us in 6.9).
 int row_split(int64_t n, int heads, int head_dim, int ahead) {
   const int passes = (heads * (head_dim / 16) + 31) / 32;
   int split = 1;

@@ -26,10 +26,11 @@
 //      which u * mass falls.
 //
 // Measured (T = 0.7; 64 rows of 151,936 bf16 = 19 MB, 3 us at the copy rate): greedy 10 us, temperature alone 24, top-k 50 22,
-// top-k 50 and top-p 0.95 24, top-p 0.95 61; one row: 5, 10, 13, 14, 27 us.  Bounds: for one row the steps' latency (two cluster
-// barriers for temperature alone, five with top-k, seven with top-p, about 1 us each with what is read behind them); for many rows
+// top-k 50 and top-p 0.95 24, top-p 0.95 61 to 66 (by the rows); one row: 5, 10, 13, 14, 30 us.  Bounds: for one row the steps' latency
+// (cluster barriers, that at the end included: three for temperature alone, seven with a small top-k, eight with top-p besides, nine and
+// three per refining histogram with top-p alone; about 1 us each with what is read behind them); for many rows
 // the double-precision weights of all elements (13 us of the 24) and, with top-p alone, three shared-memory atomics for
-// each element of the first 22 octaves (about 25 us of the 61).  Tried for these: weights in single precision from 24
+// each element of the first 22 octaves (about 25 us).  Tried for these: weights in single precision from 24
 // octaves on (the branch costs more than the arithmetic: 87 us); a histogram of counts alone and masses of the few bins that they leave
 // open (96 us, for the same reason).
 #include <cooperative_groups.h>
@@ -770,9 +771,9 @@ extern "C" bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t r
   if ((words & 3) || (reinterpret_cast<uintptr_t>(out) & 7) || (reinterpret_cast<uintptr_t>(logits) & (logits_f32 ? 3 : 1)))
     return BC_ERR_INVALID_ARG;
   if (vocab > kMaxVocab || n > 0x7fffffff / kCluster) return BC_ERR_UNSUPPORTED;
-  // 512 threads where a block has an SM to itself: few rows (8 of 151,936 bf16, top-p: 30 us, with 256 threads 35; 32 rows: 43
-  // and 41), or slices of more than 95 KB (64 rows of 200,000 fp32, top-p: 172 and 213 us; of 151,936: 91 and 90, temperature
-  // alone 38 and 30).
+  // 512 threads where a block has an SM to itself: few rows (8 of 151,936 bf16, top-p: 30 us, with 256 threads 36; 32 rows: 43
+  // and 42), or slices of more than 95 KB (64 rows of 200,000 fp32, top-p: 172 and 211 us; of 151,936: 90 and 89, temperature
+  // alone 39 and 31).
   const bool wide = n * kCluster <= 148 || (int64_t)vocab * (logits_f32 ? 4 : 2) > (int64_t)kCluster * 95 * 1024;
   const auto f = wide ? (logits_f32 ? launch<float, 512> : launch<__nv_bfloat16, 512>)
                                          : (logits_f32 ? launch<float, 256> : launch<__nv_bfloat16, 256>);
