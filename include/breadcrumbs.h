@@ -399,6 +399,34 @@ BC_API bc_status bc_add_rmsnorm(const void* h, const void* delta, const void* we
 BC_API bc_status bc_swiglu(const void* gate_up, int32_t n, int32_t m, void* out, void* stream);
 BC_API bc_status bc_argmax(const void* logits, int32_t n, int32_t vocab, int64_t* out, void* stream);
 
+/* ---- the norms around a block, with its gate and residual scale ------------------------------------
+ * bc_add_rmsnorm for models that also normalise a block's output, gate it or scale it ahead of the residual add, with
+ * rms(v) = 1 / sqrt(mean(v^2) + eps) over the hidden dimension:
+ *   u = x rms(x) post_weight (post_norm != 0), or u = x;   h_out = h + scale gate u, rounded to bf16;
+ *   y = h_out rms(h_out) pre_weight (the mean over the stored bf16 values).
+ * x (the block's output), h (the residual stream), h_out, y [n, hidden] bf16, contiguous; h_out may be h itself; y NULL: not
+ * wanted (the last block).  post_weight, pre_weight [hidden] bf16, NULL = ones; gate bf16, NULL = none, [hidden] with
+ * gate_stride 0 (one vector for all rows) or [n, hidden] with gate_stride = hidden.  Any finite scale; eps >= 0; hidden a multiple
+ * of 8 and <= 8192 (else BC_ERR_UNSUPPORTED); all 16-byte aligned.  fp32 arithmetic, one rounding for each output.
+ * Stateless; one launch, ordinary stream order. */
+BC_API bc_status bc_block_norm(int32_t n, int32_t hidden, const void* x, const void* h, const void* gate, int64_t gate_stride,
+                               int32_t post_norm, const void* post_weight, const void* pre_weight, float scale, float eps,
+                               void* h_out, void* y, void* stream);
+
+/* Its gradient.  From the forward call's x, gate and weights, the h_out it wrote, and the loss's gradients for h_out (dh_out, what
+ * arrives along the residual stream) and y (dy), bf16 [n, hidden], one of which may be NULL (nothing arrives that way), to
+ *   dx, dh [n, hidden] bf16 (dh may be dh_out itself);
+ *   dgate: bf16 [n, hidden] for a gate per element, fp32 [hidden], summed over the rows, for one vector; NULL: not wanted;
+ *   dpost_weight, dpre_weight: fp32 [hidden], summed over the rows; NULL: not wanted (dpost_weight without post_norm must be NULL).
+ * fp32 arithmetic, additions in a fixed order.  workspace: device memory of at least bc_block_norm_query_bytes bytes, 16-byte
+ * aligned, one call at a time (not needed without sums over rows).  Two launches (one without such sums). */
+BC_API bc_status bc_block_norm_query_bytes(int32_t hidden, size_t* workspace_bytes);
+BC_API bc_status bc_block_norm_backward(int32_t n, int32_t hidden, const void* x, const void* h_out, const void* gate,
+                                        int64_t gate_stride, int32_t post_norm, const void* post_weight, const void* pre_weight,
+                                        float scale, float eps, const void* dh_out, const void* dy, void* dx, void* dh, void* dgate,
+                                        float* dpost_weight, float* dpre_weight, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
 /* Sampling of the next token (Algorithm 1 samples from the model's distribution), one token per row from a
  * given uniform random number per row.  For a row x of logits with maximum m, temperature T > 0 and
  * e_j = exp((x_j - m) / T):
@@ -420,6 +448,35 @@ BC_API bc_status bc_argmax(const void* logits, int32_t n, int32_t vocab, int64_t
 BC_API bc_status bc_sample(const void* logits, int32_t logits_f32, int64_t row_stride, int32_t n, int32_t vocab,
                            const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                            const float* uniform, int64_t* out, void* stream);
+
+/* ---- log-probabilities of given tokens ------------------------------------------------------------
+ * What scores a trajectory: per row of logits the log-probability of a given token (a sampled one, the next one of a
+ * stored trajectory), the entropy, and the top_k most likely tokens with their log-probabilities -- laid out as
+ * bc_distill_loss takes a teacher's entries.  For a row x with maximum m and ln s = ln sum_j exp(x_j - m):
+ *   log p_j = (x_j - m) - ln s;   logprob = log p_target;   entropy = - sum_j p_j log p_j;   stats = (m, ln s)
+ *   top_idx: the top_k largest elements, largest first, of equal ones the lowest index first; top_logprob: their log p.
+ * A target outside [0, vocab) means that none is given: logprob 0, and no gradient from it.  -inf and NaN logits have
+ * no mass (log p = -inf; NaN orders as -inf), magnitudes above 2^126 count as 2^126 (so +inf logits share the mass).  A row
+ * without a logit above -2^126 has no distribution: log p = -inf, entropy 0, stats (-inf, 0), gradient 0.
+ * logits: device, n rows of vocab elements, bf16 (logits_f32 == 0) or fp32, row i at logits + i * row_stride elements
+ * (row_stride >= vocab, any value), aligned to the element; targets int64 [n]; logprob, entropy fp32 [n], stats fp32 [n, 2]:
+ * NULL = not wanted (targets may be NULL without logprob); top_idx int32, top_logprob fp32 [n, top_k] (top_k == 0: unused).
+ * top_k <= vocab, and <= 256 and vocab <= 262144 (else BC_ERR_UNSUPPORTED).  fp32 arithmetic, additions in a fixed order.
+ * Stateless; one launch. */
+BC_API bc_status bc_token_logprobs(const void* logits, int32_t logits_f32, int64_t row_stride, int32_t n, int32_t vocab,
+                                   const int64_t* targets, int32_t top_k, float* logprob, float* entropy, float* stats,
+                                   int32_t* top_idx, float* top_logprob, void* stream);
+
+/* Its gradient with respect to the logits, for d_logprob and d_entropy (fp32 [n], the loss's gradients for logprob and
+ * entropy; one of them may be NULL):
+ *   grad_j = d_logprob ([j = target] - p_j) - d_entropy p_j (log p_j + entropy)
+ * in the logits' type, row i at grad + i * grad_row_stride elements (>= vocab; only the vocab elements are written; rows that
+ * lie to 16 bytes as the logits' do are faster).  stats and entropy (may be NULL without d_entropy): what the forward call
+ * wrote for these logits.  grad must not overlap logits unless it is logits itself with the same strides.  No gradient goes
+ * through the alternatives.  One launch. */
+BC_API bc_status bc_token_logprobs_backward(const void* logits, int32_t logits_f32, int64_t row_stride, int32_t n, int32_t vocab,
+                                            const int64_t* targets, const float* stats, const float* entropy, const float* d_logprob,
+                                            const float* d_entropy, void* grad, int64_t grad_row_stride, void* stream);
 
 /* Limits of bc_decode_attn_static. */
 #define BC_STATIC_MAX_BATCH 128   /* sequences per call */
@@ -570,6 +627,43 @@ BC_API bc_status bc_mask_attn_set_wait_limit(uint32_t polls);
 BC_API bc_status bc_mask_attn_status(const void* workspace, int32_t n_seqs, int32_t q_heads, int32_t kv_heads,
                                      int64_t total_prompt, int64_t total_tokens, int64_t total_beacons,
                                      void* stream, int32_t* code);
+
+/* bc_mask_attn_forward that also writes what its gradient needs: lse_tok [sum T, q_heads], lse_beacon [sum nb, q_heads], fp32, the
+ * natural logarithm of every row's sum of exp(sm_scale * <q, K_j>) over the keys it sees.  Everything else is as there, the
+ * outputs included. */
+BC_API bc_status bc_mask_attn_forward_lse(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+                                          const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
+                                          const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
+                                          const void* beacon_q, const void* beacon_k, const void* beacon_v, void* out_tok,
+                                          void* out_beacon, float* lse_tok, float* lse_beacon, float sm_scale, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/* The gradient of the mask form: from the forward call's inputs, its outputs (out_tok, out_beacon, lse_tok, lse_beacon) and the loss's
+ * gradients for the outputs (d_out_tok, d_out_beacon, bf16, laid out like the outputs) to the gradients of every input, bf16, laid out
+ * like the inputs and all written whole (a prompt's K/V summed over every row of the trajectory, a KV head's over its query heads).
+ * Limits as for the forward call; inputs 16-byte aligned, the gradients 32-byte aligned and not overlapping anything else; arrays
+ * without rows may be NULL.  fp32 accumulation; softmax weights and score gradients rounded to bf16 before the second products; no
+ * atomic additions, results are reproducible.  Within one trajectory all inputs must be finite (rows that do not see an entry have
+ * weight 0 on it); nothing spreads from one trajectory to another.
+ * cu_prompt, cu_tokens: HOST int32 [n_seqs + 1] as in the forward call, beginning with 0.  workspace: device memory of at least
+ * bc_mask_attn_backward_query_bytes bytes, 256-byte aligned, one call at a time: work lists, row statistics, and the partial sums of
+ * keys that many rows see.  Asynchronous on `stream`, up to four launches; the host arrays are read before the call returns, so not
+ * inside a stream capture.  A bounded device-side wait that expires is reported by bc_mask_attn_backward_status as
+ * BC_ERR_TIMEOUT (the gradients are then incomplete); bc_mask_attn_backward_set_wait_limit sets the waits' poll limit
+ * (process-wide; 0 = the default) as bc_mask_attn_set_wait_limit does for the forward call. */
+BC_API bc_status bc_mask_attn_backward_query_bytes(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+                                                   const int32_t* cu_prompt, const int32_t* cu_tokens, size_t* workspace_bytes);
+BC_API bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+                                       const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
+                                       const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
+                                       const void* beacon_q, const void* beacon_k, const void* beacon_v, const void* out_tok,
+                                       const void* out_beacon, const float* lse_tok, const float* lse_beacon, const void* d_out_tok,
+                                       const void* d_out_beacon, void* d_prompt_k, void* d_prompt_v, void* d_tok_q, void* d_tok_k,
+                                       void* d_tok_v, void* d_beacon_q, void* d_beacon_k, void* d_beacon_v, float sm_scale,
+                                       void* workspace, size_t workspace_bytes, void* stream);
+BC_API bc_status bc_mask_attn_backward_set_wait_limit(uint32_t polls);
+/* Synchronises `stream` and returns in *code the status the last bc_mask_attn_backward on this workspace left on the device. */
+BC_API bc_status bc_mask_attn_backward_status(const void* workspace, void* stream, int32_t* code);
 
 /* ---- the distillation loss (Section 3.2, Eq. 1) -------------------------------------------------
  * loss = (1 / n_traj) * sum_b (1 / |x_b|) * sum_{positions r of trajectory b} KL_K(teacher_r || student_r),

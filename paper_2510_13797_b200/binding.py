@@ -8,6 +8,7 @@ of `lib()` raises: there is no CPU or PyTorch fallback.
 from __future__ import annotations
 
 import ctypes as C
+import itertools
 import os
 from typing import Optional
 
@@ -97,6 +98,16 @@ SYMBOLS = {
     "bc_chunk_attn": (_I32, [_P, _I32, _P, _P, _P, _I32, _I32, _P, _P, _F, _P]),
     "bc_prefill_chunk": (_I32, [_P, _I32, _P, _P, _P, _I32, _I32, _P, _P, _P, _P, _F, _P]),
     "bc_sample": (_I32, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _P]),
+    "bc_mask_attn_forward_lse": (_I32, [_I32, _I32, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(_I32)] + [_P] * 12 + [_F, _P, C.c_size_t, _P]),
+    "bc_mask_attn_backward_query_bytes": (_I32, [_I32, _I32, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(_I32), C.POINTER(C.c_size_t)]),
+    "bc_mask_attn_backward": (_I32, [_I32, _I32, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(_I32)] + [_P] * 22 + [_F, _P, C.c_size_t, _P]),
+    "bc_mask_attn_backward_set_wait_limit": (_I32, [C.c_uint32]),
+    "bc_mask_attn_backward_status": (_I32, [_P, _P, C.POINTER(_I32)]),
+    "bc_token_logprobs": (_I32, [_P, _I32, _I64, _I32, _I32, _P, _I32, _P, _P, _P, _P, _P, _P]),
+    "bc_token_logprobs_backward": (_I32, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "bc_block_norm": (_I32, [_I32, _I32, _P, _P, _P, _I64, _I32, _P, _P, _F, _F, _P, _P, _P]),
+    "bc_block_norm_query_bytes": (_I32, [_I32, C.POINTER(C.c_size_t)]),
+    "bc_block_norm_backward": (_I32, [_I32, _I32, _P, _P, _P, _I64, _I32, _P, _P, _F, _F] + [_P] * 8 + [C.c_size_t, _P]),
     "bc_kernel_launches": (_I64, [_P]),
     "bc_last_cuda_error": (_I32, [_P]),
     "bc_status_string": (C.c_char_p, [_I32]),
@@ -519,3 +530,166 @@ def bc_sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=N
     _call(where, dev, lib().bc_sample, logits.data_ptr(), 1 if logits.dtype is f32 else 0, row_stride if n > 1 else max(row_stride, vocab), n, vocab,
           _at(temperature), _at(top_k), _at(top_p), _at(min_p), uniform.data_ptr(), res.data_ptr(), s)
     return res
+
+
+def _logit_rows(logits, where):
+    """Rows, vocabulary, row stride and whether 32-bit, of bf16 or fp32 logits whose rows may be strided."""
+    if logits.dim() != 2 or (logits.dtype is not torch.bfloat16 and logits.dtype is not torch.float32):
+        raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    n, vocab = logits.shape
+    stride = logits.stride(0)
+    _require(vocab == 1 or logits.stride(1) == 1, where)
+    return n, vocab, stride if n > 1 else max(stride, vocab), 1 if logits.dtype is torch.float32 else 0
+
+
+def bc_token_logprobs(logits, targets=None, top_k=0, stream=None):
+    """Log-probabilities of given tokens (int64 [n]; outside [0, vocab): none), entropies and the top_k most likely tokens of every row
+    of bf16 or fp32 logits [n, vocab], rows may be strided (breadcrumbs.h): returns (logprob [n] or None, entropy [n], stats [n, 2] for
+    the gradient, top_idx int32 and top_logprob [n, top_k] or None)."""
+    where, f32 = "bc_token_logprobs", torch.float32
+    n, vocab, row_stride, wide = _logit_rows(logits, where)
+    dev, s, other = _on(where, logits, ((targets, torch.int64, (n,)),), stream)
+    logprob = None if targets is None else _new(logits, n, f32, other)
+    entropy = _new(logits, n, f32, other)
+    stats = _new(logits, (n, 2), f32, other)
+    idx, top = (_new(logits, (n, top_k), torch.int32, other), _new(logits, (n, top_k), f32, other)) if top_k > 0 else (None, None)
+    _call(where, dev, lib().bc_token_logprobs, logits.data_ptr(), wide, row_stride, n, vocab, _at(targets), top_k, _at(logprob),
+          entropy.data_ptr(), stats.data_ptr(), _at(idx), _at(top), s)
+    return logprob, entropy, stats, idx, top
+
+
+def bc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_entropy=None, grad=None, stream=None):
+    """Gradient of bc_token_logprobs for d_logprob and d_entropy (fp32 [n], one may be None): returns grad [n, vocab] in the logits' type.
+
+    When not given, grad is allocated with rows that lie to 16 bytes as the logits' rows do, so it may be a view of wider rows."""
+    where, f32 = "bc_token_logprobs_backward", torch.float32
+    n, vocab, row_stride, wide = _logit_rows(logits, where)
+    dev, s, other = _on(where, logits, ((targets, torch.int64, (n,)), (stats, f32, (n, 2)), (entropy, f32, (n,)), (d_logprob, f32, (n,)),
+                                        (d_entropy, f32, (n,))), stream)
+    _require(stats is not None, where)
+    if grad is None:
+        per = 16 // logits.element_size()
+        width = -(-vocab // per) * per if row_stride % per == 0 else (row_stride if row_stride - vocab < per else vocab)
+        grad = _new(logits, (n, width), logits.dtype, other)
+        if width != vocab:
+            grad = grad[:, :vocab]
+    _require(grad.shape == logits.shape and grad.dtype is logits.dtype and grad.get_device() == dev and (vocab == 1 or grad.stride(1) == 1), where)
+    _call(where, dev, lib().bc_token_logprobs_backward, logits.data_ptr(), wide, row_stride, n, vocab, _at(targets), stats.data_ptr(),
+          _at(entropy), _at(d_logprob), _at(d_entropy), grad.data_ptr(), grad.stride(0) if n > 1 else max(grad.stride(0), vocab), s)
+    return grad
+
+
+def _block_norm_tensors(x, h, gate, post_weight, pre_weight, where):
+    if x.dim() != 2 or (gate is not None and gate.dim() not in (1, 2)):
+        raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    n, hidden = x.shape
+    bf16, w = torch.bfloat16, (hidden,)
+    rows = gate is not None and gate.dim() == 2
+    return n, hidden, hidden if rows else 0, ((x, bf16, (n, hidden)), (h, bf16, (n, hidden)), (gate, bf16, (n, hidden) if rows else w),
+                                              (post_weight, bf16, w), (pre_weight, bf16, w))
+
+
+def bc_block_norm(x, h, gate, post_weight, pre_weight, eps, scale=1.0, post_norm=True, h_out=None, y=None, want_y=True, stream=None):
+    """h_out = h + scale * gate * norm(x), y = norm(h_out) (breadcrumbs.h): returns (h_out, y).  x, h [n, hidden] bf16; gate None,
+    [hidden] or [n, hidden]; post_norm False: x is not normalised; weights may be None (ones); h_out may be h; want_y False: y is
+    not computed."""
+    where, bf16 = "bc_block_norm", torch.bfloat16
+    n, hidden, gate_stride, tensors = _block_norm_tensors(x, h, gate, post_weight, pre_weight, where)
+    dev, s, other = _on(where, x, tensors + ((h_out, bf16, (n, hidden)), (y, bf16, (n, hidden))), stream)
+    _require(h is not None, where)
+    ho = _new(x, (n, hidden), bf16, other) if h_out is None else h_out
+    yo = _new(x, (n, hidden), bf16, other) if y is None and want_y else y
+    _call(where, dev, lib().bc_block_norm, n, hidden, x.data_ptr(), h.data_ptr(), _at(gate), gate_stride, 1 if post_norm else 0,
+          _at(post_weight), _at(pre_weight), scale, eps, ho.data_ptr(), _at(yo), s)
+    return ho, yo
+
+
+def bc_block_norm_backward(x, h_out, gate, post_weight, pre_weight, eps, scale, post_norm, dh_out, dy, weight_grads=True, stream=None):
+    """Gradient of bc_block_norm (breadcrumbs.h) from what its h_out and y receive (one may be None): returns (dx, dh [n, hidden] bf16,
+    dgate -- bf16 [n, hidden], fp32 [hidden] for one vector, None without a gate --, dpost_weight, dpre_weight fp32 [hidden] or None).
+
+    weight_grads False: no sums over the rows (dgate of one vector, dpost_weight, dpre_weight)."""
+    where, bf16 = "bc_block_norm_backward", torch.bfloat16
+    n, hidden, gate_stride, tensors = _block_norm_tensors(x, h_out, gate, post_weight, pre_weight, where)
+    dev, s, other = _on(where, x, tensors + ((dh_out, bf16, (n, hidden)), (dy, bf16, (n, hidden))), stream)
+    _require(h_out is not None, where)
+    dx, dh = _new(x, (n, hidden), bf16, other), _new(x, (n, hidden), bf16, other)
+    dgate = _new(x, (n, hidden), bf16, other) if gate_stride else None
+    ws, size, sums = None, C.c_size_t(), (None, None, None)
+    if weight_grads:
+        _check(lib().bc_block_norm_query_bytes(hidden, C.byref(size)), "bc_block_norm_query_bytes")
+        # the sums over rows and the scratch in one allocation
+        ws = _new(x, 3 * hidden + size.value // 4, torch.float32, other)
+        vector = gate is not None and not gate_stride
+        sums = (ws[:hidden] if vector else None, ws[hidden:2 * hidden] if post_norm else None, ws[2 * hidden:3 * hidden])
+    _call(where, dev, lib().bc_block_norm_backward, n, hidden, x.data_ptr(), h_out.data_ptr(), _at(gate), gate_stride, 1 if post_norm else 0,
+          _at(post_weight), _at(pre_weight), scale, eps, _at(dh_out), _at(dy), dx.data_ptr(), dh.data_ptr(),
+          _at(dgate if dgate is not None else sums[0]), _at(sums[1]), _at(sums[2]), None if ws is None else ws.data_ptr() + 12 * hidden,
+          size.value, s)
+    return dx, dh, dgate if dgate is not None else sums[0], sums[1], sums[2]
+
+
+def _mask_inputs(where, prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k, beacon_v):
+    """Head counts, prefix sums, the number of beacons, and the inputs with their dtypes and shapes."""
+    _require(tok_q is not None and tok_k is not None and tok_q.dim() == 3 and tok_k.dim() == 3 and len(prompt_lens) == len(token_lens) and len(token_lens) > 0 and c >= 1, where)
+    n, bf16 = len(prompt_lens), torch.bfloat16
+    q_heads, kv_heads, head_dim = tok_q.shape[1], tok_k.shape[1], tok_q.shape[2]
+    cu = [(C.c_int32 * (n + 1))(0, *itertools.accumulate(lens)) for lens in (prompt_lens, token_lens)]
+    total_b = sum(t // c for t in token_lens) if c > 1 else 0
+    q, kv = (lambda rows: (rows, q_heads, head_dim)), (lambda rows: (rows, kv_heads, head_dim))
+    P, T = cu[0][n], cu[1][n]
+    none = lambda t, rows: None if t is None and rows == 0 else t
+    need = ((none(prompt_k, P), kv(P)), (none(prompt_v, P), kv(P)), (tok_q, q(T)), (tok_k, kv(T)), (tok_v, kv(T)), (none(beacon_q, total_b), q(total_b)),
+            (none(beacon_k, total_b), kv(total_b)), (none(beacon_v, total_b), kv(total_b)))
+    for t, shape in need:
+        _require(t is not None or shape[0] == 0, where)
+    return n, q_heads, kv_heads, head_dim, cu, total_b, tuple((t, bf16, shape) for t, shape in need)
+
+
+def bc_mask_attn_forward_lse(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k, beacon_v, sm_scale,
+                             stream=None, check=True):
+    """bc_mask_attn_forward that also returns what the gradient needs (breadcrumbs.h): (out_tok, out_beacon, lse_tok [sum T, q_heads] fp32,
+    lse_beacon)."""
+    where = "bc_mask_attn_forward_lse"
+    n, hq, hk, d, cu, total_b, inputs = _mask_inputs(where, prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k,
+                                                     beacon_v)
+    dev, s, other = _on(where, tok_q, inputs, stream)
+    size = C.c_size_t()
+    _check(lib().bc_mask_attn_query_bytes(n, hq, hk, d, cu[0][n], cu[1][n], total_b, C.byref(size)), "bc_mask_attn_query_bytes")
+    ws = _new(tok_q, size.value, torch.uint8, other)
+    out = [_new(tok_q, (rows, hq, d), tok_q.dtype, other) for rows in (cu[1][n], total_b)]
+    lse = [_new(tok_q, (rows, hq), torch.float32, other) for rows in (cu[1][n], total_b)]
+    _call(where, dev, lib().bc_mask_attn_forward_lse, n, hq, hk, d, c, cu[0], cu[1], *[_at(t) for t, _, _ in inputs], _at(out[0]), _at(out[1]),
+          _at(lse[0]), _at(lse[1]), sm_scale, _at(ws), size.value, s)
+    if check:
+        code = C.c_int32()
+        _call("bc_mask_attn_status", dev, lib().bc_mask_attn_status, _at(ws), n, hq, hk, cu[0][n], cu[1][n], total_b, s, C.byref(code))
+        _check(code.value, where + " (device)")
+    return out[0], out[1], lse[0], lse[1]
+
+
+def bc_mask_attn_backward(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k, beacon_v, out_tok, out_beacon,
+                          lse_tok, lse_beacon, d_out_tok, d_out_beacon, sm_scale, stream=None, check=True):
+    """Gradient of the mask form (breadcrumbs.h) from the forward call's inputs and results (bc_mask_attn_forward_lse) and the gradients of
+    its two outputs: returns (d_prompt_k, d_prompt_v, d_tok_q, d_tok_k, d_tok_v, d_beacon_q, d_beacon_k, d_beacon_v), bf16, laid out
+    like the inputs.  check: waits for the result and raises if a device-side wait ran out."""
+    where, bf16, f32 = "bc_mask_attn_backward", torch.bfloat16, torch.float32
+    n, hq, hk, d, cu, total_b, inputs = _mask_inputs(where, prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k,
+                                                     beacon_v)
+    T = cu[1][n]
+    _require(all(t is not None for t in (out_tok, lse_tok, d_out_tok) if T) and all(t is not None for t in (out_beacon, lse_beacon, d_out_beacon) if total_b),
+             where)
+    more = ((out_tok, bf16, (T, hq, d)), (out_beacon, bf16, (total_b, hq, d)), (lse_tok, f32, (T, hq)), (lse_beacon, f32, (total_b, hq)),
+            (d_out_tok, bf16, (T, hq, d)), (d_out_beacon, bf16, (total_b, hq, d)))
+    dev, s, other = _on(where, tok_q, inputs + more, stream)
+    size = C.c_size_t()
+    _check(lib().bc_mask_attn_backward_query_bytes(n, hq, hk, d, c, cu[0], cu[1], C.byref(size)), "bc_mask_attn_backward_query_bytes")
+    ws = _new(tok_q, size.value, torch.uint8, other)
+    grads = [_new(tok_q, shape, bf16, other) for _, _, shape in inputs]
+    _call(where, dev, lib().bc_mask_attn_backward, n, hq, hk, d, c, cu[0], cu[1], *[_at(t) for t, _, _ in inputs + more], *[_at(t) for t in grads],
+          sm_scale, _at(ws), size.value, s)
+    if check:
+        code = C.c_int32()
+        _call("bc_mask_attn_backward_status", dev, lib().bc_mask_attn_backward_status, _at(ws), s, C.byref(code))
+        _check(code.value, where + " (device)")
+    return tuple(grads)

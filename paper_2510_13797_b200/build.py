@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libbreadcrumbs.so")
 SOURCES = ["bc_api.cu", "bc_book.cu", "bc_attn.cu", "bc_mask_attn.cu", "bc_distill.cu", "bc_rope.cu", "bc_model_ops.cu",
-           "bc_norm_rope.cu", "bc_chunk.cu", "bc_sample.cu"]
+           "bc_norm_rope.cu", "bc_chunk.cu", "bc_sample.cu", "bc_logprobs.cu", "bc_block_norm.cu",
+           "bc_mask_grad.cu"]
 
 
 def _nvcc():

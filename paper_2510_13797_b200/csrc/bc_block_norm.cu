@@ -1,0 +1,368 @@
+// The norms around a block of a decoder layer, fused with its gate and the residual add, and their gradient.
+//
+// x: the block's output, h: the residual stream, g: the gate (one vector, a value per element, or none), s: a scale;
+// rms(v) = 1 / sqrt(mean(v^2) + eps) over the hidden dimension:
+//     u  = x rms(x) w_post    (or x, for a block without a norm behind it)
+//     h' = h + s g u          (rounded to bf16: the residual stream as it is stored)
+//     y  = h' rms(h') w_pre   (the next block's input)
+// and with a = d loss / d h' (from the stream), b = d loss / d y, r2 = rms(h'), r1 = rms(x), means over the hidden dimension:
+//     dH = a + r2 (w_pre b - h' r2^2 mean(h' w_pre b))                     -> the gradient of h, and of what was added to it
+//     du = s g dH,   dg = s u dH,   dx = r1 (w_post du - x r1^2 mean(x w_post du))     (or du)
+//     dw_pre = sum over rows of b h' r2,   dw_post = sum over rows of du x r1.
+// All of it is bound by memory: 8 bytes an element forward, 12 for the gradient, 2 and 4 more with a gate per element.
+#include "bc_common.cuh"
+
+namespace {
+
+constexpr int kMaxHidden = 8192;
+constexpr int kMaxThreads = 512;
+
+__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
+  f[0] = bf_lo(v.x); f[1] = bf_hi(v.x); f[2] = bf_lo(v.y); f[3] = bf_hi(v.y);
+  f[4] = bf_lo(v.z); f[5] = bf_hi(v.z); f[6] = bf_lo(v.w); f[7] = bf_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+// A row belongs to `warps` warps of a block (all of it to one warp for up to 256 elements), chunk j of 8 elements to thread
+// j % (32 warps) of them; a block works on blockDim / (32 warps) rows at a time.
+struct NormArgs {
+  const uint4 *x, *h, *gate, *post_weight, *pre_weight;   // weights NULL: ones; gate NULL: none
+  uint4 *h_out, *y;                                       // y NULL: not wanted
+  int64_t n;
+  int chunks, warps;
+  int64_t gate_chunks;                                    // from one row's gate to the next one's; 0: one vector
+  int post;
+  float scale, inv_hidden, eps;
+};
+
+// Sum over the threads of a row, in a fixed order.  `part`: kMaxThreads / 32 floats of shared memory; two barriers when the row has
+// more than one warp.
+__device__ __forceinline__ float row_sum(float v, int warps, float* part) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  if (warps == 1) return v;
+  const int warp = threadIdx.x >> 5, first = warp / warps * warps;
+  if ((threadIdx.x & 31) == 0) part[warp] = v;
+  __syncthreads();
+  v = 0.f;
+  for (int i = 0; i < warps; ++i) v += part[first + i];
+  __syncthreads();
+  return v;
+}
+
+template <int K>
+__global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
+  __shared__ float part[kMaxThreads / 32];
+  const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
+  const int64_t row = (int64_t)blockIdx.x * rows + slot;
+  const bool live = row < a.n;                            // the threads of a row past the end stay for the barriers
+  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), zero = make_uint4(0, 0, 0, 0);
+  uint4 xs[K], hs[K], gs[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = j0 + k * per_row;
+    const bool in = live && j < a.chunks;
+    xs[k] = in ? __ldcs(a.x + row * a.chunks + j) : zero;
+    hs[k] = in ? __ldcs(a.h + row * a.chunks + j) : zero;
+    gs[k] = in && a.gate ? a.gate[row * a.gate_chunks + j] : ones;
+  }
+  float r1 = 1.f;
+  if (a.post) {
+    float sq = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float x[8];
+      unpack8(xs[k], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
+    }
+    r1 = rsqrtf(row_sum(sq, a.warps, part) * a.inv_hidden + a.eps);
+  }
+  float sq = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = j0 + k * per_row;
+    float x[8], h[8], g[8], w[8];
+    unpack8(xs[k], x); unpack8(hs[k], h); unpack8(gs[k], g);
+    unpack8(a.post && a.post_weight && j < a.chunks ? a.post_weight[j] : ones, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = fmaf(a.scale * g[i], x[i] * r1 * w[i], h[i]);
+    hs[k] = pack8(h);
+    if (live && j < a.chunks) a.h_out[row * a.chunks + j] = hs[k];
+    unpack8(hs[k], h);                                    // the norm sees the stream as it is stored
+    if (j < a.chunks)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sq = fmaf(h[i], h[i], sq);
+  }
+  if (a.y == nullptr) return;
+  const float r2 = rsqrtf(row_sum(sq, a.warps, part) * a.inv_hidden + a.eps);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = j0 + k * per_row;
+    if (live && j < a.chunks) {
+      float h[8], w[8];
+      unpack8(hs[k], h);
+      unpack8(a.pre_weight ? a.pre_weight[j] : ones, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] = h[i] * r2 * w[i];
+      a.y[row * a.chunks + j] = pack8(h);
+    }
+  }
+}
+
+struct NormGradArgs {
+  const uint4 *x, *h, *gate, *post_weight, *pre_weight, *dh_out, *dy;   // dh_out, dy: NULL where nothing arrives that way
+  uint4 *dx, *dh, *dgate;                                 // dgate: of a gate per element (NULL: not wanted)
+  float* partial;                                         // [blocks][3][8 chunks]: sums for w_pre, w_post, the gate vector; NULL: not wanted
+  int64_t n;
+  int chunks, warps;
+  int64_t gate_chunks;
+  int post, sum_gate;
+  float scale, inv_hidden, eps;
+};
+
+// The three sums a row needs beside its two squares follow from one pass, since dH is linear in them:
+//     mean(x v dH) with v = s g w_post:   sum(x v a) + r2 (sum(x v b') - r2^2 mean(h' b') sum(x v h')),   b' = w_pre b.
+// A thread has the same columns of every row it meets, so the weights' gradients are sums in its registers; after kFold rows
+// they go to the block's sums in memory and begin again, so that no chain of additions grows with the number of rows but that of
+// the folds.  A second kernel adds the blocks' sums, all in a fixed order.
+constexpr int kFold = 64;
+template <int K>
+__global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradArgs a) {
+  __shared__ float part[2][6][kMaxThreads / 32];
+  const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp / a.warps * a.warps;
+  const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), zero = make_uint4(0, 0, 0, 0);
+  const bool weights = a.partial != nullptr;
+  uint4 wpost[K], wpre[K];
+  float dpre[K][8], dpost[K][8], dgate[K][8];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = j0 + k * per_row;
+    wpost[k] = a.post && a.post_weight && j < a.chunks ? a.post_weight[j] : ones;
+    wpre[k] = a.pre_weight && j < a.chunks ? a.pre_weight[j] : ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dpre[k][i] = dpost[k][i] = dgate[k][i] = 0.f;
+  }
+  const int64_t step = (int64_t)gridDim.x * rows;
+  int left = kFold, turn = 0;
+  bool begun = false;
+  for (int64_t row0 = (int64_t)blockIdx.x * rows; row0 < a.n; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + slot;
+    const bool live = row < a.n;
+    uint4 xs[K], hs[K], as[K], bs[K], gs[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int j = j0 + k * per_row;
+      const bool in = live && j < a.chunks;
+      const int64_t at = row * a.chunks + j;
+      xs[k] = in ? __ldcs(a.x + at) : zero;
+      hs[k] = in ? __ldcs(a.h + at) : zero;
+      as[k] = in && a.dh_out ? __ldcs(a.dh_out + at) : zero;
+      bs[k] = in && a.dy ? __ldcs(a.dy + at) : zero;
+      gs[k] = in && a.gate ? a.gate[row * a.gate_chunks + j] : ones;
+    }
+    float sum[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};        // h'^2, h' b', x^2, x v a, x v b', x v h'
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8];
+      unpack8(xs[k], x); unpack8(hs[k], h); unpack8(as[k], da); unpack8(bs[k], b); unpack8(gs[k], g);
+      unpack8(wpost[k], w1); unpack8(wpre[k], w2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float bw = b[i] * w2[i], xv = x[i] * (a.scale * g[i] * w1[i]);
+        sum[0] = fmaf(h[i], h[i], sum[0]); sum[1] = fmaf(h[i], bw, sum[1]); sum[2] = fmaf(x[i], x[i], sum[2]);
+        sum[3] = fmaf(xv, da[i], sum[3]); sum[4] = fmaf(xv, bw, sum[4]); sum[5] = fmaf(xv, h[i], sum[5]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 6; ++i)
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], d);
+    if (a.warps > 1) {
+      if (lane < 6) {
+        float v = sum[0];
+#pragma unroll
+        for (int i = 1; i < 6; ++i) v = lane == i ? sum[i] : v;
+        part[turn][lane][warp] = v;
+      }
+      __syncthreads();                                    // the other half of `part` is written next: one barrier per round
+#pragma unroll
+      for (int i = 0; i < 6; ++i) {
+        sum[i] = 0.f;
+        for (int w = 0; w < a.warps; ++w) sum[i] += part[turn][i][first + w];
+      }
+    }
+    // the means are brought down by one factor r at a time: r^3 alone would vanish for large rows
+    const float r2 = rsqrtf(sum[0] * a.inv_hidden + a.eps), c2 = r2 * (r2 * (r2 * (sum[1] * a.inv_hidden)));
+    const float r1 = a.post ? rsqrtf(sum[2] * a.inv_hidden + a.eps) : 1.f;
+    const float c1 = a.post ? r1 * (r1 * (r1 * ((sum[3] + r2 * sum[4] - c2 * sum[5]) * a.inv_hidden))) : 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int j = j0 + k * per_row;
+      if (!live || j >= a.chunks) continue;
+      float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8], ox[8], oh[8], og[8];
+      unpack8(xs[k], x); unpack8(hs[k], h); unpack8(as[k], da); unpack8(bs[k], b); unpack8(gs[k], g);
+      unpack8(wpost[k], w1); unpack8(wpre[k], w2);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float dh = da[i] + fmaf(r2, b[i] * w2[i], -c2 * h[i]);
+        const float u = x[i] * r1, sd = a.scale * dh, du = sd * g[i];
+        oh[i] = dh;
+        ox[i] = fmaf(r1, du * w1[i], -c1 * x[i]);
+        og[i] = sd * (u * w1[i]);
+        dpre[k][i] = fmaf(b[i], h[i] * r2, dpre[k][i]);
+        dpost[k][i] = fmaf(du, u, dpost[k][i]);
+        dgate[k][i] += og[i];
+      }
+      const int64_t at = row * a.chunks + j;
+      __stcs(a.dx + at, pack8(ox));
+      __stcs(a.dh + at, pack8(oh));
+      if (a.dgate) __stcs(a.dgate + at, pack8(og));
+    }
+    if (weights && (--left == 0 || row0 + step >= a.n)) {
+      left = kFold;
+      // the block's sums of this slot of rows
+      float* mine = a.partial + ((int64_t)blockIdx.x * rows + slot) * 3 * a.chunks * 8;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int j = j0 + k * per_row;
+        if (j >= a.chunks) continue;
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          if ((t == 1 && !a.post) || (t == 2 && !a.sum_gate)) continue;
+          float* acc = t == 0 ? dpre[k] : (t == 1 ? dpost[k] : dgate[k]);
+          float4* to = reinterpret_cast<float4*>(mine + ((int64_t)t * a.chunks + j) * 8);
+          float4 lo = make_float4(acc[0], acc[1], acc[2], acc[3]), hi = make_float4(acc[4], acc[5], acc[6], acc[7]);
+          if (begun) {
+            const float4 l = to[0], u = to[1];
+            lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
+            hi.x += u.x; hi.y += u.y; hi.z += u.z; hi.w += u.w;
+          }
+          to[0] = lo; to[1] = hi;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+        }
+      }
+      begun = true;
+    }
+  }
+}
+
+// Adds the blocks' sums: a block has 32 columns, 32 threads per column.
+__global__ void __launch_bounds__(1024) k_block_norm_weights(const float* __restrict__ partial, int parts, int hidden, float* __restrict__ dpre,
+                                                            float* __restrict__ dpost, float* __restrict__ dgate) {
+  __shared__ float sh[32][33];
+  float* dst = blockIdx.y == 0 ? dpre : (blockIdx.y == 1 ? dpost : dgate);
+  if (dst == nullptr) return;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + lane;
+  float t = 0.f;
+  if (col < hidden)
+    for (int p = grp; p < parts; p += 32) t += partial[((int64_t)p * 3 + blockIdx.y) * hidden + col];
+  sh[grp][lane] = t;
+  __syncthreads();
+  if (grp == 0 && col < hidden) {
+#pragma unroll
+    for (int g = 1; g < 32; ++g) t += sh[g][lane];
+    dst[col] = t;
+  }
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+struct Shape {
+  int chunks, warps, rows, threads, k;
+};
+Shape shape_of(int hidden) {
+  Shape s;
+  s.chunks = hidden / 8;
+  const int warps = (s.chunks + 31) / 32;
+  s.warps = warps < kMaxThreads / 32 ? warps : kMaxThreads / 32;
+  s.k = (s.chunks + s.warps * 32 - 1) / (s.warps * 32);
+  s.rows = kMaxThreads / 32 / s.warps;
+  s.threads = s.rows * s.warps * 32;
+  return s;
+}
+constexpr int kGradBlocks = 148;
+
+bc_status check(int64_t n, int32_t hidden, const void* x, const void* h, const void* gate, int64_t gate_stride, const void* post_weight,
+                const void* pre_weight, float scale, float eps) {
+  if (n <= 0 || hidden <= 0 || !x || !h || !(eps >= 0.f) || !(scale - scale == 0.f)) return BC_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(h) || !aligned16(gate) || !aligned16(post_weight) || !aligned16(pre_weight)) return BC_ERR_INVALID_ARG;
+  if (gate && gate_stride != 0 && gate_stride != hidden) return BC_ERR_INVALID_ARG;
+  if (hidden % 8 || hidden > kMaxHidden) return BC_ERR_UNSUPPORTED;
+  return BC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+bc_status bc_block_norm(int32_t n, int32_t hidden, const void* x, const void* h, const void* gate, int64_t gate_stride,
+                        int32_t post_norm, const void* post_weight, const void* pre_weight, float scale, float eps, void* h_out, void* y,
+                        void* stream) {
+  const bc_status st = check(n, hidden, x, h, gate, gate_stride, post_weight, pre_weight, scale, eps);
+  if (st) return st;
+  if (!h_out || !aligned16(h_out) || !aligned16(y)) return BC_ERR_INVALID_ARG;
+  const Shape s = shape_of(hidden);
+  NormArgs a;
+  a.x = (const uint4*)x; a.h = (const uint4*)h; a.gate = (const uint4*)gate;
+  a.post_weight = (const uint4*)post_weight; a.pre_weight = (const uint4*)pre_weight;
+  a.h_out = (uint4*)h_out; a.y = (uint4*)y;
+  a.n = n; a.chunks = s.chunks; a.warps = s.warps; a.gate_chunks = gate_stride / 8; a.post = post_norm != 0;
+  a.scale = scale; a.inv_hidden = 1.f / (float)hidden; a.eps = eps;
+  const unsigned blocks = (unsigned)(((int64_t)n + s.rows - 1) / s.rows);
+  if (s.k == 1) k_block_norm<1><<<blocks, s.threads, 0, (cudaStream_t)stream>>>(a);
+  else k_block_norm<2><<<blocks, s.threads, 0, (cudaStream_t)stream>>>(a);
+  return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+
+bc_status bc_block_norm_query_bytes(int32_t hidden, size_t* workspace_bytes) {
+  if (!workspace_bytes || hidden <= 0) return BC_ERR_INVALID_ARG;
+  if (hidden % 8 || hidden > kMaxHidden) return BC_ERR_UNSUPPORTED;
+  *workspace_bytes = (size_t)kGradBlocks * shape_of(hidden).rows * 3 * hidden * sizeof(float);
+  return BC_OK;
+}
+
+bc_status bc_block_norm_backward(int32_t n, int32_t hidden, const void* x, const void* h_out, const void* gate, int64_t gate_stride,
+                                 int32_t post_norm, const void* post_weight, const void* pre_weight, float scale, float eps,
+                                 const void* dh_out, const void* dy, void* dx, void* dh, void* dgate, float* dpost_weight,
+                                 float* dpre_weight, void* workspace, size_t workspace_bytes, void* stream) {
+  const bc_status st = check(n, hidden, x, h_out, gate, gate_stride, post_weight, pre_weight, scale, eps);
+  if (st) return st;
+  const bool vector = gate && gate_stride == 0;
+  if ((!dh_out && !dy) || !dx || !dh || !aligned16(dh_out) || !aligned16(dy) || !aligned16(dx) || !aligned16(dh) || !aligned16(dgate) ||
+      !aligned16(workspace) || (dgate && !gate) || (dpost_weight && !post_norm) ||
+      ((reinterpret_cast<uintptr_t>(dpost_weight) | reinterpret_cast<uintptr_t>(dpre_weight)) & 3))
+    return BC_ERR_INVALID_ARG;
+  const Shape s = shape_of(hidden);
+  const bool sums = dpost_weight || dpre_weight || (vector && dgate);
+  if (sums && (!workspace || workspace_bytes < (size_t)kGradBlocks * s.rows * 3 * hidden * sizeof(float))) return BC_ERR_INVALID_ARG;
+  NormGradArgs a;
+  a.x = (const uint4*)x; a.h = (const uint4*)h_out; a.gate = (const uint4*)gate;
+  a.post_weight = (const uint4*)post_weight; a.pre_weight = (const uint4*)pre_weight;
+  a.dh_out = (const uint4*)dh_out; a.dy = (const uint4*)dy;
+  a.dx = (uint4*)dx; a.dh = (uint4*)dh; a.dgate = vector ? nullptr : (uint4*)dgate;
+  a.partial = sums ? (float*)workspace : nullptr;
+  a.n = n; a.chunks = s.chunks; a.warps = s.warps; a.gate_chunks = gate_stride / 8; a.post = post_norm != 0; a.sum_gate = vector && dgate;
+  a.scale = scale; a.inv_hidden = 1.f / (float)hidden; a.eps = eps;
+  const int64_t want = ((int64_t)n + s.rows - 1) / s.rows;
+  const int blocks = (int)(want < kGradBlocks ? want : kGradBlocks);
+  if (s.k == 1) k_block_norm_grad<1><<<blocks, s.threads, 0, (cudaStream_t)stream>>>(a);
+  else k_block_norm_grad<2><<<blocks, s.threads, 0, (cudaStream_t)stream>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return BC_ERR_CUDA;
+  if (!sums) return BC_OK;
+  k_block_norm_weights<<<dim3((unsigned)((hidden + 31) / 32), 3), 1024, 0, (cudaStream_t)stream>>>(
+      a.partial, blocks * s.rows, hidden, dpre_weight, dpost_weight, vector ? (float*)dgate : nullptr);
+  return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -87,6 +87,7 @@ struct MaskArgs {
   const TileDesc* tiles;   // sequence by sequence, heaviest query tiles of a sequence first
   int32_t n_items;         // tiles x kv_heads; item i = (tile i / kv_heads, head i % kv_heads)
   __nv_bfloat16 *out_tok, *out_bea;
+  float *lse_tok, *lse_bea;   // LSE instantiation: logarithm of every row's sum, [rows][Hq]
   int32_t* status;     // device int: first error code
   int32_t Hq, Hkv, G, c, rows_per_tile;  // rows_per_tile = tokens per query tile = 128 / G
   float scale_log2;
@@ -113,7 +114,7 @@ struct MaskArgs {
 //   bar_s: completion t = S of tile t is ready (and every earlier product has finished)
 //   bar_p: the 128 row threads have stored P of tile t                bar_o: P V of a tile has completed
 //   bar_f: completion e = O of item e is final                       bar_e: the rows have read O of item e
-template <bool SHORTW>
+template <bool SHORTW, bool LSE>
 __global__ void __launch_bounds__(kThreads, 2) k_mask_attn(const MaskArgs a, const __grid_constant__ MaskMaps maps) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -438,6 +439,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_mask_attn(const MaskArgs a, con
       mbar_arrive_cta(bar_e);
       if (row_valid) {
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+        if (LSE)   // every row sees itself at least, so the sum is positive
+          (td.kind == 0 ? a.lse_tok + (int64_t)(td.tok_row + my_idx) * Hq : a.lse_bea + (int64_t)(td.bea_row + my_idx) * Hq)[kvh * G + my_head] =
+              (m_ref + log2f(l_run)) * 0.6931471805599453f;
         __nv_bfloat16* dst = (td.kind == 0 ? a.out_tok + (int64_t)(td.tok_row + my_idx) * Hq * kD
                                            : a.out_bea + (int64_t)(td.bea_row + my_idx) * Hq * kD) +
                              (int64_t)(kvh * G + my_head) * kD;
@@ -506,27 +510,12 @@ int sm_count() {
   return n;
 }
 
-}  // namespace
-
-extern "C" {
-
-bc_status bc_mask_attn_query_bytes(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                                   int64_t total_prompt, int64_t total_tokens, int64_t total_beacons,
-                                   size_t* workspace_bytes) {
-  if (!workspace_bytes || n_seqs < 1 || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads || total_prompt < 0 ||
-      total_tokens < 0 || total_beacons < 0)
-    return BC_ERR_INVALID_ARG;
-  if (head_dim != kD || q_heads / kv_heads > 16) return BC_ERR_UNSUPPORTED;
-  *workspace_bytes = mask_layout(n_seqs, q_heads, kv_heads, total_tokens, total_beacons).total;
-  return BC_OK;
-}
-
-bc_status bc_mask_attn_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+bc_status mask_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
                                const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
                                const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
                                const void* beacon_q, const void* beacon_k, const void* beacon_v, void* out_tok,
-                               void* out_beacon, float sm_scale, void* workspace, size_t workspace_bytes,
-                               void* stream) {
+                               void* out_beacon, float* lse_tok, float* lse_beacon, bool lse, float sm_scale, void* workspace,
+                               size_t workspace_bytes, void* stream) {
   if (n_seqs < 1 || !cu_prompt || !cu_tokens || c < 1 || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads || !workspace)
     return BC_ERR_INVALID_ARG;
   if (head_dim != kD || q_heads / kv_heads > 16) return BC_ERR_UNSUPPORTED;
@@ -541,6 +530,9 @@ bc_status bc_mask_attn_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads
   }
   if ((total_prompt && (!prompt_k || !prompt_v)) || (total_tokens && (!tok_q || !tok_k || !tok_v || !out_tok)) ||
       (total_beacons && (!beacon_q || !beacon_k || !beacon_v || !out_beacon)))
+    return BC_ERR_INVALID_ARG;
+  if (lse && ((total_tokens && !lse_tok) || (total_beacons && !lse_beacon) ||
+              ((reinterpret_cast<uintptr_t>(lse_tok) | reinterpret_cast<uintptr_t>(lse_beacon)) & 3)))
     return BC_ERR_INVALID_ARG;
   const MaskLayout l = mask_layout(n_seqs, q_heads, kv_heads, total_tokens, total_beacons);
   if (workspace_bytes < l.total) return BC_ERR_INVALID_ARG;
@@ -579,14 +571,15 @@ bc_status bc_mask_attn_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads
   a.tiles = reinterpret_cast<const TileDesc*>(ws + l.tiles);
   a.n_items = (int32_t)tiles.size() * kv_heads;
   a.out_tok = (__nv_bfloat16*)out_tok; a.out_bea = (__nv_bfloat16*)out_beacon;
+  a.lse_tok = lse_tok; a.lse_bea = lse_beacon;
   a.status = reinterpret_cast<int32_t*>(ws + l.status);
   a.Hq = q_heads; a.Hkv = kv_heads; a.G = G; a.c = c; a.rows_per_tile = per;
   a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.wait_limit = g_mask_wait_limit ? g_mask_wait_limit : kWaitLimit;
   const int smem_bytes = 3 * kOperandBytes + 1024;
   const bool shortw = g_mask_wait_limit != 0;
-  if (cudaFuncSetAttribute(shortw ? k_mask_attn<true> : k_mask_attn<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes) != cudaSuccess)
-    return BC_ERR_CUDA;
+  auto* kernel = lse ? (shortw ? k_mask_attn<true, true> : k_mask_attn<false, true>) : (shortw ? k_mask_attn<true, false> : k_mask_attn<false, false>);
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes) != cudaSuccess) return BC_ERR_CUDA;
   if (!encode_tiled()) return BC_ERR_CUDA;
   MaskMaps maps;
   const void* dummy = ws;   // arrays that do not exist (no prompt, no beacons) get a map that is never used
@@ -600,9 +593,43 @@ bc_status bc_mask_attn_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads
             map_3d(&maps.v_bea, beacon_v ? beacon_v : dummy, kv_heads, total_beacons, 1, kTile);
   if (!ok) return BC_ERR_CUDA;
   const int grid = a.n_items < 2 * sm_count() ? a.n_items : 2 * sm_count();   // two resident blocks per SM
-  if (shortw) k_mask_attn<true><<<grid, kThreads, smem_bytes, s>>>(a, maps);
-  else k_mask_attn<false><<<grid, kThreads, smem_bytes, s>>>(a, maps);
+  kernel<<<grid, kThreads, smem_bytes, s>>>(a, maps);
   return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+bc_status bc_mask_attn_query_bytes(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                                   int64_t total_prompt, int64_t total_tokens, int64_t total_beacons,
+                                   size_t* workspace_bytes) {
+  if (!workspace_bytes || n_seqs < 1 || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads || total_prompt < 0 ||
+      total_tokens < 0 || total_beacons < 0)
+    return BC_ERR_INVALID_ARG;
+  if (head_dim != kD || q_heads / kv_heads > 16) return BC_ERR_UNSUPPORTED;
+  *workspace_bytes = mask_layout(n_seqs, q_heads, kv_heads, total_tokens, total_beacons).total;
+  return BC_OK;
+}
+
+bc_status bc_mask_attn_forward(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+                               const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
+                               const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
+                               const void* beacon_q, const void* beacon_k, const void* beacon_v, void* out_tok,
+                               void* out_beacon, float sm_scale, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  return mask_forward(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q,
+                      beacon_k, beacon_v, out_tok, out_beacon, nullptr, nullptr, false, sm_scale, workspace, workspace_bytes, stream);
+}
+
+bc_status bc_mask_attn_forward_lse(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
+                                   const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
+                                   const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
+                                   const void* beacon_q, const void* beacon_k, const void* beacon_v, void* out_tok,
+                                   void* out_beacon, float* lse_tok, float* lse_beacon, float sm_scale, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  return mask_forward(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q,
+                      beacon_k, beacon_v, out_tok, out_beacon, lse_tok, lse_beacon, true, sm_scale, workspace, workspace_bytes, stream);
 }
 
 bc_status bc_mask_attn_set_wait_limit(uint32_t polls) {
