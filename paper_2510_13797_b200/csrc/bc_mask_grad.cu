@@ -6,14 +6,14 @@
 // Nothing of size rows x keys is stored: S and dP = dO V^T are computed again from tiles.  Two kernels share that work, so
 // that every gradient is added up by one block in a fixed order and no atomic operation is needed (seven products instead
 // of five; the results are reproducible):
-//   k_dkv  one item per tile of 128 keys and KV head; walks the query tiles (64 rows = 64 / G tokens or beacons times the G
+//   k_dkv  one item per tile of 128 keys and KV head; walks the query tiles (128 rows = 128 / G tokens or beacons times the G
 //          query heads of the KV head) that see any of its keys.  Transposed: S^T = K Q^T and dP^T = V dO^T (keys are the
 //          rows of tensor memory), then P^T and dS^T, bf16, go back to tensor memory as the first operands of
 //          dV += P^T dO and dK += dS^T Q, so the heads of a group are added up in the accumulator.
-//   k_dq   one item per 256 query rows in two groups of 128, which share tiles of 64 keys: S = Q K^T, dP = dO V^T,
-//          dS in tensor memory as the first operand of dQ += dS K.
-// Both: one block per SM; a copy warp (tensor copies into a ring), a product warp, and two groups of four warps that turn S
-// and dP into P and dS, one tile each in turn, so that the tensor pipe has the other tile's products to run meanwhile.
+//   k_dq   one item per tile of 128 query rows; walks the tiles of 128 keys they see: S = Q K^T, dP = dO V^T, dS in tensor
+//          memory as the first operand of dQ += dS K.
+// Both: one block per SM; a copy warp (tensor copies into a ring), a product warp, and sixteen warps that turn S and dP into P
+// and dS, each for 32 rows and 32 columns of tensor memory, while the tensor pipe runs the products of the neighbouring tile.
 // The operands that are read along their rows (dO, Q, K in the second products) are the tiles as they are stored, N-major.
 // Long items of k_dkv (the prompt's keys are seen by every row of a trajectory) are cut into pieces whose fp32 sums
 // k_join adds up in order.  k_delta computes D and lays D and L out by KV head beforehand.
@@ -23,6 +23,7 @@
 #include <cuda.h>
 
 #include <algorithm>
+#include <cstring>
 #include <vector>
 
 #include "bc_common.cuh"
@@ -32,47 +33,46 @@ namespace {
 #include "bc_tc.cuh"
 
 constexpr int kD = 128;                            // head_dim
-constexpr int kHalf = 64;                          // query rows of a k_dkv tile, keys of a k_dq tile
-constexpr int kWide = kTile * kD * 2;              // bytes of a 128-row operand
-constexpr int kSlim = kHalf * kD * 2;              // bytes of a 64-row operand
-constexpr int kGroups = 2;
-constexpr int kThreads = 64 + kGroups * 128;       // warp 0: copies, warp 1: products, then the groups
-constexpr int kKvRing = 4, kQRing = 3;
+constexpr int kWide = kTile * kD * 2;              // bytes of an operand
+constexpr uint32_t kWeighers = 16;                 // warps that turn S and dP into P and dS
+constexpr int kThreads = 64 + 32 * kWeighers;      // warp 0: copies, warp 1: products, then those
+constexpr uint32_t kReaders = 1 + kWeighers;       // warps that read the item numbers
+constexpr int kRing = 2;
 constexpr float kLog2e = 1.4426950408889634f;
-
-constexpr uint32_t kIdescN64 = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kHalf >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
 
 struct SeqDesc {
   int32_t P, T, nb;                                // lengths
   int32_t prompt_row, tok_row, bea_row;            // first rows in the packed arrays
 };
-// A tile of keys and the query tiles that see any of them (tiles of 64 / G tokens or beacons)
+// The work lists are for all KV heads: item i of a list of n is entry i / kv_heads for head i % kv_heads.
+// A tile of keys and the query tiles that see any of them (tiles of 128 / G tokens or beacons)
 struct KvItem {
   SeqDesc s;
-  int32_t seg, k0, kvh;                            // 0 prompt, 1 beacons, 2 tokens; first key
+  int32_t seg, k0;                                 // 0 prompt, 1 beacons, 2 tokens; first key
   int32_t ta, nt, ba, nb_tiles;                    // first token tile, how many, first beacon tile, how many
-  int32_t slot;                                    // place of the partial sums, -1: the whole item in one piece
-  int32_t pad[2];
+  int32_t slot;                                    // place of the partial sums (times kv_heads, plus head); -1: not cut into pieces
+  int32_t pad[3];
 };
-// Up to 256 / G tokens or beacons
+// Up to 128 / G tokens or beacons
 struct QItem {
   SeqDesc s;
-  int32_t kind, first, count, kvh;                 // 0 tokens, 1 beacons
-  int32_t nt0, nt1, nt2, lo2;                      // tiles of 64 keys: prompt, beacons, tokens from lo2 on
-  int32_t pad[2];
+  int32_t kind, first, count;                      // 0 tokens, 1 beacons
+  int32_t nt0, nt1, nt2, lo2;                      // tiles of 128 keys: prompt, beacons, tokens from lo2 on
+  int32_t pad[3];
 };
-// A split item: its pieces are the slots first .. first + count - 1
+// A tile of keys that was cut: its pieces are the places first .. first + count - 1
 struct JoinItem {
   SeqDesc s;
-  int32_t seg, k0, kvh, first, count;
-  int32_t pad[5];
+  int32_t seg, k0, first, count;
+  int32_t pad[6];
 };
 static_assert(sizeof(KvItem) == 64 && sizeof(QItem) == 64 && sizeof(JoinItem) == 64, "descriptors are 64 bytes");
 
 struct KvMaps { CUtensorMap q[2], o[2], k[3], v[3]; };   // q, dO by kind; k, v by segment
 struct GradArgs {
   const void* items;
-  int32_t n_items;
+  int32_t n_items;                                 // entries times kv_heads
+  int32_t* next;                                   // the next item to be taken
   const float *lse2, *delta;                       // [kv_heads][rows][G]: log2(e) L and D; rows: tokens, then beacons
   int64_t rows, tok_rows;
   __nv_bfloat16 *dk[3], *dv[3], *dq[2];
@@ -87,56 +87,121 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
 }
-__device__ __forceinline__ uint32_t swz64(int r, int ch16) {   // as swz, for operands of 64 rows
-  return (uint32_t)((ch16 >> 3) * (kHalf * 128) + r * 128 + (((ch16 & 7) ^ (r & 7)) << 4));
-}
 __device__ __forceinline__ int64_t stat_at(const GradArgs& a, const SeqDesc& s, int kvh, int kind, int first) {
   return ((int64_t)kvh * a.rows + (kind == 0 ? s.tok_row : a.tok_rows + s.bea_row) + first) * a.G;
 }
-// One row of an accumulator: 128 columns, times f, as bf16
-__device__ __forceinline__ void store_row(__nv_bfloat16* dst, const float* o, float f) {
+// Half a row of an accumulator, 64 columns, times f, as bf16
+__device__ __forceinline__ void store_half_row(__nv_bfloat16* dst, const float* o, float f) {
 #pragma unroll
-  for (int d = 0; d < kD; d += 16)
+  for (int d = 0; d < kD / 2; d += 16)
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + d), "r"(pack2(o[d] * f, o[d + 1] * f)),
                  "r"(pack2(o[d + 2] * f, o[d + 3] * f)), "r"(pack2(o[d + 4] * f, o[d + 5] * f)), "r"(pack2(o[d + 6] * f, o[d + 7] * f)),
                  "r"(pack2(o[d + 8] * f, o[d + 9] * f)), "r"(pack2(o[d + 10] * f, o[d + 11] * f)), "r"(pack2(o[d + 12] * f, o[d + 13] * f)),
                  "r"(pack2(o[d + 14] * f, o[d + 15] * f))
                  : "memory");
 }
-// Items of this block: round r hands out items [r * grid, (r + 1) * grid), forwards in even rounds, backwards in odd ones.
-__device__ __forceinline__ int item_of(int r, int n) {
-  const int grid = (int)gridDim.x, it = r * grid + ((r & 1) ? grid - 1 - (int)blockIdx.x : (int)blockIdx.x);
-  return it < n ? it : -1;
+// Items are handed out as blocks become free, longest first.  The copy warp draws them, one ahead of the work, and the other
+// warps read their numbers from two places in shared memory; an item is worked on by one block, so results do not depend on who
+// draws it.
+struct Queue {
+  uint32_t item, full, empty;                      // shared addresses: two numbers, two barriers each
+  __device__ __forceinline__ int at(uint32_t e) const {
+    int v;
+    asm volatile("ld.shared.s32 %0, [%1];" : "=r"(v) : "r"(item + 4 * (e & 1u)) : "memory");
+    return v;
+  }
+  // the copy warp, all lanes: draws item number e of this block
+  template <bool SHORTW>
+  __device__ __forceinline__ bool draw(uint32_t e, const GradArgs& a, volatile int* fail, int* got) const {
+    bool ok = true;
+    if (e >= 2) ok = __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(empty + 8 * (e & 1u), ((e >> 1) - 1) & 1u, fail, a.wait_limit)) != 0;
+    int it = -1;
+    if (ok) {
+      if ((threadIdx.x & 31) == 0) {
+        it = atomicAdd(a.next, 1);
+        if (it >= a.n_items) it = -1;
+        asm volatile("st.shared.s32 [%0], %1;" ::"r"(item + 4 * (e & 1u)), "r"(it) : "memory");
+        mbar_arrive_cta(full + 8 * (e & 1u));
+      }
+      it = __shfl_sync(0xffffffffu, it, 0);
+    }
+    *got = it;
+    return ok;
+  }
+  // the other warps, all lanes
+  template <bool SHORTW>
+  __device__ __forceinline__ bool read(uint32_t e, const GradArgs& a, volatile int* fail, int* got) const {
+    const bool ok = __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(full + 8 * (e & 1u), (e >> 1) & 1u, fail, a.wait_limit)) != 0;
+    *got = ok ? at(e) : -1;
+    __syncwarp();
+    if (ok && (threadIdx.x & 31) == 0) mbar_arrive_cta(empty + 8 * (e & 1u));
+    return ok;
+  }
+};
+
+// Pairs of fp32 numbers in one register pair: one instruction for both.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(F2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// Bits [lo, hi) of 32
+__device__ __forceinline__ uint32_t bits(int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, 32);
+  return hi > lo ? (0xffffffffu >> (32 - (hi - lo))) << lo : 0u;
 }
 
 // ---- dK and dV ---------------------------------------------------------------------------------------------------------------
-// Tensor memory: stage b (tile t & 1): columns [128 b, 128 b + 64) S^T, then P^T in its first 32; [128 b + 64, 128 b + 128) dP^T, then
-// dS^T in its first 32; [256, 384) dV, [384, 512) dK.  The tensor pipe runs a block's products in the order they were issued, so the
-// products of tile t + 2 overwrite P and dS of tile t only after the products that read them.
+// Tensor memory: columns [0, 128) S^T, then P^T in the first 16 columns of every 32; [128, 256) dP^T, then dS^T likewise; [256, 384) dV,
+// [384, 512) dK.  The tensor pipe runs a block's products in the order they are issued:
+//     S(t + 1) behind dV += P(t) dO, which reads what it overwrites, while the weights' warps turn dP(t) into dS(t);
+//     dP(t + 1) behind dK += dS(t) Q, while they turn S(t + 1) into P(t + 1).
 //
 // Barriers (t counts query tiles, e items; parity = uses so far & 1):
-//   full[r] / empty[r]: Q and dO of ring place r have landed / been read      kv / kvfree: K and V of item e have landed / been read
-//   s[b]: S^T and dP^T of the stage are there      p[b]: the group has stored P^T and dS^T
-//   f: dK and dV of item e are final               x: both groups have read them          d: drain on the give-up path
+//   full[r] / empty[r]: Q and dO of ring place r have landed / been read      k, v / kfree, vfree: K, V of item e have landed / been read
+//   s, dp: S^T, dP^T of tile t are there      p, ds: P^T, dS^T of tile t have been stored
+//   f: dK and dV of item e are final          x: they have been read          d: drain on the give-up path
 template <bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __grid_constant__ KvMaps maps) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sK = smem_addr(smem), sV = sK + kWide, sRing = sV + kWide;   // ring place r: Q at sRing + r * 2 kSlim, dO behind it
-  __shared__ __align__(8) uint64_t s_bars[2 * kKvRing + 9];
-  __shared__ __align__(16) float s_stat[kGroups * 4][2][kHalf];   // a warp's copy of the tile's L and D
+  const uint32_t sK = smem_addr(smem), sV = sK + kWide, sRing = sV + kWide;   // ring place r: Q at sRing + r * 2 kWide, dO behind it
+  constexpr int kBars = 2 * kRing + 15;
+  __shared__ __align__(8) uint64_t s_bars[kBars];
+  __shared__ int s_item[2];
+  __shared__ __align__(16) float s_stat[kWeighers][2][32];   // a warp's copy of its columns' -L and -D
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail_word;
   volatile int* s_fail = &s_fail_word;
-  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kKvRing, bar_kv = bar_empty + 8 * kKvRing, bar_kvfree = bar_kv + 8,
-                 bar_s = bar_kv + 16, bar_p = bar_kv + 32, bar_f = bar_kv + 48, bar_x = bar_kv + 56, bar_d = bar_kv + 64;
+  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kRing, bar_k = bar_empty + 8 * kRing, bar_v = bar_k + 8, bar_kfree = bar_k + 16,
+                 bar_vfree = bar_k + 24, bar_s = bar_k + 32, bar_dp = bar_k + 40, bar_p = bar_k + 48, bar_ds = bar_k + 56, bar_f = bar_k + 64,
+                 bar_x = bar_k + 72, bar_d = bar_k + 80;
+  const Queue queue = {smem_addr(s_item), bar_k + 88, bar_k + 104};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const KvItem* items = static_cast<const KvItem*>(a.items);
 
   if (tid == 0) {
-    for (int i = 0; i < 2 * kKvRing + 9; ++i) {
+    for (int i = 0; i < kBars; ++i) {
       const uint32_t bar = bar_full + 8 * i;
-      const uint32_t count = bar == bar_p || bar == bar_p + 8 ? 128u : (bar == bar_x ? 256u : 1u);
+      const uint32_t count = bar == bar_p || bar == bar_ds || bar == bar_x ? kWeighers : (bar >= queue.empty ? kReaders : 1u);
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -146,137 +211,159 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const int box_rows = a.per * a.G;      // rows that a copy writes; the others (G does not divide 64) stay zero
-  for (int idx = tid; idx < (kHalf - box_rows) * 16 * 2 * kKvRing; idx += kThreads) {
-    const int op = idx / ((kHalf - box_rows) * 16), rest = idx % ((kHalf - box_rows) * 16);
-    st_zero16(sRing + op * kSlim + swz64(box_rows + (rest >> 4), rest & 15));
+  const int box_rows = a.per * a.G;      // rows that a copy writes; the others (G does not divide 128) stay zero
+  for (int idx = tid; idx < (kTile - box_rows) * 16 * 2 * kRing; idx += kThreads) {
+    const int op = idx / ((kTile - box_rows) * 16), rest = idx % ((kTile - box_rows) * 16);
+    st_zero16(sRing + op * kWide + swz(box_rows + (rest >> 4), rest & 15));
   }
   proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem, tV = tmem + 256, tK = tmem + 384;
+  const uint32_t tmem = s_tmem, tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+  auto wait_all = [&](uint32_t bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
+  };
 
   if (warp == 0) {
     // ---- copies ----------------------------------------------------------------------------------------------------------
     bool ok = true;
-    uint32_t t = 0, e = 0;
-    auto wait_all = [&](uint32_t bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
-    };
+    uint32_t t = 0, e = 0, e_v = 0;
     const uint32_t bytes = (uint32_t)(2 * box_rows * kD * 2);
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const KvItem im = items[it];
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.draw<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const int kvh = it % a.Hkv;
+      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
-      if (e > 0) ok = wait_all(bar_kvfree, (e - 1) & 1u);
+      const int key_row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0;
+      if (e > 0) ok = wait_all(bar_kfree, (e - 1) & 1u);
       if (!ok) break;
       if (elect_one()) {
-        const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0;
-        mbar_expect_tx(bar_kv, 2 * kWide);
-        tma_3d(sK, &maps.k[im.seg], 0, im.kvh, row, bar_kv);
-        tma_3d(sK + kTile * 128, &maps.k[im.seg], 64, im.kvh, row, bar_kv);
-        tma_3d(sV, &maps.v[im.seg], 0, im.kvh, row, bar_kv);
-        tma_3d(sV + kTile * 128, &maps.v[im.seg], 64, im.kvh, row, bar_kv);
+        mbar_expect_tx(bar_k, kWide);
+        tma_3d(sK, &maps.k[im.seg], 0, kvh, key_row, bar_k);
+        tma_3d(sK + kTile * 128, &maps.k[im.seg], 64, kvh, key_row, bar_k);
       }
       __syncwarp();
       ++e;
       for (int n = 0; n < N; ++n, ++t) {
-        const uint32_t place = t % kKvRing;
-        if (t >= kKvRing) ok = wait_all(bar_empty + 8 * place, (t / kKvRing - 1) & 1u);
+        const uint32_t place = t % kRing;
+        if (t >= kRing) ok = wait_all(bar_empty + 8 * place, (t / kRing - 1) & 1u);
         if (!ok) break;
         if (elect_one()) {
           const int kind = n < im.nt ? 0 : 1, tile = kind == 0 ? im.ta + n : im.ba + n - im.nt;
           const int row = (kind == 0 ? im.s.tok_row : im.s.bea_row) + tile * a.per;
-          const uint32_t dst = sRing + place * 2 * kSlim, bar = bar_full + 8 * place;
+          const uint32_t dst = sRing + place * 2 * kWide, bar = bar_full + 8 * place;
           mbar_expect_tx(bar, bytes);
-          tma_3d(dst, &maps.q[kind], 0, im.kvh * a.G, row, bar);
-          tma_3d(dst + kHalf * 128, &maps.q[kind], 64, im.kvh * a.G, row, bar);
-          tma_3d(dst + kSlim, &maps.o[kind], 0, im.kvh * a.G, row, bar);
-          tma_3d(dst + kSlim + kHalf * 128, &maps.o[kind], 64, im.kvh * a.G, row, bar);
+          tma_3d(dst, &maps.q[kind], 0, kvh * a.G, row, bar);
+          tma_3d(dst + kTile * 128, &maps.q[kind], 64, kvh * a.G, row, bar);
+          tma_3d(dst + kWide, &maps.o[kind], 0, kvh * a.G, row, bar);
+          tma_3d(dst + kWide + kTile * 128, &maps.o[kind], 64, kvh * a.G, row, bar);
         }
         __syncwarp();
+        if (n == 0) {                              // V is wanted a little later than K and the first Q
+          if (e > 1) ok = wait_all(bar_vfree, (e - 2) & 1u);
+          if (!ok) { ++t; break; }
+          if (elect_one()) {
+            mbar_expect_tx(bar_v, kWide);
+            tma_3d(sV, &maps.v[im.seg], 0, kvh, key_row, bar_v);
+            tma_3d(sV + kTile * 128, &maps.v[im.seg], 64, kvh, key_row, bar_v);
+          }
+          __syncwarp();
+          ++e_v;
+        }
       }
+      if (!ok) break;
     }
     // no copy may be on its way when the block leaves: every one that was begun is waited for (at the end of ordinary work all have landed)
     if (!ok) *s_fail = 1;
     __syncwarp();
     int never = 0;
-    if (e > 0) mbar_wait_or_fail<false>(bar_kv, (e - 1) & 1u, &never, kWaitLimit);
-    for (uint32_t b = t > kKvRing ? t - kKvRing : 0; b < t; ++b)
-      mbar_wait_or_fail<false>(bar_full + 8 * (b % kKvRing), (b / kKvRing) & 1u, &never, kWaitLimit);
+    if (e > 0) mbar_wait_or_fail<false>(bar_k, (e - 1) & 1u, &never, kWaitLimit);
+    if (e_v > 0) mbar_wait_or_fail<false>(bar_v, (e_v - 1) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t > kRing ? t - kRing : 0; b < t; ++b)
+      mbar_wait_or_fail<false>(bar_full + 8 * (b % kRing), (b / kRing) & 1u, &never, kWaitLimit);
     __syncwarp();
   } else if (warp == 1) {
     // ---- products --------------------------------------------------------------------------------------------------------
     bool ok = true, issued = false;
-    uint32_t t0 = 0, e = 0;
-    auto wait_all = [&](uint32_t bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
+    uint32_t t = 0, e = 0;
+    const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sRing), dQn = umma_desc_nmajor(sRing);
+    auto first = [&](uint32_t to, uint64_t key, uint64_t q, uint32_t bar, uint32_t bar_free, bool last) {   // S^T or dP^T
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < kD / 16; ++kk) {
+          const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
+          umma(to, key + off, q + off, kk > 0);
+        }
+        umma_commit(bar);
+        if (last) umma_commit(bar_free);
+      }
+      __syncwarp();
+      issued = true;
     };
-    const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sRing), dQn = umma_desc_nmajor(sRing, kHalf * 128);
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const KvItem im = items[it];
+    auto second = [&](uint32_t to, uint32_t from, uint64_t q, bool fresh) {   // dV or dK
+#pragma unroll
+      for (int kk = 0; kk < kTile / 16; ++kk)
+        umma_ts(to, from + (kk >> 1) * 32 + (kk & 1) * 8, q + (uint64_t)((kk * 16 * 128) >> 4), (!fresh || kk > 0) ? 1u : 0u);
+    };
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
-      auto first_products = [&](int n) {           // S^T and dP^T of tile n
-        const uint32_t t = t0 + n, place = t % kKvRing, stage = t & 1u;
-        if (!wait_all(bar_full + 8 * place, (t / kKvRing) & 1u)) return false;
-        const int kind = n < im.nt ? 0 : 1, tile = kind == 0 ? im.ta + n : im.ba + n - im.nt;
-        const int valid = min((kind == 0 ? im.s.T : im.s.nb) - tile * a.per, a.per) * a.G;
-        if (valid < box_rows) {                    // rows of the next sequence: cleared, they are factors of the second products
+      auto at = [&](uint32_t tile) { return (uint64_t)((tile % kRing) * 2 * kWide >> 4); };
+      auto landed = [&](int n) {                   // Q and dO of the item's tile n; rows of the next sequence are cleared: they are factors
+        const uint32_t tile = t + n, place = tile % kRing;
+        if (!wait_all(bar_full + 8 * place, (tile / kRing) & 1u)) return false;
+        const int kind = n < im.nt ? 0 : 1, q = kind == 0 ? im.ta + n : im.ba + n - im.nt;
+        const int valid = min((kind == 0 ? im.s.T : im.s.nb) - q * a.per, a.per) * a.G;
+        if (valid < box_rows) {
           for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) {
-            st_zero16(sRing + place * 2 * kSlim + swz64(idx >> 4, idx & 15));
-            st_zero16(sRing + place * 2 * kSlim + kSlim + swz64(idx >> 4, idx & 15));
+            st_zero16(sRing + place * 2 * kWide + swz(idx >> 4, idx & 15));
+            st_zero16(sRing + place * 2 * kWide + kWide + swz(idx >> 4, idx & 15));
           }
           proxy_fence();
           __syncwarp();
         }
         tc_fence_after();
-        if (elect_one()) {
-          const uint64_t q = dQ + (uint64_t)((place * 2 * kSlim) >> 4), o = q + (uint64_t)(kSlim >> 4);
-          const uint32_t tS = tmem + stage * 128;
-#pragma unroll
-          for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off_a = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4), off_b = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
-            umma<kIdescN64>(tS, dK + off_a, q + off_b, kk > 0);
-          }
-#pragma unroll
-          for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off_a = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4), off_b = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
-            umma<kIdescN64>(tS + 64, dV + off_a, o + off_b, kk > 0);
-          }
-          umma_commit(bar_s + 8 * stage);
-          if (n == N - 1) umma_commit(bar_kvfree);
-        }
-        __syncwarp();
-        issued = true;
         return true;
       };
-      ok = wait_all(bar_kv, e & 1u) && first_products(0) && (N < 2 || first_products(1));
-      for (int n = 0; n < N && ok; ++n) {
-        const uint32_t t = t0 + n, place = t % kKvRing, stage = t & 1u;
-        ok = wait_all(bar_p + 8 * stage, (t >> 1) & 1u);
-        if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the groups have read the last item's sums
+      ok = wait_all(bar_k, e & 1u) && landed(0);
+      if (!ok) break;
+      first(tS, dK, dQ + at(t), bar_s, bar_kfree, N == 1);
+      ok = wait_all(bar_v, e & 1u);
+      if (!ok) break;
+      tc_fence_after();
+      first(tdP, dV, dQ + at(t) + (kWide >> 4), bar_dp, bar_vfree, N == 1);
+      for (int n = 0; n < N; ++n) {
+        const bool more = n + 1 < N;
+        const uint32_t tile = t + n;
+        if (more) ok = landed(n + 1);
+        ok = ok && wait_all(bar_p, tile & 1u);
+        if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) second(tV, tS, dQn + at(tile) + (kWide >> 4), n == 0);
+        __syncwarp();
+        if (more) first(tS, dK, dQ + at(tile + 1), bar_s, bar_kfree, n + 2 == N);
+        ok = wait_all(bar_ds, tile & 1u);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          const uint64_t q = dQn + (uint64_t)((place * 2 * kSlim) >> 4), o = q + (uint64_t)(kSlim >> 4);
-          const uint32_t tP = tmem + stage * 128, tdS = tP + 64;
-#pragma unroll
-          for (int kk = 0; kk < kHalf / 16; ++kk) umma_ts(tV, tP + kk * 8, o + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
-#pragma unroll
-          for (int kk = 0; kk < kHalf / 16; ++kk) umma_ts(tK, tdS + kk * 8, q + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
-          umma_commit(bar_empty + 8 * place);
-          if (n == N - 1) umma_commit(bar_f);
+          second(tK, tdP, dQn + at(tile), n == 0);
+          umma_commit(bar_empty + 8 * (tile % kRing));
+          if (!more) umma_commit(bar_f);
         }
         __syncwarp();
-        if (n + 2 < N) ok = first_products(n + 2);
+        if (more) first(tdP, dV, dQ + at(tile + 1) + (kWide >> 4), bar_dp, bar_vfree, n + 2 == N);
       }
-      t0 += N;
+      if (!ok) break;
+      t += N;
       ++e;
     }
     if (!ok) {
@@ -290,19 +377,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     }
     __syncwarp();
   } else {
-    // ---- weights: one key per thread -----------------------------------------------------------------------------------------
-    const int grp = (warp - 2) >> 2;
-    float (*stats)[kHalf] = s_stat[warp - 2];
+    // ---- weights: one key and 32 query rows per thread ------------------------------------------------------------------------
+    const int part = (warp - 2) >> 2;              // columns [32 part, + 32)
+    float (*stats)[32] = s_stat[warp - 2];
     // a warp reaches the 32 lanes of tensor memory that belong to its number modulo 4; its keys are those lanes
     const int key = (warp & 3) * 32 + lane;
-    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t tS = tmem + grp * 128 + lane_base, tP = tS, tD = tS + 64;
+    const uint32_t mine = ((uint32_t)((warp & 3) * 32) << 16) + part * 32;
+    const F2 scale2 = pair(a.scale_log2, a.scale_log2);
     bool ok = true;
-    uint32_t t0 = 0, e = 0;
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const KvItem im = items[it];
+    uint32_t t = 0, e = 0;
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const int kvh = it % a.Hkv;
+      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles, G = a.G, c = a.c;
       const int k = im.k0 + key, seg_len = im.seg == 0 ? im.s.P : (im.seg == 1 ? im.s.nb : im.s.T);
       const bool live = k < seg_len;
@@ -314,91 +403,107 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         if (c > 1) { tok_hi = min(im.s.T, (k / c + 1) * c); bea_lo = k / c; bea_hi = min(im.s.nb, k / c + 1); }
       }
       if (!live) tok_hi = bea_hi = 0;
-      float4 stat;                                 // this lane's share of the next tile's numbers: L and D of rows lane and lane + 32
+      float my_l, my_d;                            // of this lane's query row of the next tile
       auto fetch = [&](int n) {
         const int kind = n < im.nt ? 0 : 1, first = (kind == 0 ? im.ta + n : im.ba + n - im.nt) * a.per;
         const int valid = min((kind == 0 ? im.s.T : im.s.nb) - first, a.per) * G;
-        const int64_t at = stat_at(a, im.s, im.kvh, kind, first) + lane;
-        stat = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (lane < valid) { stat.x = a.lse2[at]; stat.z = a.delta[at]; }
-        if (lane + 32 < valid) { stat.y = a.lse2[at + 32]; stat.w = a.delta[at + 32]; }
+        const int64_t at = stat_at(a, im.s, kvh, kind, first) + part * 32 + lane;
+        const bool in = part * 32 + lane < valid;
+        my_l = in ? a.lse2[at] : 0.f;
+        my_d = in ? a.delta[at] : 0.f;
       };
-      const int n_first = (int)((t0 & 1u) ^ (uint32_t)grp);
-      if (n_first < N) fetch(n_first);
-      for (int n = n_first; n < N; n += 2) {
-        const uint32_t t = t0 + n;
+      if (N > 0) fetch(0);
+      for (int n = 0; n < N; ++n, ++t) {
         __syncwarp();                              // the last tile's numbers have been read
-        stats[0][lane] = stat.x; stats[0][lane + 32] = stat.y; stats[1][lane] = stat.z; stats[1][lane + 32] = stat.w;
+        stats[0][lane] = -my_l; stats[1][lane] = -my_d;
         __syncwarp();
-        if (n + 2 < N) fetch(n + 2);
+        if (n + 1 < N) fetch(n + 1);
         const int kind = n < im.nt ? 0 : 1, first = (kind == 0 ? im.ta + n : im.ba + n - im.nt) * a.per;
         const int all = min((kind == 0 ? im.s.T : im.s.nb) - first, a.per) * G;
         const int lo = kind == 0 ? tok_lo : bea_lo, hi = kind == 0 ? tok_hi : bea_hi;
         const int jlo = min(max(lo - first, 0), a.per) * G, jhi = min(min(hi - first, a.per) * G, all);
-        const bool ok1 = mbar_wait_or_fail<SHORTW>(bar_s + 8 * grp, (t >> 1) & 1u, s_fail, a.wait_limit);
-        ok = __all_sync(0xffffffffu, ok1);
+        const uint32_t mask = bits(jlo - part * 32, jhi - part * 32);
+        const bool whole = __all_sync(0xffffffffu, mask == 0xffffffffu), some = __any_sync(0xffffffffu, mask != 0u);
+        ok = wait_all(bar_s, t & 1u);
         if (!ok) break;
         tc_fence_after();
-        const bool whole = __all_sync(0xffffffffu, jlo == 0 && jhi == kHalf);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float s[32], dp[32];
-          tmem_ld32_async(tS + h * 32, s);
-          tmem_ld32_async(tD + h * 32, dp);
-          tmem_wait_ld();
-          uint32_t pp[16], ds[16];
+        float p[32];
+        tmem_ld32_async(tS + mine, p);
+        tmem_wait_ld();
+        uint32_t out[16];
+        if (some) {                                // uniform over the warp, no access to tensor memory inside
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            const float4 l4 = *reinterpret_cast<const float4*>(&stats[0][h * 32 + j]);
-            const float4 d4 = *reinterpret_cast<const float4*>(&stats[1][h * 32 + j]);
-            const float ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-            float p[4], q[4];
+            const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(&stats[0][j]);
+            split(fma2(pair(p[j], p[j + 1]), scale2, l.x), &p[j], &p[j + 1]);
+            split(fma2(pair(p[j + 2], p[j + 3]), scale2, l.y), &p[j + 2], &p[j + 3]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p[i] = fast_exp2(fmaf(s[j + i], a.scale_log2, -ll[i]));
-              q[i] = p[i] * (dp[j + i] - dd[i]);
-              if (!whole) {
-                const bool sees = h * 32 + j + i >= jlo && h * 32 + j + i < jhi;
-                p[i] = sees ? p[i] : 0.f;
-                q[i] = sees ? q[i] : 0.f;
-              }
-            }
-            pp[j / 2] = pack2(p[0], p[1]); pp[j / 2 + 1] = pack2(p[2], p[3]);
-            ds[j / 2] = pack2(q[0], q[1]); ds[j / 2 + 1] = pack2(q[2], q[3]);
+            for (int u = 0; u < 4; ++u) p[j + u] = fast_exp2(p[j + u]);
           }
-          tmem_st16(tP + h * 16, pp);
-          tmem_st16(tD + h * 16, ds);
+          if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) p[j] = (mask & (1u << j)) ? p[j] : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) p[j] = 0.f;
         }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) out[j] = pack2(p[2 * j], p[2 * j + 1]);
+        tmem_st16(tS + mine, out);                 // over the warp's own columns, which it has read
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive_cta(bar_p + 8 * grp);
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_p);
+        ok = wait_all(bar_dp, t & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        float dp[32];
+        tmem_ld32_async(tdP + mine, dp);
+        tmem_wait_ld();
+        // where the weight is 0 the score gradient is, too: dP is finite there, rows of other sequences having been cleared
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(&stats[1][j]);
+          float q[4];
+          split(mul2(pair(p[j], p[j + 1]), add2(pair(dp[j], dp[j + 1]), d.x)), &q[0], &q[1]);
+          split(mul2(pair(p[j + 2], p[j + 3]), add2(pair(dp[j + 2], dp[j + 3]), d.y)), &q[2], &q[3]);
+          out[j / 2] = pack2(q[0], q[1]);
+          out[j / 2 + 1] = pack2(q[2], q[3]);
+        }
+        tmem_st16(tdP + mine, out);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_ds);
       }
       if (!ok) break;
-      // ---- the item's sums: the first group has dV, the second dK
-      float o[kD];
+      // ---- the item's sums: parts 0 and 1 have dV, 2 and 3 dK, 64 columns each
+      float o[kD / 2];
+      const bool is_k = part >= 2;
+      const int col = (part & 1) * 64;
       if (N > 0) {
-        const bool ok1 = mbar_wait_or_fail<SHORTW>(bar_f, e & 1u, s_fail, a.wait_limit);
-        ok = __all_sync(0xffffffffu, ok1);
+        ok = wait_all(bar_f, e & 1u);
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb) tmem_ld32_async((grp == 0 ? tV : tK) + lane_base + cb * 32, o + cb * 32);
+        for (int cb = 0; cb < 2; ++cb) tmem_ld32_async((is_k ? tK : tV) + ((uint32_t)((warp & 3) * 32) << 16) + col + cb * 32, o + cb * 32);
         tmem_wait_ld();
         tc_fence_before();
-        mbar_arrive_cta(bar_x);
-        t0 += N;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_x);
         ++e;
       } else {
 #pragma unroll
-        for (int d = 0; d < kD; ++d) o[d] = 0.f;
+        for (int d = 0; d < kD / 2; ++d) o[d] = 0.f;
       }
       if (im.slot >= 0) {
-        float4* dst = reinterpret_cast<float4*>(a.partial + (((int64_t)im.slot * 2 + grp) * kTile + key) * kD);
+        float4* dst = reinterpret_cast<float4*>(a.partial + ((((int64_t)im.slot * a.Hkv + kvh) * 2 + is_k) * kTile + key) * kD + col);
 #pragma unroll
-        for (int d = 0; d < kD; d += 4) dst[d / 4] = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+        for (int d = 0; d < kD / 2; d += 4) dst[d / 4] = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
       } else if (live) {
         const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + k;
-        store_row((grp == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + im.kvh) * kD, o, grp == 0 ? 1.f : a.scale);
+        store_half_row((is_k ? a.dk : a.dv)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + col, o, is_k ? a.scale : 1.f);
       }
     }
     if (!ok) *s_fail = 1;
@@ -413,26 +518,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
 }
 
 // ---- dQ ------------------------------------------------------------------------------------------------------------------------
-// Tensor memory, group g: columns [256 g, + 64) S, then dS in its first 32; [256 g + 64, + 64) dP; [256 g + 128, + 128) dQ.
-// Barriers as above, with q / qfree for the item's Q and dO, and f, x per group.
+// Tensor memory: columns [0, 128) and [128, 256) S of even and odd tiles, then dS in the first 16 columns of every 32; [256, 384) dP,
+// [384, 512) dQ.  S(n + 1) is made while the weights' warps work on tile n, dP(n + 1) as soon as they have read dP(n).
+// Barriers as above, with q / qfree for the item's Q and dO, and r: dP of tile t has been read.
 template <bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __grid_constant__ KvMaps maps) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sQ = smem_addr(smem), sRing = sQ + 4 * kWide;   // group g: Q at sQ + g * 2 kWide, dO behind it; ring place r: K, V
-  __shared__ __align__(8) uint64_t s_bars[2 * kQRing + 11];
+  const uint32_t sQ = smem_addr(smem), sO = sQ + kWide, sRing = sO + kWide;   // ring place r: K at sRing + r * 2 kWide, V behind it
+  constexpr int kBars = 2 * kRing + 14;
+  __shared__ __align__(8) uint64_t s_bars[kBars];
+  __shared__ int s_item[2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail_word;
   volatile int* s_fail = &s_fail_word;
-  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kQRing, bar_q = bar_empty + 8 * kQRing, bar_qfree = bar_q + 8,
-                 bar_s = bar_q + 16, bar_p = bar_q + 32, bar_f = bar_q + 48, bar_x = bar_q + 64, bar_d = bar_q + 80;
+  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kRing, bar_q = bar_empty + 8 * kRing, bar_qfree = bar_q + 8, bar_s = bar_q + 16,
+                 bar_dp = bar_q + 32, bar_r = bar_q + 40, bar_ds = bar_q + 48, bar_f = bar_q + 56, bar_x = bar_q + 64, bar_d = bar_q + 72;
+  const Queue queue = {smem_addr(s_item), bar_q + 80, bar_q + 96};   // bar_q + 24: the second S's
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const QItem* items = static_cast<const QItem*>(a.items);
 
   if (tid == 0) {
-    for (int i = 0; i < 2 * kQRing + 11; ++i) {
+    for (int i = 0; i < kBars; ++i) {
       const uint32_t bar = bar_full + 8 * i;
-      const uint32_t count = bar == bar_p || bar == bar_p + 8 || bar == bar_x || bar == bar_x + 8 ? 128u : 1u;
+      const uint32_t count = bar == bar_r || bar == bar_ds ? kWeighers : (bar == bar_x ? kWeighers / 2 : (bar >= queue.empty ? kReaders : 1u));
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -443,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int box_rows = a.per * a.G;
-  for (int idx = tid; idx < (kTile - box_rows) * 16 * 4; idx += kThreads) {
+  for (int idx = tid; idx < (kTile - box_rows) * 16 * 2; idx += kThreads) {
     const int op = idx / ((kTile - box_rows) * 16), rest = idx % ((kTile - box_rows) * 16);
     st_zero16(sQ + op * kWide + swz(box_rows + (rest >> 4), rest & 15));
   }
@@ -451,139 +560,135 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
+  const uint32_t tmem = s_tmem, tdP = tmem + 256, tO = tmem + 384;
   auto key_tile = [](const QItem& im, int n, int* k0) {          // segment and first key of tile n
     const int seg = n < im.nt0 ? 0 : (n < im.nt0 + im.nt1 ? 1 : 2);
-    *k0 = seg == 0 ? n * kHalf : (seg == 1 ? (n - im.nt0) * kHalf : im.lo2 + (n - im.nt0 - im.nt1) * kHalf);
+    *k0 = seg == 0 ? n * kTile : (seg == 1 ? (n - im.nt0) * kTile : im.lo2 + (n - im.nt0 - im.nt1) * kTile);
     return seg;
+  };
+  auto wait_all = [&](uint32_t bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
   };
 
   if (warp == 0) {
     bool ok = true;
     uint32_t t = 0, e = 0;
-    auto wait_all = [&](uint32_t bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
-    };
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const QItem im = items[it];
-      const int N = im.nt0 + im.nt1 + im.nt2, groups = im.count > a.per ? 2 : 1;
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.draw<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const int kvh = it % a.Hkv;
+      const QItem im = items[it / a.Hkv];
+      const int N = im.nt0 + im.nt1 + im.nt2;
       if (e > 0) ok = wait_all(bar_qfree, (e - 1) & 1u);
       if (!ok) break;
       if (elect_one()) {
-        mbar_expect_tx(bar_q, (uint32_t)(groups * 2 * box_rows * kD * 2));
-        for (int g = 0; g < groups; ++g) {
-          const int row = (im.kind == 0 ? im.s.tok_row : im.s.bea_row) + im.first + g * a.per;
-          const uint32_t dst = sQ + g * 2 * kWide;
-          tma_3d(dst, &maps.q[im.kind], 0, im.kvh * a.G, row, bar_q);
-          tma_3d(dst + kTile * 128, &maps.q[im.kind], 64, im.kvh * a.G, row, bar_q);
-          tma_3d(dst + kWide, &maps.o[im.kind], 0, im.kvh * a.G, row, bar_q);
-          tma_3d(dst + kWide + kTile * 128, &maps.o[im.kind], 64, im.kvh * a.G, row, bar_q);
-        }
+        const int row = (im.kind == 0 ? im.s.tok_row : im.s.bea_row) + im.first;
+        mbar_expect_tx(bar_q, (uint32_t)(2 * box_rows * kD * 2));
+        tma_3d(sQ, &maps.q[im.kind], 0, kvh * a.G, row, bar_q);
+        tma_3d(sQ + kTile * 128, &maps.q[im.kind], 64, kvh * a.G, row, bar_q);
+        tma_3d(sO, &maps.o[im.kind], 0, kvh * a.G, row, bar_q);
+        tma_3d(sO + kTile * 128, &maps.o[im.kind], 64, kvh * a.G, row, bar_q);
       }
       __syncwarp();
       ++e;
       for (int n = 0; n < N; ++n, ++t) {
-        const uint32_t place = t % kQRing;
-        if (t >= kQRing) ok = wait_all(bar_empty + 8 * place, (t / kQRing - 1) & 1u);
+        const uint32_t place = t % kRing;
+        if (t >= kRing) ok = wait_all(bar_empty + 8 * place, (t / kRing - 1) & 1u);
         if (!ok) break;
         if (elect_one()) {
           int k0;
           const int seg = key_tile(im, n, &k0);
           const int row = (seg == 0 ? im.s.prompt_row : (seg == 1 ? im.s.bea_row : im.s.tok_row)) + k0;
-          const uint32_t dst = sRing + place * 2 * kSlim, bar = bar_full + 8 * place;
-          mbar_expect_tx(bar, 2 * kSlim);
-          tma_3d(dst, &maps.k[seg], 0, im.kvh, row, bar);
-          tma_3d(dst + kHalf * 128, &maps.k[seg], 64, im.kvh, row, bar);
-          tma_3d(dst + kSlim, &maps.v[seg], 0, im.kvh, row, bar);
-          tma_3d(dst + kSlim + kHalf * 128, &maps.v[seg], 64, im.kvh, row, bar);
+          const uint32_t dst = sRing + place * 2 * kWide, bar = bar_full + 8 * place;
+          mbar_expect_tx(bar, 2 * kWide);
+          tma_3d(dst, &maps.k[seg], 0, kvh, row, bar);
+          tma_3d(dst + kTile * 128, &maps.k[seg], 64, kvh, row, bar);
+          tma_3d(dst + kWide, &maps.v[seg], 0, kvh, row, bar);
+          tma_3d(dst + kWide + kTile * 128, &maps.v[seg], 64, kvh, row, bar);
         }
         __syncwarp();
       }
+      if (!ok) break;
     }
     if (!ok) *s_fail = 1;
     __syncwarp();
     int never = 0;
     if (e > 0) mbar_wait_or_fail<false>(bar_q, (e - 1) & 1u, &never, kWaitLimit);
-    for (uint32_t b = t > kQRing ? t - kQRing : 0; b < t; ++b)
-      mbar_wait_or_fail<false>(bar_full + 8 * (b % kQRing), (b / kQRing) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t > kRing ? t - kRing : 0; b < t; ++b)
+      mbar_wait_or_fail<false>(bar_full + 8 * (b % kRing), (b / kRing) & 1u, &never, kWaitLimit);
     __syncwarp();
   } else if (warp == 1) {
     bool ok = true, issued = false;
-    uint32_t t0 = 0, e = 0, used[2] = {0, 0}, begun[2] = {0, 0};   // per group: tiles and items so far
-    auto wait_all = [&](uint32_t bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
-    };
-    const uint64_t dQ = umma_desc(sQ), dK = umma_desc(sRing), dKn = umma_desc_nmajor(sRing, kHalf * 128);
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const QItem im = items[it];
-      const int N = im.nt0 + im.nt1 + im.nt2, groups = im.count > a.per ? 2 : 1;
-      auto landed = [&](int n) {                   // K and V of tile n; keys past the segment are cleared: K is a factor of dS K
-        const uint32_t t = t0 + n, place = t % kQRing;
-        if (!wait_all(bar_full + 8 * place, (t / kQRing) & 1u)) return false;
+    uint32_t t = 0, e = 0;
+    const uint64_t dQ = umma_desc(sQ), dO = umma_desc(sO), dK = umma_desc(sRing), dKn = umma_desc_nmajor(sRing);
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const QItem im = items[it / a.Hkv];
+      const int N = im.nt0 + im.nt1 + im.nt2;
+      auto landed = [&](int n) {                   // K and V of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
+        const uint32_t tile = t + n, place = tile % kRing;
+        if (!wait_all(bar_full + 8 * place, (tile / kRing) & 1u)) return false;
         int k0;
-        const int seg = key_tile(im, n, &k0), valid = min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kHalf);
-        if (valid < kHalf) {
-          for (int idx = valid * 16 + lane; idx < kHalf * 16; idx += 32) st_zero16(sRing + place * 2 * kSlim + swz64(idx >> 4, idx & 15));
+        const int seg = key_tile(im, n, &k0), valid = min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kTile);
+        if (valid < kTile) {
+          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) {
+            st_zero16(sRing + place * 2 * kWide + swz(idx >> 4, idx & 15));
+            st_zero16(sRing + place * 2 * kWide + kWide + swz(idx >> 4, idx & 15));
+          }
           proxy_fence();
           __syncwarp();
         }
+        tc_fence_after();
         return true;
       };
-      auto first_products = [&](int g, int n) {
-        const uint32_t place = (t0 + n) % kQRing;
-        tc_fence_after();
+      auto at = [&](uint32_t tile) { return (uint64_t)((tile % kRing) * 2 * kWide >> 4); };
+      auto first = [&](uint32_t to, uint64_t row, uint64_t key, uint32_t bar, bool last) {   // S or dP
         if (elect_one()) {
-          const uint64_t q = dQ + (uint64_t)((g * 2 * kWide) >> 4), o = q + (uint64_t)(kWide >> 4);
-          const uint64_t k = dK + (uint64_t)((place * 2 * kSlim) >> 4), v = k + (uint64_t)(kSlim >> 4);
-          const uint32_t tS = tmem + g * 256;
 #pragma unroll
           for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off_a = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4), off_b = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
-            umma<kIdescN64>(tS, q + off_a, k + off_b, kk > 0);
+            const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
+            umma(to, row + off, key + off, kk > 0);
           }
-#pragma unroll
-          for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off_a = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4), off_b = (uint64_t)(((kk >> 2) * (kHalf * 128) + (kk & 3) * 32) >> 4);
-            umma<kIdescN64>(tS + 64, o + off_a, v + off_b, kk > 0);
-          }
-          umma_commit(bar_s + 8 * g);
-          if (n == N - 1 && g == groups - 1) umma_commit(bar_qfree);
+          umma_commit(bar);
+          if (last) umma_commit(bar_qfree);
         }
         __syncwarp();
         issued = true;
       };
       ok = wait_all(bar_q, e & 1u) && landed(0);
       if (!ok) break;
-      for (int g = 0; g < groups; ++g) first_products(g, 0);
-      for (int n = 0; n < N && ok; ++n) {
-        const uint32_t place = (t0 + n) % kQRing;
-        for (int g = 0; g < groups && ok; ++g) {
-          ok = wait_all(bar_p + 8 * g, used[g] & 1u);
-          ++used[g];
-          if (ok && n == 0 && begun[g] > 0) ok = wait_all(bar_x + 8 * g, (begun[g] - 1) & 1u);
+      first(tmem + (t & 1u) * 128, dQ, dK + at(t), bar_s + 8 * (t & 1u), false);
+      first(tdP, dO, dK + at(t) + (kWide >> 4), bar_dp, N == 1);
+      for (int n = 0; n < N; ++n) {
+        const bool more = n + 1 < N;
+        const uint32_t tile = t + n, odd = tile & 1u;
+        if (more) {
+          ok = landed(n + 1);
+          if (!ok) break;
+          first(tmem + (odd ^ 1u) * 128, dQ, dK + at(tile + 1), bar_s + 8 * (odd ^ 1u), false);
+          ok = wait_all(bar_r, odd);
           if (!ok) break;
           tc_fence_after();
-          if (elect_one()) {
-            const uint64_t k = dKn + (uint64_t)((place * 2 * kSlim) >> 4);
-            const uint32_t tdS = tmem + g * 256, tO = tdS + 128;
-#pragma unroll
-            for (int kk = 0; kk < kHalf / 16; ++kk) umma_ts(tO, tdS + kk * 8, k + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
-            if (g == groups - 1) umma_commit(bar_empty + 8 * place);
-            if (n == N - 1) umma_commit(bar_f + 8 * g);
-          }
-          __syncwarp();
-          if (n + 1 < N) {
-            if (g == 0) ok = landed(n + 1);
-            if (ok) first_products(g, n + 1);
-          }
+          first(tdP, dO, dK + at(tile + 1) + (kWide >> 4), bar_dp, n + 2 == N);
         }
+        ok = wait_all(bar_ds, odd);
+        if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
+        if (!ok) break;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            umma_ts(tO, tmem + odd * 128 + (kk >> 1) * 32 + (kk & 1) * 8, dKn + at(tile) + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
+          umma_commit(bar_empty + 8 * (tile % kRing));
+          if (!more) umma_commit(bar_f);
+        }
+        __syncwarp();
       }
-      for (int g = 0; g < groups; ++g) ++begun[g];
-      t0 += N;
+      if (!ok) break;
+      t += N;
       ++e;
     }
     if (!ok) {
@@ -597,22 +702,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     }
     __syncwarp();
   } else {
-    // ---- weights: one query row per thread
-    const int grp = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, G = a.G, c = a.c;
-    const uint32_t tS = tmem + grp * 256 + ((uint32_t)((warp & 3) * 32) << 16), tD = tS + 64, tO = tS + 128;
+    // ---- weights: one query row and 32 keys per thread --------------------------------------------------------------------------
+    const int part = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, G = a.G, c = a.c;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine = lanes + part * 32;
     const int my_local = row / G, my_head = row % G;
+    const F2 scale2 = pair(a.scale_log2, a.scale_log2);
     bool ok = true;
     uint32_t t = 0, e = 0;
-    for (int r = 0; ok; ++r) {
-      const int it = item_of(r, a.n_items);
-      if (it < 0) break;
-      const QItem im = items[it];
-      const int N = im.nt0 + im.nt1 + im.nt2, first = im.first + grp * a.per, count = min(im.count - grp * a.per, a.per);
-      if (count <= 0) continue;
-      const bool live = row < count * G;
-      const int64_t at = stat_at(a, im.s, im.kvh, im.kind, first) + row;
-      const float l2 = live ? a.lse2[at] : 0.f, dl = live ? a.delta[at] : 0.f;
-      const int idx = first + my_local;
+    for (uint32_t i = 0;; ++i) {
+      int it;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      if (!ok || it < 0) break;
+      const int kvh = it % a.Hkv;
+      const QItem im = items[it / a.Hkv];
+      const int N = im.nt0 + im.nt1 + im.nt2;
+      const bool live = row < im.count * G;
+      const int64_t at = stat_at(a, im.s, kvh, im.kind, im.first) + row;
+      const float l2 = live ? -a.lse2[at] : 0.f, dl = live ? -a.delta[at] : 0.f;
+      const F2 minus_l = pair(l2, l2), minus_d = pair(dl, dl);
+      const int idx = im.first + my_local;
       int bea_hi, tok_lo, tok_hi;                  // visible: the prompt, beacons [0, bea_hi), tokens [tok_lo, tok_hi)
       if (im.kind == 0) { bea_hi = c > 1 ? idx / c : 0; tok_lo = c > 1 ? idx / c * c : 0; tok_hi = idx + 1; }
       else { bea_hi = idx + 1; tok_lo = idx * c; tok_hi = (idx + 1) * c; }
@@ -623,49 +731,67 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
         if (seg == 1) hi = min(bea_hi, im.s.nb);
         if (seg == 2) { lo = tok_lo; hi = min(tok_hi, im.s.T); }
         if (!live) hi = lo;
-        const int jlo = max(lo - k0, 0), jhi = min(hi - k0, kHalf);
-        const bool ok1 = mbar_wait_or_fail<SHORTW>(bar_s + 8 * grp, t & 1u, s_fail, a.wait_limit);
-        ok = __all_sync(0xffffffffu, ok1);
+        const uint32_t mask = bits(lo - k0 - part * 32, hi - k0 - part * 32);
+        const bool whole = __all_sync(0xffffffffu, mask == 0xffffffffu), some = __any_sync(0xffffffffu, mask != 0u);
+        const uint32_t tS = tmem + (t & 1u) * 128 + mine;
+        ok = wait_all(bar_s + 8 * (t & 1u), (t >> 1) & 1u);
         if (!ok) break;
         tc_fence_after();
-        const bool whole = __all_sync(0xffffffffu, jlo == 0 && jhi == kHalf);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float s[32], dp[32];
-          tmem_ld32_async(tS + h * 32, s);
-          tmem_ld32_async(tD + h * 32, dp);
-          tmem_wait_ld();
-          uint32_t ds[16];
+        float p[32], dp[32];
+        tmem_ld32_async(tS, p);
+        tmem_wait_ld();
+        if (some) {                                // uniform over the warp, no access to tensor memory inside
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            float q[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              q[i] = fast_exp2(fmaf(s[j + i], a.scale_log2, -l2)) * (dp[j + i] - dl);
-              if (!whole) q[i] = h * 32 + j + i >= jlo && h * 32 + j + i < jhi ? q[i] : 0.f;
-            }
-            ds[j / 2] = pack2(q[0], q[1]);
+            split(fma2(pair(p[j], p[j + 1]), scale2, minus_l), &p[j], &p[j + 1]);
+            p[j] = fast_exp2(p[j]);
+            p[j + 1] = fast_exp2(p[j + 1]);
           }
-          tmem_st16(tS + h * 16, ds);
+          if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) p[j] = (mask & (1u << j)) ? p[j] : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) p[j] = 0.f;
         }
+        ok = wait_all(bar_dp, t & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_ld32_async(tdP + mine, dp);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_r);
+        uint32_t ds[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          float q0, q1;
+          split(mul2(pair(p[j], p[j + 1]), add2(pair(dp[j], dp[j + 1]), minus_d)), &q0, &q1);
+          ds[j / 2] = pack2(q0, q1);
+        }
+        tmem_st16(tS, ds);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive_cta(bar_p + 8 * grp);
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_ds);
       }
       if (!ok) break;
-      const bool ok1 = mbar_wait_or_fail<SHORTW>(bar_f + 8 * grp, e & 1u, s_fail, a.wait_limit);
-      ok = __all_sync(0xffffffffu, ok1);
+      if (part >= 2) { ++e; continue; }            // two parts have 64 columns each
+      ok = wait_all(bar_f, e & 1u);
       if (!ok) break;
       tc_fence_after();
-      float o[kD];
+      float o[kD / 2];
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb) tmem_ld32_async(tO + cb * 32, o + cb * 32);
+      for (int cb = 0; cb < 2; ++cb) tmem_ld32_async(tO + lanes + part * 64 + cb * 32, o + cb * 32);
       tmem_wait_ld();
       tc_fence_before();
-      mbar_arrive_cta(bar_x + 8 * grp);
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cta(bar_x);
       ++e;
       if (live)
-        store_row(a.dq[im.kind] + ((int64_t)((im.kind == 0 ? im.s.tok_row : im.s.bea_row) + idx) * a.Hq + im.kvh * G + my_head) * kD, o, a.scale);
+        store_half_row(a.dq[im.kind] + ((int64_t)((im.kind == 0 ? im.s.tok_row : im.s.bea_row) + idx) * a.Hq + kvh * G + my_head) * kD + part * 64, o,
+                       a.scale);
     }
     if (!ok) *s_fail = 1;
   }
@@ -709,22 +835,23 @@ __global__ void __launch_bounds__(256) k_delta(const uint4* __restrict__ out_tok
   }
 }
 
-// Adds the pieces of the split items in order: one block per item, of dK or dV, and eight keys.
+// Adds the pieces of the split items in order: one block per item and head, of dK or dV, and eight keys.
 __global__ void __launch_bounds__(256) k_join(const JoinItem* __restrict__ items, const GradArgs a) {
-  const JoinItem im = items[blockIdx.x];
-  const int which = blockIdx.y & 1, key = (int)(blockIdx.y >> 1) * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const JoinItem im = items[blockIdx.x / a.Hkv];
+  const int kvh = blockIdx.x % a.Hkv, which = blockIdx.y & 1, key = (int)(blockIdx.y >> 1) * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int seg_len = im.seg == 0 ? im.s.P : (im.seg == 1 ? im.s.nb : im.s.T);
   if (im.k0 + key >= seg_len) return;
   float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int p = 0; p < im.count; ++p) {
-    const float4 v = *reinterpret_cast<const float4*>(a.partial + ((((int64_t)im.first + p) * 2 + which) * kTile + key) * kD + lane * 4);
+    const float4 v = *reinterpret_cast<const float4*>(a.partial + (((((int64_t)im.first + p) * a.Hkv + kvh) * 2 + which) * kTile + key) * kD + lane * 4);
     t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
   }
   const float f = which == 0 ? 1.f : a.scale;
   const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0 + key;
   uint2 o;
   o.x = pack2(t.x * f, t.y * f); o.y = pack2(t.z * f, t.w * f);
-  *reinterpret_cast<uint2*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + im.kvh) * kD + lane * 4) = o;
+  *reinterpret_cast<uint2*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + lane * 4) = o;
 }
 
 bool map_3d(CUtensorMap* m, const void* base, int heads, int64_t rows, int box_heads, int box_rows) {
@@ -743,32 +870,48 @@ struct Plan {
   std::vector<JoinItem> join;
   int64_t prompts = 0, tokens = 0, beacons = 0;
   int32_t slots = 0;
-  size_t at_kv = 0, at_q = 0, at_join = 0, at_lse = 0, at_delta = 0, at_partial = 0, total = 0;   // the status word is at 0
+  // the status word is at 0, the two queues' counters at 128 and 192
+  size_t at_kv = 0, at_q = 0, at_join = 0, lists = 0, at_lse = 0, at_delta = 0, at_partial = 0, total = 0;
 };
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kSms = 148;
-constexpr int kMinPiece = 24;   // query tiles: a piece's partial sums cost about five tiles' time
+constexpr int kMinPiece = 12;   // query tiles: a piece's partial sums cost about two tiles' time
+
+// Longest first: a counting sort, in the order of the list among equals.
+template <class Item, class Length>
+void longest_first(std::vector<Item>* items, Length length) {
+  int most = 0;
+  for (const Item& x : *items) most = std::max(most, length(x));
+  std::vector<int32_t> at(most + 2, 0);
+  for (const Item& x : *items) ++at[most - length(x) + 1];
+  for (int i = 0; i <= most; ++i) at[i + 1] += at[i];
+  std::vector<Item> sorted(items->size());
+  for (const Item& x : *items) sorted[at[most - length(x)]++] = x;
+  items->swap(sorted);
+}
 
 bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, const int32_t* cu_prompt, const int32_t* cu_tokens, Plan* p) {
   if (n_seqs < 1 || !cu_prompt || !cu_tokens || c < 1 || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads) return BC_ERR_INVALID_ARG;
   if (head_dim != kD || q_heads / kv_heads > 16) return BC_ERR_UNSUPPORTED;
-  const int G = q_heads / kv_heads, per = kHalf / G, wide = 2 * (kTile / G);
-  int64_t beacons = 0, work = 0, n_kv = 0, n_q = 0;
+  const int G = q_heads / kv_heads, per = kTile / G;
+  int64_t n_kv = 0, n_q = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const int64_t P = (int64_t)cu_prompt[i + 1] - cu_prompt[i], T = (int64_t)cu_tokens[i + 1] - cu_tokens[i];
     if (P < 0 || T < 0) return BC_ERR_INVALID_ARG;
     const int64_t nb = c > 1 ? T / c : 0;
-    beacons += nb;
+    p->beacons += nb;
     n_kv += (P + kTile - 1) / kTile + (nb + kTile - 1) / kTile + (T + kTile - 1) / kTile;
-    n_q += (T + wide - 1) / wide + (nb + wide - 1) / wide;
+    n_q += (T + per - 1) / per + (nb + per - 1) / per;
   }
   if (cu_prompt[0] != 0 || cu_tokens[0] != 0) return BC_ERR_INVALID_ARG;
   if ((n_kv + n_q) * kv_heads > (1 << 24)) return BC_ERR_UNSUPPORTED;
-  p->prompts = cu_prompt[n_seqs]; p->tokens = cu_tokens[n_seqs]; p->beacons = beacons;
+  p->prompts = cu_prompt[n_seqs]; p->tokens = cu_tokens[n_seqs];
 
-  auto tiles = [&](int rows) { return (rows + per - 1) / per; };
+  auto tiles = [&](int64_t rows) { return (int)((rows + per - 1) / per); };
   std::vector<KvItem> whole;
-  int64_t bea_row = 0;
+  whole.reserve(n_kv);
+  p->q.reserve(n_q);
+  int64_t bea_row = 0, work = 0;
   for (int i = 0; i < n_seqs; ++i) {
     SeqDesc s;
     s.P = cu_prompt[i + 1] - cu_prompt[i]; s.T = cu_tokens[i + 1] - cu_tokens[i]; s.nb = c > 1 ? s.T / c : 0;
@@ -786,70 +929,61 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
         }
         KvItem im = {};
         im.s = s; im.seg = seg; im.k0 = k0; im.slot = -1;
-        im.ta = (int)t_lo / per; im.nt = t_hi > t_lo ? tiles((int)t_hi) - im.ta : 0;
-        im.ba = (int)b_lo / per; im.nb_tiles = b_hi > b_lo ? tiles((int)b_hi) - im.ba : 0;
+        im.ta = (int)t_lo / per; im.nt = t_hi > t_lo ? tiles(t_hi) - im.ta : 0;
+        im.ba = (int)b_lo / per; im.nb_tiles = b_hi > b_lo ? tiles(b_hi) - im.ba : 0;
         work += im.nt + im.nb_tiles;
         whole.push_back(im);
       }
     }
     for (int kind = 0; kind < 2; ++kind) {
       const int len = kind == 0 ? s.T : s.nb;
-      for (int f = 0; f < len; f += wide) {
+      for (int f = 0; f < len; f += per) {
         QItem im = {};
-        im.s = s; im.kind = kind; im.first = f; im.count = std::min(wide, len - f);
+        im.s = s; im.kind = kind; im.first = f; im.count = std::min(per, len - f);
         const int last = f + im.count - 1;
         const int b_hi = kind == 0 ? (c > 1 ? last / c : 0) : last + 1;
         const int t_lo = kind == 0 ? (c > 1 ? f / c * c : 0) : f * c, t_hi = kind == 0 ? last + 1 : (last + 1) * c;
-        im.lo2 = t_lo / kHalf * kHalf;
-        im.nt0 = (s.P + kHalf - 1) / kHalf; im.nt1 = (b_hi + kHalf - 1) / kHalf; im.nt2 = (t_hi - im.lo2 + kHalf - 1) / kHalf;
-        for (int h = 0; h < kv_heads; ++h) { im.kvh = h; p->q.push_back(im); }
+        im.lo2 = t_lo / kTile * kTile;
+        im.nt0 = (s.P + kTile - 1) / kTile; im.nt1 = (b_hi + kTile - 1) / kTile; im.nt2 = (t_hi - im.lo2 + kTile - 1) / kTile;
+        p->q.push_back(im);
       }
     }
   }
-  // An item is cut where it is longer than a third of an SM's share of all the work, so that the last items to end are short
-  const int64_t piece = std::max<int64_t>(kMinPiece, work * kv_heads / (kSms * 3));
+  // An item is cut where it is longer than a quarter of an SM's share of all the work, so that the last ones to end are short
+  const int64_t piece = std::max<int64_t>(kMinPiece, work * kv_heads / (kSms * 4));
   for (const KvItem& w : whole) {
     const int N = w.nt + w.nb_tiles;
     const int pieces = N > piece + piece / 2 ? (int)((N + piece - 1) / piece) : 1;
-    for (int h = 0; h < kv_heads; ++h) {
+    if (pieces == 1) {
+      p->kv.push_back(w);
+      continue;
+    }
+    JoinItem j = {};
+    j.s = w.s; j.seg = w.seg; j.k0 = w.k0; j.first = p->slots; j.count = pieces;
+    p->join.push_back(j);
+    for (int q = 0; q < pieces; ++q) {
+      const int a = (int)((int64_t)N * q / pieces), b = (int)((int64_t)N * (q + 1) / pieces);   // tiles [a, b) of the item
       KvItem im = w;
-      im.kvh = h;
-      if (pieces > 1) {
-        JoinItem j = {};
-        j.s = w.s; j.seg = w.seg; j.k0 = w.k0; j.kvh = h; j.first = p->slots; j.count = pieces;
-        p->join.push_back(j);
-      }
-      for (int q = 0; q < pieces; ++q) {
-        const int a = (int)((int64_t)N * q / pieces), b = (int)((int64_t)N * (q + 1) / pieces);   // tiles [a, b) of the item
-        im.ta = w.ta + std::min(a, w.nt); im.nt = std::min(b, w.nt) - std::min(a, w.nt);
-        im.ba = w.ba + std::max(a - w.nt, 0); im.nb_tiles = std::max(b - w.nt, 0) - std::max(a - w.nt, 0);
-        im.slot = pieces > 1 ? p->slots++ : -1;
-        p->kv.push_back(im);
-      }
+      im.ta = w.ta + std::min(a, w.nt); im.nt = std::min(b, w.nt) - std::min(a, w.nt);
+      im.ba = w.ba + std::max(a - w.nt, 0); im.nb_tiles = std::max(b - w.nt, 0) - std::max(a - w.nt, 0);
+      im.slot = p->slots++;
+      p->kv.push_back(im);
     }
   }
-  std::stable_sort(p->kv.begin(), p->kv.end(), [](const KvItem& x, const KvItem& y) { return x.nt + x.nb_tiles > y.nt + y.nb_tiles; });
-  std::stable_sort(p->q.begin(), p->q.end(), [](const QItem& x, const QItem& y) { return x.nt0 + x.nt1 + x.nt2 > y.nt0 + y.nt1 + y.nt2; });
+  longest_first(&p->kv, [](const KvItem& x) { return x.nt + x.nb_tiles; });
+  longest_first(&p->q, [](const QItem& x) { return x.nt0 + x.nt1 + x.nt2; });
   size_t o = 256;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes); return at; };
   p->at_kv = take(p->kv.size() * sizeof(KvItem));
   p->at_q = take(p->q.size() * sizeof(QItem));
   p->at_join = take(p->join.size() * sizeof(JoinItem));
+  p->lists = o;
   const size_t stats = (size_t)(p->tokens + p->beacons) * q_heads * sizeof(float);
   p->at_lse = take(stats);
   p->at_delta = take(stats);
-  p->at_partial = take((size_t)p->slots * 2 * kTile * kD * sizeof(float));
+  p->at_partial = take((size_t)p->slots * kv_heads * 2 * kTile * kD * sizeof(float));
   p->total = o;
   return BC_OK;
-}
-
-int sm_count() {
-  static int n = 0;
-  if (!n) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = kSms;
-  }
-  return n;
 }
 
 uint32_t g_wait_limit = 0;   // bc_mask_attn_backward_set_wait_limit (0: kWaitLimit)
@@ -897,13 +1031,14 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     cudaStream_t s = (cudaStream_t)stream;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (!encode_tiled()) return BC_ERR_CUDA;
-    // the lists are pageable host memory: they have been staged when the calls return
-    if (cudaMemsetAsync(ws, 0, 4, s) != cudaSuccess) return BC_ERR_CUDA;
+    // pageable host memory: it has been staged when the copy returns
+    std::vector<uint8_t> lists(p.lists, 0);        // the status word, the queues' counters, the lists: one copy
+    auto put = [&](size_t at, const void* from, size_t bytes) { if (bytes) memcpy(lists.data() + at, from, bytes); };
+    put(p.at_kv, p.kv.data(), p.kv.size() * sizeof(KvItem));
+    put(p.at_q, p.q.data(), p.q.size() * sizeof(QItem));
+    put(p.at_join, p.join.data(), p.join.size() * sizeof(JoinItem));
+    if (cudaMemcpyAsync(ws, lists.data(), p.lists, cudaMemcpyHostToDevice, s) != cudaSuccess) return BC_ERR_CUDA;
     if (p.kv.empty()) return BC_OK;
-    if (cudaMemcpyAsync(ws + p.at_kv, p.kv.data(), p.kv.size() * sizeof(KvItem), cudaMemcpyHostToDevice, s) != cudaSuccess ||
-        (!p.q.empty() && cudaMemcpyAsync(ws + p.at_q, p.q.data(), p.q.size() * sizeof(QItem), cudaMemcpyHostToDevice, s) != cudaSuccess) ||
-        (!p.join.empty() && cudaMemcpyAsync(ws + p.at_join, p.join.data(), p.join.size() * sizeof(JoinItem), cudaMemcpyHostToDevice, s) != cudaSuccess))
-      return BC_ERR_CUDA;
 
     GradArgs a = {};
     a.lse2 = reinterpret_cast<float*>(ws + p.at_lse); a.delta = reinterpret_cast<float*>(ws + p.at_delta);
@@ -913,7 +1048,7 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     a.dq[0] = (__nv_bfloat16*)d_tok_q; a.dq[1] = (__nv_bfloat16*)d_beacon_q;
     a.partial = reinterpret_cast<float*>(ws + p.at_partial);
     a.status = reinterpret_cast<int32_t*>(ws);
-    a.Hq = q_heads; a.Hkv = kv_heads; a.G = G; a.c = c;
+    a.Hq = q_heads; a.Hkv = kv_heads; a.G = G; a.c = c; a.per = kTile / G;
     a.scale = sm_scale; a.scale_log2 = sm_scale * kLog2e;
     a.wait_limit = g_wait_limit ? g_wait_limit : kWaitLimit;
     const void* dummy = ws;   // arrays that do not exist get a map that is never used
@@ -932,28 +1067,28 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
              map_3d(&m->v[i], k_rows[i] ? v[i] : dummy, kv_heads, k_rows[i], 1, k_box);
       return ok;
     };
-    KvMaps kv_maps, q_maps;
-    if (!maps_for(&kv_maps, kHalf / G, kTile) || !maps_for(&q_maps, kTile / G, kHalf)) return BC_ERR_CUDA;
+    KvMaps maps;
+    if (!maps_for(&maps, kTile / G, kTile)) return BC_ERR_CUDA;
     const bool shortw = g_wait_limit != 0;
-    const int kv_smem = 2 * kWide + kKvRing * 2 * kSlim + 1024, q_smem = 4 * kWide + kQRing * 2 * kSlim + 1024;
+    const int smem = 2 * kWide + kRing * 2 * kWide + 1024;   // of either kernel
     auto* dkv = shortw ? k_dkv<true> : k_dkv<false>;
     auto* dq = shortw ? k_dq<true> : k_dq<false>;
-    if (cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, kv_smem) != cudaSuccess ||
-        cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, q_smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+        cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
       return BC_ERR_CUDA;
-    const int sms = sm_count();
     if (a.rows > 0) {
       const int64_t blocks = (a.rows * q_heads + 15) / 16;
-      k_delta<<<(unsigned)std::min<int64_t>(blocks, sms * 8), 256, 0, s>>>(
+      k_delta<<<(unsigned)std::min<int64_t>(blocks, kSms * 8), 256, 0, s>>>(
           (const uint4*)out_tok, (const uint4*)d_out_tok, lse_tok, (const uint4*)out_beacon, (const uint4*)d_out_beacon, lse_beacon, p.tokens,
           a.rows, q_heads, G, const_cast<float*>(a.lse2), const_cast<float*>(a.delta));
       GradArgs b = a;
-      b.items = ws + p.at_q; b.n_items = (int32_t)p.q.size(); b.per = kTile / G;
-      dq<<<std::min(b.n_items, sms), kThreads, q_smem, s>>>(b, q_maps);
+      b.items = ws + p.at_q; b.n_items = (int32_t)p.q.size() * kv_heads; b.next = reinterpret_cast<int32_t*>(ws + 128);
+      dq<<<std::min(b.n_items, kSms), kThreads, smem, s>>>(b, maps);
     }
-    a.items = ws + p.at_kv; a.n_items = (int32_t)p.kv.size(); a.per = kHalf / G;
-    dkv<<<std::min(a.n_items, sms), kThreads, kv_smem, s>>>(a, kv_maps);
-    if (!p.join.empty()) k_join<<<dim3((unsigned)p.join.size(), 2 * kTile / 8), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
+    a.items = ws + p.at_kv; a.n_items = (int32_t)p.kv.size() * kv_heads; a.next = reinterpret_cast<int32_t*>(ws + 192);
+    dkv<<<std::min(a.n_items, kSms), kThreads, smem, s>>>(a, maps);
+    if (!p.join.empty())
+      k_join<<<dim3((unsigned)p.join.size() * kv_heads, 2 * kTile / 8), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
     return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
   } catch (...) {
     return BC_ERR_UNSUPPORTED;
