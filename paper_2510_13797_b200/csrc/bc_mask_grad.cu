@@ -16,7 +16,7 @@
 // and dS, each for 32 rows and 32 columns of tensor memory, while the tensor pipe runs the products of the neighbouring tile.
 // The operands that are read along their rows (dO, Q, K in the second products) are the tiles as they are stored, N-major.
 // Long items of k_dkv (the prompt's keys are seen by every row of a trajectory) are cut into pieces whose fp32 sums
-// k_join adds up in order.  k_delta computes D and lays D and L out by KV head beforehand.
+// k_join adds up in order.  k_dq runs first: it also computes D and leaves D and L by tiles for k_dkv.
 //
 // Rows that a copy brings in past a sequence's end belong to its neighbour: their weights are set to zero by selection, and
 // where such a row is itself a factor (K in dS K; Q and dO in dS^T Q and P^T dO) it is cleared in shared memory first.
@@ -37,12 +37,14 @@ constexpr int kWide = kTile * kD * 2;              // bytes of an operand
 constexpr uint32_t kWeighers = 16;                 // warps that turn S and dP into P and dS
 constexpr int kThreads = 64 + 32 * kWeighers;      // warp 0: copies, warp 1: products, then those
 constexpr uint32_t kReaders = 1 + kWeighers;       // warps that read the item numbers
-constexpr int kRing = 2;
+constexpr int kRing3 = 3, kRing2 = 2;              // places for tiles that are needed long (Q, K in dS K) and short (dO, V)
+constexpr int kSmem = 7 * kWide + 2048 + 512;      // seven operands, numbers, barriers: all of a block's shared memory
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct SeqDesc {
   int32_t P, T, nb;                                // lengths
   int32_t prompt_row, tok_row, bea_row;            // first rows in the packed arrays
+  int32_t tok_tile, bea_tile;                      // numbers of the first query tiles (128 / G tokens or beacons each)
 };
 // The work lists are for all KV heads: item i of a list of n is entry i / kv_heads for head i % kv_heads.
 // A tile of keys and the query tiles that see any of them (tiles of 128 / G tokens or beacons)
@@ -51,20 +53,20 @@ struct KvItem {
   int32_t seg, k0;                                 // 0 prompt, 1 beacons, 2 tokens; first key
   int32_t ta, nt, ba, nb_tiles;                    // first token tile, how many, first beacon tile, how many
   int32_t slot;                                    // place of the partial sums (times kv_heads, plus head); -1: not cut into pieces
-  int32_t pad[3];
+  int32_t pad;
 };
 // Up to 128 / G tokens or beacons
 struct QItem {
   SeqDesc s;
   int32_t kind, first, count;                      // 0 tokens, 1 beacons
   int32_t nt0, nt1, nt2, lo2;                      // tiles of 128 keys: prompt, beacons, tokens from lo2 on
-  int32_t pad[3];
+  int32_t tile;                                    // its number
 };
 // A tile of keys that was cut: its pieces are the places first .. first + count - 1
 struct JoinItem {
   SeqDesc s;
   int32_t seg, k0, first, count;
-  int32_t pad[6];
+  int32_t pad[4];
 };
 static_assert(sizeof(KvItem) == 64 && sizeof(QItem) == 64 && sizeof(JoinItem) == 64, "descriptors are 64 bytes");
 
@@ -73,8 +75,9 @@ struct GradArgs {
   const void* items;
   int32_t n_items;                                 // entries times kv_heads
   int32_t* next;                                   // the next item to be taken
-  const float *lse2, *delta;                       // [kv_heads][rows][G]: log2(e) L and D; rows: tokens, then beacons
-  int64_t rows, tok_rows;
+  const __nv_bfloat16* out[2];                     // by kind
+  const float* lse[2];
+  float* stats;                                    // [query tiles][kv_heads][2][128]: -log2(e) L and -D of the tile's rows, left by k_dq for k_dkv
   __nv_bfloat16 *dk[3], *dv[3], *dq[2];
   float* partial;                                  // [slots][2][128][128]
   int32_t* status;
@@ -86,9 +89,6 @@ struct GradArgs {
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&t);
-}
-__device__ __forceinline__ int64_t stat_at(const GradArgs& a, const SeqDesc& s, int kvh, int kind, int first) {
-  return ((int64_t)kvh * a.rows + (kind == 0 ? s.tok_row : a.tok_rows + s.bea_row) + first) * a.G;
 }
 // Half a row of an accumulator, 64 columns, times f, as bf16
 __device__ __forceinline__ void store_half_row(__nv_bfloat16* dst, const float* o, float f) {
@@ -162,6 +162,30 @@ __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// 2^y for two numbers below 128, by arithmetic: the special-function unit, at a quarter of the rate of the others, would bound the kernels
+// by its 16,384 exponentials per tile.  y = n + f with n the nearest integer, 2^f by a polynomial of degree 4 (minimax on
+// [-1/2, 1/2], within 3e-6), n added to the exponent.  Below -126 the result stays at 2^-126.
+__device__ __forceinline__ void exp2_pair(F2 y, float* a, float* b) {
+  float y0, y1;
+  split(y, &y0, &y1);
+  y = pair(fmaxf(y0, -126.f), fmaxf(y1, -126.f));
+  const F2 magic = pair(12582912.f, 12582912.f);   // 1.5 * 2^23: adding it rounds to an integer, in the last bits of the sum
+  const F2 t = add2(y, magic);
+  const F2 f = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), y);
+  F2 q = fma2(f, pair(0.009570086f, 0.009570086f), pair(0.055917852f, 0.055917852f));
+  q = fma2(q, f, pair(0.24024744f, 0.24024744f));
+  q = fma2(q, f, pair(0.6931218f, 0.6931218f));
+  q = fma2(q, f, pair(0.9999993f, 0.9999993f));
+  float t0, t1, q0, q1;
+  split(t, &t0, &t1);
+  split(q, &q0, &q1);
+  *a = __int_as_float(__float_as_int(q0) + (__float_as_int(t0) << 23));
+  *b = __int_as_float(__float_as_int(q1) + (__float_as_int(t1) << 23));
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
 // Bits [lo, hi) of 32
 __device__ __forceinline__ uint32_t bits(int lo, int hi) {
   lo = max(lo, 0);
@@ -176,51 +200,53 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
 //     dP(t + 1) behind dK += dS(t) Q, while they turn S(t + 1) into P(t + 1).
 //
 // Barriers (t counts query tiles, e items; parity = uses so far & 1):
-//   full[r] / empty[r]: Q and dO of ring place r have landed / been read      k, v / kfree, vfree: K, V of item e have landed / been read
-//   s, dp: S^T, dP^T of tile t are there      p, ds: P^T, dS^T of tile t have been stored
-//   f: dK and dV of item e are final          x: they have been read          d: drain on the give-up path
+//   fq[r] / eq[r], fo[r] / eo[r]: Q, or dO with the tile's numbers, has landed in a ring place / been read
+//   k, v / kfree, vfree: K, V of item e have landed / been read      s, dp: S^T, dP^T of tile t are there
+//   p, ds: P^T, dS^T of tile t have been stored      f: dK and dV of item e are final      x: they have been read
+//   d: drain on the give-up path
 template <bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __grid_constant__ KvMaps maps) {
-  extern __shared__ __align__(1024) uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sK = smem_addr(smem), sV = sK + kWide, sRing = sV + kWide;   // ring place r: Q at sRing + r * 2 kWide, dO behind it
-  constexpr int kBars = 2 * kRing + 15;
-  __shared__ __align__(8) uint64_t s_bars[kBars];
-  __shared__ int s_item[2];
-  __shared__ __align__(16) float s_stat[kWeighers][2][32];   // a warp's copy of its columns' -L and -D
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_fail_word;
-  volatile int* s_fail = &s_fail_word;
-  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kRing, bar_k = bar_empty + 8 * kRing, bar_v = bar_k + 8, bar_kfree = bar_k + 16,
-                 bar_vfree = bar_k + 24, bar_s = bar_k + 32, bar_dp = bar_k + 40, bar_p = bar_k + 48, bar_ds = bar_k + 56, bar_f = bar_k + 64,
-                 bar_x = bar_k + 72, bar_d = bar_k + 80;
-  const Queue queue = {smem_addr(s_item), bar_k + 88, bar_k + 104};
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sK = smem_addr(smem), sV = sK + kWide, sQ = sV + kWide, sO = sQ + kRing3 * kWide, sStat = sO + kRing2 * kWide, sBars = sStat + 2048;
+  const float* stats = reinterpret_cast<const float*>(smem + 7 * kWide);   // [kRing2][2][128]
+  volatile int* s_misc = reinterpret_cast<volatile int*>(smem + 7 * kWide + 2048 + 256);   // two item numbers, the tensor memory, failure
+  volatile int* s_fail = s_misc + 3;
+  const uint32_t bar_fq = sBars, bar_eq = bar_fq + 8 * kRing3, bar_fo = bar_eq + 8 * kRing3, bar_eo = bar_fo + 8 * kRing2, bar_k = bar_eo + 8 * kRing2,
+                 bar_v = bar_k + 8, bar_kfree = bar_k + 16, bar_vfree = bar_k + 24, bar_s = bar_k + 32, bar_dp = bar_k + 40, bar_p = bar_k + 48,
+                 bar_ds = bar_k + 56, bar_f = bar_k + 64, bar_x = bar_k + 72, bar_d = bar_k + 80;
+  const Queue queue = {smem_addr(const_cast<int*>(s_misc)), bar_k + 88, bar_k + 104};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const KvItem* items = static_cast<const KvItem*>(a.items);
 
+  if (sK & 1023) {                       // the operands' layouts need it; shared memory begins so
+    if (tid == 0) atomicCAS(a.status, 0, BC_ERR_CUDA);
+    return;
+  }
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) {
-      const uint32_t bar = bar_full + 8 * i;
-      const uint32_t count = bar == bar_p || bar == bar_ds || bar == bar_x ? kWeighers : (bar >= queue.empty ? kReaders : 1u);
+    for (uint32_t bar = sBars; bar < queue.empty + 16; bar += 8) {
+      const uint32_t count = bar == bar_p || bar == bar_ds || bar == bar_x ? kWeighers
+                             : bar >= bar_eo && bar < bar_k                ? 1 + kWeighers
+                             : bar >= queue.empty                          ? kReaders
+                                                                           : 1u;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_misc + 2))), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int box_rows = a.per * a.G;      // rows that a copy writes; the others (G does not divide 128) stay zero
-  for (int idx = tid; idx < (kTile - box_rows) * 16 * 2 * kRing; idx += kThreads) {
+  for (int idx = tid; idx < (kTile - box_rows) * 16 * (kRing3 + kRing2); idx += kThreads) {
     const int op = idx / ((kTile - box_rows) * 16), rest = idx % ((kTile - box_rows) * 16);
-    st_zero16(sRing + op * kWide + swz(box_rows + (rest >> 4), rest & 15));
+    st_zero16(sQ + op * kWide + swz(box_rows + (rest >> 4), rest & 15));
   }
   proxy_fence();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem, tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+  const uint32_t tmem = (uint32_t)s_misc[2], tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
   auto wait_all = [&](uint32_t bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
   };
@@ -228,8 +254,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   if (warp == 0) {
     // ---- copies ----------------------------------------------------------------------------------------------------------
     bool ok = true;
-    uint32_t t = 0, e = 0, e_v = 0;
-    const uint32_t bytes = (uint32_t)(2 * box_rows * kD * 2);
+    uint32_t t_q = 0, t_o = 0, e = 0, e_v = 0;     // copies begun
+    const uint32_t bytes = (uint32_t)(box_rows * kD * 2);
     for (uint32_t i = 0;; ++i) {
       int it;
       ok = queue.draw<SHORTW>(i, a, s_fail, &it);
@@ -248,24 +274,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
       }
       __syncwarp();
       ++e;
-      for (int n = 0; n < N; ++n, ++t) {
-        const uint32_t place = t % kRing;
-        if (t >= kRing) ok = wait_all(bar_empty + 8 * place, (t / kRing - 1) & 1u);
+      for (int n = 0; n < N; ++n) {
+        const int kind = n < im.nt ? 0 : 1, tile = kind == 0 ? im.ta + n : im.ba + n - im.nt;
+        const int row = (kind == 0 ? im.s.tok_row : im.s.bea_row) + tile * a.per;
+        const uint32_t pq = t_q % kRing3, po = t_o % kRing2;
+        if (t_q >= kRing3) ok = wait_all(bar_eq + 8 * pq, (t_q / kRing3 - 1) & 1u);
         if (!ok) break;
         if (elect_one()) {
-          const int kind = n < im.nt ? 0 : 1, tile = kind == 0 ? im.ta + n : im.ba + n - im.nt;
-          const int row = (kind == 0 ? im.s.tok_row : im.s.bea_row) + tile * a.per;
-          const uint32_t dst = sRing + place * 2 * kWide, bar = bar_full + 8 * place;
+          const uint32_t dst = sQ + pq * kWide, bar = bar_fq + 8 * pq;
           mbar_expect_tx(bar, bytes);
           tma_3d(dst, &maps.q[kind], 0, kvh * a.G, row, bar);
           tma_3d(dst + kTile * 128, &maps.q[kind], 64, kvh * a.G, row, bar);
-          tma_3d(dst + kWide, &maps.o[kind], 0, kvh * a.G, row, bar);
-          tma_3d(dst + kWide + kTile * 128, &maps.o[kind], 64, kvh * a.G, row, bar);
         }
         __syncwarp();
+        ++t_q;
         if (n == 0) {                              // V is wanted a little later than K and the first Q
-          if (e > 1) ok = wait_all(bar_vfree, (e - 2) & 1u);
-          if (!ok) { ++t; break; }
+          if (e_v > 0) ok = wait_all(bar_vfree, (e_v - 1) & 1u);
+          if (!ok) break;
           if (elect_one()) {
             mbar_expect_tx(bar_v, kWide);
             tma_3d(sV, &maps.v[im.seg], 0, kvh, key_row, bar_v);
@@ -274,6 +299,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
           __syncwarp();
           ++e_v;
         }
+        if (t_o >= kRing2) ok = wait_all(bar_eo + 8 * po, (t_o / kRing2 - 1) & 1u);
+        if (!ok) break;
+        if (elect_one()) {
+          const uint32_t dst = sO + po * kWide, bar = bar_fo + 8 * po;
+          mbar_expect_tx(bar, bytes + 1024);
+          tma_3d(dst, &maps.o[kind], 0, kvh * a.G, row, bar);
+          tma_3d(dst + kTile * 128, &maps.o[kind], 64, kvh * a.G, row, bar);
+          bulk_copy(sStat + po * 1024, a.stats + ((int64_t)((kind == 0 ? im.s.tok_tile : im.s.bea_tile) + tile) * a.Hkv + kvh) * 256, 1024, bar);
+        }
+        __syncwarp();
+        ++t_o;
       }
       if (!ok) break;
     }
@@ -283,14 +319,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     int never = 0;
     if (e > 0) mbar_wait_or_fail<false>(bar_k, (e - 1) & 1u, &never, kWaitLimit);
     if (e_v > 0) mbar_wait_or_fail<false>(bar_v, (e_v - 1) & 1u, &never, kWaitLimit);
-    for (uint32_t b = t > kRing ? t - kRing : 0; b < t; ++b)
-      mbar_wait_or_fail<false>(bar_full + 8 * (b % kRing), (b / kRing) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t_q > kRing3 ? t_q - kRing3 : 0; b < t_q; ++b)
+      mbar_wait_or_fail<false>(bar_fq + 8 * (b % kRing3), (b / kRing3) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t_o > kRing2 ? t_o - kRing2 : 0; b < t_o; ++b)
+      mbar_wait_or_fail<false>(bar_fo + 8 * (b % kRing2), (b / kRing2) & 1u, &never, kWaitLimit);
     __syncwarp();
   } else if (warp == 1) {
     // ---- products --------------------------------------------------------------------------------------------------------
     bool ok = true, issued = false;
     uint32_t t = 0, e = 0;
-    const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sRing), dQn = umma_desc_nmajor(sRing);
+    const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sQ), dO = umma_desc(sO), dQn = umma_desc_nmajor(sQ), dOn = umma_desc_nmajor(sO);
     auto first = [&](uint32_t to, uint64_t key, uint64_t q, uint32_t bar, uint32_t bar_free, bool last) {   // S^T or dP^T
       if (elect_one()) {
 #pragma unroll
@@ -316,51 +354,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
       const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
-      auto at = [&](uint32_t tile) { return (uint64_t)((tile % kRing) * 2 * kWide >> 4); };
-      auto landed = [&](int n) {                   // Q and dO of the item's tile n; rows of the next sequence are cleared: they are factors
-        const uint32_t tile = t + n, place = tile % kRing;
-        if (!wait_all(bar_full + 8 * place, (tile / kRing) & 1u)) return false;
+      auto at_q = [&](uint32_t tile) { return (uint64_t)(tile % kRing3 * kWide >> 4); };
+      auto at_o = [&](uint32_t tile) { return (uint64_t)(tile % kRing2 * kWide >> 4); };
+      auto landed = [&](int n, uint32_t bar, uint32_t parity, uint32_t at) {   // an operand of tile n; rows of the next sequence are cleared: they are factors
+        if (!wait_all(bar, parity)) return false;
         const int kind = n < im.nt ? 0 : 1, q = kind == 0 ? im.ta + n : im.ba + n - im.nt;
         const int valid = min((kind == 0 ? im.s.T : im.s.nb) - q * a.per, a.per) * a.G;
         if (valid < box_rows) {
-          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) {
-            st_zero16(sRing + place * 2 * kWide + swz(idx >> 4, idx & 15));
-            st_zero16(sRing + place * 2 * kWide + kWide + swz(idx >> 4, idx & 15));
-          }
+          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(at + swz(idx >> 4, idx & 15));
           proxy_fence();
           __syncwarp();
         }
         tc_fence_after();
         return true;
       };
-      ok = wait_all(bar_k, e & 1u) && landed(0);
+      auto landed_q = [&](int n) { const uint32_t tile = t + n, r = tile % kRing3; return landed(n, bar_fq + 8 * r, (tile / kRing3) & 1u, sQ + r * kWide); };
+      auto landed_o = [&](int n) { const uint32_t tile = t + n, r = tile % kRing2; return landed(n, bar_fo + 8 * r, (tile / kRing2) & 1u, sO + r * kWide); };
+      ok = wait_all(bar_k, e & 1u) && landed_q(0);
       if (!ok) break;
-      first(tS, dK, dQ + at(t), bar_s, bar_kfree, N == 1);
-      ok = wait_all(bar_v, e & 1u);
+      first(tS, dK, dQ + at_q(t), bar_s, bar_kfree, N == 1);
+      ok = wait_all(bar_v, e & 1u) && landed_o(0);
       if (!ok) break;
-      tc_fence_after();
-      first(tdP, dV, dQ + at(t) + (kWide >> 4), bar_dp, bar_vfree, N == 1);
+      first(tdP, dV, dO + at_o(t), bar_dp, bar_vfree, N == 1);
       for (int n = 0; n < N; ++n) {
         const bool more = n + 1 < N;
         const uint32_t tile = t + n;
-        if (more) ok = landed(n + 1);
-        ok = ok && wait_all(bar_p, tile & 1u);
+        ok = wait_all(bar_p, tile & 1u);
         if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
         if (!ok) break;
         tc_fence_after();
-        if (elect_one()) second(tV, tS, dQn + at(tile) + (kWide >> 4), n == 0);
+        if (elect_one()) {
+          second(tV, tS, dOn + at_o(tile), n == 0);
+          umma_commit(bar_eo + 8 * (tile % kRing2));
+        }
         __syncwarp();
-        if (more) first(tS, dK, dQ + at(tile + 1), bar_s, bar_kfree, n + 2 == N);
+        if (more) {
+          ok = landed_q(n + 1);
+          if (!ok) break;
+          first(tS, dK, dQ + at_q(tile + 1), bar_s, bar_kfree, n + 2 == N);
+        }
         ok = wait_all(bar_ds, tile & 1u);
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
-          second(tK, tdP, dQn + at(tile), n == 0);
-          umma_commit(bar_empty + 8 * (tile % kRing));
+          second(tK, tdP, dQn + at_q(tile), n == 0);
+          umma_commit(bar_eq + 8 * (tile % kRing3));
           if (!more) umma_commit(bar_f);
         }
         __syncwarp();
-        if (more) first(tdP, dV, dQ + at(tile + 1) + (kWide >> 4), bar_dp, bar_vfree, n + 2 == N);
+        if (more) {
+          ok = landed_o(n + 1);
+          if (!ok) break;
+          first(tdP, dV, dO + at_o(tile + 1), bar_dp, bar_vfree, n + 2 == N);
+        }
       }
       if (!ok) break;
       t += N;
@@ -379,7 +425,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   } else {
     // ---- weights: one key and 32 query rows per thread ------------------------------------------------------------------------
     const int part = (warp - 2) >> 2;              // columns [32 part, + 32)
-    float (*stats)[32] = s_stat[warp - 2];
     // a warp reaches the 32 lanes of tensor memory that belong to its number modulo 4; its keys are those lanes
     const int key = (warp & 3) * 32 + lane;
     const uint32_t mine = ((uint32_t)((warp & 3) * 32) << 16) + part * 32;
@@ -403,30 +448,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         if (c > 1) { tok_hi = min(im.s.T, (k / c + 1) * c); bea_lo = k / c; bea_hi = min(im.s.nb, k / c + 1); }
       }
       if (!live) tok_hi = bea_hi = 0;
-      float my_l, my_d;                            // of this lane's query row of the next tile
-      auto fetch = [&](int n) {
-        const int kind = n < im.nt ? 0 : 1, first = (kind == 0 ? im.ta + n : im.ba + n - im.nt) * a.per;
-        const int valid = min((kind == 0 ? im.s.T : im.s.nb) - first, a.per) * G;
-        const int64_t at = stat_at(a, im.s, kvh, kind, first) + part * 32 + lane;
-        const bool in = part * 32 + lane < valid;
-        my_l = in ? a.lse2[at] : 0.f;
-        my_d = in ? a.delta[at] : 0.f;
-      };
-      if (N > 0) fetch(0);
       for (int n = 0; n < N; ++n, ++t) {
-        __syncwarp();                              // the last tile's numbers have been read
-        stats[0][lane] = -my_l; stats[1][lane] = -my_d;
-        __syncwarp();
-        if (n + 1 < N) fetch(n + 1);
         const int kind = n < im.nt ? 0 : 1, first = (kind == 0 ? im.ta + n : im.ba + n - im.nt) * a.per;
         const int all = min((kind == 0 ? im.s.T : im.s.nb) - first, a.per) * G;
         const int lo = kind == 0 ? tok_lo : bea_lo, hi = kind == 0 ? tok_hi : bea_hi;
         const int jlo = min(max(lo - first, 0), a.per) * G, jhi = min(min(hi - first, a.per) * G, all);
         const uint32_t mask = bits(jlo - part * 32, jhi - part * 32);
         const bool whole = __all_sync(0xffffffffu, mask == 0xffffffffu), some = __any_sync(0xffffffffu, mask != 0u);
-        ok = wait_all(bar_s, t & 1u);
+        ok = wait_all(bar_fo + 8 * (t % kRing2), (t / kRing2) & 1u) && wait_all(bar_s, t & 1u);   // the numbers have landed with dO
         if (!ok) break;
         tc_fence_after();
+        const float *minus_l = stats + t % kRing2 * 256 + part * 32, *minus_d = minus_l + 128;
         float p[32];
         tmem_ld32_async(tS + mine, p);
         tmem_wait_ld();
@@ -434,11 +466,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         if (some) {                                // uniform over the warp, no access to tensor memory inside
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(&stats[0][j]);
+            const ulonglong2 l = *reinterpret_cast<const ulonglong2*>(minus_l + j);
             split(fma2(pair(p[j], p[j + 1]), scale2, l.x), &p[j], &p[j + 1]);
-            split(fma2(pair(p[j + 2], p[j + 3]), scale2, l.y), &p[j + 2], &p[j + 3]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) p[j + u] = fast_exp2(p[j + u]);
+            p[j] = fast_exp2(p[j]);                // every other pair on the special-function unit
+            p[j + 1] = fast_exp2(p[j + 1]);
+            exp2_pair(fma2(pair(p[j + 2], p[j + 3]), scale2, l.y), &p[j + 2], &p[j + 3]);
           }
           if (!whole) {
 #pragma unroll
@@ -464,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         // where the weight is 0 the score gradient is, too: dP is finite there, rows of other sequences having been cleared
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
-          const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(&stats[1][j]);
+          const ulonglong2 d = *reinterpret_cast<const ulonglong2*>(minus_d + j);
           float q[4];
           split(mul2(pair(p[j], p[j + 1]), add2(pair(dp[j], dp[j + 1]), d.x)), &q[0], &q[1]);
           split(mul2(pair(p[j + 2], p[j + 3]), add2(pair(dp[j + 2], dp[j + 3]), d.y)), &q[2], &q[3]);
@@ -475,7 +507,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cta(bar_ds);
+        if (lane == 0) {
+          mbar_arrive_cta(bar_ds);
+          mbar_arrive_cta(bar_eo + 8 * (t % kRing2));   // the numbers have been read
+        }
       }
       if (!ok) break;
       // ---- the item's sums: parts 0 and 1 have dV, 2 and 3 dK, 64 columns each
@@ -520,35 +555,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
 // ---- dQ ------------------------------------------------------------------------------------------------------------------------
 // Tensor memory: columns [0, 128) and [128, 256) S of even and odd tiles, then dS in the first 16 columns of every 32; [256, 384) dP,
 // [384, 512) dQ.  S(n + 1) is made while the weights' warps work on tile n, dP(n + 1) as soon as they have read dP(n).
-// Barriers as above, with q / qfree for the item's Q and dO, and r: dP of tile t has been read.
+// At the beginning of an item those warps compute D from dO and O and leave it, with L, for k_dkv.
+// Barriers as above, with q / qfree for the item's Q and dO, r: dP of tile t has been read, w: the parts of D have been written.
 template <bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __grid_constant__ KvMaps maps) {
-  extern __shared__ __align__(1024) uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sQ = smem_addr(smem), sO = sQ + kWide, sRing = sO + kWide;   // ring place r: K at sRing + r * 2 kWide, V behind it
-  constexpr int kBars = 2 * kRing + 14;
-  __shared__ __align__(8) uint64_t s_bars[kBars];
-  __shared__ int s_item[2];
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_fail_word;
-  volatile int* s_fail = &s_fail_word;
-  const uint32_t bar_full = smem_addr(s_bars), bar_empty = bar_full + 8 * kRing, bar_q = bar_empty + 8 * kRing, bar_qfree = bar_q + 8, bar_s = bar_q + 16,
-                 bar_dp = bar_q + 32, bar_r = bar_q + 40, bar_ds = bar_q + 48, bar_f = bar_q + 56, bar_x = bar_q + 64, bar_d = bar_q + 72;
-  const Queue queue = {smem_addr(s_item), bar_q + 80, bar_q + 96};   // bar_q + 24: the second S's
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t sQ = smem_addr(smem), sO = sQ + kWide, sK = sO + kWide, sV = sK + kRing3 * kWide, sBars = sV + kRing2 * kWide + 2048;
+  float* parts = reinterpret_cast<float*>(smem + 7 * kWide);               // [4][128]
+  volatile int* s_misc = reinterpret_cast<volatile int*>(smem + 7 * kWide + 2048 + 256);
+  volatile int* s_fail = s_misc + 3;
+  const uint32_t bar_fk = sBars, bar_ek = bar_fk + 8 * kRing3, bar_fv = bar_ek + 8 * kRing3, bar_ev = bar_fv + 8 * kRing2, bar_q = bar_ev + 8 * kRing2,
+                 bar_qfree = bar_q + 8, bar_s = bar_q + 16, bar_dp = bar_q + 32, bar_r = bar_q + 40, bar_ds = bar_q + 48, bar_f = bar_q + 56,
+                 bar_x = bar_q + 64, bar_w = bar_q + 72, bar_d = bar_q + 80;   // bar_q + 24: the odd tiles' S
+  const Queue queue = {smem_addr(const_cast<int*>(s_misc)), bar_q + 88, bar_q + 104};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const QItem* items = static_cast<const QItem*>(a.items);
 
+  if (sQ & 1023) {
+    if (tid == 0) atomicCAS(a.status, 0, BC_ERR_CUDA);
+    return;
+  }
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) {
-      const uint32_t bar = bar_full + 8 * i;
-      const uint32_t count = bar == bar_r || bar == bar_ds ? kWeighers : (bar == bar_x ? kWeighers / 2 : (bar >= queue.empty ? kReaders : 1u));
+    for (uint32_t bar = sBars; bar < queue.empty + 16; bar += 8) {
+      const uint32_t count = bar == bar_r || bar == bar_ds || bar == bar_w ? kWeighers
+                             : bar == bar_qfree                            ? 1 + kWeighers
+                             : bar == bar_x                                ? kWeighers / 2
+                             : bar >= queue.empty                          ? kReaders
+                                                                           : 1u;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     *s_fail = 0;
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_misc + 2))), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int box_rows = a.per * a.G;
@@ -560,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem, tdP = tmem + 256, tO = tmem + 384;
+  const uint32_t tmem = (uint32_t)s_misc[2], tdP = tmem + 256, tO = tmem + 384;
   auto key_tile = [](const QItem& im, int n, int* k0) {          // segment and first key of tile n
     const int seg = n < im.nt0 ? 0 : (n < im.nt0 + im.nt1 ? 1 : 2);
     *k0 = seg == 0 ? n * kTile : (seg == 1 ? (n - im.nt0) * kTile : im.lo2 + (n - im.nt0 - im.nt1) * kTile);
@@ -572,7 +612,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
 
   if (warp == 0) {
     bool ok = true;
-    uint32_t t = 0, e = 0;
+    uint32_t t_k = 0, t_v = 0, e = 0;
     for (uint32_t i = 0;; ++i) {
       int it;
       ok = queue.draw<SHORTW>(i, a, s_fail, &it);
@@ -580,34 +620,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
       const int kvh = it % a.Hkv;
       const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
-      if (e > 0) ok = wait_all(bar_qfree, (e - 1) & 1u);
-      if (!ok) break;
-      if (elect_one()) {
-        const int row = (im.kind == 0 ? im.s.tok_row : im.s.bea_row) + im.first;
-        mbar_expect_tx(bar_q, (uint32_t)(2 * box_rows * kD * 2));
-        tma_3d(sQ, &maps.q[im.kind], 0, kvh * a.G, row, bar_q);
-        tma_3d(sQ + kTile * 128, &maps.q[im.kind], 64, kvh * a.G, row, bar_q);
-        tma_3d(sO, &maps.o[im.kind], 0, kvh * a.G, row, bar_q);
-        tma_3d(sO + kTile * 128, &maps.o[im.kind], 64, kvh * a.G, row, bar_q);
-      }
-      __syncwarp();
-      ++e;
-      for (int n = 0; n < N; ++n, ++t) {
-        const uint32_t place = t % kRing;
-        if (t >= kRing) ok = wait_all(bar_empty + 8 * place, (t / kRing - 1) & 1u);
-        if (!ok) break;
+      auto copy = [&](int n, const CUtensorMap* m, uint32_t dst, uint32_t bar) {
         if (elect_one()) {
           int k0;
-          const int seg = key_tile(im, n, &k0);
-          const int row = (seg == 0 ? im.s.prompt_row : (seg == 1 ? im.s.bea_row : im.s.tok_row)) + k0;
-          const uint32_t dst = sRing + place * 2 * kWide, bar = bar_full + 8 * place;
-          mbar_expect_tx(bar, 2 * kWide);
-          tma_3d(dst, &maps.k[seg], 0, kvh, row, bar);
-          tma_3d(dst + kTile * 128, &maps.k[seg], 64, kvh, row, bar);
-          tma_3d(dst + kWide, &maps.v[seg], 0, kvh, row, bar);
-          tma_3d(dst + kWide + kTile * 128, &maps.v[seg], 64, kvh, row, bar);
+          const int seg = key_tile(im, n, &k0), row = (seg == 0 ? im.s.prompt_row : (seg == 1 ? im.s.bea_row : im.s.tok_row)) + k0;
+          mbar_expect_tx(bar, kWide);
+          tma_3d(dst, m + seg, 0, kvh, row, bar);
+          tma_3d(dst + kTile * 128, m + seg, 64, kvh, row, bar);
         }
         __syncwarp();
+      };
+      for (int n = 0; n < N; ++n) {
+        const uint32_t pk = t_k % kRing3, pv = t_v % kRing2;
+        if (t_k >= kRing3) ok = wait_all(bar_ek + 8 * pk, (t_k / kRing3 - 1) & 1u);
+        if (!ok) break;
+        copy(n, maps.k, sK + pk * kWide, bar_fk + 8 * pk);
+        ++t_k;
+        if (n == 0) {                              // K's place is free before Q's and dO's are
+          if (e > 0) ok = wait_all(bar_qfree, (e - 1) & 1u);
+          if (!ok) break;
+          if (elect_one()) {
+            const int row = (im.kind == 0 ? im.s.tok_row : im.s.bea_row) + im.first;
+            mbar_expect_tx(bar_q, (uint32_t)(2 * box_rows * kD * 2));
+            tma_3d(sQ, &maps.q[im.kind], 0, kvh * a.G, row, bar_q);
+            tma_3d(sQ + kTile * 128, &maps.q[im.kind], 64, kvh * a.G, row, bar_q);
+            tma_3d(sO, &maps.o[im.kind], 0, kvh * a.G, row, bar_q);
+            tma_3d(sO + kTile * 128, &maps.o[im.kind], 64, kvh * a.G, row, bar_q);
+          }
+          __syncwarp();
+          ++e;
+        }
+        if (t_v >= kRing2) ok = wait_all(bar_ev + 8 * pv, (t_v / kRing2 - 1) & 1u);
+        if (!ok) break;
+        copy(n, maps.v, sV + pv * kWide, bar_fv + 8 * pv);
+        ++t_v;
       }
       if (!ok) break;
     }
@@ -615,37 +661,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     __syncwarp();
     int never = 0;
     if (e > 0) mbar_wait_or_fail<false>(bar_q, (e - 1) & 1u, &never, kWaitLimit);
-    for (uint32_t b = t > kRing ? t - kRing : 0; b < t; ++b)
-      mbar_wait_or_fail<false>(bar_full + 8 * (b % kRing), (b / kRing) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t_k > kRing3 ? t_k - kRing3 : 0; b < t_k; ++b)
+      mbar_wait_or_fail<false>(bar_fk + 8 * (b % kRing3), (b / kRing3) & 1u, &never, kWaitLimit);
+    for (uint32_t b = t_v > kRing2 ? t_v - kRing2 : 0; b < t_v; ++b)
+      mbar_wait_or_fail<false>(bar_fv + 8 * (b % kRing2), (b / kRing2) & 1u, &never, kWaitLimit);
     __syncwarp();
   } else if (warp == 1) {
     bool ok = true, issued = false;
     uint32_t t = 0, e = 0;
-    const uint64_t dQ = umma_desc(sQ), dO = umma_desc(sO), dK = umma_desc(sRing), dKn = umma_desc_nmajor(sRing);
+    const uint64_t dQ = umma_desc(sQ), dO = umma_desc(sO), dK = umma_desc(sK), dV = umma_desc(sV), dKn = umma_desc_nmajor(sK);
     for (uint32_t i = 0;; ++i) {
       int it;
       ok = queue.read<SHORTW>(i, a, s_fail, &it);
       if (!ok || it < 0) break;
       const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
-      auto landed = [&](int n) {                   // K and V of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
-        const uint32_t tile = t + n, place = tile % kRing;
-        if (!wait_all(bar_full + 8 * place, (tile / kRing) & 1u)) return false;
+      // K or V of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
+      auto landed = [&](int n, uint32_t bar, uint32_t parity, uint32_t at) {
+        if (!wait_all(bar, parity)) return false;
         int k0;
         const int seg = key_tile(im, n, &k0), valid = min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kTile);
         if (valid < kTile) {
-          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) {
-            st_zero16(sRing + place * 2 * kWide + swz(idx >> 4, idx & 15));
-            st_zero16(sRing + place * 2 * kWide + kWide + swz(idx >> 4, idx & 15));
-          }
+          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) st_zero16(at + swz(idx >> 4, idx & 15));
           proxy_fence();
           __syncwarp();
         }
         tc_fence_after();
         return true;
       };
-      auto at = [&](uint32_t tile) { return (uint64_t)((tile % kRing) * 2 * kWide >> 4); };
-      auto first = [&](uint32_t to, uint64_t row, uint64_t key, uint32_t bar, bool last) {   // S or dP
+      auto landed_k = [&](int n) { const uint32_t tile = t + n, r = tile % kRing3; return landed(n, bar_fk + 8 * r, (tile / kRing3) & 1u, sK + r * kWide); };
+      auto landed_v = [&](int n) { const uint32_t tile = t + n, r = tile % kRing2; return landed(n, bar_fv + 8 * r, (tile / kRing2) & 1u, sV + r * kWide); };
+      auto at_k = [&](uint32_t tile) { return (uint64_t)(tile % kRing3 * kWide >> 4); };
+      auto at_v = [&](uint32_t tile) { return (uint64_t)(tile % kRing2 * kWide >> 4); };
+      auto first = [&](uint32_t to, uint64_t row, uint64_t key, uint32_t bar, uint32_t bar_free, bool last) {   // S or dP
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kD / 16; ++kk) {
@@ -653,26 +701,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
             umma(to, row + off, key + off, kk > 0);
           }
           umma_commit(bar);
+          if (bar_free) umma_commit(bar_free);
           if (last) umma_commit(bar_qfree);
         }
         __syncwarp();
         issued = true;
       };
-      ok = wait_all(bar_q, e & 1u) && landed(0);
+      ok = wait_all(bar_q, e & 1u) && landed_k(0);
       if (!ok) break;
-      first(tmem + (t & 1u) * 128, dQ, dK + at(t), bar_s + 8 * (t & 1u), false);
-      first(tdP, dO, dK + at(t) + (kWide >> 4), bar_dp, N == 1);
+      first(tmem + (t & 1u) * 128, dQ, dK + at_k(t), bar_s + 8 * (t & 1u), 0, false);
+      ok = landed_v(0);
+      if (!ok) break;
+      first(tdP, dO, dV + at_v(t), bar_dp, bar_ev + 8 * (t % kRing2), N == 1);
       for (int n = 0; n < N; ++n) {
         const bool more = n + 1 < N;
         const uint32_t tile = t + n, odd = tile & 1u;
         if (more) {
-          ok = landed(n + 1);
+          ok = landed_k(n + 1);
           if (!ok) break;
-          first(tmem + (odd ^ 1u) * 128, dQ, dK + at(tile + 1), bar_s + 8 * (odd ^ 1u), false);
-          ok = wait_all(bar_r, odd);
+          first(tmem + (odd ^ 1u) * 128, dQ, dK + at_k(tile + 1), bar_s + 8 * (odd ^ 1u), 0, false);
+          ok = landed_v(n + 1) && wait_all(bar_r, odd);
           if (!ok) break;
           tc_fence_after();
-          first(tdP, dO, dK + at(tile + 1) + (kWide >> 4), bar_dp, n + 2 == N);
+          first(tdP, dO, dV + at_v(tile + 1), bar_dp, bar_ev + 8 * ((tile + 1) % kRing2), n + 2 == N);
         }
         ok = wait_all(bar_ds, odd);
         if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
@@ -681,8 +732,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)
-            umma_ts(tO, tmem + odd * 128 + (kk >> 1) * 32 + (kk & 1) * 8, dKn + at(tile) + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
-          umma_commit(bar_empty + 8 * (tile % kRing));
+            umma_ts(tO, tmem + odd * 128 + (kk >> 1) * 32 + (kk & 1) * 8, dKn + at_k(tile) + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
+          umma_commit(bar_ek + 8 * (tile % kRing3));
           if (!more) umma_commit(bar_f);
         }
         __syncwarp();
@@ -717,10 +768,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
       const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
       const bool live = row < im.count * G;
-      const int64_t at = stat_at(a, im.s, kvh, im.kind, im.first) + row;
-      const float l2 = live ? -a.lse2[at] : 0.f, dl = live ? -a.delta[at] : 0.f;
-      const F2 minus_l = pair(l2, l2), minus_d = pair(dl, dl);
       const int idx = im.first + my_local;
+      const int64_t at = ((int64_t)((im.kind == 0 ? im.s.tok_row : im.s.bea_row) + idx) * a.Hq + kvh * G + my_head);   // the row's place in q, O, dQ
+      // D of the row: a part has 32 of its 128 terms
+      uint4 o4[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) o4[q] = live ? __ldcs(reinterpret_cast<const uint4*>(a.out[im.kind] + at * kD + part * 32) + q) : make_uint4(0, 0, 0, 0);
+      const float l2 = live ? -a.lse[im.kind][at] * kLog2e : 0.f;
+      ok = wait_all(bar_q, e & 1u);
+      if (!ok) break;
+      float dsum = 0.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4 g4 = *reinterpret_cast<const uint4*>(smem + kWide + swz(row, part * 4 + q));
+        const uint32_t u[4] = {o4[q].x, o4[q].y, o4[q].z, o4[q].w}, v[4] = {g4.x, g4.y, g4.z, g4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          dsum = fmaf(__uint_as_float(u[j] << 16), __uint_as_float(v[j] << 16), dsum);
+          dsum = fmaf(__uint_as_float(u[j] & 0xffff0000u), __uint_as_float(v[j] & 0xffff0000u), dsum);
+        }
+      }
+      parts[part * 128 + row] = dsum;
+      __syncwarp();
+      if (lane == 0) { mbar_arrive_cta(bar_w); mbar_arrive_cta(bar_qfree); }
+      ok = wait_all(bar_w, e & 1u);
+      if (!ok) break;
+      const float dl = live ? -((parts[row] + parts[128 + row]) + (parts[256 + row] + parts[384 + row])) : 0.f;
+      if (part == 0) {
+        float* st = a.stats + ((int64_t)im.tile * a.Hkv + kvh) * 256 + row;
+        st[0] = l2;
+        st[128] = dl;
+      }
+      const F2 minus_l = pair(l2, l2), minus_d = pair(dl, dl);
       int bea_hi, tok_lo, tok_hi;                  // visible: the prompt, beacons [0, bea_hi), tokens [tok_lo, tok_hi)
       if (im.kind == 0) { bea_hi = c > 1 ? idx / c : 0; tok_lo = c > 1 ? idx / c * c : 0; tok_hi = idx + 1; }
       else { bea_hi = idx + 1; tok_lo = idx * c; tok_hi = (idx + 1) * c; }
@@ -742,10 +821,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
         tmem_wait_ld();
         if (some) {                                // uniform over the warp, no access to tensor memory inside
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) {
+          for (int j = 0; j < 32; j += 4) {
             split(fma2(pair(p[j], p[j + 1]), scale2, minus_l), &p[j], &p[j + 1]);
-            p[j] = fast_exp2(p[j]);
+            p[j] = fast_exp2(p[j]);                // every other pair on the special-function unit
             p[j + 1] = fast_exp2(p[j + 1]);
+            exp2_pair(fma2(pair(p[j + 2], p[j + 3]), scale2, minus_l), &p[j + 2], &p[j + 3]);
           }
           if (!whole) {
 #pragma unroll
@@ -777,9 +857,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
         if (lane == 0) mbar_arrive_cta(bar_ds);
       }
       if (!ok) break;
-      if (part >= 2) { ++e; continue; }            // two parts have 64 columns each
-      ok = wait_all(bar_f, e & 1u);
+      ok = wait_all(bar_f, e & 1u);                // all wait: behind it every warp has read the parts of D
       if (!ok) break;
+      ++e;
+      if (part >= 2) continue;                     // two parts have 64 columns each
       tc_fence_after();
       float o[kD / 2];
 #pragma unroll
@@ -788,10 +869,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cta(bar_x);
-      ++e;
-      if (live)
-        store_half_row(a.dq[im.kind] + ((int64_t)((im.kind == 0 ? im.s.tok_row : im.s.bea_row) + idx) * a.Hq + kvh * G + my_head) * kD + part * 64, o,
-                       a.scale);
+      if (live) store_half_row(a.dq[im.kind] + at * kD + part * 64, o, a.scale);
     }
     if (!ok) *s_fail = 1;
   }
@@ -801,37 +879,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   if (warp == 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
-  }
-}
-
-// D = sum_d dO O of every row and head, and L, laid out by KV head: 16 lanes per head row, both 16-byte loads.
-__global__ void __launch_bounds__(256) k_delta(const uint4* __restrict__ out_tok, const uint4* __restrict__ d_tok, const float* __restrict__ lse_tok,
-                                               const uint4* __restrict__ out_bea, const uint4* __restrict__ d_bea, const float* __restrict__ lse_bea,
-                                               int64_t tok_rows, int64_t rows, int Hq, int G, float* __restrict__ lse2, float* __restrict__ delta) {
-  const int64_t units = rows * Hq;
-  const int lane = threadIdx.x & 15;
-  // the 16 lanes of a row are in one warp, and the warp's two rows run the loop equally often (an odd last row is computed twice)
-  for (int64_t u0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4; u0 < units + (units & 1); u0 += (int64_t)gridDim.x * 16) {
-    const int64_t u = u0 < units ? u0 : units - 1;
-    const int64_t row = u / Hq;
-    const int head = (int)(u - row * Hq);
-    const bool tok = row < tok_rows;
-    const int64_t in = tok ? u : u - tok_rows * Hq;
-    const uint4 x = __ldcs((tok ? out_tok : out_bea) + in * 16 + lane), y = __ldcs((tok ? d_tok : d_bea) + in * 16 + lane);
-    const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), s);
-      s = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), s);
-    }
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (lane == 0) {
-      const int64_t to = ((int64_t)(head / G) * rows + row) * G + head % G;
-      delta[to] = s;
-      lse2[to] = (tok ? lse_tok : lse_bea)[in] * kLog2e;
-    }
   }
 }
 
@@ -871,7 +918,7 @@ struct Plan {
   int64_t prompts = 0, tokens = 0, beacons = 0;
   int32_t slots = 0;
   // the status word is at 0, the two queues' counters at 128 and 192
-  size_t at_kv = 0, at_q = 0, at_join = 0, lists = 0, at_lse = 0, at_delta = 0, at_partial = 0, total = 0;
+  size_t at_kv = 0, at_q = 0, at_join = 0, lists = 0, at_stats = 0, at_partial = 0, total = 0;
 };
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kSms = 148;
@@ -912,11 +959,15 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
   whole.reserve(n_kv);
   p->q.reserve(n_q);
   int64_t bea_row = 0, work = 0;
+  int32_t tile = 0;
+  std::vector<size_t> ends;                                    // of the sequences in `whole`
   for (int i = 0; i < n_seqs; ++i) {
     SeqDesc s;
     s.P = cu_prompt[i + 1] - cu_prompt[i]; s.T = cu_tokens[i + 1] - cu_tokens[i]; s.nb = c > 1 ? s.T / c : 0;
     s.prompt_row = cu_prompt[i]; s.tok_row = cu_tokens[i]; s.bea_row = (int32_t)bea_row;
     bea_row += s.nb;
+    s.tok_tile = tile; s.bea_tile = tile + tiles(s.T);
+    tile = s.bea_tile + tiles(s.nb);
     for (int seg = 0; seg < 3; ++seg) {
       const int len = seg == 0 ? s.P : (seg == 1 ? s.nb : s.T);
       for (int k0 = 0; k0 < len; k0 += kTile) {
@@ -944,31 +995,44 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
         const int b_hi = kind == 0 ? (c > 1 ? last / c : 0) : last + 1;
         const int t_lo = kind == 0 ? (c > 1 ? f / c * c : 0) : f * c, t_hi = kind == 0 ? last + 1 : (last + 1) * c;
         im.lo2 = t_lo / kTile * kTile;
+        im.tile = (kind == 0 ? s.tok_tile : s.bea_tile) + f / per;
         im.nt0 = (s.P + kTile - 1) / kTile; im.nt1 = (b_hi + kTile - 1) / kTile; im.nt2 = (t_hi - im.lo2 + kTile - 1) / kTile;
         p->q.push_back(im);
       }
     }
+    ends.push_back(whole.size());
   }
   // An item is cut where it is longer than a quarter of an SM's share of all the work, so that the last ones to end are short
   const int64_t piece = std::max<int64_t>(kMinPiece, work * kv_heads / (kSms * 4));
-  for (const KvItem& w : whole) {
-    const int N = w.nt + w.nb_tiles;
-    const int pieces = N > piece + piece / 2 ? (int)((N + piece - 1) / piece) : 1;
-    if (pieces == 1) {
-      p->kv.push_back(w);
-      continue;
+  size_t from = 0;
+  for (size_t end : ends) {
+    // a sequence's first pieces, then its second ones: blocks at work at the same time read the same queries
+    std::vector<int> pieces;
+    int most = 1;
+    for (size_t w = from; w < end; ++w) {
+      const int N = whole[w].nt + whole[w].nb_tiles, cuts = N > piece + piece / 2 ? (int)((N + piece - 1) / piece) : 1;
+      pieces.push_back(cuts);
+      most = std::max(most, cuts);
+      if (cuts > 1) {
+        JoinItem j = {};
+        j.s = whole[w].s; j.seg = whole[w].seg; j.k0 = whole[w].k0; j.first = p->slots; j.count = cuts;
+        whole[w].slot = p->slots;
+        p->slots += cuts;
+        p->join.push_back(j);
+      }
     }
-    JoinItem j = {};
-    j.s = w.s; j.seg = w.seg; j.k0 = w.k0; j.first = p->slots; j.count = pieces;
-    p->join.push_back(j);
-    for (int q = 0; q < pieces; ++q) {
-      const int a = (int)((int64_t)N * q / pieces), b = (int)((int64_t)N * (q + 1) / pieces);   // tiles [a, b) of the item
-      KvItem im = w;
-      im.ta = w.ta + std::min(a, w.nt); im.nt = std::min(b, w.nt) - std::min(a, w.nt);
-      im.ba = w.ba + std::max(a - w.nt, 0); im.nb_tiles = std::max(b - w.nt, 0) - std::max(a - w.nt, 0);
-      im.slot = p->slots++;
-      p->kv.push_back(im);
-    }
+    for (int q = 0; q < most; ++q)
+      for (size_t w = from; w < end; ++w) {
+        const int cuts = pieces[w - from];
+        if (q >= cuts) continue;
+        KvItem im = whole[w];
+        const int N = im.nt + im.nb_tiles, a = (int)((int64_t)N * q / cuts), b = (int)((int64_t)N * (q + 1) / cuts);   // tiles [a, b) of the item
+        im.ta += std::min(a, whole[w].nt); im.nt = std::min(b, whole[w].nt) - std::min(a, whole[w].nt);
+        im.ba += std::max(a - whole[w].nt, 0); im.nb_tiles = std::max(b - whole[w].nt, 0) - std::max(a - whole[w].nt, 0);
+        if (cuts > 1) im.slot += q;
+        p->kv.push_back(im);
+      }
+    from = end;
   }
   longest_first(&p->kv, [](const KvItem& x) { return x.nt + x.nb_tiles; });
   longest_first(&p->q, [](const QItem& x) { return x.nt0 + x.nt1 + x.nt2; });
@@ -978,9 +1042,7 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
   p->at_q = take(p->q.size() * sizeof(QItem));
   p->at_join = take(p->join.size() * sizeof(JoinItem));
   p->lists = o;
-  const size_t stats = (size_t)(p->tokens + p->beacons) * q_heads * sizeof(float);
-  p->at_lse = take(stats);
-  p->at_delta = take(stats);
+  p->at_stats = take((size_t)tile * kv_heads * 2 * kTile * sizeof(float));
   p->at_partial = take((size_t)p->slots * kv_heads * 2 * kTile * kD * sizeof(float));
   p->total = o;
   return BC_OK;
@@ -1041,8 +1103,9 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     if (p.kv.empty()) return BC_OK;
 
     GradArgs a = {};
-    a.lse2 = reinterpret_cast<float*>(ws + p.at_lse); a.delta = reinterpret_cast<float*>(ws + p.at_delta);
-    a.rows = p.tokens + p.beacons; a.tok_rows = p.tokens;
+    a.out[0] = (const __nv_bfloat16*)out_tok; a.out[1] = (const __nv_bfloat16*)out_beacon;
+    a.lse[0] = lse_tok; a.lse[1] = lse_beacon;
+    a.stats = reinterpret_cast<float*>(ws + p.at_stats);
     a.dk[0] = (__nv_bfloat16*)d_prompt_k; a.dk[1] = (__nv_bfloat16*)d_beacon_k; a.dk[2] = (__nv_bfloat16*)d_tok_k;
     a.dv[0] = (__nv_bfloat16*)d_prompt_v; a.dv[1] = (__nv_bfloat16*)d_beacon_v; a.dv[2] = (__nv_bfloat16*)d_tok_v;
     a.dq[0] = (__nv_bfloat16*)d_tok_q; a.dq[1] = (__nv_bfloat16*)d_beacon_q;
@@ -1070,23 +1133,18 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     KvMaps maps;
     if (!maps_for(&maps, kTile / G, kTile)) return BC_ERR_CUDA;
     const bool shortw = g_wait_limit != 0;
-    const int smem = 2 * kWide + kRing * 2 * kWide + 1024;   // of either kernel
     auto* dkv = shortw ? k_dkv<true> : k_dkv<false>;
     auto* dq = shortw ? k_dq<true> : k_dq<false>;
-    if (cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-        cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(dkv, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess ||
+        cudaFuncSetAttribute(dq, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess)
       return BC_ERR_CUDA;
-    if (a.rows > 0) {
-      const int64_t blocks = (a.rows * q_heads + 15) / 16;
-      k_delta<<<(unsigned)std::min<int64_t>(blocks, kSms * 8), 256, 0, s>>>(
-          (const uint4*)out_tok, (const uint4*)d_out_tok, lse_tok, (const uint4*)out_beacon, (const uint4*)d_out_beacon, lse_beacon, p.tokens,
-          a.rows, q_heads, G, const_cast<float*>(a.lse2), const_cast<float*>(a.delta));
+    if (!p.q.empty()) {
       GradArgs b = a;
       b.items = ws + p.at_q; b.n_items = (int32_t)p.q.size() * kv_heads; b.next = reinterpret_cast<int32_t*>(ws + 128);
-      dq<<<std::min(b.n_items, kSms), kThreads, smem, s>>>(b, maps);
+      dq<<<std::min(b.n_items, kSms), kThreads, kSmem, s>>>(b, maps);
     }
     a.items = ws + p.at_kv; a.n_items = (int32_t)p.kv.size() * kv_heads; a.next = reinterpret_cast<int32_t*>(ws + 192);
-    dkv<<<std::min(a.n_items, kSms), kThreads, smem, s>>>(a, maps);
+    dkv<<<std::min(a.n_items, kSms), kThreads, kSmem, s>>>(a, maps);
     if (!p.join.empty())
       k_join<<<dim3((unsigned)p.join.size() * kv_heads, 2 * kTile / 8), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
     return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
