@@ -35,8 +35,9 @@ namespace {
 constexpr int kD = 128;                            // head_dim
 constexpr int kWide = kTile * kD * 2;              // bytes of an operand
 constexpr uint32_t kWeighers = 16;                 // warps that turn S and dP into P and dS
-constexpr int kThreads = 64 + 32 * kWeighers;      // warp 0: copies, warp 1: products, then those
-constexpr uint32_t kReaders = 1 + kWeighers;       // warps that read the item numbers
+constexpr int kFirst = 3;                          // warp 0: copies, warps 1 and 2: products, from here on those
+constexpr int kThreads = 32 * (kFirst + kWeighers);
+constexpr uint32_t kReaders = 2 + kWeighers;       // warps that read the items
 constexpr int kRing3 = 3, kRing2 = 2;              // places for tiles that are needed long (Q, K in dS K) and short (dO, V)
 constexpr int kSmem = 7 * kWide + 2048 + 512;      // seven operands, numbers, barriers: all of a block's shared memory
 constexpr float kLog2e = 1.4426950408889634f;
@@ -79,7 +80,7 @@ struct GradArgs {
   const float* lse[2];
   float* stats;                                    // [query tiles][kv_heads][2][128]: -log2(e) L and -D of the tile's rows, left by k_dq for k_dkv
   __nv_bfloat16 *dk[3], *dv[3], *dq[2];
-  float* partial;                                  // [slots][2][128][128]
+  float* partial;                                  // [slots][kv_heads][2][32][128][4]: columns by fours, keys, column
   int32_t* status;
   int32_t Hq, Hkv, G, c, per;                      // per: tokens or beacons per query tile
   float scale, scale_log2;
@@ -100,42 +101,45 @@ __device__ __forceinline__ void store_half_row(__nv_bfloat16* dst, const float* 
                  "r"(pack2(o[d + 14] * f, o[d + 15] * f))
                  : "memory");
 }
-// Items are handed out as blocks become free, longest first.  The copy warp draws them, one ahead of the work, and the other
-// warps read their numbers from two places in shared memory; an item is worked on by one block, so results do not depend on who
-// draws it.
+// Items are handed out as blocks become free, longest first.  The copy warp draws them, one ahead of the work, and leaves number
+// and descriptor in one of two places in shared memory for the other warps.  An item is worked on by one block, so results do not
+// depend on who draws it.
 struct Queue {
-  uint32_t item, full, empty;                      // shared addresses: two numbers, two barriers each
-  __device__ __forceinline__ int at(uint32_t e) const {
-    int v;
-    asm volatile("ld.shared.s32 %0, [%1];" : "=r"(v) : "r"(item + 4 * (e & 1u)) : "memory");
-    return v;
+  volatile int* place;                             // per place: the descriptor (16 words) and the number, 32 words apart
+  uint32_t full, empty;                            // two barriers each
+  template <class Item>
+  __device__ __forceinline__ void load(uint32_t e, Item* im) const {
+    const int4* from = const_cast<const int4*>(reinterpret_cast<const volatile int4*>(place + 32 * (e & 1u)));
+    int4* to = reinterpret_cast<int4*>(im);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to[i] = from[i];
   }
-  // the copy warp, all lanes: draws item number e of this block
-  template <bool SHORTW>
-  __device__ __forceinline__ bool draw(uint32_t e, const GradArgs& a, volatile int* fail, int* got) const {
-    bool ok = true;
-    if (e >= 2) ok = __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(empty + 8 * (e & 1u), ((e >> 1) - 1) & 1u, fail, a.wait_limit)) != 0;
-    int it = -1;
-    if (ok) {
-      if ((threadIdx.x & 31) == 0) {
-        it = atomicAdd(a.next, 1);
-        if (it >= a.n_items) it = -1;
-        asm volatile("st.shared.s32 [%0], %1;" ::"r"(item + 4 * (e & 1u)), "r"(it) : "memory");
-        mbar_arrive_cta(full + 8 * (e & 1u));
-      }
-      it = __shfl_sync(0xffffffffu, it, 0);
-    }
+  // the copy warp, all lanes: draws item number e of this block (-1: none is left)
+  template <bool SHORTW, class Item>
+  __device__ __forceinline__ bool draw(uint32_t e, const GradArgs& a, volatile int* fail, int* got, Item* im) const {
+    if (e >= 2 && !__all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(empty + 8 * (e & 1u), ((e >> 1) - 1) & 1u, fail, a.wait_limit))) return false;
+    const int lane = threadIdx.x & 31;
+    int it = lane == 0 ? atomicAdd(a.next, 1) : 0;
+    it = __shfl_sync(0xffffffffu, it, 0);
+    if (it >= a.n_items) it = -1;
+    volatile int* p = place + 32 * (e & 1u);
+    if (lane < 16 && it >= 0) p[lane] = static_cast<const int*>(a.items)[(int64_t)(it / a.Hkv) * 16 + lane];
+    if (lane == 0) p[16] = it;
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cta(full + 8 * (e & 1u));
+    load(e, im);
     *got = it;
-    return ok;
+    return true;
   }
   // the other warps, all lanes
-  template <bool SHORTW>
-  __device__ __forceinline__ bool read(uint32_t e, const GradArgs& a, volatile int* fail, int* got) const {
-    const bool ok = __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(full + 8 * (e & 1u), (e >> 1) & 1u, fail, a.wait_limit)) != 0;
-    *got = ok ? at(e) : -1;
+  template <bool SHORTW, class Item>
+  __device__ __forceinline__ bool read(uint32_t e, const GradArgs& a, volatile int* fail, int* got, Item* im) const {
+    if (!__all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(full + 8 * (e & 1u), (e >> 1) & 1u, fail, a.wait_limit))) return false;
+    *got = place[32 * (e & 1u) + 16];
+    load(e, im);
     __syncwarp();
-    if (ok && (threadIdx.x & 31) == 0) mbar_arrive_cta(empty + 8 * (e & 1u));
-    return ok;
+    if ((threadIdx.x & 31) == 0) mbar_arrive_cta(empty + 8 * (e & 1u));
+    return true;
   }
 };
 
@@ -195,9 +199,11 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
 
 // ---- dK and dV ---------------------------------------------------------------------------------------------------------------
 // Tensor memory: columns [0, 128) S^T, then P^T in the first 16 columns of every 32; [128, 256) dP^T, then dS^T likewise; [256, 384) dV,
-// [384, 512) dK.  The tensor pipe runs a block's products in the order they are issued:
-//     S(t + 1) behind dV += P(t) dO, which reads what it overwrites, while the weights' warps turn dP(t) into dS(t);
-//     dP(t + 1) behind dK += dS(t) Q, while they turn S(t + 1) into P(t + 1).
+// [384, 512) dK.  Two warps issue the products; the tensor pipe runs a warp's products in the order it issued them:
+//     warp 1: S(t + 1) behind dV += P(t) dO, which reads what it overwrites, while the weights' warps turn dP(t) into dS(t);
+//     warp 2: dP(t + 1) behind dK += dS(t) Q, while they turn S(t + 1) into P(t + 1).
+// The pipe takes only a few products ahead, and a poll of a barrier takes some 200 cycles beside warps that keep the special-function
+// and shared-memory queues full: with one warp for all products it ran dry at every wait (3900 cycles a tile).
 //
 // Barriers (t counts query tiles, e items; parity = uses so far & 1):
 //   fq[r] / eq[r], fo[r] / eo[r]: Q, or dO with the tile's numbers, has landed in a ring place / been read
@@ -209,14 +215,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sK = smem_addr(smem), sV = sK + kWide, sQ = sV + kWide, sO = sQ + kRing3 * kWide, sStat = sO + kRing2 * kWide, sBars = sStat + 2048;
   const float* stats = reinterpret_cast<const float*>(smem + 7 * kWide);   // [kRing2][2][128]
-  volatile int* s_misc = reinterpret_cast<volatile int*>(smem + 7 * kWide + 2048 + 256);   // two item numbers, the tensor memory, failure
-  volatile int* s_fail = s_misc + 3;
+  volatile int* s_misc = reinterpret_cast<volatile int*>(smem + 7 * kWide + 2048 + 256);   // the queue's two places, and behind them:
+  volatile int *s_tmem = s_misc + 62, *s_fail = s_misc + 63;
   const uint32_t bar_fq = sBars, bar_eq = bar_fq + 8 * kRing3, bar_fo = bar_eq + 8 * kRing3, bar_eo = bar_fo + 8 * kRing2, bar_k = bar_eo + 8 * kRing2,
                  bar_v = bar_k + 8, bar_kfree = bar_k + 16, bar_vfree = bar_k + 24, bar_s = bar_k + 32, bar_dp = bar_k + 40, bar_p = bar_k + 48,
-                 bar_ds = bar_k + 56, bar_f = bar_k + 64, bar_x = bar_k + 72, bar_d = bar_k + 80;
-  const Queue queue = {smem_addr(const_cast<int*>(s_misc)), bar_k + 88, bar_k + 104};
+                 bar_ds = bar_k + 56, bar_f = bar_k + 64, bar_x = bar_k + 72, bar_d = bar_k + 80;   // d: one for either product warp
+  const Queue queue = {s_misc, bar_k + 96, bar_k + 112};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const KvItem* items = static_cast<const KvItem*>(a.items);
 
   if (sK & 1023) {                       // the operands' layouts need it; shared memory begins so
     if (tid == 0) atomicCAS(a.status, 0, BC_ERR_CUDA);
@@ -225,7 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   if (tid == 0) {
     for (uint32_t bar = sBars; bar < queue.empty + 16; bar += 8) {
       const uint32_t count = bar == bar_p || bar == bar_ds || bar == bar_x ? kWeighers
-                             : bar >= bar_eo && bar < bar_k                ? 1 + kWeighers
+                             : bar >= bar_eo && bar < bar_k                ? 2 + kWeighers
+                             : bar == bar_f                                ? 2u
                              : bar >= queue.empty                          ? kReaders
                                                                            : 1u;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -234,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     *s_fail = 0;
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_misc + 2))), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_tmem))), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int box_rows = a.per * a.G;      // rows that a copy writes; the others (G does not divide 128) stay zero
@@ -246,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = (uint32_t)s_misc[2], tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+  const uint32_t tmem = (uint32_t)*s_tmem, tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
   auto wait_all = [&](uint32_t bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
   };
@@ -258,10 +264,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     const uint32_t bytes = (uint32_t)(box_rows * kD * 2);
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.draw<SHORTW>(i, a, s_fail, &it);
+      KvItem im;
+      ok = queue.draw<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
       const int kvh = it % a.Hkv;
-      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
       const int key_row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0;
@@ -324,89 +330,75 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     for (uint32_t b = t_o > kRing2 ? t_o - kRing2 : 0; b < t_o; ++b)
       mbar_wait_or_fail<false>(bar_fo + 8 * (b % kRing2), (b / kRing2) & 1u, &never, kWaitLimit);
     __syncwarp();
-  } else if (warp == 1) {
-    // ---- products --------------------------------------------------------------------------------------------------------
+  } else if (warp < kFirst) {
+    // ---- products: warp 1 S and dV, warp 2 dP and dK --------------------------------------------------------------------------
+    const bool is_s = warp == 1;
     bool ok = true, issued = false;
     uint32_t t = 0, e = 0;
-    const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sQ), dO = umma_desc(sO), dQn = umma_desc_nmajor(sQ), dOn = umma_desc_nmajor(sO);
-    auto first = [&](uint32_t to, uint64_t key, uint64_t q, uint32_t bar, uint32_t bar_free, bool last) {   // S^T or dP^T
-      if (elect_one()) {
-#pragma unroll
-        for (int kk = 0; kk < kD / 16; ++kk) {
-          const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
-          umma(to, key + off, q + off, kk > 0);
-        }
-        umma_commit(bar);
-        if (last) umma_commit(bar_free);
-      }
-      __syncwarp();
-      issued = true;
-    };
-    auto second = [&](uint32_t to, uint32_t from, uint64_t q, bool fresh) {   // dV or dK
-#pragma unroll
-      for (int kk = 0; kk < kTile / 16; ++kk)
-        umma_ts(to, from + (kk >> 1) * 32 + (kk & 1) * 8, q + (uint64_t)((kk * 16 * 128) >> 4), (!fresh || kk > 0) ? 1u : 0u);
-    };
+    const uint64_t key = umma_desc(is_s ? sK : sV);
+    const uint32_t t1 = is_s ? tS : tdP, t2 = is_s ? tV : tK;                          // S or dP; dV or dK
+    const uint32_t bar_key = is_s ? bar_k : bar_v, bar_free = is_s ? bar_kfree : bar_vfree, bar_1 = is_s ? bar_s : bar_dp, bar_2 = is_s ? bar_p : bar_ds;
+    // the first product's rows: Q or dO, the second's: dO or Q
+    const uint32_t s1 = is_s ? sQ : sO, ring1 = is_s ? kRing3 : kRing2, full1 = is_s ? bar_fq : bar_fo;
+    const uint32_t ring2 = is_s ? kRing2 : kRing3, empty2 = is_s ? bar_eo : bar_eq;
+    const uint64_t rows1 = umma_desc(s1), rows2 = umma_desc_nmajor(is_s ? sO : sQ);
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      KvItem im;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
-      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
-      auto at_q = [&](uint32_t tile) { return (uint64_t)(tile % kRing3 * kWide >> 4); };
-      auto at_o = [&](uint32_t tile) { return (uint64_t)(tile % kRing2 * kWide >> 4); };
-      auto landed = [&](int n, uint32_t bar, uint32_t parity, uint32_t at) {   // an operand of tile n; rows of the next sequence are cleared: they are factors
-        if (!wait_all(bar, parity)) return false;
-        const int kind = n < im.nt ? 0 : 1, q = kind == 0 ? im.ta + n : im.ba + n - im.nt;
-        const int valid = min((kind == 0 ? im.s.T : im.s.nb) - q * a.per, a.per) * a.G;
+      // rows that the last tile of either kind holds of the next sequence are cleared: they are factors of the second products
+      const int end_tok = min(im.s.T - (im.ta + im.nt - 1) * a.per, a.per) * a.G, end_bea = min(im.s.nb - (im.ba + im.nb_tiles - 1) * a.per, a.per) * a.G;
+      auto first = [&](int n) {
+        const uint32_t tile = t + n, r = tile % ring1, at = r * kWide;
+        if (!wait_all(full1 + 8 * r, (tile / ring1) & 1u)) return false;
+        const int valid = n == im.nt - 1 ? end_tok : (n == N - 1 ? end_bea : box_rows);
         if (valid < box_rows) {
-          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(at + swz(idx >> 4, idx & 15));
+          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(s1 + at + swz(idx >> 4, idx & 15));
           proxy_fence();
           __syncwarp();
         }
         tc_fence_after();
+        if (elect_one()) {
+          const uint64_t rows = rows1 + (at >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kD / 16; ++kk) {
+            const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
+            umma(t1, key + off, rows + off, kk > 0);
+          }
+          umma_commit(bar_1);
+          if (n == N - 1) umma_commit(bar_free);
+          if (!is_s) umma_commit(bar_eo + 8 * r);                          // dO is free when dP, dV and the numbers' readers are done with it
+        }
+        __syncwarp();
+        issued = true;
         return true;
       };
-      auto landed_q = [&](int n) { const uint32_t tile = t + n, r = tile % kRing3; return landed(n, bar_fq + 8 * r, (tile / kRing3) & 1u, sQ + r * kWide); };
-      auto landed_o = [&](int n) { const uint32_t tile = t + n, r = tile % kRing2; return landed(n, bar_fo + 8 * r, (tile / kRing2) & 1u, sO + r * kWide); };
-      ok = wait_all(bar_k, e & 1u) && landed_q(0);
-      if (!ok) break;
-      first(tS, dK, dQ + at_q(t), bar_s, bar_kfree, N == 1);
-      ok = wait_all(bar_v, e & 1u) && landed_o(0);
-      if (!ok) break;
-      first(tdP, dV, dO + at_o(t), bar_dp, bar_vfree, N == 1);
-      for (int n = 0; n < N; ++n) {
-        const bool more = n + 1 < N;
-        const uint32_t tile = t + n;
-        ok = wait_all(bar_p, tile & 1u);
+      ok = wait_all(bar_key, e & 1u) && first(0);
+      for (int n = 0; n < N && ok; ++n) {
+        const uint32_t tile = t + n, r = tile % ring2;
+        ok = wait_all(bar_2, tile & 1u);
         if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
         if (!ok) break;
+        const int valid = n == im.nt - 1 ? end_tok : (n == N - 1 ? end_bea : box_rows);
+        if (is_s && valid < box_rows) {            // dO has landed (P has its numbers), but warp 2 need not have come to this tile yet
+          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(sO + r * kWide + swz(idx >> 4, idx & 15));
+          proxy_fence();
+          __syncwarp();
+        }
         tc_fence_after();
         if (elect_one()) {
-          second(tV, tS, dOn + at_o(tile), n == 0);
-          umma_commit(bar_eo + 8 * (tile % kRing2));
+          const uint64_t rows = rows2 + (uint64_t)(r * kWide >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kTile / 16; ++kk)
+            umma_ts(t2, t1 + (kk >> 1) * 32 + (kk & 1) * 8, rows + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
+          umma_commit(empty2 + 8 * r);
+          if (n == N - 1) umma_commit(bar_f);
         }
         __syncwarp();
-        if (more) {
-          ok = landed_q(n + 1);
-          if (!ok) break;
-          first(tS, dK, dQ + at_q(tile + 1), bar_s, bar_kfree, n + 2 == N);
-        }
-        ok = wait_all(bar_ds, tile & 1u);
-        if (!ok) break;
-        tc_fence_after();
-        if (elect_one()) {
-          second(tK, tdP, dQn + at_q(tile), n == 0);
-          umma_commit(bar_eq + 8 * (tile % kRing3));
-          if (!more) umma_commit(bar_f);
-        }
-        __syncwarp();
-        if (more) {
-          ok = landed_o(n + 1);
-          if (!ok) break;
-          first(tdP, dV, dO + at_o(tile + 1), bar_dp, bar_vfree, n + 2 == N);
-        }
+        if (n + 1 < N) ok = first(n + 1);
       }
       if (!ok) break;
       t += N;
@@ -417,14 +409,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
       __syncwarp();
       if (issued && elect_one()) {                 // no product may be running when the block leaves
         int never = 0;
-        umma_commit(bar_d);
-        mbar_wait_or_fail<false>(bar_d, 0, &never, kWaitLimit);
+        umma_commit(bar_d + 8 * (warp - 1));
+        mbar_wait_or_fail<false>(bar_d + 8 * (warp - 1), 0, &never, kWaitLimit);
       }
     }
     __syncwarp();
   } else {
     // ---- weights: one key and 32 query rows per thread ------------------------------------------------------------------------
-    const int part = (warp - 2) >> 2;              // columns [32 part, + 32)
+    const int part = (warp - kFirst) >> 2;         // columns [32 part, + 32)
     // a warp reaches the 32 lanes of tensor memory that belong to its number modulo 4; its keys are those lanes
     const int key = (warp & 3) * 32 + lane;
     const uint32_t mine = ((uint32_t)((warp & 3) * 32) << 16) + part * 32;
@@ -433,10 +425,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     uint32_t t = 0, e = 0;
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      KvItem im;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
       const int kvh = it % a.Hkv;
-      const KvItem im = items[it / a.Hkv];
       const int N = im.nt + im.nb_tiles, G = a.G, c = a.c;
       const int k = im.k0 + key, seg_len = im.seg == 0 ? im.s.P : (im.seg == 1 ? im.s.nb : im.s.T);
       const bool live = k < seg_len;
@@ -533,9 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         for (int d = 0; d < kD / 2; ++d) o[d] = 0.f;
       }
       if (im.slot >= 0) {
-        float4* dst = reinterpret_cast<float4*>(a.partial + ((((int64_t)im.slot * a.Hkv + kvh) * 2 + is_k) * kTile + key) * kD + col);
+        // four columns of all keys, then the next four: a warp's stores are contiguous
+        float4* dst = reinterpret_cast<float4*>(a.partial) + ((((int64_t)im.slot * a.Hkv + kvh) * 2 + is_k) * (kD / 4) + col / 4) * kTile + key;
 #pragma unroll
-        for (int d = 0; d < kD / 2; d += 4) dst[d / 4] = make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]);
+        for (int d = 0; d < kD / 2; d += 4) __stcs(dst + d / 4 * kTile, make_float4(o[d], o[d + 1], o[d + 2], o[d + 3]));
       } else if (live) {
         const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + k;
         store_half_row((is_k ? a.dk : a.dv)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + col, o, is_k ? a.scale : 1.f);
@@ -563,13 +556,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   const uint32_t sQ = smem_addr(smem), sO = sQ + kWide, sK = sO + kWide, sV = sK + kRing3 * kWide, sBars = sV + kRing2 * kWide + 2048;
   float* parts = reinterpret_cast<float*>(smem + 7 * kWide);               // [4][128]
   volatile int* s_misc = reinterpret_cast<volatile int*>(smem + 7 * kWide + 2048 + 256);
-  volatile int* s_fail = s_misc + 3;
+  volatile int *s_tmem = s_misc + 62, *s_fail = s_misc + 63;
   const uint32_t bar_fk = sBars, bar_ek = bar_fk + 8 * kRing3, bar_fv = bar_ek + 8 * kRing3, bar_ev = bar_fv + 8 * kRing2, bar_q = bar_ev + 8 * kRing2,
                  bar_qfree = bar_q + 8, bar_s = bar_q + 16, bar_dp = bar_q + 32, bar_r = bar_q + 40, bar_ds = bar_q + 48, bar_f = bar_q + 56,
-                 bar_x = bar_q + 64, bar_w = bar_q + 72, bar_d = bar_q + 80;   // bar_q + 24: the odd tiles' S
-  const Queue queue = {smem_addr(const_cast<int*>(s_misc)), bar_q + 88, bar_q + 104};
+                 bar_x = bar_q + 64, bar_w = bar_q + 72, bar_d = bar_q + 80;   // bar_q + 24: the odd tiles' S; d: one for either product warp
+  const Queue queue = {s_misc, bar_q + 96, bar_q + 112};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const QItem* items = static_cast<const QItem*>(a.items);
 
   if (sQ & 1023) {
     if (tid == 0) atomicCAS(a.status, 0, BC_ERR_CUDA);
@@ -578,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   if (tid == 0) {
     for (uint32_t bar = sBars; bar < queue.empty + 16; bar += 8) {
       const uint32_t count = bar == bar_r || bar == bar_ds || bar == bar_w ? kWeighers
-                             : bar == bar_qfree                            ? 1 + kWeighers
+                             : bar == bar_qfree                            ? 2 + kWeighers
                              : bar == bar_x                                ? kWeighers / 2
                              : bar >= queue.empty                          ? kReaders
                                                                            : 1u;
@@ -588,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     *s_fail = 0;
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_misc + 2))), "r"(512) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(const_cast<int*>(s_tmem))), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const int box_rows = a.per * a.G;
@@ -600,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = (uint32_t)s_misc[2], tdP = tmem + 256, tO = tmem + 384;
+  const uint32_t tmem = (uint32_t)*s_tmem, tdP = tmem + 256, tO = tmem + 384;
   auto key_tile = [](const QItem& im, int n, int* k0) {          // segment and first key of tile n
     const int seg = n < im.nt0 ? 0 : (n < im.nt0 + im.nt1 ? 1 : 2);
     *k0 = seg == 0 ? n * kTile : (seg == 1 ? (n - im.nt0) * kTile : im.lo2 + (n - im.nt0 - im.nt1) * kTile);
@@ -615,11 +607,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     uint32_t t_k = 0, t_v = 0, e = 0;
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.draw<SHORTW>(i, a, s_fail, &it);
+      QItem im;
+      ok = queue.draw<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
       const int kvh = it % a.Hkv;
-      const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
+      // the rows of O that the weights' warps will read for this item, into the second-level cache
+      for (int l = lane; l < im.count * a.G * 2; l += 32) {
+        const int64_t row = (int64_t)((im.kind == 0 ? im.s.tok_row : im.s.bea_row) + im.first + (l >> 1) / a.G) * a.Hq + kvh * a.G + (l >> 1) % a.G;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.out[im.kind] + row * kD + (l & 1) * 64));
+      }
       auto copy = [&](int n, const CUtensorMap* m, uint32_t dst, uint32_t bar) {
         if (elect_one()) {
           int k0;
@@ -666,79 +663,76 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     for (uint32_t b = t_v > kRing2 ? t_v - kRing2 : 0; b < t_v; ++b)
       mbar_wait_or_fail<false>(bar_fv + 8 * (b % kRing2), (b / kRing2) & 1u, &never, kWaitLimit);
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp < kFirst) {
+    // ---- products: warp 1 S and dQ, warp 2 dP
+    const bool is_s = warp == 1;
     bool ok = true, issued = false;
     uint32_t t = 0, e = 0;
-    const uint64_t dQ = umma_desc(sQ), dO = umma_desc(sO), dK = umma_desc(sK), dV = umma_desc(sV), dKn = umma_desc_nmajor(sK);
+    const uint64_t rows = umma_desc(is_s ? sQ : sO), keys1 = umma_desc(is_s ? sK : sV), keys2 = umma_desc_nmajor(sK);
+    const uint32_t s1 = is_s ? sK : sV, ring1 = is_s ? kRing3 : kRing2, full1 = is_s ? bar_fk : bar_fv;
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      QItem im;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
-      const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
-      // K or V of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
-      auto landed = [&](int n, uint32_t bar, uint32_t parity, uint32_t at) {
-        if (!wait_all(bar, parity)) return false;
+      auto first = [&](int n) {                    // S or dP of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
+        const uint32_t tile = t + n, r = tile % ring1, at = r * kWide;
+        if (!wait_all(full1 + 8 * r, (tile / ring1) & 1u)) return false;
         int k0;
         const int seg = key_tile(im, n, &k0), valid = min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kTile);
         if (valid < kTile) {
-          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) st_zero16(at + swz(idx >> 4, idx & 15));
+          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) st_zero16(s1 + at + swz(idx >> 4, idx & 15));
           proxy_fence();
           __syncwarp();
         }
         tc_fence_after();
-        return true;
-      };
-      auto landed_k = [&](int n) { const uint32_t tile = t + n, r = tile % kRing3; return landed(n, bar_fk + 8 * r, (tile / kRing3) & 1u, sK + r * kWide); };
-      auto landed_v = [&](int n) { const uint32_t tile = t + n, r = tile % kRing2; return landed(n, bar_fv + 8 * r, (tile / kRing2) & 1u, sV + r * kWide); };
-      auto at_k = [&](uint32_t tile) { return (uint64_t)(tile % kRing3 * kWide >> 4); };
-      auto at_v = [&](uint32_t tile) { return (uint64_t)(tile % kRing2 * kWide >> 4); };
-      auto first = [&](uint32_t to, uint64_t row, uint64_t key, uint32_t bar, uint32_t bar_free, bool last) {   // S or dP
         if (elect_one()) {
+          const uint64_t keys = keys1 + (at >> 4);
+          const uint32_t to = is_s ? tmem + (tile & 1u) * 128 : tdP;
 #pragma unroll
           for (int kk = 0; kk < kD / 16; ++kk) {
             const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
-            umma(to, row + off, key + off, kk > 0);
+            umma(to, rows + off, keys + off, kk > 0);
           }
-          umma_commit(bar);
-          if (bar_free) umma_commit(bar_free);
-          if (last) umma_commit(bar_qfree);
+          umma_commit(is_s ? bar_s + 8 * (tile & 1u) : bar_dp);
+          if (!is_s) umma_commit(bar_ev + 8 * r);
+          if (n == N - 1) umma_commit(bar_qfree);
         }
         __syncwarp();
         issued = true;
+        return true;
       };
-      ok = wait_all(bar_q, e & 1u) && landed_k(0);
-      if (!ok) break;
-      first(tmem + (t & 1u) * 128, dQ, dK + at_k(t), bar_s + 8 * (t & 1u), 0, false);
-      ok = landed_v(0);
-      if (!ok) break;
-      first(tdP, dO, dV + at_v(t), bar_dp, bar_ev + 8 * (t % kRing2), N == 1);
-      for (int n = 0; n < N; ++n) {
-        const bool more = n + 1 < N;
-        const uint32_t tile = t + n, odd = tile & 1u;
-        if (more) {
-          ok = landed_k(n + 1);
-          if (!ok) break;
-          first(tmem + (odd ^ 1u) * 128, dQ, dK + at_k(tile + 1), bar_s + 8 * (odd ^ 1u), 0, false);
-          ok = landed_v(n + 1) && wait_all(bar_r, odd);
-          if (!ok) break;
-          tc_fence_after();
-          first(tdP, dO, dV + at_v(tile + 1), bar_dp, bar_ev + 8 * ((tile + 1) % kRing2), n + 2 == N);
+      ok = wait_all(bar_q, e & 1u) && first(0);
+      for (int n = 0; n < N && ok; ++n) {
+        const uint32_t tile = t + n;
+        if (!is_s) {
+          if (n + 1 < N) {
+            ok = wait_all(bar_r, tile & 1u);       // dP has been read
+            if (ok) ok = first(n + 1);
+          }
+          continue;
         }
-        ok = wait_all(bar_ds, odd);
+        if (n + 1 < N) ok = first(n + 1);
+        ok = ok && wait_all(bar_ds, tile & 1u);
         if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
         if (!ok) break;
         tc_fence_after();
         if (elect_one()) {
+          const uint64_t keys = keys2 + (uint64_t)(tile % kRing3 * kWide >> 4);
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)
-            umma_ts(tO, tmem + odd * 128 + (kk >> 1) * 32 + (kk & 1) * 8, dKn + at_k(tile) + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
+            umma_ts(tO, tmem + (tile & 1u) * 128 + (kk >> 1) * 32 + (kk & 1) * 8, keys + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
           umma_commit(bar_ek + 8 * (tile % kRing3));
-          if (!more) umma_commit(bar_f);
+          if (n == N - 1) umma_commit(bar_f);
         }
         __syncwarp();
       }
       if (!ok) break;
+      if (!is_s) {                                 // the next item's dP overwrites this one's last
+        ok = wait_all(bar_r, (t + N - 1) & 1u);
+        if (!ok) break;
+      }
       t += N;
       ++e;
     }
@@ -747,14 +741,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
       __syncwarp();
       if (issued && elect_one()) {
         int never = 0;
-        umma_commit(bar_d);
-        mbar_wait_or_fail<false>(bar_d, 0, &never, kWaitLimit);
+        umma_commit(bar_d + 8 * (warp - 1));
+        mbar_wait_or_fail<false>(bar_d + 8 * (warp - 1), 0, &never, kWaitLimit);
       }
     }
     __syncwarp();
   } else {
     // ---- weights: one query row and 32 keys per thread --------------------------------------------------------------------------
-    const int part = (warp - 2) >> 2, row = (warp & 3) * 32 + lane, G = a.G, c = a.c;
+    const int part = (warp - kFirst) >> 2, row = (warp & 3) * 32 + lane, G = a.G, c = a.c;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine = lanes + part * 32;
     const int my_local = row / G, my_head = row % G;
     const F2 scale2 = pair(a.scale_log2, a.scale_log2);
@@ -762,10 +756,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
     uint32_t t = 0, e = 0;
     for (uint32_t i = 0;; ++i) {
       int it;
-      ok = queue.read<SHORTW>(i, a, s_fail, &it);
+      QItem im;
+      ok = queue.read<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
       const int kvh = it % a.Hkv;
-      const QItem im = items[it / a.Hkv];
       const int N = im.nt0 + im.nt1 + im.nt2;
       const bool live = row < im.count * G;
       const int idx = im.first + my_local;
@@ -882,23 +876,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   }
 }
 
-// Adds the pieces of the split items in order: one block per item and head, of dK or dV, and eight keys.
+// Adds the pieces of the split items in order: one block per item and head, of dK or dV, and 32 keys; a thread has 16 columns of a key.
 __global__ void __launch_bounds__(256) k_join(const JoinItem* __restrict__ items, const GradArgs a) {
   const JoinItem im = items[blockIdx.x / a.Hkv];
-  const int kvh = blockIdx.x % a.Hkv, which = blockIdx.y & 1, key = (int)(blockIdx.y >> 1) * 8 + (int)(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  const int kvh = blockIdx.x % a.Hkv, which = blockIdx.y & 1, key = (int)(blockIdx.y >> 1) * 32 + (int)(threadIdx.x & 31), col = (int)(threadIdx.x >> 5) * 16;
   const int seg_len = im.seg == 0 ? im.s.P : (im.seg == 1 ? im.s.nb : im.s.T);
   if (im.k0 + key >= seg_len) return;
-  float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+  float4 t[4] = {};
   for (int p = 0; p < im.count; ++p) {
-    const float4 v = *reinterpret_cast<const float4*>(a.partial + (((((int64_t)im.first + p) * a.Hkv + kvh) * 2 + which) * kTile + key) * kD + lane * 4);
-    t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    const float4* from = reinterpret_cast<const float4*>(a.partial) + (((((int64_t)im.first + p) * a.Hkv + kvh) * 2 + which) * (kD / 4) + col / 4) * kTile + key;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = __ldcs(from + i * kTile);
+      t[i].x += v.x; t[i].y += v.y; t[i].z += v.z; t[i].w += v.w;
+    }
   }
   const float f = which == 0 ? 1.f : a.scale;
   const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0 + key;
-  uint2 o;
-  o.x = pack2(t.x * f, t.y * f); o.y = pack2(t.z * f, t.w * f);
-  *reinterpret_cast<uint2*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + lane * 4) = o;
+  uint4* dst = reinterpret_cast<uint4*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + col);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    dst[i] = make_uint4(pack2(t[2 * i].x * f, t[2 * i].y * f), pack2(t[2 * i].z * f, t[2 * i].w * f), pack2(t[2 * i + 1].x * f, t[2 * i + 1].y * f),
+                        pack2(t[2 * i + 1].z * f, t[2 * i + 1].w * f));
 }
 
 bool map_3d(CUtensorMap* m, const void* base, int heads, int64_t rows, int box_heads, int box_rows) {
@@ -1146,7 +1145,7 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     a.items = ws + p.at_kv; a.n_items = (int32_t)p.kv.size() * kv_heads; a.next = reinterpret_cast<int32_t*>(ws + 192);
     dkv<<<std::min(a.n_items, kSms), kThreads, kSmem, s>>>(a, maps);
     if (!p.join.empty())
-      k_join<<<dim3((unsigned)p.join.size() * kv_heads, 2 * kTile / 8), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
+      k_join<<<dim3((unsigned)p.join.size() * kv_heads, 2 * kTile / 32), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
     return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
   } catch (...) {
     return BC_ERR_UNSUPPORTED;
