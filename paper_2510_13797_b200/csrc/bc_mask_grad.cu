@@ -198,17 +198,17 @@ __device__ __forceinline__ uint32_t bits(int lo, int hi) {
 }
 
 // ---- dK and dV ---------------------------------------------------------------------------------------------------------------
-// Tensor memory: columns [0, 128) S^T, then P^T in the first 16 columns of every 32; [128, 256) dP^T, then dS^T likewise; [256, 384) dV,
-// [384, 512) dK.  Two warps issue the products; the tensor pipe runs a warp's products in the order it issued them:
-//     warp 1: S(t + 1) behind dV += P(t) dO, which reads what it overwrites, while the weights' warps turn dP(t) into dS(t);
-//     warp 2: dP(t + 1) behind dK += dS(t) Q, while they turn S(t + 1) into P(t + 1).
-// The pipe takes only a few products ahead, and a poll of a barrier takes some 200 cycles beside warps that keep the special-function
-// and shared-memory queues full: with one warp for all products it ran dry at every wait (3900 cycles a tile).
+// Tensor memory: columns [0, 128) S^T and dP^T by turns, each made as soon as the other has been read; [128, 192) P^T and [192, 256) dS^T,
+// bf16; [256, 384) dV, [384, 512) dK.  With P^T over S^T and dS^T over dP^T, the products of a tile and its weights wait for each other in
+// one long chain (3900 cycles a tile); here S(t + 1) is made while dS(t) is computed, dP(t + 1) while P(t + 1) is, and dV, dK behind them.
+// Two warps issue the products, 1 S and dP, 2 dV and dK: the tensor pipe takes only a few products ahead, and a poll of a barrier
+// takes some 200 cycles beside warps that keep the special-function and shared-memory queues full.
 //
 // Barriers (t counts query tiles, e items; parity = uses so far & 1):
 //   fq[r] / eq[r], fo[r] / eo[r]: Q, or dO with the tile's numbers, has landed in a ring place / been read
 //   k, v / kfree, vfree: K, V of item e have landed / been read      s, dp: S^T, dP^T of tile t are there
-//   p, ds: P^T, dS^T of tile t have been stored      f: dK and dV of item e are final      x: they have been read
+//   rs, rdp: they have been read      p, ds: P^T, dS^T of tile t have been stored      pfree, dsfree: dV, dK have been added
+//   f: dK and dV of item e are final      x: they have been read
 //   d: drain on the give-up path
 template <bool SHORTW>
 __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __grid_constant__ KvMaps maps) {
@@ -219,8 +219,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   volatile int *s_tmem = s_misc + 62, *s_fail = s_misc + 63;
   const uint32_t bar_fq = sBars, bar_eq = bar_fq + 8 * kRing3, bar_fo = bar_eq + 8 * kRing3, bar_eo = bar_fo + 8 * kRing2, bar_k = bar_eo + 8 * kRing2,
                  bar_v = bar_k + 8, bar_kfree = bar_k + 16, bar_vfree = bar_k + 24, bar_s = bar_k + 32, bar_dp = bar_k + 40, bar_p = bar_k + 48,
-                 bar_ds = bar_k + 56, bar_f = bar_k + 64, bar_x = bar_k + 72, bar_d = bar_k + 80;   // d: one for either product warp
-  const Queue queue = {s_misc, bar_k + 96, bar_k + 112};
+                 bar_ds = bar_k + 56, bar_rs = bar_k + 64, bar_rdp = bar_k + 72, bar_pfree = bar_k + 80, bar_dsfree = bar_k + 88, bar_f = bar_k + 96,
+                 bar_x = bar_k + 104, bar_d = bar_k + 112;   // d: one for either product warp
+  const Queue queue = {s_misc, bar_k + 128, bar_k + 144};
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (sK & 1023) {                       // the operands' layouts need it; shared memory begins so
@@ -229,11 +230,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   }
   if (tid == 0) {
     for (uint32_t bar = sBars; bar < queue.empty + 16; bar += 8) {
-      const uint32_t count = bar == bar_p || bar == bar_ds || bar == bar_x ? kWeighers
-                             : bar >= bar_eo && bar < bar_k                ? 2 + kWeighers
-                             : bar == bar_f                                ? 2u
-                             : bar >= queue.empty                          ? kReaders
-                                                                           : 1u;
+      const uint32_t count = (bar >= bar_p && bar <= bar_rdp) || bar == bar_x ? kWeighers
+                             : bar >= bar_eo && bar < bar_k                   ? 1 + kWeighers
+                             : bar >= queue.empty                             ? kReaders
+                                                                              : 1u;
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = (uint32_t)*s_tmem, tS = tmem, tdP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+  const uint32_t tmem = (uint32_t)*s_tmem, tP = tmem + 128, tdS = tmem + 192, tV = tmem + 256, tK = tmem + 384;
   auto wait_all = [&](uint32_t bar, uint32_t parity) {
     return __all_sync(0xffffffffu, mbar_wait_or_fail<SHORTW>(bar, parity, s_fail, a.wait_limit)) != 0;
   };
@@ -331,17 +331,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
       mbar_wait_or_fail<false>(bar_fo + 8 * (b % kRing2), (b / kRing2) & 1u, &never, kWaitLimit);
     __syncwarp();
   } else if (warp < kFirst) {
-    // ---- products: warp 1 S and dV, warp 2 dP and dK --------------------------------------------------------------------------
-    const bool is_s = warp == 1;
+    // ---- products: warp 1 S and dP, warp 2 dV and dK --------------------------------------------------------------------------
     bool ok = true, issued = false;
     uint32_t t = 0, e = 0;
-    const uint64_t key = umma_desc(is_s ? sK : sV);
-    const uint32_t t1 = is_s ? tS : tdP, t2 = is_s ? tV : tK;                          // S or dP; dV or dK
-    const uint32_t bar_key = is_s ? bar_k : bar_v, bar_free = is_s ? bar_kfree : bar_vfree, bar_1 = is_s ? bar_s : bar_dp, bar_2 = is_s ? bar_p : bar_ds;
-    // the first product's rows: Q or dO, the second's: dO or Q
-    const uint32_t s1 = is_s ? sQ : sO, ring1 = is_s ? kRing3 : kRing2, full1 = is_s ? bar_fq : bar_fo;
-    const uint32_t ring2 = is_s ? kRing2 : kRing3, empty2 = is_s ? bar_eo : bar_eq;
-    const uint64_t rows1 = umma_desc(s1), rows2 = umma_desc_nmajor(is_s ? sO : sQ);
     for (uint32_t i = 0;; ++i) {
       int it;
       KvItem im;
@@ -349,56 +341,81 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
       if (!ok || it < 0) break;
       const int N = im.nt + im.nb_tiles;
       if (N == 0) continue;
-      // rows that the last tile of either kind holds of the next sequence are cleared: they are factors of the second products
+      // the last tile of either kind may hold rows of the next sequence: the second products take only the steps of 16 rows that hold some of
+      // this one, and what such a step holds of the next is cleared
       const int end_tok = min(im.s.T - (im.ta + im.nt - 1) * a.per, a.per) * a.G, end_bea = min(im.s.nb - (im.ba + im.nb_tiles - 1) * a.per, a.per) * a.G;
-      auto first = [&](int n) {
-        const uint32_t tile = t + n, r = tile % ring1, at = r * kWide;
-        if (!wait_all(full1 + 8 * r, (tile / ring1) & 1u)) return false;
-        const int valid = n == im.nt - 1 ? end_tok : (n == N - 1 ? end_bea : box_rows);
-        if (valid < box_rows) {
-          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(s1 + at + swz(idx >> 4, idx & 15));
-          proxy_fence();
-          __syncwarp();
-        }
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t rows = rows1 + (at >> 4);
-#pragma unroll
-          for (int kk = 0; kk < kD / 16; ++kk) {
-            const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
-            umma(t1, key + off, rows + off, kk > 0);
+      auto valid_of = [&](int n) { return n == im.nt - 1 ? end_tok : (n == N - 1 ? end_bea : box_rows); };
+      if (warp == 1) {
+        const uint64_t dK = umma_desc(sK), dV = umma_desc(sV), dQ = umma_desc(sQ), dO = umma_desc(sO);
+        auto first = [&](int n, uint32_t bar_landed, uint32_t parity, uint32_t at, uint64_t keys, uint64_t rows, uint32_t bar, uint32_t bar_free) {
+          if (!wait_all(bar_landed, parity)) return false;
+          const int valid = valid_of(n), end = min((valid + 15) & ~15, box_rows);
+          if (valid < end) {
+            for (int idx = valid * 16 + lane; idx < end * 16; idx += 32) st_zero16(at + swz(idx >> 4, idx & 15));
+            proxy_fence();
+            __syncwarp();
           }
-          umma_commit(bar_1);
-          if (n == N - 1) umma_commit(bar_free);
-          if (!is_s) umma_commit(bar_eo + 8 * r);                          // dO is free when dP, dV and the numbers' readers are done with it
-        }
-        __syncwarp();
-        issued = true;
-        return true;
-      };
-      ok = wait_all(bar_key, e & 1u) && first(0);
-      for (int n = 0; n < N && ok; ++n) {
-        const uint32_t tile = t + n, r = tile % ring2;
-        ok = wait_all(bar_2, tile & 1u);
-        if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
-        if (!ok) break;
-        const int valid = n == im.nt - 1 ? end_tok : (n == N - 1 ? end_bea : box_rows);
-        if (is_s && valid < box_rows) {            // dO has landed (P has its numbers), but warp 2 need not have come to this tile yet
-          for (int idx = valid * 16 + lane; idx < box_rows * 16; idx += 32) st_zero16(sO + r * kWide + swz(idx >> 4, idx & 15));
-          proxy_fence();
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = 0; kk < kD / 16; ++kk) {
+              const uint64_t off = (uint64_t)(((kk >> 2) * (kTile * 128) + (kk & 3) * 32) >> 4);
+              umma(tmem, keys + off, rows + off, kk > 0);
+            }
+            umma_commit(bar);
+            if (n == N - 1) umma_commit(bar_free);
+          }
           __syncwarp();
+          issued = true;
+          return true;
+        };
+        ok = wait_all(bar_k, e & 1u);
+        for (int n = 0; n < N && ok; ++n) {
+          const uint32_t tile = t + n, rq = tile % kRing3, ro = tile % kRing2;
+          if (tile > 0) ok = wait_all(bar_rdp, (tile - 1) & 1u);
+          ok = ok && first(n, bar_fq + 8 * rq, (tile / kRing3) & 1u, sQ + rq * kWide, dK, dQ + (uint64_t)(rq * kWide >> 4), bar_s, bar_kfree);
+          if (ok && n == 0) ok = wait_all(bar_v, e & 1u);
+          ok = ok && wait_all(bar_rs, tile & 1u) &&
+               first(n, bar_fo + 8 * ro, (tile / kRing2) & 1u, sO + ro * kWide, dV, dO + (uint64_t)(ro * kWide >> 4), bar_dp, bar_vfree);
         }
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t rows = rows2 + (uint64_t)(r * kWide >> 4);
+      } else {
+        const uint64_t dQ = umma_desc_nmajor(sQ), dO = umma_desc_nmajor(sO);
+        auto second = [&](uint32_t to, uint32_t from, uint64_t rows, int steps, bool fresh) {
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)
-            umma_ts(t2, t1 + (kk >> 1) * 32 + (kk & 1) * 8, rows + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
-          umma_commit(empty2 + 8 * r);
-          if (n == N - 1) umma_commit(bar_f);
+            if (kk < steps) umma_ts(to, from + kk * 8, rows + (uint64_t)((kk * 16 * 128) >> 4), (!fresh || kk > 0) ? 1u : 0u);
+        };
+        if (e > 0) ok = wait_all(bar_x, (e - 1) & 1u);                     // the last item's sums have been read
+        for (int n = 0; n < N && ok; ++n) {
+          const uint32_t tile = t + n, rq = tile % kRing3, ro = tile % kRing2;
+          const int valid = valid_of(n), steps = (valid + 15) >> 4;
+          ok = wait_all(bar_p, tile & 1u);
+          if (!ok) break;
+          if (valid & 15) {                        // dO has landed (P has its numbers), but warp 1 need not have come to it yet
+            for (int idx = valid * 16 + lane; idx < min(steps * 16, box_rows) * 16; idx += 32) st_zero16(sO + ro * kWide + swz(idx >> 4, idx & 15));
+            proxy_fence();
+            __syncwarp();
+          }
+          tc_fence_after();
+          if (elect_one()) {
+            second(tV, tP, dO + (uint64_t)(ro * kWide >> 4), steps, n == 0);
+            umma_commit(bar_pfree);
+          }
+          __syncwarp();
+          issued = true;
+          ok = wait_all(bar_ds, tile & 1u);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            second(tK, tdS, dQ + (uint64_t)(rq * kWide >> 4), steps, n == 0);
+            umma_commit(bar_dsfree);
+            // dP(t) had been read when dS(t) was stored, S(t) when P(t) was: Q and dO are free when these products are done
+            umma_commit(bar_eq + 8 * rq);
+            umma_commit(bar_eo + 8 * ro);
+            if (n == N - 1) umma_commit(bar_f);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-        if (n + 1 < N) ok = first(n + 1);
       }
       if (!ok) break;
       t += N;
@@ -419,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
     const int part = (warp - kFirst) >> 2;         // columns [32 part, + 32)
     // a warp reaches the 32 lanes of tensor memory that belong to its number modulo 4; its keys are those lanes
     const int key = (warp & 3) * 32 + lane;
-    const uint32_t mine = ((uint32_t)((warp & 3) * 32) << 16) + part * 32;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, mine = lanes + part * 32, half = lanes + part * 16;   // of fp32, of bf16 columns
     const F2 scale2 = pair(a.scale_log2, a.scale_log2);
     bool ok = true;
     uint32_t t = 0, e = 0;
@@ -452,8 +469,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         tc_fence_after();
         const float *minus_l = stats + t % kRing2 * 256 + part * 32, *minus_d = minus_l + 128;
         float p[32];
-        tmem_ld32_async(tS + mine, p);
+        tmem_ld32_async(tmem + mine, p);
         tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_rs);
         uint32_t out[16];
         if (some) {                                // uniform over the warp, no access to tensor memory inside
 #pragma unroll
@@ -474,7 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         }
 #pragma unroll
         for (int j = 0; j < 16; ++j) out[j] = pack2(p[2 * j], p[2 * j + 1]);
-        tmem_st16(tS + mine, out);                 // over the warp's own columns, which it has read
+        if (t > 0) ok = wait_all(bar_pfree, (t - 1) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_st16(tP + half, out);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -483,8 +506,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         if (!ok) break;
         tc_fence_after();
         float dp[32];
-        tmem_ld32_async(tdP + mine, dp);
+        tmem_ld32_async(tmem + mine, dp);
         tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(bar_rdp);
         // where the weight is 0 the score gradient is, too: dP is finite there, rows of other sequences having been cleared
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
@@ -495,7 +521,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
           out[j / 2] = pack2(q[0], q[1]);
           out[j / 2 + 1] = pack2(q[2], q[3]);
         }
-        tmem_st16(tdP + mine, out);
+        if (t > 0) ok = wait_all(bar_dsfree, (t - 1) & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        tmem_st16(tdS + half, out);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -514,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_dkv(const GradArgs a, const __g
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int cb = 0; cb < 2; ++cb) tmem_ld32_async((is_k ? tK : tV) + ((uint32_t)((warp & 3) * 32) << 16) + col + cb * 32, o + cb * 32);
+        for (int cb = 0; cb < 2; ++cb) tmem_ld32_async((is_k ? tK : tV) + lanes + col + cb * 32, o + cb * 32);
         tmem_wait_ld();
         tc_fence_before();
         __syncwarp();
@@ -676,13 +705,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
       ok = queue.read<SHORTW>(i, a, s_fail, &it, &im);
       if (!ok || it < 0) break;
       const int N = im.nt0 + im.nt1 + im.nt2;
-      auto first = [&](int n) {                    // S or dP of tile n; keys past the segment are cleared: K is a factor of dS K, V of dP
+      auto valid_of = [&](int n) {
+        int k0;
+        const int seg = key_tile(im, n, &k0);
+        return min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kTile);
+      };
+      // S or dP of tile n.  dS K takes only the steps of 16 keys that hold some of the segment, and what such a step holds past the segment's
+      // end is cleared: K is its factor, V that of dP
+      auto first = [&](int n) {
         const uint32_t tile = t + n, r = tile % ring1, at = r * kWide;
         if (!wait_all(full1 + 8 * r, (tile / ring1) & 1u)) return false;
-        int k0;
-        const int seg = key_tile(im, n, &k0), valid = min((seg == 0 ? im.s.P : (seg == 1 ? im.s.nb : im.s.T)) - k0, kTile);
-        if (valid < kTile) {
-          for (int idx = valid * 16 + lane; idx < kTile * 16; idx += 32) st_zero16(s1 + at + swz(idx >> 4, idx & 15));
+        const int valid = valid_of(n);
+        if (valid & 15) {
+          for (int idx = valid * 16 + lane; idx < ((valid + 15) & ~15) * 16; idx += 32) st_zero16(s1 + at + swz(idx >> 4, idx & 15));
           proxy_fence();
           __syncwarp();
         }
@@ -718,11 +753,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
         if (ok && n == 0 && e > 0) ok = wait_all(bar_x, (e - 1) & 1u);     // the last item's sums have been read
         if (!ok) break;
         tc_fence_after();
+        const int steps = (valid_of(n) + 15) >> 4;
         if (elect_one()) {
           const uint64_t keys = keys2 + (uint64_t)(tile % kRing3 * kWide >> 4);
 #pragma unroll
           for (int kk = 0; kk < kTile / 16; ++kk)
-            umma_ts(tO, tmem + (tile & 1u) * 128 + (kk >> 1) * 32 + (kk & 1) * 8, keys + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
+            if (kk < steps) umma_ts(tO, tmem + (tile & 1u) * 128 + (kk >> 1) * 32 + (kk & 1) * 8, keys + (uint64_t)((kk * 16 * 128) >> 4), (n > 0 || kk > 0) ? 1u : 0u);
           umma_commit(bar_ek + 8 * (tile % kRing3));
           if (n == N - 1) umma_commit(bar_f);
         }
