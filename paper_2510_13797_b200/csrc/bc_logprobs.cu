@@ -7,14 +7,13 @@
 // The difference to the maximum is taken first and exactly, so large logits lose nothing; the maximum and ln s are kept
 // apart for the gradient for the same reason.
 //
-// Forward: one pass over the row in memory.  A cluster of up to eight blocks has a row (304 KB for a vocabulary of 151,936 in
-// bf16); every thread copies its 16-byte pieces to shared memory, all of them in flight at once, and folds each into a
-// running (reference, s, t) as it lands.  What a thread copied only that thread reads, so the pieces need no barrier.
-// The alternatives come from the copy in shared memory: the K / blocks-th largest of a block's threads' maxima is a value
-// that at least K / blocks elements of the block reach, and the smallest of these over the blocks one that K elements of the
-// row reach; the few elements that reach it (a hundred and some for K = 100) are gathered in the first block and ranked by
-// counting.  Where more reach it than the buffer holds (many equal logits, or the large ones all with one thread), the
-// cluster finds the K-th largest (value, index) pair bit by bit, counting in shared memory.
+// Forward: one pass over the row in memory, in rounds of four 16-byte pieces per thread; five blocks of 256 threads on an SM cover
+// each other's loads and searches.  A thread folds its pieces into a running (reference, s, t).  A block has a row, or, where rows are few, a cluster of blocks share it.
+// The alternatives come from the same pass.  After its first round a block knows a bound that K elements reach at least, from its
+// threads' maxima (below); of the later rounds it notes the pieces that hold an element that reaches it, a few in a hundred.  At the
+// end the bound is that of the maxima over everything, and the elements that still reach it, a hundred or two for K = 100, are
+// taken from the noted pieces and the first round's, which are read again, and ranked by counting.  Where more reach it (many
+// equal logits, ascending rows), the blocks find the K-th largest (value, index) pair bit by bit, counting over the row.
 #include <cooperative_groups.h>
 
 #include "bc_common.cuh"
@@ -23,12 +22,11 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kMaxParts = 8;          // blocks per row
-constexpr int kPartBytes = 4096;      // a block is given at least this much of a row
-constexpr int kMaxTop = kThreads;     // alternatives per row
-constexpr int kCands = 1024;          // elements that are ranked at most
+constexpr int kThreads = 256;         // of the gradient's blocks
+constexpr int kMaxTop = 256;          // alternatives per row; no more than a forward block has threads
+constexpr int kMaxParts = 8;          // blocks that share a row
+constexpr int kNoted = 3072;          // pieces that a block notes at most
+constexpr int kRanked = 1024;         // elements that are ranked at most
 constexpr int kMaxVocab = 262144;
 constexpr int kIndexBits = 18;        // of a vocabulary index
 constexpr float kFar = 0x1p126f;      // logits count as no further from 0 than this, so that differences stay finite
@@ -148,64 +146,88 @@ struct Sums {
   }
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 struct LogprobArgs {
   const uint8_t* logits;
   int64_t row_bytes;
-  int vocab, top_k;
+  int vocab, top_k, parts;              // parts: blocks per row
   const int64_t* targets;
   float *logprob, *entropy, *stats, *top_logprob;
   int32_t* top_idx;
 };
 
-template <bool F32>
-__global__ void __launch_bounds__(kThreads, 4) k_logprobs(const LogprobArgs a) {
+// T threads per block; a round is 4 T pieces.
+template <bool F32, int T>
+__global__ void __launch_bounds__(T, 1280 / T) k_logprobs(const LogprobArgs a) {
   using L = Logits<F32>;
-  extern __shared__ __align__(16) uint4 piece[];           // this block's share of the row
-  __shared__ unsigned long long cand[kCands];              // the first block's: the elements to be ranked
+  constexpr int kWarps = T / 32;
+  __shared__ __align__(16) unsigned long long ranked[kRanked];   // the first block's
+  __shared__ int32_t noted[kNoted];
   __shared__ Sums warp_sums[kWarps];
   __shared__ Sums block_sums;
-  __shared__ uint32_t block_key;
-  __shared__ int n_cand, counts[2];
+  __shared__ float row_m, row_ls;
+  __shared__ __align__(16) uint16_t maxima[T];
+  __shared__ uint32_t block_bound, block_own, bound16[2];
+  __shared__ int n_noted, n_ranked, counts[kWarps], block_counts[2];
   cg::cluster_group cluster = cg::this_cluster();
-  const int part = (int)cluster.block_rank(), parts = (int)cluster.num_blocks();
-  const int64_t r = blockIdx.x / parts;
+  const int parts = a.parts, part = parts > 1 ? (int)cluster.block_rank() : 0;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, vocab = a.vocab;
-  const uint8_t* row = a.logits + r * a.row_bytes;
+  const F2 log2e2 = pair(kLog2e, kLog2e);
+  const uint32_t lowest = key_of<F32>(-INFINITY);
+  auto value_of = [&](uint32_t key) { return key <= lowest ? -INFINITY : key_value<F32>(key); };
   // elements ahead of the first 16-byte boundary and behind the last are taken one by one, by threads of the first and last block
+  const int64_t r = blockIdx.x / parts;
+  const uint8_t* const row = a.logits + r * a.row_bytes;
   const int head = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / L::kBytes);
-  const int pieces = (vocab - head) / L::kPer, tail0 = head + pieces * L::kPer;
-  const int per = (pieces + parts - 1) / parts, p0 = min(pieces, part * per), mine = min(pieces, p0 + per) - p0;
-  const uint4* src = reinterpret_cast<const uint4*>(row + head * L::kBytes) + p0;
-
-  if (tid == 0) n_cand = 0;
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(piece);
-  const int quarter = (mine + 4 * kThreads - 1) / (4 * kThreads) * kThreads;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    for (int i = g * quarter + tid; i < min(mine, (g + 1) * quarter); i += kThreads) copy16(dst + i * 16, src + i);
-    copies_begun();
-  }
-  int extra_at = -1;
-  if (part == 0 && tid < head) extra_at = tid;
-  if (part == parts - 1 && tid >= 32 && tail0 + tid - 32 < vocab) extra_at = tail0 + tid - 32;
-  const float extra = extra_at >= 0 ? L::load(row, extra_at) : -INFINITY;
+  const int all_pieces = (vocab - head) / L::kPer;
+  const int per = (all_pieces + parts - 1) / parts, p0 = min(all_pieces, part * per), pieces = min(all_pieces, p0 + per) - p0;
+  const uint4* const src = reinterpret_cast<const uint4*>(row + head * L::kBytes) + p0;
+  const int index0 = head + p0 * L::kPer;                  // of the block's first piece
+  if (tid == 0) n_noted = n_ranked = 0;
 
   Sums st = {-kFar, 0.f, 0.f};
   float best = -INFINITY;                                  // of this thread's elements
   F2 s2 = pair(0.f, 0.f), t2 = s2;
-  const F2 log2e2 = pair(kLog2e, kLog2e);
-  auto fold = [&](int g) {
-    for (int i = g * quarter + tid; i < min(mine, (g + 1) * quarter); i += kThreads) {
-      const uint4 v = piece[i];
-      const float top = L::top(v);
+  // Keys that at least need0, and need1, elements of the block reach: the need-th largest of the threads' maxima, to 16 bits (what reaches
+  // the whole key reaches the shorter one).  The first two warps find one each, bit by bit, every lane counting T / 32 of the maxima.
+  auto bounds_of_maxima = [&](int need0, int need1, uint32_t* b0, uint32_t* b1) {
+    maxima[tid] = (uint16_t)(key32(best) >> 16);
+    __syncthreads();
+    if (warp < 2) {
+      uint32_t k[T / 64];
+#pragma unroll
+      for (int i = 0; i < T / 64; ++i) k[i] = reinterpret_cast<const uint32_t*>(maxima)[i * 32 + lane];
+      const int need = warp == 0 ? need0 : need1;
+      uint32_t found = 0;
+      if (need > 0)
+#pragma unroll 1
+        for (int b = 15; b >= 0; --b) {
+          const uint32_t trial = found | (1u << b);
+          int n = 0;
+#pragma unroll
+          for (int i = 0; i < T / 64; ++i) n += ((k[i] & 0xffffu) >= trial) + ((k[i] >> 16) >= trial);
+          if (__reduce_add_sync(0xffffffffu, n) >= need) found = trial;
+        }
+      if (lane == 0) bound16[warp] = found;
+    }
+    __syncthreads();
+    *b0 = max(lowest, F32 ? bound16[0] << 16 : bound16[0]);
+    *b1 = max(lowest, F32 ? bound16[1] << 16 : bound16[1]);
+  };
+  // Short shares are read again at the end, and nothing is noted
+  const bool noting = pieces > 12 * T;
+  float least = -INFINITY;                                 // value of the bound
+  for (int first = 0; first < pieces; first += 4 * T) {
+    uint4 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (first + k * T + tid < pieces) v[k] = __ldg(src + first + k * T + tid);
+    uint32_t reach = 0;                                    // which of the four pieces hold an element that reaches the bound
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (first + k * T + tid >= pieces) continue;
+      const float top = L::top(v[k]);
       best = fmaxf(best, top);
+      reach |= (top < least ? 0u : 1u) << k;               // a piece of NaN alone, too: it counts where nothing else does
       if (near(top) > st.m + kSlack) {
         float s0, s1, t0, t1;
         split(s2, &s0, &s1); split(t2, &t0, &t1);
@@ -215,10 +237,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs(const LogprobArgs a) {
       }
       const F2 minus = pair(-st.m, -st.m);
       F2 x[L::kPer / 2];
-      L::near_pairs(v, x);
+      L::near_pairs(v[k], x);
 #pragma unroll
-      for (int k = 0; k < L::kPer / 2; ++k) {
-        const F2 d = add2(x[k], minus);
+      for (int i = 0; i < L::kPer / 2; ++i) {
+        const F2 d = add2(x[i], minus);
         float y0, y1;
         split(mul2(d, log2e2), &y0, &y1);
         const F2 e = pair(ex2(y0), ex2(y1));
@@ -226,11 +248,36 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs(const LogprobArgs a) {
         t2 = fma2(e, d, t2);
       }
     }
-  };
-  copies_landed<3>(); fold(0);
-  copies_landed<2>(); fold(1);
-  copies_landed<1>(); fold(2);
-  copies_landed<0>(); fold(3);
+    if (a.top_k > 0 && noting) {
+      if (first > 0 && reach != 0) {
+        int at = atomicAdd(&n_noted, __popc(reach));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (reach & (1u << k)) {
+            if (at < kNoted) noted[at] = first + k * T + tid;
+            ++at;
+          }
+      }
+      // a better bound is worth its barriers after the first, second, fourth, eighth, ... round
+      const int done = first / (4 * T) + 1;
+      if ((done & (done - 1)) == 0 && first + 4 * T < pieces) {
+        uint32_t key, none;
+        bounds_of_maxima(a.top_k, 0, &key, &none);
+        least = value_of(key);
+      }
+    }
+  }
+  const int tail0 = head + all_pieces * L::kPer;
+  int extra_at = -1;
+  if (part == 0 && tid < head) extra_at = tid;
+  if (part == parts - 1 && tid >= 32 && tail0 + tid - 32 < vocab) extra_at = tail0 + tid - 32;
+  const float extra = extra_at >= 0 ? L::load(row, extra_at) : -INFINITY;
+  float given = 0.f;
+  int target = -1;                                         // outside the vocabulary: none is given
+  if (part == 0 && tid == 0 && a.logprob) {
+    const int64_t t = a.targets[r];
+    if (t >= 0 && t < vocab) { target = (int)t; given = L::load(row, t); }
+  }
   {
     float s0, s1, t0, t1;
     split(s2, &s0, &s1); split(t2, &t0, &t1);
@@ -242,123 +289,132 @@ __global__ void __launch_bounds__(kThreads, 4) k_logprobs(const LogprobArgs a) {
   }
   if (best > -kFar) st.move(near(best));                   // from the reference, which may lie behind, to the maximum itself
   else st = {-kFar, 0.f, 0.f};                             // nothing but -inf and NaN: no mass
-
 #pragma unroll
   for (int d = 16; d; d >>= 1) {
     const Sums o = {__shfl_xor_sync(0xffffffffu, st.m, d), __shfl_xor_sync(0xffffffffu, st.s, d), __shfl_xor_sync(0xffffffffu, st.t, d)};
     st.join(o);
   }
   if (lane == 0) warp_sums[warp] = st;
-  uint32_t bound = 0;                                      // key that enough threads' maxima reach
-  if (a.top_k > 0) {
-    const int need = (a.top_k + parts - 1) / parts;
-    const uint32_t k = key_of<F32>(best);
-#pragma unroll 1
-    for (int b = L::kKeyBits - 1; b >= 0; --b) {
-      const uint32_t trial = bound | (1u << b);
-      if (__syncthreads_count(k >= trial) >= need) bound = trial;
-    }
-  }
+  // The row's bound: where blocks share it, the smallest of those that K / blocks elements of a block reach; but no smaller than any that K
+  // elements of one block reach, by whose likes the pieces were noted
+  uint32_t bound = lowest, own = lowest;
+  if (a.top_k > 0) bounds_of_maxima((a.top_k + parts - 1) / parts, parts > 1 && noting ? a.top_k : 0, &bound, &own);
   __syncthreads();
-  if (tid == 0) {
-    Sums all = warp_sums[0];
-    for (int w = 1; w < kWarps; ++w) all.join(warp_sums[w]);
-    block_sums = all;
-    block_key = bound;
+  if (warp == 0) {
+    Sums all = lane < kWarps ? warp_sums[lane] : Sums{-kFar, 0.f, 0.f};
+#pragma unroll
+    for (int d = kWarps / 2; d; d >>= 1) {
+      const Sums o = {__shfl_xor_sync(0xffffffffu, all.m, d), __shfl_xor_sync(0xffffffffu, all.s, d), __shfl_xor_sync(0xffffffffu, all.t, d)};
+      all.join(o);
+    }
+    if (lane == 0) { block_sums = all; block_bound = bound; block_own = own; }
   }
-  cluster.sync();
+  auto sync_row = [&]() {                                  // all threads that have the row
+    if (parts > 1) cluster.sync();
+    else __syncthreads();
+  };
+  sync_row();
   if (part == 0 && tid == 0) {
     Sums all = block_sums;
     for (int p = 1; p < parts; ++p) all.join(*cluster.map_shared_rank(&block_sums, p));
     const bool some = all.m > -kFar;
     const float ls = some ? logf(all.s) : 0.f, m = some ? all.m : -INFINITY;
-    warp_sums[0] = {m, ls, 0.f};                           // for the alternatives
+    row_m = m; row_ls = ls;
     if (a.stats) { a.stats[2 * r] = m; a.stats[2 * r + 1] = ls; }
     if (a.entropy) a.entropy[r] = some ? fmaxf(ls - all.t / all.s, 0.f) : 0.f;
-    if (a.logprob) {
-      const int64_t t = a.targets[r];
-      float lp = 0.f;                                      // no token is given for this row
-      if (t >= 0 && t < vocab) {
-        const float x = L::load(row, t);
-        lp = x > -kFar ? (near(x) - m) - ls : -INFINITY;
-      }
-      a.logprob[r] = lp;
-    }
+    // a row for which no token is given: 0
+    if (a.logprob) a.logprob[r] = target < 0 ? 0.f : (given > -kFar ? (near(given) - m) - ls : -INFINITY);
   }
   if (a.top_k == 0) {
-    cluster.sync();                                        // no block leaves while its sums may still be read
+    if (parts > 1) cluster.sync();                         // no block leaves while its sums may still be read
     return;
   }
 
-  // ---- the elements that reach the bound, to the first block ---------------------------------------------------------------
-  bound = block_key;
-  for (int p = 0; p < parts; ++p) bound = min(bound, *cluster.map_shared_rank(&block_key, p));
-  int* total = cluster.map_shared_rank(&n_cand, 0);
-  unsigned long long* to = cluster.map_shared_rank(cand, 0);
-  // calls f(value, index) for every element of this thread that may reach `least` (a NaN does so where nothing else counts)
-  auto each = [&](float least, auto f) {
-    for (int i = tid; i < mine; i += kThreads) {
-      const uint4 v = piece[i];
-      if (!(L::top(v) < least)) {
-        const int at = head + (p0 + i) * L::kPer;
+  // ---- the alternatives ----------------------------------------------------------------------------------------------------
+  for (int p = 1; p < parts; ++p) {
+    bound = min(bound, *cluster.map_shared_rank(&block_bound, (part + p) % parts));
+    own = max(own, *cluster.map_shared_rank(&block_own, (part + p) % parts));
+  }
+  bound = max(bound, own);
+  int* const total_ranked = parts > 1 ? cluster.map_shared_rank(&n_ranked, 0) : &n_ranked;
+  unsigned long long* const to = parts > 1 ? cluster.map_shared_rank(ranked, 0) : ranked;
+  // calls f(pair) for the elements of this thread in pieces that hold one above `low`: in the first round's and those noted, or in all
+  const bool complete = n_noted <= kNoted;
+  auto each = [&](float low, bool everything, auto f) {
+    const int again = everything || !noting ? pieces : 4 * T, all = everything ? again : again + n_noted;
+    for (int j0 = 0; j0 < all; j0 += 4 * T) {              // four loads at once
+      uint4 w[4];
+      int i[4];
 #pragma unroll
-        for (int k = 0; k < L::kPer; ++k) {
-          const float x = L::element(v, k);
-          if (!(x < least)) f(x, at + k);
-        }
+      for (int k = 0; k < 4; ++k) {
+        const int j = j0 + k * T + tid;
+        i[k] = j < again ? j : (j < all ? noted[j - again] : -1);
+        if (i[k] >= 0) w[k] = __ldg(src + i[k]);
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i[k] >= 0 && !(L::top(w[k]) < low))
+#pragma unroll
+          for (int e = 0; e < L::kPer; ++e) f(place_of<F32>(L::element(w[k], e), index0 + i[k] * L::kPer + e));
     }
-    if (extra_at >= 0 && !(extra < least)) f(extra, extra_at);
+    if (extra_at >= 0) f(place_of<F32>(extra, extra_at));
   };
-  const uint32_t lowest = key_of<F32>(-INFINITY);
-  auto push = [&](unsigned long long least) {              // two steps: the place of every element, then its store
-    const uint32_t key = (uint32_t)(least >> kIndexBits);
-    each(key <= lowest ? -INFINITY : key_value<F32>(key), [&](float x, int i) {
-      const unsigned long long c = place_of<F32>(x, i);
-      if (c >= least) {
-        const int at = atomicAdd(total, 1);
-        if (at < kCands) to[at] = c;
+  auto push = [&](unsigned long long from, bool everything) {
+    each(value_of((uint32_t)(from >> kIndexBits)), everything, [&](unsigned long long c) {
+      if (c >= from) {
+        const int at = atomicAdd(total_ranked, 1);
+        if (at < kRanked) to[at] = c;
       }
     });
   };
-  push((unsigned long long)bound << kIndexBits);
-  cluster.sync();
-  int found = *total;
-  cluster.sync();                                          // everyone has read it
-  if (found > kCands) {
-    // the K-th largest (value, index) pair, bit by bit; any pair that K to kCands elements reach will do
-    unsigned long long least = 0;
+  // where a block could not note all its pieces nothing is pushed, and the search goes over all of the row
+  if (complete) push((unsigned long long)bound << kIndexBits, false);
+  else if (tid == 0) atomicAdd(total_ranked, kRanked + 1);
+  sync_row();
+  int found = *total_ranked;
+  sync_row();                                              // all have read it
+  if (found > kRanked) {
+    // a (value, index) pair that top_k to kRanked pairs reach, bit by bit
+    unsigned long long from = 0;
     int turn = 0;
     for (int b = L::kKeyBits + kIndexBits - 1; b >= 0; --b) {
-      const unsigned long long trial = least | (1ull << b);
-      const uint32_t key = (uint32_t)(trial >> kIndexBits);
-      int mine_n = 0;
-      each(key <= lowest ? -INFINITY : key_value<F32>(key), [&](float x, int i) { mine_n += place_of<F32>(x, i) >= trial; });
-      mine_n = __reduce_add_sync(0xffffffffu, mine_n);
-      if (tid == 0) counts[turn] = 0;
+      const unsigned long long trial = from | (1ull << b);
+      int n = 0;
+      each(value_of((uint32_t)(trial >> kIndexBits)), true, [&](unsigned long long c) { n += c >= trial; });
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0) counts[warp] = n;
       __syncthreads();
-      if (lane == 0) atomicAdd(&counts[turn], mine_n);
-      cluster.sync();
-      found = 0;
-      for (int p = 0; p < parts; ++p) found += *cluster.map_shared_rank(&counts[turn], p);
+      if (tid == 0) {
+        n = 0;
+        for (int w = 0; w < kWarps; ++w) n += counts[w];
+        block_counts[turn] = n;
+      }
+      sync_row();
+      n = block_counts[turn];
+      for (int p = 1; p < parts; ++p) n += *cluster.map_shared_rank(&block_counts[turn], (part + p) % parts);
       turn ^= 1;                                           // a block may begin the next count while another reads this one
-      if (found >= a.top_k) least = trial;
-      if (found >= a.top_k && found <= kCands) break;
+      if (n >= a.top_k) from = trial;
+      if (n >= a.top_k && n <= kRanked) break;
     }
-    if (part == 0 && tid == 0) n_cand = 0;
-    cluster.sync();
-    push(least);
-    cluster.sync();
-    found = *total;
-    cluster.sync();
+    if (part == 0 && tid == 0) n_ranked = 0;
+    sync_row();
+    push(from, true);
+    sync_row();
+    found = *total_ranked;
+    if (parts > 1) cluster.sync();
   }
   if (part != 0) return;
-  // ---- rank them: a place is larger than exactly those behind it -----------------------------------------------------------
-  const float m = warp_sums[0].m, ls = warp_sums[0].s;
-  for (int i = tid; i < found; i += kThreads) {
-    const unsigned long long c = cand[i];
-    int rank = 0;
-    for (int j = 0; j < found; ++j) rank += cand[j] > c;
+  // rank them: a pair is smaller than exactly those ahead of it
+  const float m = row_m, ls = row_ls;
+  for (int i = tid; i < found; i += T) {
+    const unsigned long long c = ranked[i];
+    int rank = 0, j = 0;
+#pragma unroll 4
+    for (; j + 1 < found; j += 2) {
+      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&ranked[j]);
+      rank += (o.x > c) + (o.y > c);
+    }
+    if (j < found) rank += ranked[j] > c;
     if (rank < a.top_k) {
       const float x = key_value<F32>((uint32_t)(c >> kIndexBits));
       a.top_idx[r * a.top_k + rank] = kMaxVocab - 1 - (int)(c & (kMaxVocab - 1));
@@ -461,24 +517,25 @@ bc_status check(const void* logits, int32_t f32, int64_t row_stride, int32_t n, 
   return BC_OK;
 }
 
-template <bool F32>
+template <bool F32, int T>
 bc_status launch_logprobs(const LogprobArgs& a, int n, cudaStream_t s) {
-  using L = Logits<F32>;
-  // as many blocks per row as have kPartBytes each
-  int parts = 1;
-  while (parts < kMaxParts && (int64_t)a.vocab * L::kBytes >= 2 * parts * kPartBytes) parts *= 2;
-  if ((int64_t)n * parts > 0x7fffffff) return BC_ERR_UNSUPPORTED;
-  const int pieces = a.vocab / L::kPer, per = (pieces + parts - 1) / parts;
-  const int most = (kMaxVocab / L::kPer + kMaxParts - 1) / kMaxParts * 16;
-  // the opt-in is always that of the largest vocabulary: a setting that followed the call could be lowered under another thread's
-  if (cudaFuncSetAttribute(k_logprobs<F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return BC_ERR_CUDA;
+  if ((int64_t)n * a.parts > 0x7fffffff) return BC_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(n * parts)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = (size_t)per * 16; cfg.stream = s;
+  cfg.gridDim = dim3((unsigned)(n * a.parts)); cfg.blockDim = dim3(T); cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_logprobs<F32>, a) == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+  at[0].val.clusterDim.x = a.parts; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = a.parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k_logprobs<F32, T>, a) == cudaSuccess ? BC_OK : BC_ERR_CUDA;
+}
+template <bool F32>
+bc_status launch_logprobs(LogprobArgs a, int n, cudaStream_t s) {
+  // A row is shared by as many blocks as leave each 8 KB of it and find a place at once.  Blocks of 256 threads, five to an SM; of 512
+  // for shared rows, and for more alternatives than the maxima of 256 threads can bound sharply.
+  const int64_t bytes = (int64_t)a.vocab * Logits<F32>::kBytes;
+  a.parts = 1;
+  while (a.parts < kMaxParts && (int64_t)n * a.parts * 2 <= 2 * 148 && bytes >= a.parts * 2 * 8192) a.parts *= 2;
+  return a.top_k > 128 || a.parts > 1 ? launch_logprobs<F32, 512>(a, n, s) : launch_logprobs<F32, 256>(a, n, s);
 }
 
 }  // namespace
