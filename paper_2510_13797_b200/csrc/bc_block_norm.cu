@@ -43,24 +43,24 @@ struct NormArgs {
   float scale, inv_hidden, eps;
 };
 
-// Sum over the threads of a row, in a fixed order.  `part`: kMaxThreads / 32 floats of shared memory; two barriers when the row has
-// more than one warp.
+// Sum over the threads of a row, in a fixed order.  `part`: kMaxThreads / 32 floats of shared memory that no other sum uses; one barrier
+// when the row has more than one warp.
 __device__ __forceinline__ float row_sum(float v, int warps, float* part) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
   if (warps == 1) return v;
-  const int warp = threadIdx.x >> 5, first = warp / warps * warps;
-  if ((threadIdx.x & 31) == 0) part[warp] = v;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, first = warp / warps * warps;
+  if (lane == 0) part[warp] = v;
   __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < warps; ++i) v += part[first + i];
-  __syncthreads();
-  return v;
+  v = lane < warps ? part[first + lane] : 0.f;
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+  return __shfl_sync(0xffffffffu, v, 0);
 }
 
 template <int K>
 __global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
-  __shared__ float part[kMaxThreads / 32];
+  __shared__ float part[2][kMaxThreads / 32];
   const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
   const int64_t row = (int64_t)blockIdx.x * rows + slot;
   const bool live = row < a.n;                            // the threads of a row past the end stay for the barriers
@@ -84,7 +84,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
     }
-    r1 = rsqrtf(row_sum(sq, a.warps, part) * a.inv_hidden + a.eps);
+    r1 = rsqrtf(row_sum(sq, a.warps, part[0]) * a.inv_hidden + a.eps);
   }
   float sq = 0.f;
 #pragma unroll
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
       for (int i = 0; i < 8; ++i) sq = fmaf(h[i], h[i], sq);
   }
   if (a.y == nullptr) return;
-  const float r2 = rsqrtf(row_sum(sq, a.warps, part) * a.inv_hidden + a.eps);
+  const float r2 = rsqrtf(row_sum(sq, a.warps, part[1]) * a.inv_hidden + a.eps);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int j = j0 + k * per_row;
@@ -131,32 +131,34 @@ struct NormGradArgs {
 
 // The three sums a row needs beside its two squares follow from one pass, since dH is linear in them:
 //     mean(x v dH) with v = s g w_post:   sum(x v a) + r2 (sum(x v b') - r2^2 mean(h' b') sum(x v h')),   b' = w_pre b.
-// One block per SM; a thread copies the pieces it will use of the next rounds' rows (a round: as many rows as the block works on at
-// once) to shared memory, so that three rounds are under way whatever the threads do; no other thread reads them, so they need no
-// barrier.  A thread has the same columns of every row it meets, so the weights' gradients are sums in its registers; after kFold
+// One block per SM.  A thread copies the pieces it will use of the next round's rows (a round: two rows of every slot, whose sums share
+// a barrier; one of rows above 4096 values) to shared memory, so that 80 KB are under way whatever the threads do; no other thread
+// reads them, so they need no barrier.  A thread has the same columns of every row it meets, so the weights' gradients are sums in its registers; after kFold
 // rounds they go to the block's sums in memory and begin again, so that no chain of additions grows with the number of rows but that of
 // the folds.  A second kernel adds the blocks' sums, all in a fixed order.
-constexpr int kFold = 64;
+constexpr int kFold = 32;
 template <int K>
 __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradArgs a) {
-  constexpr int kRing = K == 1 ? 4 : 2;                   // 160 KB for 4096, and for 8192 values a row
-  extern __shared__ __align__(16) uint4 ring[];           // [kRing][x, h', a, b, gate][rows][chunks]
-  __shared__ float part[2][6][kMaxThreads / 32];
+  constexpr int kRing = 2, U = K == 1 ? 2 : 1;            // rounds; rows of a slot in a round: 160 KB for 4096, and for 8192 values a row
+  extern __shared__ __align__(16) uint4 ring[];           // [kRing][U][x, h', a, b, gate][rows][chunks]
+  __shared__ float part[2][U][8][kMaxThreads / 32];        // sums 6 and 7 are not used
   const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp / a.warps * a.warps;
   const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), zero = make_uint4(0, 0, 0, 0);
   const bool weights = a.partial != nullptr, gate_rows = a.gate != nullptr && a.gate_chunks != 0;
   const int operand = rows * a.chunks, place = (2 + (a.dh_out != nullptr) + (a.dy != nullptr) + gate_rows) * operand;
   const int at_a = 2 * operand, at_b = at_a + (a.dh_out ? operand : 0), at_g = at_b + (a.dy ? operand : 0);
-  const int64_t step = (int64_t)gridDim.x * rows;
+  const int64_t step = (int64_t)gridDim.x * rows * U;
   auto ask = [&](int64_t row0, int r) {
-    const int64_t row = row0 + slot;
-    if (row < a.n) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = row0 + u * rows + slot;
+      if (row >= a.n) continue;
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int j = j0 + k * per_row;
         if (j >= a.chunks) continue;
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + r * place + slot * a.chunks + j);
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + (r * U + u) * place + slot * a.chunks + j);
         auto copy = [&](const uint4* from, int at) {
           asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + at * 16), "l"(from + row * a.chunks + j) : "memory");
         };
@@ -169,89 +171,96 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-#pragma unroll
-  for (int r = 0; r < kRing - 1; ++r) ask((int64_t)blockIdx.x * rows + r * step, r);
+  ask((int64_t)blockIdx.x * rows * U, 0);
 
   float dpre[K][8], dpost[K][8], dgate[K][8];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dpre[k][i] = dpost[k][i] = dgate[k][i] = 0.f;
-  int left = kFold, turn = 0, r = 0;
+  int left = kFold, turn = 0;
   bool begun = false;
-  for (int64_t row0 = (int64_t)blockIdx.x * rows; row0 < a.n; row0 += step, turn ^= 1) {
-    const int64_t row = row0 + slot;
-    const bool live = row < a.n;
-    const uint4* in = ring + r * place + slot * a.chunks;
-    ask(row0 + (kRing - 1) * step, r == 0 ? kRing - 1 : r - 1);   // into the place that the last round has used
-    asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
-    float sum[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};        // h'^2, h' b', x^2, x v a, x v b', x v h'
+  for (int64_t row0 = (int64_t)blockIdx.x * rows * U; row0 < a.n; row0 += step, turn ^= 1) {
+    ask(row0 + step, turn ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int j = j0 + k * per_row;
-      if (!live || j >= a.chunks) continue;
-      float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8];
-      unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
-      unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
-      unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+    for (int u = 0; u < U; ++u) {
+      const bool live = row0 + u * rows + slot < a.n;
+      const uint4* in = ring + (turn * U + u) * place + slot * a.chunks;
+      float sum[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};      // h'^2, h' b', x^2, x v a, x v b', x v h'
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float bw = b[i] * w2[i], xv = x[i] * (a.scale * g[i] * w1[i]);
-        sum[0] = fmaf(h[i], h[i], sum[0]); sum[1] = fmaf(h[i], bw, sum[1]); sum[2] = fmaf(x[i], x[i], sum[2]);
-        sum[3] = fmaf(xv, da[i], sum[3]); sum[4] = fmaf(xv, bw, sum[4]); sum[5] = fmaf(xv, h[i], sum[5]);
+      for (int k = 0; k < K; ++k) {
+        const int j = j0 + k * per_row;
+        if (!live || j >= a.chunks) continue;
+        float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8];
+        unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
+        unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
+        unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float bw = b[i] * w2[i], xv = x[i] * (a.scale * g[i] * w1[i]);
+          sum[0] = fmaf(h[i], h[i], sum[0]); sum[1] = fmaf(h[i], bw, sum[1]); sum[2] = fmaf(x[i], x[i], sum[2]);
+          sum[3] = fmaf(xv, da[i], sum[3]); sum[4] = fmaf(xv, bw, sum[4]); sum[5] = fmaf(xv, h[i], sum[5]);
+        }
       }
-    }
-    // Six sums over the lanes: three exchanges of halves leave every lane with one of eight (two are unused), added up over the lanes that
-    // have the same: 4 + 2 + 1 + 2 exchanges instead of 30
-    {
-      const float a0 = lane & 16 ? sum[0] : sum[4], a1 = lane & 16 ? sum[1] : sum[5], a2 = lane & 16 ? sum[2] : 0.f, a3 = lane & 16 ? sum[3] : 0.f;
-      const float k0 = lane & 16 ? sum[4] : sum[0], k1 = lane & 16 ? sum[5] : sum[1], k2 = lane & 16 ? 0.f : sum[2], k3 = lane & 16 ? 0.f : sum[3];
-      const float q0 = k0 + __shfl_xor_sync(0xffffffffu, a0, 16), q1 = k1 + __shfl_xor_sync(0xffffffffu, a1, 16);
-      const float q2 = k2 + __shfl_xor_sync(0xffffffffu, a2, 16), q3 = k3 + __shfl_xor_sync(0xffffffffu, a3, 16);
-      const float p0 = (lane & 8 ? q2 : q0) + __shfl_xor_sync(0xffffffffu, lane & 8 ? q0 : q2, 8);
-      const float p1 = (lane & 8 ? q3 : q1) + __shfl_xor_sync(0xffffffffu, lane & 8 ? q1 : q3, 8);
-      float v = (lane & 4 ? p1 : p0) + __shfl_xor_sync(0xffffffffu, lane & 4 ? p0 : p1, 4);
+      // Six sums over the lanes: three exchanges of halves leave every lane with one of eight (two are not used), added up over the lanes that
+      // have the same: 4 + 2 + 1 + 2 exchanges instead of 30
+      const bool b4 = lane & 16, b3 = lane & 8, b2 = lane & 4;
+      const float q0 = (b4 ? sum[4] : sum[0]) + __shfl_xor_sync(0xffffffffu, b4 ? sum[0] : sum[4], 16);
+      const float q1 = (b4 ? sum[5] : sum[1]) + __shfl_xor_sync(0xffffffffu, b4 ? sum[1] : sum[5], 16);
+      const float q2 = (b4 ? 0.f : sum[2]) + __shfl_xor_sync(0xffffffffu, b4 ? sum[2] : 0.f, 16);
+      const float q3 = (b4 ? 0.f : sum[3]) + __shfl_xor_sync(0xffffffffu, b4 ? sum[3] : 0.f, 16);
+      const float p0 = (b3 ? q2 : q0) + __shfl_xor_sync(0xffffffffu, b3 ? q0 : q2, 8);
+      const float p1 = (b3 ? q3 : q1) + __shfl_xor_sync(0xffffffffu, b3 ? q1 : q3, 8);
+      float v = (b2 ? p1 : p0) + __shfl_xor_sync(0xffffffffu, b2 ? p0 : p1, 4);
       v += __shfl_xor_sync(0xffffffffu, v, 2);
       v += __shfl_xor_sync(0xffffffffu, v, 1);
-      const int which = (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (lane & 4 ? 1 : 0);   // the sum this lane has
-      if ((lane & 3) == 0 && which < 6) part[turn][which][warp] = v;
+      if ((lane & 3) == 0) part[turn][u][lane >> 2][warp] = v;   // bits 4, 3, 2 of the lane: the sum it has
     }
     if (a.warps > 1) __syncthreads();                     // the other half of `part` is written next: one barrier per round
     else __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 6; ++i) {
-      sum[i] = 0.f;
-      for (int w = 0; w < a.warps; ++w) sum[i] += part[turn][i][first + w];
-    }
-    // the means are brought down by one factor r at a time: r^3 alone would vanish for large rows
-    const float r2 = rsqrtf(sum[0] * a.inv_hidden + a.eps), c2 = r2 * (r2 * (r2 * (sum[1] * a.inv_hidden)));
-    const float r1 = a.post ? rsqrtf(sum[2] * a.inv_hidden + a.eps) : 1.f;
-    const float c1 = a.post ? r1 * (r1 * (r1 * ((sum[3] + r2 * sum[4] - c2 * sum[5]) * a.inv_hidden))) : 0.f;
+    for (int u = 0; u < U; ++u) {
+      const int64_t row = row0 + u * rows + slot;
+      const bool live = row < a.n;
+      const uint4* in = ring + (turn * U + u) * place + slot * a.chunks;
+      // the warps' sums: a lane adds every fourth of one of them, two exchanges join the four
+      float v = 0.f;
+      for (int w = lane & 3; w < a.warps; w += 4) v += part[turn][u][lane >> 2][first + w];
+      v += __shfl_xor_sync(0xffffffffu, v, 1);
+      v += __shfl_xor_sync(0xffffffffu, v, 2);
+      float sum[6];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int j = j0 + k * per_row;
-      if (!live || j >= a.chunks) continue;
-      float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8], ox[8], oh[8], og[8];
-      unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
-      unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
-      unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+      for (int i = 0; i < 6; ++i) sum[i] = __shfl_sync(0xffffffffu, v, 4 * i);
+      // the means are brought down by one factor r at a time: r^3 alone would vanish for large rows
+      const float r2 = rsqrtf(sum[0] * a.inv_hidden + a.eps), c2 = r2 * (r2 * (r2 * (sum[1] * a.inv_hidden)));
+      const float r1 = a.post ? rsqrtf(sum[2] * a.inv_hidden + a.eps) : 1.f;
+      const float c1 = a.post ? r1 * (r1 * (r1 * ((sum[3] + r2 * sum[4] - c2 * sum[5]) * a.inv_hidden))) : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float dh = da[i] + fmaf(r2, b[i] * w2[i], -c2 * h[i]);
-        const float u = x[i] * r1, sd = a.scale * dh, du = sd * g[i];
-        oh[i] = dh;
-        ox[i] = fmaf(r1, du * w1[i], -c1 * x[i]);
-        og[i] = sd * (u * w1[i]);
-        dpre[k][i] = fmaf(b[i], h[i] * r2, dpre[k][i]);
-        dpost[k][i] = fmaf(du, u, dpost[k][i]);
-        dgate[k][i] += og[i];
+      for (int k = 0; k < K; ++k) {
+        const int j = j0 + k * per_row;
+        if (!live || j >= a.chunks) continue;
+        float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8], ox[8], oh[8], og[8];
+        unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
+        unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
+        unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float dh = da[i] + fmaf(r2, b[i] * w2[i], -c2 * h[i]);
+          const float t = x[i] * r1, sd = a.scale * dh, du = sd * g[i];
+          oh[i] = dh;
+          ox[i] = fmaf(r1, du * w1[i], -c1 * x[i]);
+          og[i] = sd * (t * w1[i]);
+          dpre[k][i] = fmaf(b[i], h[i] * r2, dpre[k][i]);
+          dpost[k][i] = fmaf(du, t, dpost[k][i]);
+          dgate[k][i] += og[i];
+        }
+        const int64_t at = row * a.chunks + j;
+        __stcs(a.dx + at, pack8(ox));
+        __stcs(a.dh + at, pack8(oh));
+        if (a.dgate) __stcs(a.dgate + at, pack8(og));
       }
-      const int64_t at = row * a.chunks + j;
-      __stcs(a.dx + at, pack8(ox));
-      __stcs(a.dh + at, pack8(oh));
-      if (a.dgate) __stcs(a.dgate + at, pack8(og));
     }
-    if (++r == kRing) r = 0;
     if (weights && (--left == 0 || row0 + step >= a.n)) {
       left = kFold;
       // the block's sums of this slot of rows
@@ -378,7 +387,8 @@ bc_status bc_block_norm_backward(int32_t n, int32_t hidden, const void* x, const
   a.partial = sums ? (float*)workspace : nullptr;
   a.n = n; a.chunks = s.chunks; a.warps = s.warps; a.gate_chunks = gate_stride / 8; a.post = post_norm != 0; a.sum_gate = vector && dgate;
   a.scale = scale; a.inv_hidden = 1.f / (float)hidden; a.eps = eps;
-  const int64_t want = ((int64_t)n + s.rows - 1) / s.rows;
+  const int in_round = s.rows * (s.k == 1 ? 2 : 1);
+  const int64_t want = ((int64_t)n + in_round - 1) / in_round;
   const int blocks = (int)(want < kGradBlocks ? want : kGradBlocks);
   const int place = (2 + (dh_out != nullptr) + (dy != nullptr) + (gate && !vector)) * s.rows * s.chunks * 16;   // bytes of a round's rows
   auto* kernel = s.k == 1 ? k_block_norm_grad<1> : k_block_norm_grad<2>;
