@@ -31,6 +31,46 @@ __device__ __forceinline__ uint4 pack8(const float* f) {
   return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
+// Pairs of fp32 numbers in one register pair: one instruction for both.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 both(float a) { return pair(a, a); }
+__device__ __forceinline__ void split(F2 v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum_of(F2 v) {
+  float a, b;
+  split(v, &a, &b);
+  return a + b;
+}
+__device__ __forceinline__ void unpack8(const uint4& v, F2* f) {
+  f[0] = pair(bf_lo(v.x), bf_hi(v.x)); f[1] = pair(bf_lo(v.y), bf_hi(v.y));
+  f[2] = pair(bf_lo(v.z), bf_hi(v.z)); f[3] = pair(bf_lo(v.w), bf_hi(v.w));
+}
+__device__ __forceinline__ uint32_t pack_bf16(F2 v) {
+  float a, b;
+  split(v, &a, &b);
+  return pack_bf16(a, b);
+}
+__device__ __forceinline__ uint4 pack8(const F2* f) { return make_uint4(pack_bf16(f[0]), pack_bf16(f[1]), pack_bf16(f[2]), pack_bf16(f[3])); }
+
 // A row belongs to `warps` warps of a block (all of it to one warp for up to 256 elements), chunk j of 8 elements to thread
 // j % (32 warps) of them; a block works on blockDim / (32 warps) rows at a time.
 struct NormArgs {
@@ -139,8 +179,8 @@ struct NormGradArgs {
 constexpr int kFold = 32;
 template <int K>
 __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradArgs a) {
-  constexpr int kRing = 2, U = K == 1 ? 2 : 1;            // rounds; rows of a slot in a round: 160 KB for 4096, and for 8192 values a row
-  extern __shared__ __align__(16) uint4 ring[];           // [kRing][U][x, h', a, b, gate][rows][chunks]
+  constexpr int U = K == 1 ? 2 : 1;                       // rows of a slot in a round: two rounds of 4096, or 8192, values a row take 160 KB
+  extern __shared__ __align__(16) uint4 ring[];           // [2][U][x, h', a, b, gate][rows][chunks]
   __shared__ float part[2][U][8][kMaxThreads / 32];        // sums 6 and 7 are not used
   const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp / a.warps * a.warps;
@@ -173,11 +213,28 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
   };
   ask((int64_t)blockIdx.x * rows * U, 0);
 
-  float dpre[K][8], dpost[K][8], dgate[K][8];
+  F2 dpre[K][4], dpost[K][4], dgate[K][4];
 #pragma unroll
   for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dpre[k][i] = dpost[k][i] = dgate[k][i] = 0.f;
+    for (int i = 0; i < 4; ++i) dpre[k][i] = dpost[k][i] = dgate[k][i] = both(0.f);
+  // The columns' numbers: the weights and a vector's gate, times the scale.  Rows up to 4096 values have them in registers; for wider ones
+  // there is no room beside the sums, and they come from the first-level cache each time
+  struct Columns {
+    F2 post[4], pre[4], gate[4];
+  };
+  auto columns = [&](int j) {
+    Columns c;
+    const bool in = j < a.chunks;
+    unpack8(in && a.post && a.post_weight ? a.post_weight[j] : ones, c.post);
+    unpack8(in && a.pre_weight ? a.pre_weight[j] : ones, c.pre);
+    unpack8(in && a.gate && !gate_rows ? a.gate[j] : ones, c.gate);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c.gate[i] = mul2(c.gate[i], both(a.scale));
+    return c;
+  };
+  Columns kept;
+  if (K == 1) kept = columns(j0);
   int left = kFold, turn = 0;
   bool begun = false;
   for (int64_t row0 = (int64_t)blockIdx.x * rows * U; row0 < a.n; row0 += step, turn ^= 1) {
@@ -187,22 +244,29 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
     for (int u = 0; u < U; ++u) {
       const bool live = row0 + u * rows + slot < a.n;
       const uint4* in = ring + (turn * U + u) * place + slot * a.chunks;
-      float sum[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};      // h'^2, h' b', x^2, x v a, x v b', x v h'
+      F2 s2[6];                                           // h'^2, h' b', x^2, x v a, x v b', x v h'
+#pragma unroll
+      for (int i = 0; i < 6; ++i) s2[i] = both(0.f);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int j = j0 + k * per_row;
         if (!live || j >= a.chunks) continue;
-        float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8];
+        const Columns c = K == 1 ? kept : columns(j);
+        F2 x[4], h[4], da[4], b[4], g[4];
         unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
-        unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
-        unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+        if (gate_rows) unpack8(in[at_g + j], g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float bw = b[i] * w2[i], xv = x[i] * (a.scale * g[i] * w1[i]);
-          sum[0] = fmaf(h[i], h[i], sum[0]); sum[1] = fmaf(h[i], bw, sum[1]); sum[2] = fmaf(x[i], x[i], sum[2]);
-          sum[3] = fmaf(xv, da[i], sum[3]); sum[4] = fmaf(xv, bw, sum[4]); sum[5] = fmaf(xv, h[i], sum[5]);
+        for (int i = 0; i < 4; ++i) {
+          const F2 bw = mul2(b[i], c.pre[i]);
+          F2 xv = mul2(x[i], mul2(c.gate[i], c.post[i]));
+          if (gate_rows) xv = mul2(xv, g[i]);
+          s2[0] = fma2(h[i], h[i], s2[0]); s2[1] = fma2(h[i], bw, s2[1]); s2[2] = fma2(x[i], x[i], s2[2]);
+          s2[3] = fma2(xv, da[i], s2[3]); s2[4] = fma2(xv, bw, s2[4]); s2[5] = fma2(xv, h[i], s2[5]);
         }
       }
+      float sum[6];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) sum[i] = sum_of(s2[i]);
       // Six sums over the lanes: three exchanges of halves leave every lane with one of eight (two are not used), added up over the lanes that
       // have the same: 4 + 2 + 1 + 2 exchanges instead of 30
       const bool b4 = lane & 16, b3 = lane & 8, b2 = lane & 4;
@@ -240,20 +304,23 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
       for (int k = 0; k < K; ++k) {
         const int j = j0 + k * per_row;
         if (!live || j >= a.chunks) continue;
-        float x[8], h[8], da[8], b[8], g[8], w1[8], w2[8], ox[8], oh[8], og[8];
+        const Columns c = K == 1 ? kept : columns(j);
+        F2 x[4], h[4], da[4], b[4], g[4], ox[4], oh[4], og[4];
         unpack8(in[j], x); unpack8(in[operand + j], h); unpack8(a.dh_out ? in[at_a + j] : zero, da); unpack8(a.dy ? in[at_b + j] : zero, b);
-        unpack8(gate_rows ? in[at_g + j] : (a.gate ? a.gate[j] : ones), g);
-        unpack8(a.post && a.post_weight ? a.post_weight[j] : ones, w1); unpack8(a.pre_weight ? a.pre_weight[j] : ones, w2);
+        if (gate_rows) unpack8(in[at_g + j], g);
+        const F2 r1_2 = both(r1), r2_2 = both(r2), c1_2 = both(-c1), c2_2 = both(-c2), scale2 = both(a.scale);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float dh = da[i] + fmaf(r2, b[i] * w2[i], -c2 * h[i]);
-          const float t = x[i] * r1, sd = a.scale * dh, du = sd * g[i];
+        for (int i = 0; i < 4; ++i) {
+          const F2 br = mul2(b[i], r2_2), dh = fma2(br, c.pre[i], fma2(h[i], c2_2, da[i]));
+          const F2 t = mul2(x[i], r1_2), tw = mul2(t, c.post[i]);
+          F2 du = mul2(dh, c.gate[i]);
+          if (gate_rows) du = mul2(du, g[i]);
           oh[i] = dh;
-          ox[i] = fmaf(r1, du * w1[i], -c1 * x[i]);
-          og[i] = sd * (t * w1[i]);
-          dpre[k][i] = fmaf(b[i], h[i] * r2, dpre[k][i]);
-          dpost[k][i] = fmaf(du, t, dpost[k][i]);
-          dgate[k][i] += og[i];
+          ox[i] = fma2(mul2(du, c.post[i]), r1_2, mul2(x[i], c1_2));
+          og[i] = mul2(mul2(dh, scale2), tw);
+          dpre[k][i] = fma2(br, h[i], dpre[k][i]);
+          dpost[k][i] = fma2(du, t, dpost[k][i]);
+          dgate[k][i] = add2(dgate[k][i], og[i]);
         }
         const int64_t at = row * a.chunks + j;
         __stcs(a.dx + at, pack8(ox));
@@ -272,9 +339,10 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
 #pragma unroll
         for (int t = 0; t < 3; ++t) {
           if ((t == 1 && !a.post) || (t == 2 && !a.sum_gate)) continue;
-          float* acc = t == 0 ? dpre[k] : (t == 1 ? dpost[k] : dgate[k]);
+          F2* acc = t == 0 ? dpre[k] : (t == 1 ? dpost[k] : dgate[k]);
           float4* to = reinterpret_cast<float4*>(mine + ((int64_t)t * a.chunks + j) * 8);
-          float4 lo = make_float4(acc[0], acc[1], acc[2], acc[3]), hi = make_float4(acc[4], acc[5], acc[6], acc[7]);
+          float4 lo, hi;
+          split(acc[0], &lo.x, &lo.y); split(acc[1], &lo.z, &lo.w); split(acc[2], &hi.x, &hi.y); split(acc[3], &hi.z, &hi.w);
           if (begun) {
             const float4 l = to[0], u = to[1];
             lo.x += l.x; lo.y += l.y; lo.z += l.z; lo.w += l.w;
@@ -282,7 +350,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm_grad(const NormGradA
           }
           to[0] = lo; to[1] = hi;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+          for (int i = 0; i < 4; ++i) acc[i] = both(0.f);
         }
       }
       begun = true;
