@@ -23,14 +23,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&p);
 }
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-  f[0] = bf_lo(v.x); f[1] = bf_hi(v.x); f[2] = bf_lo(v.y); f[3] = bf_hi(v.y);
-  f[4] = bf_lo(v.z); f[5] = bf_hi(v.z); f[6] = bf_lo(v.w); f[7] = bf_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-}
-
 // Pairs of fp32 numbers in one register pair: one instruction for both.
 typedef unsigned long long F2;
 __device__ __forceinline__ F2 pair(float a, float b) {
@@ -99,13 +91,13 @@ __device__ __forceinline__ float row_sum(float v, int warps, float* part) {
 }
 
 template <int K>
-__global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, K == 1 ? 4 : 2) k_block_norm(const NormArgs a) {
   __shared__ float part[2][kMaxThreads / 32];
   const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
   const int64_t row = (int64_t)blockIdx.x * rows + slot;
   const bool live = row < a.n;                            // the threads of a row past the end stay for the barriers
   const uint4 ones = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), zero = make_uint4(0, 0, 0, 0);
-  uint4 xs[K], hs[K], gs[K];
+  uint4 xs[K], hs[K], gs[K], w1[K], w2[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int j = j0 + k * per_row;
@@ -113,46 +105,47 @@ __global__ void __launch_bounds__(kMaxThreads) k_block_norm(const NormArgs a) {
     xs[k] = in ? __ldcs(a.x + row * a.chunks + j) : zero;
     hs[k] = in ? __ldcs(a.h + row * a.chunks + j) : zero;
     gs[k] = in && a.gate ? a.gate[row * a.gate_chunks + j] : ones;
+    // asked for here, so that they do not wait behind the sums
+    w1[k] = in && a.post && a.post_weight ? a.post_weight[j] : ones;
+    w2[k] = in && a.y && a.pre_weight ? a.pre_weight[j] : ones;
   }
   float r1 = 1.f;
   if (a.post) {
-    float sq = 0.f;
+    F2 sq = both(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      float x[8];
+      F2 x[4];
       unpack8(xs[k], x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
+      for (int i = 0; i < 4; ++i) sq = fma2(x[i], x[i], sq);
     }
-    r1 = rsqrtf(row_sum(sq, a.warps, part[0]) * a.inv_hidden + a.eps);
+    r1 = rsqrtf(row_sum(sum_of(sq), a.warps, part[0]) * a.inv_hidden + a.eps);
   }
-  float sq = 0.f;
+  F2 sq = both(0.f);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int j = j0 + k * per_row;
-    float x[8], h[8], g[8], w[8];
-    unpack8(xs[k], x); unpack8(hs[k], h); unpack8(gs[k], g);
-    unpack8(a.post && a.post_weight && j < a.chunks ? a.post_weight[j] : ones, w);
+    F2 x[4], h[4], g[4], w[4];
+    unpack8(xs[k], x); unpack8(hs[k], h); unpack8(gs[k], g); unpack8(w1[k], w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = fmaf(a.scale * g[i], x[i] * r1 * w[i], h[i]);
+    for (int i = 0; i < 4; ++i) h[i] = fma2(mul2(g[i], both(a.scale)), mul2(mul2(x[i], both(r1)), w[i]), h[i]);
     hs[k] = pack8(h);
     if (live && j < a.chunks) a.h_out[row * a.chunks + j] = hs[k];
     unpack8(hs[k], h);                                    // the norm sees the stream as it is stored
     if (j < a.chunks)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sq = fmaf(h[i], h[i], sq);
+      for (int i = 0; i < 4; ++i) sq = fma2(h[i], h[i], sq);
   }
   if (a.y == nullptr) return;
-  const float r2 = rsqrtf(row_sum(sq, a.warps, part[1]) * a.inv_hidden + a.eps);
+  const float r2 = rsqrtf(row_sum(sum_of(sq), a.warps, part[1]) * a.inv_hidden + a.eps);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int j = j0 + k * per_row;
     if (live && j < a.chunks) {
-      float h[8], w[8];
-      unpack8(hs[k], h);
-      unpack8(a.pre_weight ? a.pre_weight[j] : ones, w);
+      F2 h[4], w[4];
+      unpack8(hs[k], h); unpack8(w2[k], w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = h[i] * r2 * w[i];
+      for (int i = 0; i < 4; ++i) h[i] = mul2(mul2(h[i], both(r2)), w[i]);
       a.y[row * a.chunks + j] = pack8(h);
     }
   }

@@ -10,9 +10,9 @@
 // Forward: one pass over the row in memory, in rounds of four 16-byte pieces per thread; five blocks of 256 threads on an SM cover
 // each other's loads and searches.  A thread folds its pieces into a running (reference, s, t).  A block has a row, or, where rows are few, a cluster of blocks share it.
 // The alternatives come from the same pass.  After its first round a block knows a bound that K elements reach at least, from its
-// threads' maxima (below); of the later rounds it notes the pieces that hold an element that reaches it, a few in a hundred.  At the
+// threads' maxima (below); from then on it notes the pieces that hold an element that reaches it, a few in a hundred.  At the
 // end the bound is that of the maxima over everything, and the elements that still reach it, a hundred or two for K = 100, are
-// taken from the noted pieces and the first round's, which are read again, and ranked by counting.  Where more reach it (many
+// taken from the noted pieces, which are read again, and ranked by counting.  Where more reach it (many
 // equal logits, ascending rows), the blocks find the K-th largest (value, index) pair bit by bit, counting over the row.
 #include <cooperative_groups.h>
 
@@ -249,7 +249,17 @@ __global__ void __launch_bounds__(T, 1280 / T) k_logprobs(const LogprobArgs a) {
       }
     }
     if (a.top_k > 0 && noting) {
-      if (first > 0 && reach != 0) {
+      // a better bound is worth its barriers after the first and after the fourth round (after every power of two: 178 us against 169)
+      if (first == 0 || first == 12 * T) {
+        uint32_t key, none;
+        bounds_of_maxima(a.top_k, 0, &key, &none);
+        least = value_of(key);
+        reach = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (first + k * T + tid < pieces) reach |= (L::top(v[k]) < least ? 0u : 1u) << k;
+      }
+      if (reach != 0) {
         int at = atomicAdd(&n_noted, __popc(reach));
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -257,13 +267,6 @@ __global__ void __launch_bounds__(T, 1280 / T) k_logprobs(const LogprobArgs a) {
             if (at < kNoted) noted[at] = first + k * T + tid;
             ++at;
           }
-      }
-      // a better bound is worth its barriers after the first, second, fourth, eighth, ... round
-      const int done = first / (4 * T) + 1;
-      if ((done & (done - 1)) == 0 && first + 4 * T < pieces) {
-        uint32_t key, none;
-        bounds_of_maxima(a.top_k, 0, &key, &none);
-        least = value_of(key);
       }
     }
   }
@@ -338,17 +341,18 @@ __global__ void __launch_bounds__(T, 1280 / T) k_logprobs(const LogprobArgs a) {
   bound = max(bound, own);
   int* const total_ranked = parts > 1 ? cluster.map_shared_rank(&n_ranked, 0) : &n_ranked;
   unsigned long long* const to = parts > 1 ? cluster.map_shared_rank(ranked, 0) : ranked;
-  // calls f(pair) for the elements of this thread in pieces that hold one above `low`: in the first round's and those noted, or in all
+  // calls f(pair) for the elements of this thread in pieces that hold one above `low`: in those noted, or in all
   const bool complete = n_noted <= kNoted;
   auto each = [&](float low, bool everything, auto f) {
-    const int again = everything || !noting ? pieces : 4 * T, all = everything ? again : again + n_noted;
+    const bool scan = everything || !noting;
+    const int all = scan ? pieces : n_noted;
     for (int j0 = 0; j0 < all; j0 += 4 * T) {              // four loads at once
       uint4 w[4];
       int i[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int j = j0 + k * T + tid;
-        i[k] = j < again ? j : (j < all ? noted[j - again] : -1);
+        i[k] = j >= all ? -1 : (scan ? j : noted[j]);
         if (i[k] >= 0) w[k] = __ldg(src + i[k]);
       }
 #pragma unroll
