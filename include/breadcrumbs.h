@@ -630,7 +630,7 @@ BC_API bc_status bc_mask_attn_status(const void* workspace, int32_t n_seqs, int3
 
 /* bc_mask_attn_forward that also writes what its gradient needs: lse_tok [sum T, q_heads], lse_beacon [sum nb, q_heads], fp32, the
  * natural logarithm of every row's sum of exp(sm_scale * <q, K_j>) over the keys it sees.  Everything else is as there, the
- * outputs included. */
+ * outputs included; inside a stream capture the call is refused (BC_ERR_UNSUPPORTED). */
 BC_API bc_status bc_mask_attn_forward_lse(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,
                                           const int32_t* cu_prompt, const int32_t* cu_tokens, const void* prompt_k,
                                           const void* prompt_v, const void* tok_q, const void* tok_k, const void* tok_v,
@@ -647,8 +647,8 @@ BC_API bc_status bc_mask_attn_forward_lse(int32_t n_seqs, int32_t q_heads, int32
  * weight 0 on it); nothing spreads from one trajectory to another.
  * cu_prompt, cu_tokens: HOST int32 [n_seqs + 1] as in the forward call, beginning with 0.  workspace: device memory of at least
  * bc_mask_attn_backward_query_bytes bytes, 256-byte aligned, one call at a time: work lists, row statistics, and the partial sums of
- * keys that many rows see.  Asynchronous on `stream`, up to four launches; the host arrays are read before the call returns, so not
- * inside a stream capture.  A bounded device-side wait that expires is reported by bc_mask_attn_backward_status as
+ * keys that many rows see.  Asynchronous on `stream`, up to four launches; the host arrays are read before the call returns; inside
+ * a stream capture the call is refused (BC_ERR_UNSUPPORTED).  A bounded device-side wait that expires is reported by bc_mask_attn_backward_status as
  * BC_ERR_TIMEOUT (the gradients are then incomplete); bc_mask_attn_backward_set_wait_limit sets the waits' poll limit
  * (process-wide; 0 = the default) as bc_mask_attn_set_wait_limit does for the forward call. */
 BC_API bc_status bc_mask_attn_backward_query_bytes(int32_t n_seqs, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t c,

@@ -25,7 +25,7 @@ namespace {
 constexpr int kThreads = 256;         // of the gradient's blocks
 constexpr int kMaxTop = 256;          // alternatives per row; no more than a forward block has threads
 constexpr int kMaxParts = 8;          // blocks that share a row
-constexpr int kNoted = 3072;          // pieces that a block notes at most
+constexpr int kNoted = 3200;          // pieces that a block notes at most
 constexpr int kRanked = 1024;         // elements that are ranked at most
 constexpr int kMaxVocab = 262144;
 constexpr int kIndexBits = 18;        // of a vocabulary index

@@ -1199,6 +1199,10 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
       return BC_ERR_INVALID_ARG;
     const int G = q_heads / kv_heads;
     cudaStream_t s = (cudaStream_t)stream;
+    // a captured copy would read the lists again at every replay, when they are gone
+    cudaStreamCaptureStatus capture;
+    if (cudaStreamIsCapturing(s, &capture) != cudaSuccess) return BC_ERR_CUDA;
+    if (capture != cudaStreamCaptureStatusNone) return BC_ERR_UNSUPPORTED;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     if (!encode_tiled()) return BC_ERR_CUDA;
     // pageable host memory: it has been staged when the copy returns
