@@ -200,6 +200,13 @@ def _new(like, shape, dtype, other):
     return t
 
 
+def _alike(t, other, dtype=None):
+    """_new in the shape of the contiguous tensor t, and its type unless another is given; in less time where `other` is None."""
+    if other is None:
+        return torch.empty_like(t, dtype=dtype)
+    return _new(t, t.shape, dtype or t.dtype, other)
+
+
 class Cache:
     """Owns the three device buffers (as torch tensors) and the library handle."""
 
@@ -549,10 +556,11 @@ def bc_token_logprobs(logits, targets=None, top_k=0, stream=None):
     where, f32 = "bc_token_logprobs", torch.float32
     n, vocab, row_stride, wide = _logit_rows(logits, where)
     dev, s, other = _on(where, logits, ((targets, torch.int64, (n,)),), stream)
-    logprob = None if targets is None else _new(logits, n, f32, other)
-    entropy = _new(logits, n, f32, other)
+    logprob = None if targets is None else _alike(targets, other, f32)
+    entropy = _new(logits, n, f32, other) if logprob is None else _alike(logprob, other)
     stats = _new(logits, (n, 2), f32, other)
-    idx, top = (_new(logits, (n, top_k), torch.int32, other), _new(logits, (n, top_k), f32, other)) if top_k > 0 else (None, None)
+    idx = _new(logits, (n, top_k), torch.int32, other) if top_k > 0 else None
+    top = _alike(idx, other, f32) if top_k > 0 else None
     _call(where, dev, lib().bc_token_logprobs, logits.data_ptr(), wide, row_stride, n, vocab, _at(targets), top_k, _at(logprob),
           entropy.data_ptr(), stats.data_ptr(), _at(idx), _at(top), s)
     return logprob, entropy, stats, idx, top
@@ -597,8 +605,8 @@ def bc_block_norm(x, h, gate, post_weight, pre_weight, eps, scale=1.0, post_norm
     n, hidden, gate_stride, tensors = _block_norm_tensors(x, h, gate, post_weight, pre_weight, where)
     dev, s, other = _on(where, x, tensors + ((h_out, bf16, (n, hidden)), (y, bf16, (n, hidden))), stream)
     _require(h is not None, where)
-    ho = _new(x, (n, hidden), bf16, other) if h_out is None else h_out
-    yo = _new(x, (n, hidden), bf16, other) if y is None and want_y else y
+    ho = _alike(x, other) if h_out is None else h_out
+    yo = _alike(x, other) if y is None and want_y else y
     _call(where, dev, lib().bc_block_norm, n, hidden, x.data_ptr(), h.data_ptr(), _at(gate), gate_stride, 1 if post_norm else 0,
           _at(post_weight), _at(pre_weight), scale, eps, ho.data_ptr(), _at(yo), s)
     return ho, yo
@@ -613,8 +621,8 @@ def bc_block_norm_backward(x, h_out, gate, post_weight, pre_weight, eps, scale, 
     n, hidden, gate_stride, tensors = _block_norm_tensors(x, h_out, gate, post_weight, pre_weight, where)
     dev, s, other = _on(where, x, tensors + ((dh_out, bf16, (n, hidden)), (dy, bf16, (n, hidden))), stream)
     _require(h_out is not None, where)
-    dx, dh = _new(x, (n, hidden), bf16, other), _new(x, (n, hidden), bf16, other)
-    dgate = _new(x, (n, hidden), bf16, other) if gate_stride else None
+    dx, dh = _alike(x, other), _alike(x, other)
+    dgate = _alike(x, other) if gate_stride else None
     ws, size, sums = None, C.c_size_t(), (None, None, None)
     if weight_grads:
         _check(lib().bc_block_norm_query_bytes(hidden, C.byref(size)), "bc_block_norm_query_bytes")
@@ -631,19 +639,21 @@ def bc_block_norm_backward(x, h_out, gate, post_weight, pre_weight, eps, scale, 
 
 def _mask_inputs(where, prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k, beacon_v):
     """Head counts, prefix sums, the number of beacons, and the inputs with their dtypes and shapes."""
-    _require(tok_q is not None and tok_k is not None and tok_q.dim() == 3 and tok_k.dim() == 3 and len(prompt_lens) == len(token_lens) and len(token_lens) > 0 and c >= 1, where)
+    _require(tok_q is not None and tok_k is not None and tok_q.dim() == 3 and tok_k.dim() == 3 and len(prompt_lens) == len(token_lens) > 0 and
+             c >= 1, where)
     n, bf16 = len(prompt_lens), torch.bfloat16
     q_heads, kv_heads, head_dim = tok_q.shape[1], tok_k.shape[1], tok_q.shape[2]
     cu = [(C.c_int32 * (n + 1))(0, *itertools.accumulate(lens)) for lens in (prompt_lens, token_lens)]
     total_b = sum(t // c for t in token_lens) if c > 1 else 0
-    q, kv = (lambda rows: (rows, q_heads, head_dim)), (lambda rows: (rows, kv_heads, head_dim))
     P, T = cu[0][n], cu[1][n]
-    none = lambda t, rows: None if t is None and rows == 0 else t
-    need = ((none(prompt_k, P), kv(P)), (none(prompt_v, P), kv(P)), (tok_q, q(T)), (tok_k, kv(T)), (tok_v, kv(T)), (none(beacon_q, total_b), q(total_b)),
-            (none(beacon_k, total_b), kv(total_b)), (none(beacon_v, total_b), kv(total_b)))
-    for t, shape in need:
-        _require(t is not None or shape[0] == 0, where)
-    return n, q_heads, kv_heads, head_dim, cu, total_b, tuple((t, bf16, shape) for t, shape in need)
+    prompt, key, beacon, query, beacon_query = [(rows, heads, head_dim) for rows, heads in
+                                                ((P, kv_heads), (T, kv_heads), (total_b, kv_heads), (T, q_heads), (total_b, q_heads))]
+    inputs = ((prompt_k, bf16, prompt), (prompt_v, bf16, prompt), (tok_q, bf16, query), (tok_k, bf16, key), (tok_v, bf16, key),
+              (beacon_q, bf16, beacon_query), (beacon_k, bf16, beacon), (beacon_v, bf16, beacon))
+    for t, _, shape in inputs:
+        if t is None and shape[0] != 0:
+            raise BreadcrumbsError(BC_ERR_INVALID_ARG, where)
+    return n, q_heads, kv_heads, head_dim, cu, total_b, inputs
 
 
 def bc_mask_attn_forward_lse(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k, beacon_v, sm_scale,
@@ -657,7 +667,7 @@ def bc_mask_attn_forward_lse(prompt_lens, token_lens, c, prompt_k, prompt_v, tok
     size = C.c_size_t()
     _check(lib().bc_mask_attn_query_bytes(n, hq, hk, d, cu[0][n], cu[1][n], total_b, C.byref(size)), "bc_mask_attn_query_bytes")
     ws = _new(tok_q, size.value, torch.uint8, other)
-    out = [_new(tok_q, (rows, hq, d), tok_q.dtype, other) for rows in (cu[1][n], total_b)]
+    out = [_alike(tok_q, other), _new(tok_q, (total_b, hq, d), tok_q.dtype, other)]
     lse = [_new(tok_q, (rows, hq), torch.float32, other) for rows in (cu[1][n], total_b)]
     _call(where, dev, lib().bc_mask_attn_forward_lse, n, hq, hk, d, c, cu[0], cu[1], *[_at(t) for t, _, _ in inputs], _at(out[0]), _at(out[1]),
           _at(lse[0]), _at(lse[1]), sm_scale, _at(ws), size.value, s)
@@ -677,15 +687,15 @@ def bc_mask_attn_backward(prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q,
     n, hq, hk, d, cu, total_b, inputs = _mask_inputs(where, prompt_lens, token_lens, c, prompt_k, prompt_v, tok_q, tok_k, tok_v, beacon_q, beacon_k,
                                                      beacon_v)
     T = cu[1][n]
-    _require(all(t is not None for t in (out_tok, lse_tok, d_out_tok) if T) and all(t is not None for t in (out_beacon, lse_beacon, d_out_beacon) if total_b),
-             where)
+    _require(not (T and (out_tok is None or lse_tok is None or d_out_tok is None)) and
+             not (total_b and (out_beacon is None or lse_beacon is None or d_out_beacon is None)), where)
     more = ((out_tok, bf16, (T, hq, d)), (out_beacon, bf16, (total_b, hq, d)), (lse_tok, f32, (T, hq)), (lse_beacon, f32, (total_b, hq)),
             (d_out_tok, bf16, (T, hq, d)), (d_out_beacon, bf16, (total_b, hq, d)))
     dev, s, other = _on(where, tok_q, inputs + more, stream)
     size = C.c_size_t()
     _check(lib().bc_mask_attn_backward_query_bytes(n, hq, hk, d, c, cu[0], cu[1], C.byref(size)), "bc_mask_attn_backward_query_bytes")
     ws = _new(tok_q, size.value, torch.uint8, other)
-    grads = [_new(tok_q, shape, bf16, other) for _, _, shape in inputs]
+    grads = [_new(tok_q, shape, bf16, other) if t is None else _alike(t, other) for t, _, shape in inputs]
     _call(where, dev, lib().bc_mask_attn_backward, n, hq, hk, d, c, cu[0], cu[1], *[_at(t) for t, _, _ in inputs + more], *[_at(t) for t in grads],
           sm_scale, _at(ws), size.value, s)
     if check:
