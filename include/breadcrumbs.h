@@ -643,7 +643,8 @@ BC_API bc_status bc_mask_attn_forward_lse(int32_t n_seqs, int32_t q_heads, int32
  * like the inputs and all written whole (a prompt's K/V summed over every row of the trajectory, a KV head's over its query heads).
  * Limits as for the forward call; inputs 16-byte aligned, the gradients 32-byte aligned and not overlapping anything else; arrays
  * without rows may be NULL.  fp32 accumulation; softmax weights and score gradients rounded to bf16 before the second products; no
- * atomic additions, results are reproducible.  Within one trajectory all inputs must be finite (rows that do not see an entry have
+ * atomic additions: the same call gives the same bits (how the sums over many rows are cut depends on all the lengths of the call, so
+ * that a trajectory's K/V gradients may differ in the last bits in another batch).  Within one trajectory all inputs must be finite (rows that do not see an entry have
  * weight 0 on it); nothing spreads from one trajectory to another.
  * cu_prompt, cu_tokens: HOST int32 [n_seqs + 1] as in the forward call, beginning with 0.  workspace: device memory of at least
  * bc_mask_attn_backward_query_bytes bytes, 256-byte aligned, one call at a time: work lists, row statistics, and the partial sums of

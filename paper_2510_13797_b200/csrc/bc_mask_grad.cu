@@ -985,28 +985,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_dq(const GradArgs a, const __gr
   }
 }
 
-// Adds the pieces of the split items in order: one block per item and head, of dK or dV, and 32 keys; a thread has 16 columns of a key.
+// Adds the pieces of the split items in order: one block per item and head, of dK or dV, 32 keys and half of the columns; a thread has
+// 8 columns of a key, and the loads of four pieces under way at once.
+constexpr int kJoinBlocks = 2 * (kTile / 32) * 2;
 __global__ void __launch_bounds__(256) k_join(const JoinItem* __restrict__ items, const GradArgs a) {
   const JoinItem im = items[blockIdx.x / a.Hkv];
-  const int kvh = blockIdx.x % a.Hkv, which = blockIdx.y & 1, key = (int)(blockIdx.y >> 1) * 32 + (int)(threadIdx.x & 31), col = (int)(threadIdx.x >> 5) * 16;
+  const int kvh = blockIdx.x % a.Hkv, which = blockIdx.y & 1, key = (int)(blockIdx.y >> 2) * 32 + (int)(threadIdx.x & 31);
+  const int col = (int)(blockIdx.y >> 1 & 1) * 64 + (int)(threadIdx.x >> 5) * 8;
   const int seg_len = im.seg == 0 ? im.s.P : (im.seg == 1 ? im.s.nb : im.s.T);
   if (im.k0 + key >= seg_len) return;
-  float4 t[4] = {};
-  for (int p = 0; p < im.count; ++p) {
-    const float4* from = reinterpret_cast<const float4*>(a.partial) + (((((int64_t)im.first + p) * a.Hkv + kvh) * 2 + which) * (kD / 4) + col / 4) * kTile + key;
+  float4 t[2] = {};
+  const int64_t step = (int64_t)a.Hkv * 2 * (kD / 4) * kTile;      // from one piece to the next
+  const float4* from = reinterpret_cast<const float4*>(a.partial) + ((((int64_t)im.first * a.Hkv + kvh) * 2 + which) * (kD / 4) + col / 4) * kTile + key;
+#pragma unroll 4
+  for (int p = 0; p < im.count; ++p, from += step) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const float4 v = __ldcs(from + i * kTile);
       t[i].x += v.x; t[i].y += v.y; t[i].z += v.z; t[i].w += v.w;
     }
   }
   const float f = which == 0 ? 1.f : a.scale;
   const int row = (im.seg == 0 ? im.s.prompt_row : (im.seg == 1 ? im.s.bea_row : im.s.tok_row)) + im.k0 + key;
-  uint4* dst = reinterpret_cast<uint4*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + col);
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    dst[i] = make_uint4(pack2(t[2 * i].x * f, t[2 * i].y * f), pack2(t[2 * i].z * f, t[2 * i].w * f), pack2(t[2 * i + 1].x * f, t[2 * i + 1].y * f),
-                        pack2(t[2 * i + 1].z * f, t[2 * i + 1].w * f));
+  *reinterpret_cast<uint4*>((which == 0 ? a.dv : a.dk)[im.seg] + ((int64_t)row * a.Hkv + kvh) * kD + col) =
+      make_uint4(pack2(t[0].x * f, t[0].y * f), pack2(t[0].z * f, t[0].w * f), pack2(t[1].x * f, t[1].y * f), pack2(t[1].z * f, t[1].w * f));
 }
 
 bool map_3d(CUtensorMap* m, const void* base, int heads, int64_t rows, int box_heads, int box_rows) {
@@ -1018,7 +1020,7 @@ bool map_3d(CUtensorMap* m, const void* base, int heads, int64_t rows, int box_h
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The work lists, and where everything is in the workspace.
+// The work lists (in the order of work, where that is asked for), and where everything is in the workspace.
 struct Plan {
   std::vector<KvItem> kv;
   std::vector<QItem> q;
@@ -1031,6 +1033,7 @@ struct Plan {
 inline size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
 constexpr int kSms = 148;
 constexpr int kMinPiece = 12;   // query tiles: a piece's partial sums cost about two tiles' time
+constexpr int kLeastPiece = 3;  // the same where SMs are idle otherwise
 
 // Longest first: a counting sort, in the order of the list among equals.
 template <class Item, class Length>
@@ -1045,7 +1048,8 @@ void longest_first(std::vector<Item>* items, Length length) {
   items->swap(sorted);
 }
 
-bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, const int32_t* cu_prompt, const int32_t* cu_tokens, Plan* p) {
+bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, const int32_t* cu_prompt, const int32_t* cu_tokens, bool ordered,
+                    Plan* p) {
   if (n_seqs < 1 || !cu_prompt || !cu_tokens || c < 1 || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads) return BC_ERR_INVALID_ARG;
   if (head_dim != kD || q_heads / kv_heads > 16) return BC_ERR_UNSUPPORTED;
   const int G = q_heads / kv_heads, per = kTile / G;
@@ -1110,8 +1114,11 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
     }
     ends.push_back(whole.size());
   }
-  // An item is cut where it is longer than a quarter of an SM's share of all the work, so that the last ones to end are short
-  const int64_t piece = std::max<int64_t>(kMinPiece, work * kv_heads / (kSms * 4));
+  // An item is cut where it is longer than a quarter of an SM's share of all the work, so that the last ones to end are short; where
+  // that is less than kMinPiece tiles, longer than these, or than two SMs' shares if there is not even that much for every block.  The three
+  // kernels for one trajectory of 509 tokens, 12 / 2 heads: 35 us; with 12 tiles 46; with 4 37, with 2 34.  Eight of 300, 14 / 2: 69 with 12 and so with
+  // this rule, 72 with one SM's share.
+  const int64_t share = work * kv_heads / kSms, piece = std::max(std::min<int64_t>(kMinPiece, std::max<int64_t>(kLeastPiece, 2 * share)), share / 4);
   size_t from = 0;
   for (size_t end : ends) {
     // a sequence's first pieces, then its second ones: blocks at work at the same time read the same queries
@@ -1142,8 +1149,8 @@ bc_status make_plan(int n_seqs, int q_heads, int kv_heads, int head_dim, int c, 
       }
     from = end;
   }
-  longest_first(&p->kv, [](const KvItem& x) { return x.nt + x.nb_tiles; });
-  longest_first(&p->q, [](const QItem& x) { return x.nt0 + x.nt1 + x.nt2; });
+  if (ordered) longest_first(&p->kv, [](const KvItem& x) { return x.nt + x.nb_tiles; });
+  if (ordered) longest_first(&p->q, [](const QItem& x) { return x.nt0 + x.nt1 + x.nt2; });
   size_t o = 256;
   auto take = [&](size_t bytes) { const size_t at = o; o = align_up(o + bytes); return at; };
   p->at_kv = take(p->kv.size() * sizeof(KvItem));
@@ -1167,7 +1174,7 @@ bc_status bc_mask_attn_backward_query_bytes(int32_t n_seqs, int32_t q_heads, int
   if (!workspace_bytes) return BC_ERR_INVALID_ARG;
   try {
     Plan p;
-    const bc_status st = make_plan(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, &p);
+    const bc_status st = make_plan(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, false, &p);
     if (st == BC_OK) *workspace_bytes = p.total;
     return st;
   } catch (...) {   // no host memory for the lists
@@ -1185,7 +1192,7 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || !(sm_scale > 0.f)) return BC_ERR_INVALID_ARG;
   try {
     Plan p;
-    const bc_status st = make_plan(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, &p);
+    const bc_status st = make_plan(n_seqs, q_heads, kv_heads, head_dim, c, cu_prompt, cu_tokens, true, &p);
     if (st != BC_OK) return st;
     if (workspace_bytes < p.total) return BC_ERR_INVALID_ARG;
     auto bad = [](std::initializer_list<const void*> v, int mask) {
@@ -1258,7 +1265,7 @@ bc_status bc_mask_attn_backward(int32_t n_seqs, int32_t q_heads, int32_t kv_head
     a.items = ws + p.at_kv; a.n_items = (int32_t)p.kv.size() * kv_heads; a.next = reinterpret_cast<int32_t*>(ws + 192);
     dkv<<<std::min(a.n_items, kSms), kThreads, kSmem, s>>>(a, maps);
     if (!p.join.empty())
-      k_join<<<dim3((unsigned)p.join.size() * kv_heads, 2 * kTile / 32), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
+      k_join<<<dim3((unsigned)p.join.size() * kv_heads, kJoinBlocks), 256, 0, s>>>(reinterpret_cast<const JoinItem*>(ws + p.at_join), a);
     return cudaGetLastError() == cudaSuccess ? BC_OK : BC_ERR_CUDA;
   } catch (...) {
     return BC_ERR_UNSUPPORTED;
