@@ -63,8 +63,7 @@ __device__ __forceinline__ uint32_t pack_bf16(F2 v) {
 }
 __device__ __forceinline__ uint4 pack8(const F2* f) { return make_uint4(pack_bf16(f[0]), pack_bf16(f[1]), pack_bf16(f[2]), pack_bf16(f[3])); }
 
-// A row belongs to `warps` warps of a block (all of it to one warp for up to 256 elements), chunk j of 8 elements to thread
-// j % (32 warps) of them; a block works on blockDim / (32 warps) rows at a time.
+// A row belongs to `warps` warps of a block, chunk j of 8 elements to thread j % (32 warps) of them; a block works on blockDim / (32 warps) rows at a time.
 struct NormArgs {
   const uint4 *x, *h, *gate, *post_weight, *pre_weight;   // weights NULL: ones; gate NULL: none
   uint4 *h_out, *y;                                       // y NULL: not wanted
@@ -90,8 +89,11 @@ __device__ __forceinline__ float row_sum(float v, int warps, float* part) {
   return __shfl_sync(0xffffffffu, v, 0);
 }
 
+// Two chunks per thread, so that a row's two sums and barriers are shared by half as many threads as with one (16384 rows of 4096 with a
+// gate per element: 108 us against 128, 8192 of 5120 73 against 103; with four and 256 threads the second takes 78); blocks of 256 threads
+// or one row.  At 6.2 TB/s the first is bound by memory, 0.94 of a copy; 64 rows of 1536 by latency (2.8 us: the launch, one load, two sums).
 template <int K>
-__global__ void __launch_bounds__(kMaxThreads, K == 1 ? 4 : 2) k_block_norm(const NormArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 2) k_block_norm(const NormArgs a) {
   __shared__ float part[2][kMaxThreads / 32];
   const int per_row = a.warps * 32, rows = blockDim.x / per_row, slot = threadIdx.x / per_row, j0 = threadIdx.x % per_row;
   const int64_t row = (int64_t)blockIdx.x * rows + slot;
@@ -375,16 +377,18 @@ inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 struct Shape {
   int chunks, warps, rows, threads, k;
 };
-Shape shape_of(int hidden) {
+// `most`: chunks per thread where a row has more than that many times 32; `threads`: of a block whose rows are not wider
+Shape shape_of(int hidden, int most, int threads) {
   Shape s;
   s.chunks = hidden / 8;
-  const int warps = (s.chunks + 31) / 32;
-  s.warps = warps < kMaxThreads / 32 ? warps : kMaxThreads / 32;
-  s.k = (s.chunks + s.warps * 32 - 1) / (s.warps * 32);
-  s.rows = kMaxThreads / 32 / s.warps;
+  s.k = s.chunks > 32 && most > 1 ? most : (s.chunks > kMaxThreads ? 2 : 1);
+  s.warps = (s.chunks + 32 * s.k - 1) / (32 * s.k);
+  s.rows = s.warps * 32 < threads ? threads / 32 / s.warps : 1;
   s.threads = s.rows * s.warps * 32;
   return s;
 }
+Shape norm_shape(int hidden) { return shape_of(hidden, 2, 256); }
+Shape grad_shape(int hidden) { return shape_of(hidden, 1, kMaxThreads); }
 constexpr int kGradBlocks = 148;
 
 bc_status check(int64_t n, int32_t hidden, const void* x, const void* h, const void* gate, int64_t gate_stride, const void* post_weight,
@@ -406,7 +410,7 @@ bc_status bc_block_norm(int32_t n, int32_t hidden, const void* x, const void* h,
   const bc_status st = check(n, hidden, x, h, gate, gate_stride, post_weight, pre_weight, scale, eps);
   if (st) return st;
   if (!h_out || !aligned16(h_out) || !aligned16(y)) return BC_ERR_INVALID_ARG;
-  const Shape s = shape_of(hidden);
+  const Shape s = norm_shape(hidden);
   NormArgs a;
   a.x = (const uint4*)x; a.h = (const uint4*)h; a.gate = (const uint4*)gate;
   a.post_weight = (const uint4*)post_weight; a.pre_weight = (const uint4*)pre_weight;
@@ -422,7 +426,7 @@ bc_status bc_block_norm(int32_t n, int32_t hidden, const void* x, const void* h,
 bc_status bc_block_norm_query_bytes(int32_t hidden, size_t* workspace_bytes) {
   if (!workspace_bytes || hidden <= 0) return BC_ERR_INVALID_ARG;
   if (hidden % 8 || hidden > kMaxHidden) return BC_ERR_UNSUPPORTED;
-  *workspace_bytes = (size_t)kGradBlocks * shape_of(hidden).rows * 3 * hidden * sizeof(float);
+  *workspace_bytes = (size_t)kGradBlocks * grad_shape(hidden).rows * 3 * hidden * sizeof(float);
   return BC_OK;
 }
 
@@ -437,7 +441,7 @@ bc_status bc_block_norm_backward(int32_t n, int32_t hidden, const void* x, const
       !aligned16(workspace) || (dgate && !gate) || (dpost_weight && !post_norm) ||
       ((reinterpret_cast<uintptr_t>(dpost_weight) | reinterpret_cast<uintptr_t>(dpre_weight)) & 3))
     return BC_ERR_INVALID_ARG;
-  const Shape s = shape_of(hidden);
+  const Shape s = grad_shape(hidden);
   const bool sums = dpost_weight || dpre_weight || (vector && dgate);
   if (sums && (!workspace || workspace_bytes < (size_t)kGradBlocks * s.rows * 3 * hidden * sizeof(float))) return BC_ERR_INVALID_ARG;
   NormGradArgs a;
