@@ -16,7 +16,7 @@
 // equal logits, ascending rows), the blocks find the K-th largest (value, index) pair bit by bit, counting over the row.
 //
 // Bounds: memory for long rows (2048 rows of 151,936 bf16: 105 us without alternatives, 5.9 TB/s or 0.90 of a copy), with exponentials
-// (2 bytes bring one, 0.6 of the time on that unit alone) and issue slots (61 % used) close behind; the search for the alternatives
+// (2 bytes bring one, 0.6 of the time on that unit alone) and issue slots (59 % used) close behind; the search for the alternatives
 // lies on top of that, partly under other blocks' loads (20 of them 133 us, 100 157 us).  Few rows wait for latencies: 64 such rows with
 // 20 alternatives 15.2 us, one fp32 row of 50,257 with 5 8.2 us -- the launch, three rounds of loads, four barriers over the cluster.
 #include <cooperative_groups.h>

@@ -18,6 +18,15 @@
 // Long items of k_dkv (the prompt's keys are seen by every row of a trajectory) are cut into pieces whose fp32 sums
 // k_join adds up in order.  k_dq runs first: it also computes D and leaves D and L by tiles for k_dkv.
 //
+// Roundings: P and dS are bf16 as first operands of the second products, each off by at most 2^-8 of itself, as the gradients
+// themselves are; D comes from O as it is stored.  The gradients are 2.4e-3 of their norm away from 64 bits (their own rounding: 1.7e-3).
+//
+// Four trajectories of 6000 tokens and 512 of prompt, c = 16, 32 / 8 heads: k_dq 605 us, k_dkv 690, k_join 17; seven products take 637 us
+// at the measured rate, five 455.  The tensor pipe is 36 - 47 % active, issue slots 38 - 44 % used, the clock at 1.66 GHz.  What bounds it:
+// the operands' way out of shared memory (a product of two operands from there reads as long as it computes), the round of waits from S to
+// dS, and some 8000 cycles at a change of item, which come after seven tiles here.  One trajectory of 509 tokens, 12 / 2 heads: 15.5 + 15.6 + 3.9 us,
+// all latency: two launches that fill tensor memory and shared memory anew, then chains of one to three tiles.
+//
 // Rows that a copy brings in past a sequence's end belong to its neighbour: their weights are set to zero by selection, and
 // where such a row is itself a factor (K in dS K; Q and dO in dS^T Q and P^T dO) it is cleared in shared memory first.
 #include <cuda.h>
