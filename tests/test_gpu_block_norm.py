@@ -135,3 +135,33 @@ def test_binding_refuses_what_does_not_fit():
     for call in bad:
         with pytest.raises(B.BreadcrumbsError):
             call()
+
+
+@pytest.mark.parametrize("n,hidden", [(700, 1536), (400, 4096), (200, 8192)])
+def test_the_streams_gradient_in_place(n, hidden):
+    """dh may be dh_out itself; rows of several rounds."""
+    x, h, gt, w1, w2, a, b = _inputs(n, n, hidden, "rows")
+    want = B.bc_block_norm_backward(x, h, gt, w1, w2, EPS, 0.5, True, a, b, weight_grads=False)
+    dx, dgate = torch.empty_like(x), torch.empty_like(x)
+    status = B.lib().bc_block_norm_backward(n, hidden, x.data_ptr(), h.data_ptr(), gt.data_ptr(), hidden, 1, w1.data_ptr(), w2.data_ptr(), 0.5, EPS,
+                                            a.data_ptr(), b.data_ptr(), dx.data_ptr(), a.data_ptr(), dgate.data_ptr(), None, None, None, 0,
+                                            torch.cuda.current_stream().cuda_stream)
+    assert status == B.BC_OK
+    assert torch.equal(dx, want[0]) and torch.equal(a, want[1]) and torch.equal(dgate, want[2])
+
+
+def test_two_graphs_of_the_gradient():
+    """Each with a workspace of its own, replayed by turns and at once."""
+    x, h, gt, w1, w2, a, b = _inputs(77, 900, 512, "vector")
+    call = lambda: B.bc_block_norm_backward(x, h, gt, w1, w2, EPS, 0.5, True, a, b)
+    want = call()
+    graphs, got, streams = [torch.cuda.CUDAGraph() for _ in range(2)], [], [torch.cuda.Stream() for _ in range(2)]
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            got.append(call())
+    for _ in range(5):
+        for graph, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, w) for out in got for t, w in zip(out, want))
