@@ -576,14 +576,17 @@ def bc_token_logprobs_backward(logits, targets, stats, entropy, d_logprob, d_ent
                                         (d_entropy, f32, (n,))), stream)
     _require(stats is not None, where)
     if grad is None:
-        per = 16 // logits.element_size()
+        per = 8 if not wide else 4
         width = -(-vocab // per) * per if row_stride % per == 0 else (row_stride if row_stride - vocab < per else vocab)
-        grad = _new(logits, (n, width), logits.dtype, other)
-        if width != vocab:
-            grad = grad[:, :vocab]
-    _require(grad.shape == logits.shape and grad.dtype is logits.dtype and grad.get_device() == dev and (vocab == 1 or grad.stride(1) == 1), where)
+        if other is None:
+            grad = logits.new_empty_strided((n, vocab), (width, 1))
+        else:
+            grad = _new(logits, (n, width), logits.dtype, other)[:, :vocab]
+    else:
+        _require(grad.shape == logits.shape and grad.dtype is logits.dtype and grad.get_device() == dev and (vocab == 1 or grad.stride(1) == 1), where)
+        width = grad.stride(0) if n > 1 else max(grad.stride(0), vocab)
     _call(where, dev, lib().bc_token_logprobs_backward, logits.data_ptr(), wide, row_stride, n, vocab, _at(targets), stats.data_ptr(),
-          _at(entropy), _at(d_logprob), _at(d_entropy), grad.data_ptr(), grad.stride(0) if n > 1 else max(grad.stride(0), vocab), s)
+          _at(entropy), _at(d_logprob), _at(d_entropy), grad.data_ptr(), width, s)
     return grad
 
 
